@@ -563,6 +563,79 @@ octo_status octo_op_compact_dense(const octo_cand* d_top, int32_t k_cap, const i
                                   octo_roi* d_rois, int32_t* d_n_rois, int32_t cap, int32_t* d_roi_of, int32_t* d_item_counts, octo_box* d_boxes,
                                   int32_t* d_flags, void* hip_stream);
 
+/* ---- tokens behind a cascade: questions that read frames and regions ----
+ * A detector's maps, or the crops of its regions, become tokens; text tokens read them.  These calls are the steps between
+ * the projections (which are 1x1 layers: octo_op_conv): norms and rotations of queries and keys, a cache of 4 bits a
+ * value, and attention to keys of another length.  All pointers are device memory; the calls only enqueue on hip_stream and
+ * keep no pointer.  Strides are in elements and may not be negative.  Inference only: no call has a gradient. */
+
+typedef enum { OCTO_PAIRS_SPLIT = 0, OCTO_PAIRS_INTERLEAVED = 1 } octo_pairs;
+typedef enum { OCTO_LADDER_AXIS = 0, OCTO_LADDER_SHARED = 1 } octo_ladder;
+#define OCTO_MAX_AXES 4
+#define OCTO_MAX_ROTATE_PARTS 2
+
+/* One tensor of octo_op_rotate: element (token, head, d) at d_x[token * x_token + head * x_head + d]; d_weight: fp32 [dim], or
+ * NULL for no norm.  d_y may be d_x with the same strides; otherwise the two must not overlap. */
+typedef struct {
+  const void* d_x; void* d_y; const float* d_weight;
+  int64_t x_token, x_head, y_token, y_head;
+  int32_t heads, pad_;
+} octo_rotate_part;
+/* Norm of every head and rotation by the token's positions, of one or two tensors (queries and keys) in one launch:
+ *   u = x * d_weight / sqrt(mean over dim of x^2 + eps)          (u = x without d_weight)
+ * then P = sum of sections pairs of elements of u are turned, pair p by the angle d_pos[token][a] * f_p, a the axis in whose
+ * section p lies (sections in order: axis 0's sections[0] pairs first):
+ *   OCTO_LADDER_AXIS:   f_p = base^(-j / sections[a]), j the index of p in its section (each axis has all wavelengths);
+ *   OCTO_LADDER_SHARED: f_p = base^(-p / P)            (the axes share one ladder).
+ *   OCTO_PAIRS_SPLIT: pair p is elements (p, p + P); OCTO_PAIRS_INTERLEAVED: (2p, 2p + 1);
+ *   (u1, u2) -> (u1 cos - u2 sin, u2 cos + u1 sin).  Elements from 2P on are not turned.
+ * Angles are reduced in fp64, so they are exact to fp32 at any position.  d_pos: int32 [n_tokens][n_axes] (n_axes 0: no
+ * rotation, NULL).  d_n: NULL, or the number of tokens present, on the device (clamped to n_tokens).  dtype: OCTO_F32, _F16 or
+ * _BF16; arithmetic in fp32, one rounding at the end.  dim: even, at most 256, and dim / 2 at most 64 times the longest vector
+ * (8, 4, 2 or 1 values of at most 16 bytes) that divides P and dim / 2 - P (split) or dim / 2 and to which all addresses and
+ * strides are aligned. */
+typedef struct octo_rotate_op {
+  int32_t dtype, n_tokens, dim, n_axes;
+  int32_t sections[OCTO_MAX_AXES];
+  int32_t pairs, ladder, n_parts, pad_;
+  double base;
+  float eps, pad2_;
+  const int32_t* d_pos;
+  const int32_t* d_n;
+  octo_rotate_part part[OCTO_MAX_ROTATE_PARTS];
+} octo_rotate_op;
+octo_status octo_op_rotate(const octo_rotate_op* op, void* hip_stream);
+
+/* Keys or values held in 4 bits: groups of 32 along dim with one exponent byte each.
+ *   e = the smallest integer with max |x| <= 7 * 2^e (so 6.x rounds to 6, off by less than the step there), stored as e + 127 in
+ *   1 .. 252 (fp16 input: at most 140, so that all values are finite in fp16);
+ *   code = x / 2^e rounded to the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 with a sign bit (OCP E2M1; ties to the even code, saturating).
+ *   A group that holds a NaN or an infinity gets the byte 255 and reads as NaN.
+ * codes: element (row, head, d) in the byte d_codes[row * code_row + head * code_head + d / 2], even d in the low half;
+ * exponents: d_exps[row * exp_row + head * exp_head + d / 32].  dim: 32, 64, 96 or 128.  d_codes 16-byte aligned, code_row and
+ * code_head multiples of 16. */
+typedef struct {
+  uint8_t* d_codes; uint8_t* d_exps;
+  int64_t code_row, code_head, exp_row, exp_head;
+} octo_cache4_plane;
+/* Store: token i of k and v ([n][heads][dim] of `dtype`, 16-byte aligned, strides multiples of 16 bytes) goes to row d_slots[i];
+ * a slot outside 0 .. rows - 1 skips the token.  Slots must differ (which of two equal ones wins is not defined).
+ * Load: the other way; a slot outside gives zeros.  d_n: NULL or the number of tokens present, on the device. */
+typedef struct octo_cache4_op {
+  int32_t dtype, n, heads, dim;
+  int64_t rows;
+  octo_cache4_plane k_plane, v_plane;
+  void* d_k; void* d_v;
+  int64_t k_token, k_head, v_token, v_head;
+  const int64_t* d_slots;
+  const int32_t* d_n;
+} octo_cache4_op;
+octo_status octo_op_cache4_store(const octo_cache4_op* op, void* hip_stream);
+octo_status octo_op_cache4_load(const octo_cache4_op* op, void* hip_stream);
+/* The same conversion on the host (no GPU): n values (a multiple of 32) to n / 2 bytes of codes and n / 32 exponent bytes, and back. */
+octo_status octo_quantize_mx4(const float* src, size_t n, uint8_t* codes, uint8_t* exps);
+octo_status octo_dequantize_mx4(const uint8_t* codes, const uint8_t* exps, size_t n, float* dst);
+
 #ifdef __cplusplus
 }
 #endif

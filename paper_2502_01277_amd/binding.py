@@ -137,6 +137,32 @@ class OctoConvOp(C.Structure):
                 ("d_y", C.c_void_p), ("res_scale", C.c_float), ("y_inv_scale", C.c_float)]
 
 
+MAX_AXES, MAX_ROTATE_PARTS = 4, 2
+PAIRS = {"split": 0, "interleaved": 1}
+LADDERS = {"axis": 0, "shared": 1}
+
+
+class OctoRotatePart(C.Structure):
+    _fields_ = [("d_x", C.c_void_p), ("d_y", C.c_void_p), ("d_weight", C.c_void_p), ("x_token", C.c_int64), ("x_head", C.c_int64),
+                ("y_token", C.c_int64), ("y_head", C.c_int64), ("heads", C.c_int32), ("pad_", C.c_int32)]
+
+
+class OctoRotateOp(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_tokens", C.c_int32), ("dim", C.c_int32), ("n_axes", C.c_int32), ("sections", C.c_int32 * MAX_AXES),
+                ("pairs", C.c_int32), ("ladder", C.c_int32), ("n_parts", C.c_int32), ("pad_", C.c_int32), ("base", C.c_double),
+                ("eps", C.c_float), ("pad2_", C.c_float), ("d_pos", C.c_void_p), ("d_n", C.c_void_p), ("part", OctoRotatePart * MAX_ROTATE_PARTS)]
+
+
+class OctoCache4Plane(C.Structure):
+    _fields_ = [("d_codes", C.c_void_p), ("d_exps", C.c_void_p), ("code_row", C.c_int64), ("code_head", C.c_int64), ("exp_row", C.c_int64), ("exp_head", C.c_int64)]
+
+
+class OctoCache4Op(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n", C.c_int32), ("heads", C.c_int32), ("dim", C.c_int32), ("rows", C.c_int64),
+                ("k_plane", OctoCache4Plane), ("v_plane", OctoCache4Plane), ("d_k", C.c_void_p), ("d_v", C.c_void_p),
+                ("k_token", C.c_int64), ("k_head", C.c_int64), ("v_token", C.c_int64), ("v_head", C.c_int64), ("d_slots", C.c_void_p), ("d_n", C.c_void_p)]
+
+
 # Every symbol include/octo.h declares.
 EXPORTS = [
     "octo_pipeline_workspace_size", "octo_pipeline_create", "octo_pipeline_destroy", "octo_submit_frames", "octo_run",
@@ -150,6 +176,7 @@ EXPORTS = [
     "octo_debug_get_detections", "octo_debug_get_rois", "octo_debug_get_labels", "octo_letterbox_geometry", "octo_op_frame_table", "octo_op_letterbox",
     "octo_op_crop_resize", "octo_op_decode", "octo_op_topk", "octo_op_nms", "octo_op_nms_scratch_bytes", "octo_op_nms_static", "octo_op_compact", "octo_op_compact_dense", "octo_probe_copy", "octo_probe_mfma",
     "octo_op_conv", "octo_op_conv_packed_bytes", "octo_op_conv_padded_cout", "octo_op_conv_pack", "octo_quantize_e4m3", "octo_dequantize_e4m3",
+    "octo_op_rotate", "octo_op_cache4_store", "octo_op_cache4_load", "octo_quantize_mx4", "octo_dequantize_mx4",
 ]
 
 _lib = None
@@ -240,6 +267,11 @@ def lib() -> C.CDLL:
         L.octo_op_conv_pack.argtypes = [i32, vp, i32, i32, i32, i32, vp]
         L.octo_quantize_e4m3.argtypes = [vp, C.c_size_t, f32, vp]
         L.octo_dequantize_e4m3.argtypes = [vp, C.c_size_t, f32, vp]
+        L.octo_op_rotate.argtypes = [vp, vp]
+        L.octo_op_cache4_store.argtypes = [vp, vp]
+        L.octo_op_cache4_load.argtypes = [vp, vp]
+        L.octo_quantize_mx4.argtypes = [vp, C.c_size_t, vp, vp]
+        L.octo_dequantize_mx4.argtypes = [vp, vp, C.c_size_t, vp]
         _lib = L
     return _lib
 
@@ -765,6 +797,144 @@ def op_conv(layer: ConvOp, x, y, res=None, res_mode=0, out_f32=False, res_scale=
     kid = C.c_int32(0)
     _st(lib().octo_op_conv(C.byref(op), _stream_ptr(stream), C.byref(kid)))
     return int(kid.value)
+
+
+# ---- tokens behind a cascade ---------------------------------------------------
+def _dtype_code(x) -> int:
+    """OCTO_F32 / _F16 / _BF16 of a tensor's type; other types are refused."""
+    t = _torch()
+    code = {t.float32: 0, t.float16: 1, t.bfloat16: 2}.get(x.dtype)
+    if code is None:
+        raise OctoError(EINVAL, "tensors of type %s are not taken" % x.dtype)
+    return code
+
+
+def _need(ok, what):
+    if not ok:
+        raise OctoError(EINVAL, what)
+
+
+def _optional(x, dtype, what, least=1):
+    """Address of an optional dense device tensor (0 where there is none)."""
+    if x is None:
+        return 0
+    _need(x.is_cuda and x.dtype == dtype and x.is_contiguous() and x.numel() >= least, what)
+    return x.data_ptr()
+
+
+class RotatePart:
+    """One tensor of op_rotate: x and y [tokens][heads][dim] (any strides, dim contiguous; y may be x), weight fp32 [dim] of the norm or None."""
+    __slots__ = ("x", "y", "weight")
+
+    def __init__(self, x, y, weight=None):
+        self.x, self.y, self.weight = x, y, weight
+
+
+def op_rotate(parts, pos, sections, base=10000.0, pairs="split", ladder="axis", eps=1e-6, n=None, stream=None):
+    """Norm of every head (parts with a weight) and rotation by the tokens' positions, of one or two tensors in one launch
+    (octo_rotate_op in octo.h).  pos: int32 [tokens][axes]; sections: pairs of each axis, () for no rotation (pos None);
+    n: int32 device tensor with the number of tokens present, or None."""
+    t = _torch()
+    _need(1 <= len(parts) <= MAX_ROTATE_PARTS and len(sections) <= MAX_AXES, "one or two parts, up to %d axes" % MAX_AXES)
+    x0 = parts[0].x
+    _need(x0.dim() == 3, "tensors are [tokens][heads][dim]")
+    tokens, _, dim = x0.shape
+    op = OctoRotateOp()
+    op.dtype, op.n_tokens, op.dim, op.n_axes = _dtype_code(x0), tokens, dim, len(sections)
+    op.sections[:len(sections)] = sections
+    op.pairs, op.ladder, op.n_parts, op.base, op.eps = PAIRS[pairs], LADDERS[ladder], len(parts), base, eps
+    if len(sections):
+        _need(pos is not None and pos.shape == (tokens, len(sections)), "positions are [tokens][axes]")
+        op.d_pos = _optional(pos, t.int32, "positions are int32, dense, on the device", 0)
+    op.d_n = _optional(n, t.int32, "n is int32 on the device")
+    for p, o in zip(parts, op.part):
+        x, y = p.x, p.y
+        _need(x.dim() == 3 and x.shape == y.shape and x.shape[0] == tokens and x.shape[2] == dim, "x and y of a part have one shape, all parts the same tokens and dim")
+        _need(x.is_cuda and y.is_cuda and x.dtype == y.dtype == x0.dtype, "x and y are device tensors of one type")
+        xs, ys = x.stride(), y.stride()
+        _need(xs[2] == 1 and ys[2] == 1, "dim is contiguous")
+        o.d_x, o.d_y, o.heads = x.data_ptr(), y.data_ptr(), x.shape[1]
+        o.x_token, o.x_head, o.y_token, o.y_head = xs[0], xs[1], ys[0], ys[1]
+        o.d_weight = _optional(p.weight, t.float32, "weight is fp32 [dim] on the device", dim)
+    _order(stream)
+    if tokens:
+        _st(lib().octo_op_rotate(C.byref(op), _stream_ptr(stream)))
+
+
+class Cache4:
+    """Keys and values held in 4 bits: codes uint8 [heads][rows][dim / 2], exponents uint8 [heads][rows][dim / 32] of each (any
+    strides, the last contiguous)."""
+    __slots__ = ("k_codes", "k_exps", "v_codes", "v_exps")
+
+    def __init__(self, k_codes, k_exps, v_codes, v_exps):
+        self.k_codes, self.k_exps, self.v_codes, self.v_exps = k_codes, k_exps, v_codes, v_exps
+
+    @classmethod
+    def zeros(cls, heads, rows, dim, device="cuda"):
+        t = _torch()
+        _need(dim % 32 == 0, "dim is a multiple of 32")
+        return cls(*[t.zeros((heads, rows, dim // d), dtype=t.uint8, device=device) for d in (2, 32, 2, 32)])
+
+    @property
+    def dims(self):
+        """(heads, rows, dim), after a look at the shapes."""
+        t = _torch()
+        h, r, b = self.k_codes.shape
+        for x, last in ((self.k_codes, b), (self.v_codes, b), (self.k_exps, b // 16), (self.v_exps, b // 16)):
+            _need(x.is_cuda and x.dtype == t.uint8 and x.shape == (h, r, last) and x.stride(2) == 1, "codes are uint8 [heads][rows][dim / 2], exponents [heads][rows][dim / 32]")
+        return h, r, 2 * b
+
+
+def _cache4_plane(o, codes, exps):
+    o.d_codes, o.d_exps = codes.data_ptr(), exps.data_ptr()
+    o.code_head, o.code_row, o.exp_head, o.exp_row = codes.stride(0), codes.stride(1), exps.stride(0), exps.stride(1)
+
+
+def _cache4_call(call, cache, k, v, slots, n, stream):
+    t = _torch()
+    heads, rows, dim = cache.dims
+    _need(k.dim() == 3 and k.shape == v.shape and tuple(k.shape[1:]) == (heads, dim) and k.is_cuda and v.is_cuda and k.dtype == v.dtype, "k and v are [tokens][heads][dim] of one type")
+    ks, vs = k.stride(), v.stride()
+    _need(ks[2] == 1 and vs[2] == 1, "dim is contiguous")
+    _need(slots.shape == k.shape[:1], "one slot a token")
+    if not k.shape[0]:
+        return
+    op = OctoCache4Op()
+    op.dtype, op.n, op.heads, op.dim, op.rows = _dtype_code(k), k.shape[0], heads, dim, rows
+    _cache4_plane(op.k_plane, cache.k_codes, cache.k_exps)
+    _cache4_plane(op.v_plane, cache.v_codes, cache.v_exps)
+    op.d_k, op.d_v, op.k_token, op.k_head, op.v_token, op.v_head = k.data_ptr(), v.data_ptr(), ks[0], ks[1], vs[0], vs[1]
+    op.d_slots = _optional(slots, t.int64, "slots are int64, dense, on the device")
+    op.d_n = _optional(n, t.int32, "n is int32 on the device")
+    _order(stream)
+    _st(call(C.byref(op), _stream_ptr(stream)))
+
+
+def op_cache4_store(cache: Cache4, k, v, slots, n=None, stream=None):
+    """Tokens k, v [tokens][heads][dim] into rows slots[i] (int64; outside the cache: skipped) of a cache of 4 bits a value."""
+    _cache4_call(lib().octo_op_cache4_store, cache, k, v, slots, n, stream)
+
+
+def op_cache4_load(cache: Cache4, slots, k, v, n=None, stream=None):
+    """What the rows slots[i] hold, into k, v [tokens][heads][dim] (zeros for a slot outside the cache)."""
+    _cache4_call(lib().octo_op_cache4_load, cache, k, v, slots, n, stream)
+
+
+def quantize_mx4(x: np.ndarray):
+    """(codes uint8 [..., n / 2], exponents uint8 [..., n / 32]) of fp32 [..., n], by the library (host)."""
+    x = np.ascontiguousarray(x, np.float32)
+    _need(x.ndim and x.shape[-1] % 32 == 0, "groups of 32 along the last axis")
+    codes, exps = np.empty(x.shape[:-1] + (x.shape[-1] // 2,), np.uint8), np.empty(x.shape[:-1] + (x.shape[-1] // 32,), np.uint8)
+    _st(lib().octo_quantize_mx4(x.ctypes.data, x.size, codes.ctypes.data, exps.ctypes.data))
+    return codes, exps
+
+
+def dequantize_mx4(codes: np.ndarray, exps: np.ndarray) -> np.ndarray:
+    codes, exps = np.ascontiguousarray(codes, np.uint8), np.ascontiguousarray(exps, np.uint8)
+    _need(codes.size == 16 * exps.size, "16 bytes of codes per exponent")
+    out = np.empty(codes.shape[:-1] + (2 * codes.shape[-1],), np.float32)
+    _st(lib().octo_dequantize_mx4(codes.ctypes.data, exps.ctypes.data, out.size, out.ctypes.data))
+    return out
 
 
 # ---- CU-masked streams --------------------------------------------------------
