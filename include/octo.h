@@ -636,6 +636,45 @@ octo_status octo_op_cache4_load(const octo_cache4_op* op, void* hip_stream);
 octo_status octo_quantize_mx4(const float* src, size_t n, uint8_t* codes, uint8_t* exps);
 octo_status octo_dequantize_mx4(const uint8_t* codes, const uint8_t* exps, size_t n, float* dst);
 
+/* Attention of ragged sequences to keys of other lengths.  Sequence b asks with the rows d_q_start[b] .. d_q_start[b + 1] - 1 of q
+ * and reads the rows d_kv_start[b] .. + d_kv_len[b] - 1 of a pool of keys and values; query head h reads key head
+ * h / (q_heads / kv_heads).  Over the visible keys j (d_key_mask NULL, or its byte for the pool row not zero):
+ *   out = sum_j exp(s_j) v_j / sum_j exp(s_j),  s_j = scale * (q . k_j),   lse = log sum_j exp(s_j)
+ * No visible key: out 0, lse -infinity.  What hidden keys and values hold does not matter, NaN neither.  Rows of q outside every
+ * sequence are not written.  Sums, maxima and products are in fp32; the weights exp(s_j - m), m a maximum of s so far, are rounded to the type of q
+ * before they multiply the values (fp32: not at all), their sum is taken before.
+ *
+ * dtype: type of q and out (fp32, fp16, bf16).  kv_format OCTO_KV_PLAIN: k and v of the same type; OCTO_KV_CACHE4: the planes that
+ * octo_op_cache4_store fills (dtype fp16 or bf16; values beyond the range of dtype are infinities).  dim: a multiple of 8 up
+ * to 128 (OCTO_KV_CACHE4: of 32).  d_q, d_k, d_v, d_out 16-byte aligned, their strides multiples of 16 bytes; rows of the
+ * pool less than 16 MiB apart.  d_q_start: int32 [n_seq + 1], ascending; d_kv_start: int64 [n_seq]; d_kv_len: int32 [n_seq]; all on the device,
+ * as lengths and regions of a cascade are.  The host states what they do not exceed: n_q rows of q, kv_rows rows of the
+ * pool, max_q and max_kv the longest sequence; what lies beyond is cut off (a sequence that starts outside the pool has no keys).  d_n_seq: NULL, or
+ * the number of sequences present, on the device.  d_lse: NULL or fp32 [n_q][q_heads].
+ * d_workspace: octo_op_attend_workspace_bytes(op) bytes, 16-byte aligned (NULL where that is 0), for this call alone until it is done:
+ * long key sequences are split over the compute units and joined in a fixed order.  The same call on the same inputs gives the same bits.
+ * *kernel_id (may be NULL): 0 nothing to do, else 1000 * kernel + the number of parts the keys were split into; kernel 1:
+ * wavefronts share the keys of up to 16 rows (queries x q_heads / kv_heads), 2: a wavefront for 16 rows. */
+typedef enum { OCTO_KV_PLAIN = 0, OCTO_KV_CACHE4 = 1 } octo_kv_format;
+typedef struct octo_attend_op {
+  int32_t dtype, kv_format, dim, q_heads, kv_heads;
+  int32_t n_seq, n_q, max_q, max_kv;
+  float scale;
+  int64_t kv_rows;
+  const void* d_q; int64_t q_row, q_head;
+  const void* d_k; const void* d_v; int64_t k_row, k_head, v_row, v_head;     /* OCTO_KV_PLAIN */
+  octo_cache4_plane k_plane, v_plane;                                          /* OCTO_KV_CACHE4 */
+  const int32_t* d_q_start; const int64_t* d_kv_start; const int32_t* d_kv_len;
+  const int32_t* d_n_seq;
+  const uint8_t* d_key_mask;
+  void* d_out; int64_t out_row, out_head;
+  float* d_lse;
+  void* d_workspace; size_t workspace_bytes;
+} octo_attend_op;
+octo_status octo_op_attend(const octo_attend_op* op, void* hip_stream, int32_t* kernel_id);
+/* Bytes of workspace of that call (0 too where the arguments are not valid); looks at sizes and types only. */
+size_t octo_op_attend_workspace_bytes(const octo_attend_op* op);
+
 #ifdef __cplusplus
 }
 #endif

@@ -60,7 +60,7 @@ def mx4_unpack(b):
     return out
 
 
-def attend(q, k, v, q_start, kv_start, kv_len, scale, key_mask=None, causal=False):
+def attend(q, k, v, q_start, kv_start, kv_len, scale, key_mask=None):
     """(out, lse) in float64.  q [n_q][Hq][D], k and v [rows][Hk][D]; sequence b owns queries q_start[b] .. q_start[b + 1] and the
     keys kv_start[b] .. + kv_len[b]; rows of no sequence stay NaN."""
     q, k, v = (np.asarray(t, np.float64) for t in (q, k, v))
@@ -71,10 +71,7 @@ def attend(q, k, v, q_start, kv_start, kv_len, scale, key_mask=None, causal=Fals
         lo, hi = int(q_start[b]), int(q_start[b + 1])
         rows = np.arange(int(kv_start[b]), int(kv_start[b]) + int(kv_len[b]))
         for i in range(lo, hi):
-            last = int(kv_len[b]) - (hi - lo) + (i - lo) if causal else int(kv_len[b]) - 1
-            see = rows[:max(0, last + 1)]
-            if key_mask is not None:
-                see = see[np.asarray(key_mask)[see] != 0]
+            see = rows if key_mask is None else rows[np.asarray(key_mask)[rows] != 0]
             for h in range(hq):
                 if not len(see):
                     out[i, h], lse[i, h] = 0.0, -np.inf

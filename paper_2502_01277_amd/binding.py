@@ -163,6 +163,15 @@ class OctoCache4Op(C.Structure):
                 ("k_token", C.c_int64), ("k_head", C.c_int64), ("v_token", C.c_int64), ("v_head", C.c_int64), ("d_slots", C.c_void_p), ("d_n", C.c_void_p)]
 
 
+class OctoAttendOp(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("kv_format", C.c_int32), ("dim", C.c_int32), ("q_heads", C.c_int32), ("kv_heads", C.c_int32),
+                ("n_seq", C.c_int32), ("n_q", C.c_int32), ("max_q", C.c_int32), ("max_kv", C.c_int32), ("scale", C.c_float), ("kv_rows", C.c_int64),
+                ("d_q", C.c_void_p), ("q_row", C.c_int64), ("q_head", C.c_int64), ("d_k", C.c_void_p), ("d_v", C.c_void_p),
+                ("k_row", C.c_int64), ("k_head", C.c_int64), ("v_row", C.c_int64), ("v_head", C.c_int64), ("k_plane", OctoCache4Plane), ("v_plane", OctoCache4Plane),
+                ("d_q_start", C.c_void_p), ("d_kv_start", C.c_void_p), ("d_kv_len", C.c_void_p), ("d_n_seq", C.c_void_p), ("d_key_mask", C.c_void_p),
+                ("d_out", C.c_void_p), ("out_row", C.c_int64), ("out_head", C.c_int64), ("d_lse", C.c_void_p), ("d_workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
 # Every symbol include/octo.h declares.
 EXPORTS = [
     "octo_pipeline_workspace_size", "octo_pipeline_create", "octo_pipeline_destroy", "octo_submit_frames", "octo_run",
@@ -177,6 +186,7 @@ EXPORTS = [
     "octo_op_crop_resize", "octo_op_decode", "octo_op_topk", "octo_op_nms", "octo_op_nms_scratch_bytes", "octo_op_nms_static", "octo_op_compact", "octo_op_compact_dense", "octo_probe_copy", "octo_probe_mfma",
     "octo_op_conv", "octo_op_conv_packed_bytes", "octo_op_conv_padded_cout", "octo_op_conv_pack", "octo_quantize_e4m3", "octo_dequantize_e4m3",
     "octo_op_rotate", "octo_op_cache4_store", "octo_op_cache4_load", "octo_quantize_mx4", "octo_dequantize_mx4",
+    "octo_op_attend", "octo_op_attend_workspace_bytes",
 ]
 
 _lib = None
@@ -270,6 +280,9 @@ def lib() -> C.CDLL:
         L.octo_op_rotate.argtypes = [vp, vp]
         L.octo_op_cache4_store.argtypes = [vp, vp]
         L.octo_op_cache4_load.argtypes = [vp, vp]
+        L.octo_op_attend.argtypes = [vp, vp, vp]
+        L.octo_op_attend_workspace_bytes.argtypes = [vp]
+        L.octo_op_attend_workspace_bytes.restype = C.c_size_t
         L.octo_quantize_mx4.argtypes = [vp, C.c_size_t, vp, vp]
         L.octo_dequantize_mx4.argtypes = [vp, vp, C.c_size_t, vp]
         _lib = L
@@ -918,6 +931,72 @@ def op_cache4_store(cache: Cache4, k, v, slots, n=None, stream=None):
 def op_cache4_load(cache: Cache4, slots, k, v, n=None, stream=None):
     """What the rows slots[i] hold, into k, v [tokens][heads][dim] (zeros for a slot outside the cache)."""
     _cache4_call(lib().octo_op_cache4_load, cache, k, v, slots, n, stream)
+
+
+def _attend_op(q, held, out, q_start, kv_start, kv_len, scale, max_q, max_kv, key_mask, lse, n_seq):
+    t = _torch()
+    _need(q.dim() == 3 and q.shape == out.shape and q.dtype == out.dtype and q.is_cuda and out.is_cuda, "q and out are [rows][heads][dim] of one type")
+    qs, os_ = q.stride(), out.stride()
+    _need(qs[2] == 1 and os_[2] == 1, "dim is contiguous")
+    rows, heads, dim = q.shape
+    op = OctoAttendOp()
+    op.dtype, op.n_q, op.q_heads, op.dim = _dtype_code(q), rows, heads, dim
+    if isinstance(held, Cache4):
+        op.kv_format = 1
+        op.kv_heads, op.kv_rows, kv_dim = held.dims
+        _cache4_plane(op.k_plane, held.k_codes, held.k_exps)
+        _cache4_plane(op.v_plane, held.v_codes, held.v_exps)
+    else:
+        k, v = held
+        _need(k.dim() == 3 and k.shape == v.shape and k.dtype == v.dtype == q.dtype and k.is_cuda and v.is_cuda, "k and v are [rows][heads][dim] of the type of q")
+        ks, vs = k.stride(), v.stride()
+        _need(ks[2] == 1 and vs[2] == 1, "dim is contiguous")
+        op.kv_rows, op.kv_heads, kv_dim = k.shape
+        op.d_k, op.d_v, op.k_row, op.k_head, op.v_row, op.v_head = k.data_ptr(), v.data_ptr(), ks[0], ks[1], vs[0], vs[1]
+    _need(kv_dim == dim, "q and the keys have one dim")
+    n = kv_start.shape[0]
+    _need(q_start.shape == (n + 1,) and kv_len.shape == (n,) and kv_start.dim() == 1, "q_start is [sequences + 1], kv_start and kv_len [sequences]")
+    op.n_seq = n
+    op.max_q = rows if max_q is None else max_q
+    op.max_kv = min(op.kv_rows, 0x7FFFFF00) if max_kv is None else max_kv
+    op.scale = dim ** -0.5 if scale is None else scale
+    op.d_q, op.q_row, op.q_head, op.d_out, op.out_row, op.out_head = q.data_ptr(), qs[0], qs[1], out.data_ptr(), os_[0], os_[1]
+    op.d_q_start = _optional(q_start, t.int32, "q_start is int32 on the device")
+    op.d_kv_start = _optional(kv_start, t.int64, "kv_start is int64 on the device", 0)
+    op.d_kv_len = _optional(kv_len, t.int32, "kv_len is int32 on the device", 0)
+    op.d_n_seq = _optional(n_seq, t.int32, "n_seq is int32 on the device")
+    op.d_key_mask = _optional(key_mask, t.uint8, "key_mask is uint8 [rows of the pool] on the device", op.kv_rows)
+    op.d_lse = _optional(lse, t.float32, "lse is fp32 [rows][heads] on the device", rows * heads)
+    return op
+
+
+def op_attend(q, held, out, q_start, kv_start, kv_len, scale=None, max_q=None, max_kv=None, key_mask=None, lse=None, n_seq=None, workspace=None, stream=None) -> int:
+    """Attention of ragged sequences to keys of other lengths (octo_attend_op in octo.h).  q, out: [rows][q heads][dim]; held: (k, v),
+    each [pool rows][kv heads][dim] of the type of q, or a Cache4.  q_start int32 [sequences + 1], kv_start int64, kv_len int32
+    [sequences], key_mask uint8 [pool rows], n_seq int32 [1]: on the device.  scale: dim ** -0.5 unless given; max_q, max_kv: the longest
+    sequences (all rows unless given).  workspace: uint8 device tensor of attend_workspace_bytes(...) or None to take one here.
+    Returns the id of the kernel that ran."""
+    op = _attend_op(q, held, out, q_start, kv_start, kv_len, scale, max_q, max_kv, key_mask, lse, n_seq)
+    if not op.n_seq or not op.n_q:
+        return 0
+    L = lib()
+    need = L.octo_op_attend_workspace_bytes(C.byref(op))
+    scratch = ()
+    if need:
+        if workspace is None:
+            t = _torch()
+            workspace = t.empty(need, dtype=t.uint8, device=q.device)
+            scratch = (workspace,)
+        op.d_workspace, op.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    _order(stream, *scratch)
+    kid = C.c_int32(0)
+    _st(L.octo_op_attend(C.byref(op), _stream_ptr(stream), C.byref(kid)))
+    return kid.value
+
+
+def attend_workspace_bytes(q, held, out, q_start, kv_start, kv_len, max_q=None, max_kv=None) -> int:
+    """Bytes of workspace op_attend needs for these sizes (what the tensors hold does not matter)."""
+    return lib().octo_op_attend_workspace_bytes(C.byref(_attend_op(q, held, out, q_start, kv_start, kv_len, 1.0, max_q, max_kv, None, None, None)))
 
 
 def quantize_mx4(x: np.ndarray):

@@ -44,10 +44,6 @@ def test_attention_by_hand():
     assert np.allclose(out[0], 4.0) and np.allclose(lse[0], np.log(4.0)) and np.all(out[1] == 0) and np.all(np.isneginf(lse[1]))
     out, _ = tokens.attend(q[:1], k, v, [0, 1], [0], [3], 1.0, key_mask=[0, 1, 0])
     assert np.allclose(out, 5.0)
-    out, _ = tokens.attend(q, k, v, [0, 2], [0], [2], 1.0, causal=True)
-    assert np.allclose(out[0], 1.0) and np.allclose(out[1], 4.0)
-    out, _ = tokens.attend(np.ones((3, 1, 1)), k, v, [0, 3], [0], [2], 1.0, causal=True)     # more queries than keys: the first sees none
-    assert np.all(out[0] == 0) and np.allclose(out[1], 1.0) and np.allclose(out[2], 4.0)
 
 
 def _awkward(rng):
@@ -177,3 +173,55 @@ def test_cache4_takes_nothing_and_refuses_too_much():
     op.n, op.heads = 0x7FFFFFFF, 64                          # beyond 32-bit thread numbers
     assert L.octo_op_cache4_store(C.byref(op), None) == binding.EINVAL
     assert L.octo_op_cache4_store(None, None) == binding.EINVAL
+
+
+def _attend_op(fmt=0):
+    op = binding.OctoAttendOp()
+    op.dtype, op.kv_format, op.dim, op.q_heads, op.kv_heads, op.n_seq, op.n_q, op.max_q, op.max_kv, op.scale, op.kv_rows = 2, fmt, 64, 8, 2, 3, 9, 4, 50, 0.1, 100
+    op.d_q, op.q_row, op.q_head, op.d_out, op.out_row, op.out_head = 4096, 512, 64, 8192, 512, 64
+    op.d_k, op.d_v, op.k_row, op.k_head, op.v_row, op.v_head = 4096, 4096, 128, 64, 128, 64
+    for p in (op.k_plane, op.v_plane):
+        p.d_codes, p.d_exps, p.code_row, p.code_head, p.exp_row, p.exp_head = 4096, 4097, 32, 3200, 2, 200
+    op.d_q_start, op.d_kv_start, op.d_kv_len = 4096, 4096, 4096
+    return op
+
+
+ATTEND_BAD = [("dtype", 3), ("dtype", -1), ("kv_format", 2), ("dim", 60), ("dim", 136), ("dim", 0), ("q_heads", 7), ("q_heads", 0), ("kv_heads", 0), ("kv_heads", 16), ("n_seq", -1), ("n_q", -1), ("max_q", 10),
+              ("max_q", -1), ("max_kv", -1), ("scale", 0.0), ("scale", -1.0), ("scale", float("inf")), ("kv_rows", -1), ("d_q", 0), ("d_q", 4098), ("q_row", 4), ("q_head", -64), ("d_out", 0), ("d_out", 4100),
+              ("out_row", 12), ("d_q_start", 0), ("d_q_start", 4098), ("d_kv_start", 0), ("d_kv_start", 4100), ("d_kv_len", 0), ("d_lse", 2)]
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+@pytest.mark.parametrize("field,value", ATTEND_BAD)
+def test_attend_refuses(fmt, field, value):
+    op = _attend_op(fmt)
+    setattr(op, field, value)
+    assert binding.lib().octo_op_attend(C.byref(op), None, None) == binding.EINVAL
+
+
+@pytest.mark.parametrize("field,value", [("d_k", 0), ("d_v", 4104), ("k_row", 4), ("v_head", -8), ("k_row", 8 << 20), ("v_row", 1 << 40)])
+def test_attend_refuses_pools(field, value):
+    op = _attend_op()
+    setattr(op, field, value)
+    assert binding.lib().octo_op_attend(C.byref(op), None, None) == binding.EINVAL
+
+
+@pytest.mark.parametrize("field,value", [("d_codes", 0), ("d_codes", 4104), ("d_exps", 0), ("code_row", 24), ("code_head", -16), ("exp_row", -2), ("code_row", 16 << 20), ("exp_row", 16 << 20)])
+def test_attend_refuses_planes(field, value):
+    op = _attend_op(1)
+    setattr(op.k_plane, field, value)
+    assert binding.lib().octo_op_attend(C.byref(op), None, None) == binding.EINVAL
+
+
+def test_attend_refuses_fp32_on_four_bits_and_takes_nothing():
+    L = binding.lib()
+    op = _attend_op(1)
+    op.dtype = 0
+    assert L.octo_op_attend(C.byref(op), None, None) == binding.EINVAL and L.octo_op_attend_workspace_bytes(C.byref(op)) == 0
+    kid = C.c_int32(5)
+    for name in ("n_seq", "max_q"):
+        op = _attend_op()
+        setattr(op, name, 0)
+        assert L.octo_op_attend(C.byref(op), None, C.byref(kid)) == binding.OK and kid.value == 0
+        assert L.octo_op_attend_workspace_bytes(C.byref(op)) == 0
+    assert L.octo_op_attend(None, None, None) == binding.EINVAL and L.octo_op_attend_workspace_bytes(None) == 0
