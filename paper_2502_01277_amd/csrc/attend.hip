@@ -2,7 +2,7 @@
 #include <cmath>
 #include <mutex>
 
-#include "attend.h"
+#include "attend_tile.h"
 
 namespace octo {
 namespace {
@@ -31,17 +31,20 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   store4<T>((T*)a.out + (sp.q0 + (long long)qi) * a.out_row + head * a.out_head + d, o * inv);
 }
 
-struct Plan { int share, row_blocks, n_split; };
+enum { SHARED_KEYS = 1, OWN_ROWS = 2, TILES = 3 };          // kernels, as in the id
+struct Plan { int kernel, row_blocks, n_split; };
 
-// Rows of the longest sequence, 16 a wavefront: up to 16 of them share their keys over the four wavefronts of a block.
-// Parts: as many as give every compute unit two blocks, each with at least two tiles a wavefront.
+// By the rows of the longest sequence.  Up to 16: one wavefront's, the four of a block share the keys.  fp32 and up to 32 rows: 16 a wavefront.
+// More: tiles in LDS for 128 rows.
+// Parts: as many as give every compute unit two blocks, of at least eight (shared keys) or two or four tiles.
 Plan plan_of(const octo_attend_op* op, int cus) {
   Plan p{};
   const long long rows = (long long)op->max_q * (op->q_heads / op->kv_heads);
-  p.share = rows <= 16;
-  p.row_blocks = (int)((rows + (p.share ? 15 : 63)) / (p.share ? 16 : 64));
+  p.kernel = rows <= 16 ? SHARED_KEYS : op->dtype == OCTO_F32 || rows <= 32 ? OWN_ROWS : TILES;
+  const int block_rows = p.kernel == SHARED_KEYS ? 16 : p.kernel == OWN_ROWS ? 64 : 128, part_keys = p.kernel == OWN_ROWS ? 64 : 256;
+  p.row_blocks = (int)((rows + block_rows - 1) / block_rows);
   const long long blocks = (long long)op->n_seq * op->kv_heads * p.row_blocks;
-  const int most = (op->max_kv + 32 * 2 * (p.share ? 4 : 1) - 1) / (32 * 2 * (p.share ? 4 : 1));
+  const int most = (op->max_kv + part_keys - 1) / part_keys;
   long long n = blocks > 0 ? (2ll * cus + blocks - 1) / blocks : 1;
   if (n > most) n = most;
   if (n > 64) n = 64;
@@ -134,9 +137,11 @@ octo_status octo_op_attend(const octo_attend_op* op, void* hip_stream, int32_t* 
     a.part_ml = (float2*)(a.part_o + (size_t)p.n_split * op->n_q * op->q_heads * op->dim);
   }
   hipStream_t s = (hipStream_t)hip_stream;
-  hipError_t e = op->dtype == OCTO_F32 ? launch_attend_direct_f32(op->kv_format, p.share, a, p.row_blocks, s)
-               : op->dtype == OCTO_F16 ? launch_attend_direct_f16(op->kv_format, p.share, a, p.row_blocks, s)
-                                       : launch_attend_direct_bf16(op->kv_format, p.share, a, p.row_blocks, s);
+  const int share = p.kernel == SHARED_KEYS;
+  hipError_t e = p.kernel == TILES ? (op->dtype == OCTO_F16 ? launch_attend_tile_f16(op->kv_format, a, p.row_blocks, s) : launch_attend_tile_bf16(op->kv_format, a, p.row_blocks, s))
+               : op->dtype == OCTO_F32 ? launch_attend_direct_f32(op->kv_format, share, a, p.row_blocks, s)
+               : op->dtype == OCTO_F16 ? launch_attend_direct_f16(op->kv_format, share, a, p.row_blocks, s)
+                                       : launch_attend_direct_bf16(op->kv_format, share, a, p.row_blocks, s);
   if (e == hipSuccess && p.n_split > 1) {      // then blocks of rows are few: max_q * q_heads is below 64 * 2 * 256
     const dim3 grid((unsigned)op->n_seq, (unsigned)(((long long)op->max_q * op->q_heads + 7) / 8));
     if (op->dtype == OCTO_F32) hipLaunchKernelGGL(attend_join_kernel<float>, grid, dim3(256), 0, s, a);
@@ -144,7 +149,7 @@ octo_status octo_op_attend(const octo_attend_op* op, void* hip_stream, int32_t* 
     else hipLaunchKernelGGL(attend_join_kernel<__bf16>, grid, dim3(256), 0, s, a);
     e = hipGetLastError();
   }
-  if (kernel_id && e == hipSuccess) *kernel_id = 1000 * (p.share ? 1 : 2) + p.n_split;
+  if (kernel_id && e == hipSuccess) *kernel_id = 1000 * p.kernel + p.n_split;
   return e == hipSuccess ? OCTO_OK : OCTO_EHIP;
 }
 

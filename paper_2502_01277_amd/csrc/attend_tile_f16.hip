@@ -1,0 +1,6 @@
+// The attention kernel for many rows, one storage type.
+#include "attend_tile.h"
+
+namespace octo {
+hipError_t launch_attend_tile_f16(int format, const AttendArgs& a, int row_blocks, hipStream_t s) { return launch_attend_tile<_Float16>(format, a, row_blocks, s); }
+}  // namespace octo
