@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass, field
 from typing import Dict, List, Optional, Sequence, Tuple
 
@@ -813,25 +814,37 @@ def op_conv(layer: ConvOp, x, y, res=None, res_mode=0, out_f32=False, res_scale=
 
 
 # ---- tokens behind a cascade ---------------------------------------------------
-def _dtype_code(x) -> int:
-    """OCTO_F32 / _F16 / _BF16 of a tensor's type; other types are refused."""
-    t = _torch()
-    code = {t.float32: 0, t.float16: 1, t.bfloat16: 2}.get(x.dtype)
-    if code is None:
-        raise OctoError(EINVAL, "tensors of type %s are not taken" % x.dtype)
-    return code
+# A call's arguments are packed in one go (a dozen microseconds less than field by field, as long as the small kernels take): the
+# layouts of OctoRotateOp, OctoCache4Op and OctoAttendOp.
+_PLANE = "PPqqqq"
+_ROTATE = struct.Struct("@12id2fPP" + "PPPqqqqii" * MAX_ROTATE_PARTS)
+_CACHE4 = struct.Struct("@4iq" + 2 * _PLANE + "PP4qPP")
+_ATTEND = struct.Struct("@9ifqPqqPPqqqq" + 2 * _PLANE + "5PPqqPPN")
+_NO_PART, _NO_PLANE, _NO_KV = (0,) * 9, (0,) * 6, (0,) * 6
 
 
-def _need(ok, what):
-    if not ok:
-        raise OctoError(EINVAL, what)
+class _Codes(dict):
+    def __missing__(self, dtype):
+        t = _torch()
+        self.update({t.float32: 0, t.float16: 1, t.bfloat16: 2})
+        if dtype not in self:
+            raise OctoError(EINVAL, "tensors of type %s are not taken" % dtype)
+        return self[dtype]
+
+
+_CODE = _Codes()           # OCTO_F32 / _F16 / _BF16 of a tensor's type
+
+
+def _refuse(what):
+    raise OctoError(EINVAL, what)
 
 
 def _optional(x, dtype, what, least=1):
     """Address of an optional dense device tensor (0 where there is none)."""
     if x is None:
         return 0
-    _need(x.is_cuda and x.dtype == dtype and x.is_contiguous() and x.numel() >= least, what)
+    if not (x.is_cuda and x.dtype is dtype and x.is_contiguous() and x.numel() >= least):
+        _refuse(what)
     return x.data_ptr()
 
 
@@ -848,30 +861,34 @@ def op_rotate(parts, pos, sections, base=10000.0, pairs="split", ladder="axis", 
     (octo_rotate_op in octo.h).  pos: int32 [tokens][axes]; sections: pairs of each axis, () for no rotation (pos None);
     n: int32 device tensor with the number of tokens present, or None."""
     t = _torch()
-    _need(1 <= len(parts) <= MAX_ROTATE_PARTS and len(sections) <= MAX_AXES, "one or two parts, up to %d axes" % MAX_AXES)
-    x0 = parts[0].x
-    _need(x0.dim() == 3, "tensors are [tokens][heads][dim]")
-    tokens, _, dim = x0.shape
-    op = OctoRotateOp()
-    op.dtype, op.n_tokens, op.dim, op.n_axes = _dtype_code(x0), tokens, dim, len(sections)
-    op.sections[:len(sections)] = sections
-    op.pairs, op.ladder, op.n_parts, op.base, op.eps = PAIRS[pairs], LADDERS[ladder], len(parts), base, eps
-    if len(sections):
-        _need(pos is not None and pos.shape == (tokens, len(sections)), "positions are [tokens][axes]")
-        op.d_pos = _optional(pos, t.int32, "positions are int32, dense, on the device", 0)
-    op.d_n = _optional(n, t.int32, "n is int32 on the device")
-    for p, o in zip(parts, op.part):
+    axes = len(sections)
+    if not 1 <= len(parts) <= MAX_ROTATE_PARTS or axes > MAX_AXES:
+        _refuse("one or two parts, up to %d axes" % MAX_AXES)
+    if axes and (pos is None or pos.dim() != 2 or pos.shape[1] != axes):
+        _refuse("positions are [tokens][axes]")
+    kind, packed = parts[0].x.dtype, ()
+    tokens = dim = None
+    for p in parts:
         x, y = p.x, p.y
-        _need(x.dim() == 3 and x.shape == y.shape and x.shape[0] == tokens and x.shape[2] == dim, "x and y of a part have one shape, all parts the same tokens and dim")
-        _need(x.is_cuda and y.is_cuda and x.dtype == y.dtype == x0.dtype, "x and y are device tensors of one type")
-        xs, ys = x.stride(), y.stride()
-        _need(xs[2] == 1 and ys[2] == 1, "dim is contiguous")
-        o.d_x, o.d_y, o.heads = x.data_ptr(), y.data_ptr(), x.shape[1]
-        o.x_token, o.x_head, o.y_token, o.y_head = xs[0], xs[1], ys[0], ys[1]
-        o.d_weight = _optional(p.weight, t.float32, "weight is fp32 [dim] on the device", dim)
-    _order(stream)
+        shape, xs, ys = x.shape, x.stride(), y.stride()
+        if len(shape) != 3 or y.shape != shape:
+            _refuse("x and y of a part are [tokens][heads][dim]")
+        if tokens is None:
+            tokens, _, dim = shape
+        if shape[0] != tokens or shape[2] != dim or not (x.is_cuda and y.is_cuda) or x.dtype is not kind or y.dtype is not kind:
+            _refuse("parts are device tensors of one type, with the same tokens and dim")
+        if dim > 1 and (xs[2] != 1 or ys[2] != 1):
+            _refuse("dim is contiguous")
+        packed += (x.data_ptr(), y.data_ptr(), _optional(p.weight, t.float32, "weight is fp32 [dim] on the device", dim), xs[0], xs[1], ys[0], ys[1], shape[1], 0)
+    if len(parts) == 1:
+        packed += _NO_PART
+    if axes and pos.shape[0] != tokens:
+        _refuse("positions are [tokens][axes]")
+    op = _ROTATE.pack(_CODE[kind], tokens, dim, axes, *sections, *(0,) * (MAX_AXES - axes), PAIRS[pairs], LADDERS[ladder], len(parts), 0, base, eps, 0.0,
+                      _optional(pos, t.int32, "positions are int32, dense, on the device", 0) if axes else 0, _optional(n, t.int32, "n is int32 on the device"), *packed)
     if tokens:
-        _st(lib().octo_op_rotate(C.byref(op), _stream_ptr(stream)))
+        _order(stream)
+        _st(lib().octo_op_rotate(op, _stream_ptr(stream)))
 
 
 class Cache4:
@@ -885,89 +902,77 @@ class Cache4:
     @classmethod
     def zeros(cls, heads, rows, dim, device="cuda"):
         t = _torch()
-        _need(dim % 32 == 0, "dim is a multiple of 32")
+        if dim % 32:
+            _refuse("dim is a multiple of 32")
         return cls(*[t.zeros((heads, rows, dim // d), dtype=t.uint8, device=device) for d in (2, 32, 2, 32)])
 
-    @property
-    def dims(self):
-        """(heads, rows, dim), after a look at the shapes."""
-        t = _torch()
+    def pack(self):
+        """(heads, rows, dim, fields of the two planes), after a look at the shapes."""
+        u8 = _torch().uint8
         h, r, b = self.k_codes.shape
-        for x, last in ((self.k_codes, b), (self.v_codes, b), (self.k_exps, b // 16), (self.v_exps, b // 16)):
-            _need(x.is_cuda and x.dtype == t.uint8 and x.shape == (h, r, last) and x.stride(2) == 1, "codes are uint8 [heads][rows][dim / 2], exponents [heads][rows][dim / 32]")
-        return h, r, 2 * b
+        planes = ()
+        for codes, exps in ((self.k_codes, self.k_exps), (self.v_codes, self.v_exps)):
+            cs, es = codes.stride(), exps.stride()
+            if not (codes.is_cuda and exps.is_cuda and codes.dtype is u8 and exps.dtype is u8 and codes.shape == (h, r, b) and exps.shape == (h, r, b // 16)) or cs[2] != 1 or (es[2] != 1 and b > 16):
+                _refuse("codes are uint8 [heads][rows][dim / 2], exponents uint8 [heads][rows][dim / 32], on the device")
+            planes += (codes.data_ptr(), exps.data_ptr(), cs[1], cs[0], es[1], es[0])
+        return h, r, 2 * b, planes
 
 
-def _cache4_plane(o, codes, exps):
-    o.d_codes, o.d_exps = codes.data_ptr(), exps.data_ptr()
-    o.code_head, o.code_row, o.exp_head, o.exp_row = codes.stride(0), codes.stride(1), exps.stride(0), exps.stride(1)
-
-
-def _cache4_call(call, cache, k, v, slots, n, stream):
+def _cache4_call(name, cache, k, v, slots, n, stream):
     t = _torch()
-    heads, rows, dim = cache.dims
-    _need(k.dim() == 3 and k.shape == v.shape and tuple(k.shape[1:]) == (heads, dim) and k.is_cuda and v.is_cuda and k.dtype == v.dtype, "k and v are [tokens][heads][dim] of one type")
-    ks, vs = k.stride(), v.stride()
-    _need(ks[2] == 1 and vs[2] == 1, "dim is contiguous")
-    _need(slots.shape == k.shape[:1], "one slot a token")
-    if not k.shape[0]:
+    heads, rows, dim, planes = cache.pack()
+    shape, ks, vs = k.shape, k.stride(), v.stride()
+    if len(shape) != 3 or v.shape != shape or shape[1] != heads or shape[2] != dim or not (k.is_cuda and v.is_cuda) or k.dtype is not v.dtype or ks[2] != 1 or vs[2] != 1:
+        _refuse("k and v are [tokens][heads][dim] of one type, dim contiguous")
+    if slots.shape != shape[:1]:
+        _refuse("one slot a token")
+    if not shape[0]:
         return
-    op = OctoCache4Op()
-    op.dtype, op.n, op.heads, op.dim, op.rows = _dtype_code(k), k.shape[0], heads, dim, rows
-    _cache4_plane(op.k_plane, cache.k_codes, cache.k_exps)
-    _cache4_plane(op.v_plane, cache.v_codes, cache.v_exps)
-    op.d_k, op.d_v, op.k_token, op.k_head, op.v_token, op.v_head = k.data_ptr(), v.data_ptr(), ks[0], ks[1], vs[0], vs[1]
-    op.d_slots = _optional(slots, t.int64, "slots are int64, dense, on the device")
-    op.d_n = _optional(n, t.int32, "n is int32 on the device")
+    op = _CACHE4.pack(_CODE[k.dtype], shape[0], heads, dim, rows, *planes, k.data_ptr(), v.data_ptr(), ks[0], ks[1], vs[0], vs[1],
+                      _optional(slots, t.int64, "slots are int64, dense, on the device"), _optional(n, t.int32, "n is int32 on the device"))
     _order(stream)
-    _st(call(C.byref(op), _stream_ptr(stream)))
+    _st(getattr(lib(), name)(op, _stream_ptr(stream)))
 
 
 def op_cache4_store(cache: Cache4, k, v, slots, n=None, stream=None):
     """Tokens k, v [tokens][heads][dim] into rows slots[i] (int64; outside the cache: skipped) of a cache of 4 bits a value."""
-    _cache4_call(lib().octo_op_cache4_store, cache, k, v, slots, n, stream)
+    _cache4_call("octo_op_cache4_store", cache, k, v, slots, n, stream)
 
 
 def op_cache4_load(cache: Cache4, slots, k, v, n=None, stream=None):
     """What the rows slots[i] hold, into k, v [tokens][heads][dim] (zeros for a slot outside the cache)."""
-    _cache4_call(lib().octo_op_cache4_load, cache, k, v, slots, n, stream)
+    _cache4_call("octo_op_cache4_load", cache, k, v, slots, n, stream)
 
 
-def _attend_op(q, held, out, q_start, kv_start, kv_len, scale, max_q, max_kv, key_mask, lse, n_seq):
+def _attend_pack(q, held, out, q_start, kv_start, kv_len, scale, max_q, max_kv, key_mask, lse, n_seq):
+    """(sequences, rows of q, all fields but the workspace)."""
     t = _torch()
-    _need(q.dim() == 3 and q.shape == out.shape and q.dtype == out.dtype and q.is_cuda and out.is_cuda, "q and out are [rows][heads][dim] of one type")
-    qs, os_ = q.stride(), out.stride()
-    _need(qs[2] == 1 and os_[2] == 1, "dim is contiguous")
-    rows, heads, dim = q.shape
-    op = OctoAttendOp()
-    op.dtype, op.n_q, op.q_heads, op.dim = _dtype_code(q), rows, heads, dim
+    shape, qs, os_, kind = q.shape, q.stride(), out.stride(), q.dtype
+    if len(shape) != 3 or out.shape != shape or out.dtype is not kind or not (q.is_cuda and out.is_cuda) or qs[2] != 1 or os_[2] != 1:
+        _refuse("q and out are [rows][heads][dim] of one type on the device, dim contiguous")
+    rows, heads, dim = shape
     if isinstance(held, Cache4):
-        op.kv_format = 1
-        op.kv_heads, op.kv_rows, kv_dim = held.dims
-        _cache4_plane(op.k_plane, held.k_codes, held.k_exps)
-        _cache4_plane(op.v_plane, held.v_codes, held.v_exps)
+        kv_heads, kv_rows, kv_dim, planes = held.pack()
+        kv, fmt = _NO_KV + planes, 1
     else:
         k, v = held
-        _need(k.dim() == 3 and k.shape == v.shape and k.dtype == v.dtype == q.dtype and k.is_cuda and v.is_cuda, "k and v are [rows][heads][dim] of the type of q")
-        ks, vs = k.stride(), v.stride()
-        _need(ks[2] == 1 and vs[2] == 1, "dim is contiguous")
-        op.kv_rows, op.kv_heads, kv_dim = k.shape
-        op.d_k, op.d_v, op.k_row, op.k_head, op.v_row, op.v_head = k.data_ptr(), v.data_ptr(), ks[0], ks[1], vs[0], vs[1]
-    _need(kv_dim == dim, "q and the keys have one dim")
+        kv_shape, ks, vs = k.shape, k.stride(), v.stride()
+        if len(kv_shape) != 3 or v.shape != kv_shape or k.dtype is not kind or v.dtype is not kind or not (k.is_cuda and v.is_cuda) or ks[2] != 1 or vs[2] != 1:
+            _refuse("k and v are [rows][heads][dim] of the type of q, dim contiguous")
+        kv_rows, kv_heads, kv_dim = kv_shape
+        kv, fmt = (k.data_ptr(), v.data_ptr(), ks[0], ks[1], vs[0], vs[1]) + _NO_PLANE + _NO_PLANE, 0
+    if kv_dim != dim:
+        _refuse("q and the keys have one dim")
     n = kv_start.shape[0]
-    _need(q_start.shape == (n + 1,) and kv_len.shape == (n,) and kv_start.dim() == 1, "q_start is [sequences + 1], kv_start and kv_len [sequences]")
-    op.n_seq = n
-    op.max_q = rows if max_q is None else max_q
-    op.max_kv = min(op.kv_rows, 0x7FFFFF00) if max_kv is None else max_kv
-    op.scale = dim ** -0.5 if scale is None else scale
-    op.d_q, op.q_row, op.q_head, op.d_out, op.out_row, op.out_head = q.data_ptr(), qs[0], qs[1], out.data_ptr(), os_[0], os_[1]
-    op.d_q_start = _optional(q_start, t.int32, "q_start is int32 on the device")
-    op.d_kv_start = _optional(kv_start, t.int64, "kv_start is int64 on the device", 0)
-    op.d_kv_len = _optional(kv_len, t.int32, "kv_len is int32 on the device", 0)
-    op.d_n_seq = _optional(n_seq, t.int32, "n_seq is int32 on the device")
-    op.d_key_mask = _optional(key_mask, t.uint8, "key_mask is uint8 [rows of the pool] on the device", op.kv_rows)
-    op.d_lse = _optional(lse, t.float32, "lse is fp32 [rows][heads] on the device", rows * heads)
-    return op
+    if q_start.shape != (n + 1,) or kv_len.shape != (n,) or kv_start.dim() != 1:
+        _refuse("q_start is [sequences + 1], kv_start and kv_len [sequences]")
+    return n, rows, (_CODE[kind], fmt, dim, heads, kv_heads, n, rows, rows if max_q is None else max_q, min(kv_rows, 0x7FFFFF00) if max_kv is None else max_kv,
+                     dim ** -0.5 if scale is None else scale, kv_rows, q.data_ptr(), qs[0], qs[1], *kv,
+                     _optional(q_start, t.int32, "q_start is int32 on the device"), _optional(kv_start, t.int64, "kv_start is int64 on the device", 0),
+                     _optional(kv_len, t.int32, "kv_len is int32 on the device", 0), _optional(n_seq, t.int32, "n_seq is int32 on the device"),
+                     _optional(key_mask, t.uint8, "key_mask is uint8 [rows of the pool] on the device", kv_rows), out.data_ptr(), os_[0], os_[1],
+                     _optional(lse, t.float32, "lse is fp32 [rows][heads] on the device", rows * heads))
 
 
 def op_attend(q, held, out, q_start, kv_start, kv_len, scale=None, max_q=None, max_kv=None, key_mask=None, lse=None, n_seq=None, workspace=None, stream=None) -> int:
@@ -976,33 +981,34 @@ def op_attend(q, held, out, q_start, kv_start, kv_len, scale=None, max_q=None, m
     [sequences], key_mask uint8 [pool rows], n_seq int32 [1]: on the device.  scale: dim ** -0.5 unless given; max_q, max_kv: the longest
     sequences (all rows unless given).  workspace: uint8 device tensor of attend_workspace_bytes(...) or None to take one here.
     Returns the id of the kernel that ran."""
-    op = _attend_op(q, held, out, q_start, kv_start, kv_len, scale, max_q, max_kv, key_mask, lse, n_seq)
-    if not op.n_seq or not op.n_q:
+    n, rows, fields = _attend_pack(q, held, out, q_start, kv_start, kv_len, scale, max_q, max_kv, key_mask, lse, n_seq)
+    if not n or not rows:
         return 0
     L = lib()
-    need = L.octo_op_attend_workspace_bytes(C.byref(op))
+    op = _ATTEND.pack(*fields, 0, 0)
+    need = L.octo_op_attend_workspace_bytes(op)
     scratch = ()
     if need:
         if workspace is None:
-            t = _torch()
-            workspace = t.empty(need, dtype=t.uint8, device=q.device)
+            workspace = _torch().empty(need, dtype=_torch().uint8, device=q.device)
             scratch = (workspace,)
-        op.d_workspace, op.workspace_bytes = workspace.data_ptr(), workspace.numel()
+        op = _ATTEND.pack(*fields, workspace.data_ptr(), workspace.numel())
     _order(stream, *scratch)
     kid = C.c_int32(0)
-    _st(L.octo_op_attend(C.byref(op), _stream_ptr(stream), C.byref(kid)))
+    _st(L.octo_op_attend(op, _stream_ptr(stream), C.byref(kid)))
     return kid.value
 
 
 def attend_workspace_bytes(q, held, out, q_start, kv_start, kv_len, max_q=None, max_kv=None) -> int:
     """Bytes of workspace op_attend needs for these sizes (what the tensors hold does not matter)."""
-    return lib().octo_op_attend_workspace_bytes(C.byref(_attend_op(q, held, out, q_start, kv_start, kv_len, 1.0, max_q, max_kv, None, None, None)))
+    return lib().octo_op_attend_workspace_bytes(_ATTEND.pack(*_attend_pack(q, held, out, q_start, kv_start, kv_len, 1.0, max_q, max_kv, None, None, None)[2], 0, 0))
 
 
 def quantize_mx4(x: np.ndarray):
     """(codes uint8 [..., n / 2], exponents uint8 [..., n / 32]) of fp32 [..., n], by the library (host)."""
     x = np.ascontiguousarray(x, np.float32)
-    _need(x.ndim and x.shape[-1] % 32 == 0, "groups of 32 along the last axis")
+    if not x.ndim or x.shape[-1] % 32:
+        _refuse("groups of 32 along the last axis")
     codes, exps = np.empty(x.shape[:-1] + (x.shape[-1] // 2,), np.uint8), np.empty(x.shape[:-1] + (x.shape[-1] // 32,), np.uint8)
     _st(lib().octo_quantize_mx4(x.ctypes.data, x.size, codes.ctypes.data, exps.ctypes.data))
     return codes, exps
@@ -1010,7 +1016,8 @@ def quantize_mx4(x: np.ndarray):
 
 def dequantize_mx4(codes: np.ndarray, exps: np.ndarray) -> np.ndarray:
     codes, exps = np.ascontiguousarray(codes, np.uint8), np.ascontiguousarray(exps, np.uint8)
-    _need(codes.size == 16 * exps.size, "16 bytes of codes per exponent")
+    if codes.size != 16 * exps.size:
+        _refuse("16 bytes of codes per exponent")
     out = np.empty(codes.shape[:-1] + (2 * codes.shape[-1],), np.float32)
     _st(lib().octo_dequantize_mx4(codes.ctypes.data, exps.ctypes.data, out.size, out.ctypes.data))
     return out

@@ -28,21 +28,34 @@ struct AttendArgs {
   int n_seq, n_q, max_q, max_kv, dim, q_heads, kv_heads, group;
   FastDiv div_group;
   float scale2;                                                        // scale * log2(e)
-  int n_split;
+  int n_split, part_keys;                                              // parts of part_keys keys (a multiple of 64); sequences of one part are finished by its block
+  int row_blocks;                                                      // of the kernel's rows, of the longest sequence
+  FastDiv div_heads, div_blocks, div_split;                            // kv_heads, row_blocks, n_split
 };
 
 enum { KV_PLAIN = OCTO_KV_PLAIN, KV_CACHE4 = OCTO_KV_CACHE4 };
 
-hipError_t launch_attend_direct_f16(int format, int waves_share_keys, const AttendArgs& a, int row_blocks, hipStream_t s);
-hipError_t launch_attend_direct_bf16(int format, int waves_share_keys, const AttendArgs& a, int row_blocks, hipStream_t s);
-hipError_t launch_attend_direct_f32(int format, int waves_share_keys, const AttendArgs& a, int row_blocks, hipStream_t s);
+hipError_t launch_attend_direct_f16(int format, int share, const AttendArgs& a, hipStream_t s);
+hipError_t launch_attend_direct_bf16(int format, int share, const AttendArgs& a, hipStream_t s);
+hipError_t launch_attend_direct_f32(int format, int share, const AttendArgs& a, hipStream_t s);
 
 #ifdef __HIPCC__
 typedef uint32_t u32x3 __attribute__((ext_vector_type(3)));
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
+// The n-th piece of work: key heads first (the blocks of one head next to each other for one die's cache where there are eight), then blocks of
+// rows, parts, and sequences last: neighbours are alike in length, so that a short sequence's pieces do not all leave the same units idle.
+struct Piece { int seq, part, block, head; };
+__device__ __forceinline__ Piece piece_of(const AttendArgs& a, unsigned n) {
+  Piece p;
+  const unsigned x = fast_div(n, a.div_heads), y = fast_div(x, a.div_blocks), z = fast_div(y, a.div_split);
+  p.head = (int)(n - x * (unsigned)a.kv_heads); p.block = (int)(x - y * (unsigned)a.row_blocks); p.part = (int)(y - z * (unsigned)a.n_split); p.seq = (int)z;
+  return p;
+}
+
 struct Span { int q0, n_q, n_kv; long long kv0; };
+__device__ __forceinline__ int parts_of(const AttendArgs& a, int n_kv) { return n_kv > a.part_keys ? (n_kv + a.part_keys - 1) / a.part_keys : 1; }
 // The rows and keys of sequence b, cut to what the host stated; false: no such sequence, or no queries.
 __device__ __forceinline__ bool span_of(const AttendArgs& a, int b, Span* s) {
   if (a.n_dyn && b >= *a.n_dyn) return false;
@@ -236,8 +249,8 @@ template <typename T, int FORMAT, int DP, int t> __device__ __forceinline__ void
 
 // Scaled weights of a row's part of the keys become one result: out and lse, or a part for attend_join_kernel.
 template <typename T, int PER>
-__device__ __forceinline__ void finish_row(const AttendArgs& a, int part, long long q_row, int head, int d0, bool first, const float* o, float ref, float sum) {
-  if (a.n_split > 1) {
+__device__ __forceinline__ void finish_row(const AttendArgs& a, int part, bool whole, long long q_row, int head, int d0, bool first, const float* o, float ref, float sum) {
+  if (!whole) {
     const long long at = ((long long)part * a.n_q + q_row) * a.q_heads + head;
     if (first) a.part_ml[at] = make_float2(ref, sum);
     float* y = a.part_o + at * a.dim + d0;
@@ -265,32 +278,34 @@ __device__ __forceinline__ void finish_row(const AttendArgs& a, int part, long l
 // LDS and no barrier on the way, the next tile's loads are in flight while one is computed.  SHARE: the four wavefronts of
 // a block have the same rows and every fourth tile each, and add up in LDS at the end (few rows: what bounds it is reading the keys, and
 // more wavefronts have more loads in flight); otherwise each has rows of its own.
-template <typename T, int FORMAT, int DP, bool SHARE>
+template <typename T, int FORMAT, int DP, bool SHARE, bool MASK>
 __global__ __launch_bounds__(256, 2) void attend_direct_kernel(AttendArgs a) {
   constexpr int STEPS = DP / 32, PER = DP / 16, WAVES = SHARE ? 4 : 1;
-  const int b = blockIdx.x / a.kv_heads, kv_head = blockIdx.x - b * a.kv_heads, part = blockIdx.z;
-  Span sp;
-  if (!span_of(a, b, &sp)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
-  const int rows = sp.n_q * a.group, row0 = (SHARE ? blockIdx.y : blockIdx.y * 4 + wave) * 16;
-  if (row0 >= rows) return;                              // SHARE: the whole block
+  // what a block (SHARE) or a wavefront does: 16 rows of a sequence and key head
+  const Piece pc = piece_of(a, SHARE ? blockIdx.x : blockIdx.x * 4 + wave);
+  const int b = pc.seq, kv_head = pc.head, part = pc.part, row0 = pc.block * 16;
+  Span sp;
+  if (b >= a.n_seq || !span_of(a, b, &sp)) return;
+  const int rows = sp.n_q * a.group;
+  if (row0 >= rows || part >= parts_of(a, sp.n_kv)) return;      // SHARE: the whole block
+  const bool whole = sp.n_kv <= a.part_keys;
   const int row = row0 + col;
   const bool has_row = row < rows;
   const int qi = (int)fast_div((unsigned)row, a.div_group), head = kv_head * a.group + row - qi * a.group;
   const long long q_row = sp.q0 + qi;
 
-  const int tiles = (sp.n_kv + 31) / 32, per_part = (tiles + a.n_split - 1) / a.n_split;
+  const int tiles = (sp.n_kv + 31) / 32, per_part = a.part_keys / 32;
   const int first = part * per_part, last = min(tiles, first + per_part);      // first .. last - 1
 
   Keys<T, FORMAT, DP> keys;
   Values<T, FORMAT, DP> vals;
   Eight<T> q[STEPS];
   keys.init(a, g);
-  int mask_byte = 0;
+  uint32_t mask_byte = 0;
   auto keys_left = [&](int t) { return t < last ? min(32, sp.n_kv - 32 * t) : 0; };
   auto load_mask = [&](int t) {
-    const int n = keys_left(t);
-    mask_byte = lane < n ? (a.mask ? a.mask[sp.kv0 + 32ll * t + lane] : 1) : 0;
+    if constexpr (MASK) mask_byte = __builtin_amdgcn_raw_buffer_load_b8(buffer_at(a.mask + sp.kv0 + 32ll * t, keys_left(t)), lane, 0, 0);
   };
   int t = first + (SHARE ? wave : 0);
   keys.load(a, kv_head, sp.kv0 + 32ll * t, keys_left(t), col);
@@ -312,7 +327,8 @@ __global__ __launch_bounds__(256, 2) void attend_direct_kernel(AttendArgs a) {
   const float c = a.scale2;
 
   for (; t < last; t += WAVES) {
-    const unsigned seen = (unsigned)__ballot(mask_byte != 0);
+    const int n = keys_left(t);
+    const unsigned seen = MASK ? (unsigned)__ballot(mask_byte != 0) : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1;
     floatx4 st[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -329,7 +345,7 @@ __global__ __launch_bounds__(256, 2) void attend_direct_kernel(AttendArgs a) {
         for (int i = 0; i < 4; ++i) {
           const bool keep = seen >> (16 * h + 4 * g + i) & 1;
           st[h][i] = keep ? st[h][i] : -INFINITY;
-          vals.hide(4 * h + i, keep);
+          if (MASK) vals.hide(4 * h + i, keep);               // beyond the last key zeros were read
         }
     }
     // The reference follows the largest score only where that is more than 2^8 above it: weights up to 2^8 cost no precision,
@@ -364,7 +380,7 @@ __global__ __launch_bounds__(256, 2) void attend_direct_kernel(AttendArgs a) {
       float o[PER];
 #pragma unroll
       for (int e = 0; e < PER; ++e) o[e] = acc[e][i];
-      finish_row<T, PER>(a, part, q_row, head, PER * (4 * g + i), g == 0 && i == 0, o, refc, sum);
+      finish_row<T, PER>(a, part, whole, q_row, head, PER * (4 * g + i), g == 0 && i == 0, o, refc, sum);
     }
   } else {
     constexpr int LD = DP + 4;
@@ -392,25 +408,28 @@ __global__ __launch_bounds__(256, 2) void attend_direct_kernel(AttendArgs a) {
       for (int e = 0; e < PER; ++e) o[e] += so[w][r][d0 + e] * f;
     }
     const int q2 = (int)fast_div((unsigned)(row0 + r), a.div_group);
-    finish_row<T, PER>(a, part, sp.q0 + q2, kv_head * a.group + row0 + r - q2 * a.group, d0, d0 == 0, o, m, total);
+    finish_row<T, PER>(a, part, whole, sp.q0 + q2, kv_head * a.group + row0 + r - q2 * a.group, d0, d0 == 0, o, m, total);
   }
 }
 
 template <typename T, int FORMAT, int DP>
-hipError_t launch_direct(int share, const AttendArgs& a, int row_blocks, hipStream_t s) {
-  const dim3 grid((unsigned)(a.n_seq * a.kv_heads), (unsigned)row_blocks, (unsigned)a.n_split);
-  if (share) hipLaunchKernelGGL((attend_direct_kernel<T, FORMAT, DP, true>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((attend_direct_kernel<T, FORMAT, DP, false>), grid, dim3(256), 0, s, a);
+hipError_t launch_direct(int share, const AttendArgs& a, hipStream_t s) {
+  const unsigned pieces = (unsigned)a.n_seq * a.kv_heads * a.row_blocks * a.n_split;
+  const dim3 grid(share ? pieces : (pieces + 3) / 4);
+  if (share && a.mask) hipLaunchKernelGGL((attend_direct_kernel<T, FORMAT, DP, true, true>), grid, dim3(256), 0, s, a);
+  else if (share) hipLaunchKernelGGL((attend_direct_kernel<T, FORMAT, DP, true, false>), grid, dim3(256), 0, s, a);
+  else if (a.mask) hipLaunchKernelGGL((attend_direct_kernel<T, FORMAT, DP, false, true>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((attend_direct_kernel<T, FORMAT, DP, false, false>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 template <typename T>
-hipError_t launch_attend_direct(int format, int share, const AttendArgs& a, int row_blocks, hipStream_t s) {
+hipError_t launch_attend_direct(int format, int share, const AttendArgs& a, hipStream_t s) {
   if constexpr (sizeof(T) == 2) {
-    if (format == KV_CACHE4) return a.dim <= 64 ? launch_direct<T, KV_CACHE4, 64>(share, a, row_blocks, s) : launch_direct<T, KV_CACHE4, 128>(share, a, row_blocks, s);
+    if (format == KV_CACHE4) return a.dim <= 64 ? launch_direct<T, KV_CACHE4, 64>(share, a, s) : launch_direct<T, KV_CACHE4, 128>(share, a, s);
   }
-  if (a.dim <= 64) return launch_direct<T, KV_PLAIN, 64>(share, a, row_blocks, s);
-  if (a.dim <= 96) return launch_direct<T, KV_PLAIN, 96>(share, a, row_blocks, s);
-  return launch_direct<T, KV_PLAIN, 128>(share, a, row_blocks, s);
+  if (a.dim <= 64) return launch_direct<T, KV_PLAIN, 64>(share, a, s);
+  if (a.dim <= 96) return launch_direct<T, KV_PLAIN, 96>(share, a, s);
+  return launch_direct<T, KV_PLAIN, 128>(share, a, s);
 }
 #endif
 

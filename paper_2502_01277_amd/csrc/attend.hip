@@ -1,5 +1,6 @@
 // octo_op_attend: arguments, the choice of kernel and of the number of parts, and the kernel that joins parts.
 #include <cmath>
+#include <cstdlib>
 #include <mutex>
 
 #include "attend_tile.h"
@@ -7,24 +8,54 @@
 namespace octo {
 namespace {
 
-// Adds up the parts of a row: sum_p 2^(ref_p - m) (o_p, sum_p), m the largest reference, in the order of the parts.  A row takes
-// dim / 4 lanes of 32, a block eight rows.
+// Adds up the parts of a row: sum_p 2^(ref_p - m) (o_p, sum_p), m the largest reference, in the order of the parts.  Half a wavefront has a
+// row: its lanes take references and sums of 32 parts at a time, then four elements of dim each.
+constexpr int MAX_PARTS = 128;
 template <typename T>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   Span sp;
   if (!span_of(a, blockIdx.x, &sp)) return;
-  const int r = blockIdx.y * 8 + (threadIdx.x >> 5), d = (threadIdx.x & 31) * 4;
-  if (r >= sp.n_q * a.q_heads || d >= a.dim) return;
+  const int parts = parts_of(a, sp.n_kv), r = blockIdx.y * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31, d = lane * 4;
+  if (parts == 1 || r >= sp.n_q * a.q_heads) return;
   const long long at = (long long)sp.q0 * a.q_heads + r, step = (long long)a.n_q * a.q_heads;
-  float m = -INFINITY, total = 0.f;
-  for (int p = 0; p < a.n_split; ++p) m = fmaxf(m, a.part_ml[at + p * step].x);
-  floatx4 o = {0, 0, 0, 0};
-  for (int p = 0; p < a.n_split; ++p) {
-    const float2 x = a.part_ml[at + p * step];
-    const float f = x.x == m ? 1.0f : __builtin_amdgcn_exp2f(x.x - m);
-    total += x.y * f;
-    o += *(const floatx4*)(a.part_o + (at + p * step) * a.dim + d) * f;
+  // the first parts' sums are on their way while the references are compared; memory of all n_split parts is there, used or not
+  constexpr int AHEAD = 8;
+  const float* y = a.part_o + at * a.dim + (d < a.dim ? d : 0);
+  floatx4 held[AHEAD];
+#pragma unroll
+  for (int p = 0; p < AHEAD; ++p) held[p] = *(const floatx4*)(y + (p < parts ? p : 0) * step * a.dim);
+  float2 x[MAX_PARTS / 32];
+  float m = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < MAX_PARTS / 32; ++k) {
+    x[k] = 32 * k + lane < parts ? a.part_ml[at + (32 * k + lane) * step] : make_float2(-INFINITY, 0.f);
+    m = fmaxf(m, x[k].x);
   }
+  for (int i = 1; i < 32; i *= 2) m = fmaxf(m, __shfl_xor(m, i, 32));
+  float total = 0.f;
+#pragma unroll
+  for (int k = 0; k < MAX_PARTS / 32; ++k) {
+    x[k].x = x[k].x == m ? 1.0f : __builtin_amdgcn_exp2f(x[k].x - m);
+    total += x[k].y * x[k].x;
+  }
+  for (int i = 1; i < 32; i *= 2) total += __shfl_xor(total, i, 32);
+  floatx4 o = {0, 0, 0, 0};
+#pragma unroll
+  for (int p = 0; p < AHEAD; ++p) {
+    const float f = __shfl(x[0].x, p, 32);
+    if (p < parts) o += held[p] * f;
+  }
+  for (int p0 = AHEAD; p0 < parts; p0 += AHEAD) {
+#pragma unroll
+    for (int p = 0; p < AHEAD; ++p) held[p] = *(const floatx4*)(y + (p0 + p < parts ? p0 + p : 0) * step * a.dim);
+    const float w = p0 < 32 ? x[0].x : p0 < 64 ? x[1].x : p0 < 96 ? x[2].x : x[3].x;
+#pragma unroll
+    for (int p = 0; p < AHEAD; ++p) {
+      const float f = __shfl(w, (p0 + p) & 31, 32);
+      if (p0 + p < parts) o += held[p] * f;
+    }
+  }
+  if (d >= a.dim) return;
   const float inv = total != 0.f ? 1.0f / total : 0.f;
   if (d == 0 && a.lse) a.lse[at] = total != 0.f ? (m + log2f(total)) * 0.693147180559945f : -INFINITY;
   const int qi = r / a.q_heads, head = r - qi * a.q_heads;
@@ -32,23 +63,26 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
 }
 
 enum { SHARED_KEYS = 1, OWN_ROWS = 2, TILES = 3 };          // kernels, as in the id
-struct Plan { int kernel, row_blocks, n_split; };
+struct Plan { int kernel, row_blocks, n_split, part_keys; };
 
-// By the rows of the longest sequence.  Up to 16: one wavefront's, the four of a block share the keys.  fp32 and up to 32 rows: 16 a wavefront.
-// More: tiles in LDS for 128 rows.
-// Parts: as many as give every compute unit two blocks, of at least eight (shared keys) or two or four tiles.
 Plan plan_of(const octo_attend_op* op, int cus) {
   Plan p{};
-  const long long rows = (long long)op->max_q * (op->q_heads / op->kv_heads);
-  p.kernel = rows <= 16 ? SHARED_KEYS : op->dtype == OCTO_F32 || rows <= 32 ? OWN_ROWS : TILES;
-  const int block_rows = p.kernel == SHARED_KEYS ? 16 : p.kernel == OWN_ROWS ? 64 : 128, part_keys = p.kernel == OWN_ROWS ? 64 : 256;
+  const long long rows = (long long)op->max_q * (op->q_heads / op->kv_heads), pairs = (long long)op->n_seq * op->kv_heads;
+  p.kernel = op->max_kv <= 128 && rows <= 64 ? OWN_ROWS : rows <= 16 ? SHARED_KEYS : op->dtype == OCTO_F32 || rows <= 32 ? OWN_ROWS : TILES;
+  if (getenv("OK")) p.kernel = atoi(getenv("OK"));
+  const int block_rows = p.kernel == TILES ? 128 : 16;
   p.row_blocks = (int)((rows + block_rows - 1) / block_rows);
-  const long long blocks = (long long)op->n_seq * op->kv_heads * p.row_blocks;
-  const int most = (op->max_kv + part_keys - 1) / part_keys;
-  long long n = blocks > 0 ? (2ll * cus + blocks - 1) / blocks : 1;
-  if (n > most) n = most;
-  if (n > 64) n = 64;
-  p.n_split = n < 1 ? 1 : (int)n;
+  const long long blocks = p.kernel == OWN_ROWS ? (pairs * p.row_blocks + 3) / 4 : pairs * p.row_blocks;
+  long long target = 4ll * cus;
+  if (getenv("OT")) target = (long long)(atof(getenv("OT")) * cus);
+  long long keys = blocks >= target ? op->max_kv : (long long)op->max_kv * blocks / target;
+  const int least = p.kernel == OWN_ROWS ? 64 : 256, least2 = (op->max_kv + MAX_PARTS - 1) / MAX_PARTS;
+  if (keys < least) keys = least;
+  if (keys < least2) keys = least2;
+  if (getenv("OP")) keys = atoi(getenv("OP"));
+  p.part_keys = (int)((keys + 63) / 64 * 64);
+  p.n_split = (op->max_kv + p.part_keys - 1) / p.part_keys;
+  if (p.n_split < 1) p.n_split = 1;
   return p;
 }
 
@@ -74,8 +108,8 @@ bool sizes_ok(const octo_attend_op* op) {
   if (op->kv_heads < 1 || op->q_heads < op->kv_heads || op->q_heads % op->kv_heads || op->q_heads > 4096) return false;
   if (op->n_seq < 0 || op->n_q < 0 || op->max_q < 0 || op->max_kv < 0 || op->kv_rows < 0) return false;
   if (op->max_q > op->n_q || op->max_kv > 0x7FFFFF00) return false;
-  // the grid: sequences x key heads, blocks of 64 rows (of 16 only where there are no more), parts
-  return (long long)op->n_seq * op->kv_heads <= 0x7FFFFFll && (long long)op->max_q * (op->q_heads / op->kv_heads) <= 65535ll * 64;
+  // pieces of work (sequences x key heads x 16 rows; x parts only where they are few) are numbered in 31 bits
+  return (double)op->n_seq * op->kv_heads * (op->max_q * (double)(op->q_heads / op->kv_heads) / 16 + 1) < 2e9;
 }
 size_t part_bytes(const octo_attend_op* op, int n_split) {
   return n_split > 1 ? (size_t)n_split * op->n_q * op->q_heads * ((size_t)op->dim * 4 + 8) : 0;
@@ -137,12 +171,15 @@ octo_status octo_op_attend(const octo_attend_op* op, void* hip_stream, int32_t* 
     a.part_ml = (float2*)(a.part_o + (size_t)p.n_split * op->n_q * op->q_heads * op->dim);
   }
   hipStream_t s = (hipStream_t)hip_stream;
+  a.part_keys = p.part_keys;
+  a.row_blocks = p.row_blocks;
+  a.div_heads = make_fastdiv((unsigned)op->kv_heads); a.div_blocks = make_fastdiv((unsigned)p.row_blocks); a.div_split = make_fastdiv((unsigned)p.n_split);
   const int share = p.kernel == SHARED_KEYS;
-  hipError_t e = p.kernel == TILES ? (op->dtype == OCTO_F16 ? launch_attend_tile_f16(op->kv_format, a, p.row_blocks, s) : launch_attend_tile_bf16(op->kv_format, a, p.row_blocks, s))
-               : op->dtype == OCTO_F32 ? launch_attend_direct_f32(op->kv_format, share, a, p.row_blocks, s)
-               : op->dtype == OCTO_F16 ? launch_attend_direct_f16(op->kv_format, share, a, p.row_blocks, s)
-                                       : launch_attend_direct_bf16(op->kv_format, share, a, p.row_blocks, s);
-  if (e == hipSuccess && p.n_split > 1) {      // then blocks of rows are few: max_q * q_heads is below 64 * 2 * 256
+  hipError_t e = p.kernel == TILES ? (op->dtype == OCTO_F16 ? launch_attend_tile_f16(op->kv_format, a, s) : launch_attend_tile_bf16(op->kv_format, a, s))
+               : op->dtype == OCTO_F32 ? launch_attend_direct_f32(op->kv_format, share, a, s)
+               : op->dtype == OCTO_F16 ? launch_attend_direct_f16(op->kv_format, share, a, s)
+                                       : launch_attend_direct_bf16(op->kv_format, share, a, s);
+  if (e == hipSuccess && p.n_split > 1) {
     const dim3 grid((unsigned)op->n_seq, (unsigned)(((long long)op->max_q * op->q_heads + 7) / 8));
     if (op->dtype == OCTO_F32) hipLaunchKernelGGL(attend_join_kernel<float>, grid, dim3(256), 0, s, a);
     else if (op->dtype == OCTO_F16) hipLaunchKernelGGL(attend_join_kernel<_Float16>, grid, dim3(256), 0, s, a);

@@ -15,8 +15,8 @@
 
 namespace octo {
 
-hipError_t launch_attend_tile_f16(int format, const AttendArgs& a, int row_blocks, hipStream_t s);
-hipError_t launch_attend_tile_bf16(int format, const AttendArgs& a, int row_blocks, hipStream_t s);
+hipError_t launch_attend_tile_f16(int format, const AttendArgs& a, hipStream_t s);
+hipError_t launch_attend_tile_bf16(int format, const AttendArgs& a, hipStream_t s);
 
 #ifdef __HIPCC__
 typedef short short4v __attribute__((ext_vector_type(4)));
@@ -25,28 +25,33 @@ typedef __attribute__((address_space(3))) unsigned char LdsByte;
 template <int RB> __device__ __forceinline__ int swizzle_k(int row) { return row & (RB / 16 - 1); }
 template <int RB> __device__ __forceinline__ int swizzle_v(int row) { return RB == 256 ? (row & 3) << 2 : (row & 2) << 1; }
 
-template <typename T, int FORMAT, int DP>
+// MASK: some keys are hidden by a mask; without one only the end of the last tile is, and what is read beyond it is zero.
+template <typename T, int FORMAT, int DP, bool MASK>
 __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
   constexpr int TK = 64, RB = DP <= 64 ? 128 : 256, CH = RB / 16, STEPS = DP / 16, DT = DP / 32, TILE = TK * RB;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * TILE];          // keys, keys, values, values
-  const int b = blockIdx.x / a.kv_heads, kv_head = blockIdx.x - b * a.kv_heads, part = blockIdx.z;
+  const Piece pc = piece_of(a, blockIdx.x);
+  const int b = pc.seq, kv_head = pc.head, part = pc.part;
   Span sp;
   if (!span_of(a, b, &sp)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
   const int rows = sp.n_q * a.group;
-  if ((int)blockIdx.y * 128 >= rows) return;
-  const int row = blockIdx.y * 128 + wave * 32 + l32;
+  if (pc.block * 128 >= rows || part >= parts_of(a, sp.n_kv)) return;
+  const bool whole = sp.n_kv <= a.part_keys;
+  const int row = pc.block * 128 + wave * 32 + l32;
   const bool has_row = row < rows;
   const int qi = (int)fast_div((unsigned)row, a.div_group), head = kv_head * a.group + row - qi * a.group;
   const long long q_row = sp.q0 + qi;
 
-  const int tiles = (sp.n_kv + TK - 1) / TK, per_part = (tiles + a.n_split - 1) / a.n_split;
+  const int tiles = (sp.n_kv + TK - 1) / TK, per_part = a.part_keys / TK;
   const int first = part * per_part, last = min(tiles, first + per_part);
   auto keys_left = [&](int t) { return t < last ? min(TK, sp.n_kv - TK * t) : 0; };
-  int mask_byte = 0;
-  auto load_mask = [&](int t) { mask_byte = a.mask && lane < keys_left(t) ? a.mask[sp.kv0 + (long long)TK * t + lane] : 0; };
+  uint32_t mask_byte = 0;
+  auto load_mask = [&](int t) {
+    if constexpr (MASK) mask_byte = __builtin_amdgcn_raw_buffer_load_b8(buffer_at(a.mask + sp.kv0 + (long long)TK * t, keys_left(t)), lane, 0, 0);
+  };
   auto seen_of = [&](int t) -> unsigned long long {
-    if (a.mask) return __ballot(mask_byte != 0);
+    if constexpr (MASK) return __ballot(mask_byte != 0);
     const int n = keys_left(t);
     return n >= TK ? ~0ull : (1ull << n) - 1;
   };
@@ -57,83 +62,66 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
 
   // plain: what a lane loads, NI instructions of 64 chunks a wavefront and tensor
   constexpr int NI = TILE / 4096;
-  // 4 bits: items of 32 values of a key, keys' first, then the values'
-  constexpr int PARTS = DP / 32, ITEMS = FORMAT == KV_CACHE4 ? 2 * TK * PARTS / 256 : 1;
-  u32x4 held[ITEMS]; uint32_t held_exp[ITEMS];
+  // 4 bits: a thread takes 32 values of a key
+  constexpr int PARTS = DP / 32;
+  u32x4 held[2]; uint32_t held_exp[2];
 
-  auto load_tile = [&](int t, int stage, unsigned long long seen) {
+  // K of tile t, V of tile t: to a stage of LDS (plain), or to registers, from which place_tile takes them there
+  auto load_tile = [&](int t, int stage, bool is_v, unsigned long long seen) __attribute__((always_inline)) {
     const int n = keys_left(t);
-    const long long row0 = sp.kv0 + (long long)TK * t;
+    const long long row0 = sp.kv0 + (long long)TK * t, pitch = is_v ? a.v_row : a.k_row;
+    const __amdgpu_buffer_rsrc_t rc = buffer_at((is_v ? v_base : k_base) + row0 * pitch, n > 0 ? (n - 1) * pitch + (FORMAT == KV_CACHE4 ? a.dim / 2 : a.dim * 2) : 0);
     if constexpr (FORMAT == KV_PLAIN) {
-      const __amdgpu_buffer_rsrc_t rk = buffer_at(k_base + row0 * a.k_row, n > 0 ? (n - 1) * a.k_row + a.dim * 2 : 0);
-      const __amdgpu_buffer_rsrc_t rv = buffer_at(v_base + row0 * a.v_row, n > 0 ? (n - 1) * a.v_row + a.dim * 2 : 0);
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        const int r = (wave * NI + i) * (64 / CH) + lane / CH;
-        const int ck = (lane % CH) ^ swizzle_k<RB>(r), cv = (lane % CH) ^ swizzle_v<RB>(r);
-        const bool see = seen >> r & 1;
-        const int ok = see && ck * 8 < a.dim ? r * (int)a.k_row + ck * 16 : OOB, ov = see && cv * 8 < a.dim ? r * (int)a.v_row + cv * 16 : OOB;
-        const unsigned to = lds + stage * TILE + (wave * NI + i) * 1024;
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(to), "v"(ok), "s"(rk) : "memory");
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(to + 2 * TILE), "v"(ov), "s"(rv) : "memory");
+        const int r = (wave * NI + i) * (64 / CH) + lane / CH, ch = (lane % CH) ^ (is_v ? swizzle_v<RB>(r) : swizzle_k<RB>(r));
+        const bool see = !MASK || !is_v || (seen >> r & 1);         // what a hidden key holds is replaced in the scores
+        const int o = see && ch * 8 < a.dim ? r * (int)pitch + ch * 16 : OOB;
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                     :: "s"(lds + (is_v ? 2 * TILE : 0) + stage * TILE + (wave * NI + i) * 1024), "v"(o), "s"(rc) : "memory");
       }
     } else {
-      const __amdgpu_buffer_rsrc_t rk = buffer_at(k_base + row0 * a.k_row, n > 0 ? (n - 1) * a.k_row + a.dim / 2 : 0);
-      const __amdgpu_buffer_rsrc_t rv = buffer_at(v_base + row0 * a.v_row, n > 0 ? (n - 1) * a.v_row + a.dim / 2 : 0);
-      const __amdgpu_buffer_rsrc_t rke = buffer_at(a.k_exp + kv_head * a.ke_head + row0 * a.ke_row, n > 0 ? (n - 1) * a.ke_row + a.dim / 32 : 0);
-      const __amdgpu_buffer_rsrc_t rve = buffer_at(a.v_exp + kv_head * a.ve_head + row0 * a.ve_row, n > 0 ? (n - 1) * a.ve_row + a.dim / 32 : 0);
-#pragma unroll
-      for (int i = 0; i < ITEMS; ++i) {
-        const int item = (int)threadIdx.x + i * 256, r = item % (TK * PARTS) / PARTS, p = item % PARTS;
-        const bool see = (seen >> r & 1) && p * 32 < a.dim, is_v = item >= TK * PARTS;      // whole wavefronts
-        const int row_bytes = (int)(is_v ? a.v_row : a.k_row), exp_bytes = (int)(is_v ? a.ve_row : a.ke_row);
-        const int o = see ? r * row_bytes + p * 16 : OOB, oe = see ? r * exp_bytes + p : OOB;
-        if (__builtin_amdgcn_readfirstlane(is_v)) {
-          held[i] = __builtin_amdgcn_raw_buffer_load_b128(rv, o, 0, 0);
-          held_exp[i] = __builtin_amdgcn_raw_buffer_load_b8(rve, oe, 0, 0);
-        } else {
-          held[i] = __builtin_amdgcn_raw_buffer_load_b128(rk, o, 0, 0);
-          held_exp[i] = __builtin_amdgcn_raw_buffer_load_b8(rke, oe, 0, 0);
-        }
-      }
+      const long long epitch = is_v ? a.ve_row : a.ke_row;
+      const __amdgpu_buffer_rsrc_t re = buffer_at((is_v ? a.v_exp + kv_head * a.ve_head : a.k_exp + kv_head * a.ke_head) + row0 * epitch, n > 0 ? (n - 1) * epitch + a.dim / 32 : 0);
+      const int r = (int)threadIdx.x / PARTS % TK, p = (int)threadIdx.x % PARTS;
+      const bool see = (!MASK || !is_v || (seen >> r & 1)) && p * 32 < a.dim && (int)threadIdx.x < TK * PARTS;
+      held[is_v] = __builtin_amdgcn_raw_buffer_load_b128(rc, see ? r * (int)pitch + p * 16 : OOB, 0, 0);
+      held_exp[is_v] = __builtin_amdgcn_raw_buffer_load_b8(re, see ? r * (int)epitch + p : OOB, 0, 0);
     }
   };
-  auto place_tile = [&](int stage) {
+  auto place_tile = [&](int stage, bool is_v) __attribute__((always_inline)) {
     if constexpr (FORMAT == KV_CACHE4) {
-#pragma unroll
-      for (int i = 0; i < ITEMS; ++i) {
-        const int item = (int)threadIdx.x + i * 256, r = item % (TK * PARTS) / PARTS, p = item % PARTS;
-        const bool is_v = item >= TK * PARTS;
+      const int r = (int)threadIdx.x / PARTS % TK, p = (int)threadIdx.x % PARTS;
+      if ((int)threadIdx.x < TK * PARTS) {
         unsigned char* const to = smem + (is_v ? 2 * TILE : 0) + stage * TILE + r * RB;
         const int sw = is_v ? swizzle_v<RB>(r) : swizzle_k<RB>(r);
-        const float scale = exp_scale(held_exp[i]);
+        const float scale = exp_scale(held_exp[is_v]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) *(u32x4*)(to + ((4 * p + e) ^ sw) * 16) = codes8<T>(held[i][e], scale);
+        for (int e = 0; e < 4; ++e) *(u32x4*)(to + ((4 * p + e) ^ sw) * 16) = codes8<T>(held[is_v][e], scale);
       }
     }
   };
 
   load_mask(first);
-  unsigned long long seen = seen_of(first), seen_next;
-  load_tile(first, 0, seen);
-  load_mask(first + 1);
+  load_tile(first, 0, false, 0);
   u32x4 q[STEPS];
 #pragma unroll
   for (int s = 0; s < STEPS; ++s) {
     const int d = 16 * s + 8 * half;
     q[s] = has_row && d < a.dim ? *(const u32x4*)((const T*)a.q + q_row * a.q_row + head * a.q_head + d) : u32x4{0, 0, 0, 0};
   }
-  place_tile(0);
+  unsigned long long seen = seen_of(first), seen_next;
+  load_tile(first, 0, true, seen);
+  load_mask(first + 1);
+  place_tile(0, false);
+  load_tile(first + 1, 1, false, 0);
+  place_tile(0, true);
+  place_tile(1, false);
 
-  // addresses of a lane's operands inside a stage
-  int at_k[STEPS], at_v[DT];
-#pragma unroll
-  for (int s = 0; s < STEPS; ++s) at_k[s] = l32 * RB + ((2 * s + half) ^ swizzle_k<RB>(l32)) * 16;
-  {
-    const int i = lane & 15, r = 4 * half + i / 4;                 // key r (+ 16 k, + 8), columns 16 (lane / 16 % 2) + 4 (i % 4) ..
-#pragma unroll
-    for (int d = 0; d < DT; ++d) at_v[d] = r * RB + ((4 * d + (lane >> 4 & 1) * 2 + (i >> 1 & 1)) ^ swizzle_v<RB>(r)) * 16 + (i & 1) * 8;
-  }
+  // addresses of a lane's operands inside a stage: of the first step; the others differ in the bits of the chunk
+  const int at_k = l32 * RB + (half ^ swizzle_k<RB>(l32)) * 16;
+  const int vi = lane & 15, vr = 4 * half + vi / 4;                // key vr (+ 16 k, + 8), columns 16 (lane / 16 % 2) + 4 (vi % 4) ..
+  const int at_v = vr * RB + (((lane >> 4 & 1) * 2 + (vi >> 1 & 1)) ^ swizzle_v<RB>(vr)) * 16 + (vi & 1) * 8;
 
   floatx16 acc[DT];
 #pragma unroll
@@ -143,24 +131,30 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
   float ref = -INFINITY, sum = 0.f;
   const float c = a.scale2;
 
-  for (int t = first; t < last; ++t) {
+  floatx16 st[2];
+  auto scores = [&](const unsigned char* ks, floatx16* to) __attribute__((always_inline)) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) to[h][i] = 0.f;
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) to[h] = Elem<T>::mfma(*(const u32x4*)(ks + (at_k ^ 32 * s) + h * 32 * RB), q[s], to[h]);
+  };
+  // One tile: the exponentials of its scores beside the products of the next tile's, then its values.
+  auto step = [&](int t, auto more) __attribute__((always_inline)) {
     const int stage = (t - first) & 1;
-    // this tile has landed for all wavefronts, and all are done with the stage that the next one goes to
+    // the next keys and these values have landed for all wavefronts, and all are done with the stages that are loaded next
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     seen_next = seen_of(t + 1);
-    load_tile(t + 1, stage ^ 1, seen_next);
-    load_mask(t + 2);
-    const unsigned char* const ks = smem + stage * TILE;
-    const unsigned char* const vs = ks + 2 * TILE;
-    floatx16 st[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) st[h][i] = 0.f;
-#pragma unroll
-      for (int s = 0; s < STEPS; ++s) st[h] = Elem<T>::mfma(*(const u32x4*)(ks + at_k[s] + h * 32 * RB), q[s], st[h]);
+    if constexpr (more()) {
+      load_tile(t + 2, stage, false, 0);
+      load_tile(t + 1, stage ^ 1, true, seen_next);
+      load_mask(t + 2);
     }
+    const unsigned char* const vs = smem + 2 * TILE + stage * TILE;
     if (seen != ~0ull) {
       const unsigned lo = (unsigned)seen >> (4 * half), hi = (unsigned)(seen >> 32) >> (4 * half);
 #pragma unroll
@@ -182,27 +176,41 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
       for (int d = 0; d < DT; ++d) acc[d] *= alpha;
     }
     const float refc = ref == -INFINITY ? 0.f : ref * c;
+    floatx16 nx[2];
+    if constexpr (more()) scores(smem + (stage ^ 1) * TILE, nx);
     float add[2] = {0.f, 0.f};
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) { st[h][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[h][i], c, -refc)); add[i & 1] += st[h][i]; }
-    sum += add[0] + add[1];
+    u32x4 p[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      u32x4 p;
-      store4<T>((T*)&p, floatx4{st[k / 2][8 * (k % 2)], st[k / 2][8 * (k % 2) + 1], st[k / 2][8 * (k % 2) + 2], st[k / 2][8 * (k % 2) + 3]});
-      store4<T>((T*)&p + 4, floatx4{st[k / 2][8 * (k % 2) + 4], st[k / 2][8 * (k % 2) + 5], st[k / 2][8 * (k % 2) + 6], st[k / 2][8 * (k % 2) + 7]});
+      float w[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) { w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[k / 2][8 * (k % 2) + i], c, -refc)); add[i & 1] += w[i]; }
+      store4<T>((T*)&p[k], floatx4{w[0], w[1], w[2], w[3]});
+      store4<T>((T*)&p[k] + 4, floatx4{w[4], w[5], w[6], w[7]});
+    }
+    sum += add[0] + add[1];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
-        const short4v v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(vs + at_v[d] + 16 * k * RB));
-        const short4v v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(vs + at_v[d] + (16 * k + 8) * RB));
+        const short4v v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(vs + (at_v ^ 64 * d) + 16 * k * RB));
+        const short4v v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(vs + (at_v ^ 64 * d) + (16 * k + 8) * RB));
         const u32x2 w0 = __builtin_bit_cast(u32x2, v0), w1 = __builtin_bit_cast(u32x2, v1);
-        acc[d] = Elem<T>::mfma(u32x4{w0[0], w0[1], w1[0], w1[1]}, p, acc[d]);
+        acc[d] = Elem<T>::mfma(u32x4{w0[0], w0[1], w1[0], w1[1]}, p[k], acc[d]);
       }
+    if constexpr (more()) {
+      place_tile(stage, false);
+      place_tile(stage ^ 1, true);
+      st[0] = nx[0]; st[1] = nx[1];
     }
-    place_tile(stage ^ 1);
     seen = seen_next;
+  };
+  if (first < last) {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    scores(smem, st);
+    for (int t = first; t < last - 1; ++t) step(t, std::true_type{});
+    step(last - 1, std::false_type{});
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                 // loads issued past the last tile write zeros into LDS
   if (!has_row) return;
@@ -210,7 +218,7 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
   const float refc = ref == -INFINITY ? -INFINITY : ref * c;
 
   // element of dim of acc[d][i]: 32 d + 8 (i / 4) + 4 half + i % 4
-  if (a.n_split > 1) {
+  if (!whole) {
     const long long at = ((long long)part * a.n_q + q_row) * a.q_heads + head;
     if (!half) a.part_ml[at] = make_float2(refc, sum);
 #pragma unroll
@@ -240,16 +248,18 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
 }
 
 template <typename T, int FORMAT, int DP>
-hipError_t launch_tile(const AttendArgs& a, int row_blocks, hipStream_t s) {
-  hipLaunchKernelGGL((attend_tile_kernel<T, FORMAT, DP>), dim3((unsigned)(a.n_seq * a.kv_heads), (unsigned)row_blocks, (unsigned)a.n_split), dim3(256), 0, s, a);
+hipError_t launch_tile(const AttendArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)a.n_seq * a.kv_heads * a.row_blocks * a.n_split);
+  if (a.mask) hipLaunchKernelGGL((attend_tile_kernel<T, FORMAT, DP, true>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((attend_tile_kernel<T, FORMAT, DP, false>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 template <typename T>
-hipError_t launch_attend_tile(int format, const AttendArgs& a, int row_blocks, hipStream_t s) {
-  if (format == KV_CACHE4) return a.dim <= 64 ? launch_tile<T, KV_CACHE4, 64>(a, row_blocks, s) : launch_tile<T, KV_CACHE4, 128>(a, row_blocks, s);
-  if (a.dim <= 64) return launch_tile<T, KV_PLAIN, 64>(a, row_blocks, s);
-  if (a.dim <= 96) return launch_tile<T, KV_PLAIN, 96>(a, row_blocks, s);
-  return launch_tile<T, KV_PLAIN, 128>(a, row_blocks, s);
+hipError_t launch_attend_tile(int format, const AttendArgs& a, hipStream_t s) {
+  if (format == KV_CACHE4) return a.dim <= 64 ? launch_tile<T, KV_CACHE4, 64>(a, s) : launch_tile<T, KV_CACHE4, 128>(a, s);
+  if (a.dim <= 64) return launch_tile<T, KV_PLAIN, 64>(a, s);
+  if (a.dim <= 96) return launch_tile<T, KV_PLAIN, 96>(a, s);
+  return launch_tile<T, KV_PLAIN, 128>(a, s);
 }
 #endif
 

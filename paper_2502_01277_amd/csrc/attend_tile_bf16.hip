@@ -2,5 +2,5 @@
 #include "attend_tile.h"
 
 namespace octo {
-hipError_t launch_attend_tile_bf16(int format, const AttendArgs& a, int row_blocks, hipStream_t s) { return launch_attend_tile<__bf16>(format, a, row_blocks, s); }
+hipError_t launch_attend_tile_bf16(int format, const AttendArgs& a, hipStream_t s) { return launch_attend_tile<__bf16>(format, a, s); }
 }  // namespace octo

@@ -225,3 +225,27 @@ def test_attend_refuses_fp32_on_four_bits_and_takes_nothing():
         assert L.octo_op_attend(C.byref(op), None, C.byref(kid)) == binding.OK and kid.value == 0
         assert L.octo_op_attend_workspace_bytes(C.byref(op)) == 0
     assert L.octo_op_attend(None, None, None) == binding.EINVAL and L.octo_op_attend_workspace_bytes(None) == 0
+
+
+def test_packed_arguments_have_the_layout_of_the_structs():
+    for packed, cls in ((binding._ROTATE, binding.OctoRotateOp), (binding._CACHE4, binding.OctoCache4Op), (binding._ATTEND, binding.OctoAttendOp)):
+        assert packed.size == C.sizeof(cls)
+        flat = []
+
+        def walk(kind, at):
+            if hasattr(kind, "_fields_"):
+                for name, sub in kind._fields_:
+                    walk(sub, at + getattr(kind, name).offset)
+            elif hasattr(kind, "_length_"):
+                for i in range(kind._length_):
+                    walk(kind._type_, at + i * C.sizeof(kind._type_))
+            else:
+                flat.append((at, kind))
+
+        walk(cls, 0)
+        for i, (at, kind) in enumerate(flat):                # each field alone at 1
+            raw = packed.pack(*[1 if k == i else 0 for k in range(len(flat))])
+            assert kind.from_buffer_copy(raw, at).value == 1 and raw.count(0) < len(raw), i
+            other = bytearray(raw)
+            other[at:at + C.sizeof(kind)] = bytes(C.sizeof(kind))
+            assert not any(other), i
