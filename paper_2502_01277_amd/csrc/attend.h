@@ -31,6 +31,7 @@ struct AttendArgs {
   int n_split, part_keys;                                              // parts of part_keys keys (a multiple of 64); sequences of one part are finished by its block
   int row_blocks;                                                      // of the kernel's rows, of the longest sequence
   FastDiv div_heads, div_blocks, div_split;                            // kv_heads, row_blocks, n_split
+  int by_die;                                                          // blocks that read the same keys run on one die
 };
 
 enum { KV_PLAIN = OCTO_KV_PLAIN, KV_CACHE4 = OCTO_KV_CACHE4 };
@@ -44,14 +45,21 @@ typedef uint32_t u32x3 __attribute__((ext_vector_type(3)));
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-// The n-th piece of work: key heads first (the blocks of one head next to each other for one die's cache where there are eight), then blocks of
-// rows, parts, and sequences last: neighbours are alike in length, so that a short sequence's pieces do not all leave the same units idle.
+// The n-th piece of work.  Blocks of rows that read the same keys come one after the other, on one die (every eighth block runs there) where
+// the sets of keys share out evenly over the eight, so that its cache has the keys for all of them; then come key heads, parts, and sequences last: neighbours are
+// alike in length, and a short sequence's pieces do not all leave the same units idle.
 struct Piece { int seq, part, block, head; };
-__device__ __forceinline__ Piece piece_of(const AttendArgs& a, unsigned n) {
+__device__ __forceinline__ Piece piece_of(const AttendArgs& a, unsigned n, bool by_die) {
   Piece p;
-  const unsigned x = fast_div(n, a.div_heads), y = fast_div(x, a.div_blocks), z = fast_div(y, a.div_split);
-  p.head = (int)(n - x * (unsigned)a.kv_heads); p.block = (int)(x - y * (unsigned)a.row_blocks); p.part = (int)(y - z * (unsigned)a.n_split); p.seq = (int)z;
+  const unsigned q = by_die ? n >> 3 : n, r = fast_div(q, a.div_blocks);
+  const unsigned w = by_die ? r * 8 + (n & 7) : r, y = fast_div(w, a.div_heads), z = fast_div(y, a.div_split);
+  p.block = (int)(q - r * (unsigned)a.row_blocks); p.head = (int)(w - y * (unsigned)a.kv_heads); p.part = (int)(y - z * (unsigned)a.n_split); p.seq = (int)z;
   return p;
+}
+// blocks to start for pieces of a block each
+__host__ inline unsigned piece_blocks(const AttendArgs& a) {
+  const unsigned sets = (unsigned)a.n_seq * a.kv_heads * a.n_split;
+  return (a.by_die ? (sets + 7) / 8 * 8 : sets) * a.row_blocks;
 }
 
 struct Span { int q0, n_q, n_kv; long long kv0; };
@@ -283,7 +291,7 @@ __global__ __launch_bounds__(256, 2) void attend_direct_kernel(AttendArgs a) {
   constexpr int STEPS = DP / 32, PER = DP / 16, WAVES = SHARE ? 4 : 1;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
   // what a block (SHARE) or a wavefront does: 16 rows of a sequence and key head
-  const Piece pc = piece_of(a, SHARE ? blockIdx.x : blockIdx.x * 4 + wave);
+  const Piece pc = piece_of(a, SHARE ? blockIdx.x : blockIdx.x * 4 + wave, SHARE && a.by_die);
   const int b = pc.seq, kv_head = pc.head, part = pc.part, row0 = pc.block * 16;
   Span sp;
   if (b >= a.n_seq || !span_of(a, b, &sp)) return;
@@ -414,8 +422,7 @@ __global__ __launch_bounds__(256, 2) void attend_direct_kernel(AttendArgs a) {
 
 template <typename T, int FORMAT, int DP>
 hipError_t launch_direct(int share, const AttendArgs& a, hipStream_t s) {
-  const unsigned pieces = (unsigned)a.n_seq * a.kv_heads * a.row_blocks * a.n_split;
-  const dim3 grid(share ? pieces : (pieces + 3) / 4);
+  const dim3 grid(share ? piece_blocks(a) : ((unsigned)a.n_seq * a.kv_heads * a.row_blocks * a.n_split + 3) / 4);
   if (share && a.mask) hipLaunchKernelGGL((attend_direct_kernel<T, FORMAT, DP, true, true>), grid, dim3(256), 0, s, a);
   else if (share) hipLaunchKernelGGL((attend_direct_kernel<T, FORMAT, DP, true, false>), grid, dim3(256), 0, s, a);
   else if (a.mask) hipLaunchKernelGGL((attend_direct_kernel<T, FORMAT, DP, false, true>), grid, dim3(256), 0, s, a);

@@ -1,6 +1,6 @@
 // octo_op_attend: arguments, the choice of kernel and of the number of parts, and the kernel that joins parts.
+#include <algorithm>
 #include <cmath>
-#include <cstdlib>
 #include <mutex>
 
 #include "attend_tile.h"
@@ -65,24 +65,35 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
 enum { SHARED_KEYS = 1, OWN_ROWS = 2, TILES = 3 };          // kernels, as in the id
 struct Plan { int kernel, row_blocks, n_split, part_keys; };
 
+// Which kernel, by the rows of the longest sequence, the blocks of SHARED_KEYS (16 rows each) and their keys.
+//   OWN_ROWS where there are enough rows for all wavefronts and few keys to share: 512 sequences of 2 heads and 49 keys, dim 128, bf16, 8 / 16 / 32 / 40
+//     rows 9.7 / 11.4 / 15.0 / 18.6 us against 12.1 / 13.3 / 20.1 / 26.7 (SHARED_KEYS) and 14.1 / 14.5 / 15.3 / 16.2 (TILES); from 4 bits also 400 keys, 20 and 40
+//     rows: 22.7, 29.8 : 26.2, 36.1 : 31.6, 36.6; fp32, 400 keys, dim 64, 20 and 128 rows: 52.8, 154 : 63.6, 194.
+//   SHARED_KEYS for up to 16 rows, for all else in fp32, and where the whole call is short, as its wavefronts are quickly done: 4 sequences of 400 keys, 128 rows
+//     8.1 us against 12.9 (TILES); 64 x 400, 32, 64 and 96 rows: 10.6, 15.0, 19.9 : 13.0, 14.1, 15.0; 4 x 24000, 32 and 40 rows: 29.2, 43.0 : 36.1, 37.4; from
+//     4 bits, where TILES has conversions to do first, up to three times as far: 64 x 3000, 64 and 96 rows: 38.8, 50.3 : 41.7, 47.2.
+//   TILES for the rest: 64 x 3000, 128 rows 69 us against 144; 512 x 400: 65 against 163.
+// Parts of the keys: as many as give every compute unit two (SHARED_KEYS), four or three blocks (TILES), of at least 256 keys, and, where sequences may
+//   differ in length, up to eight blocks of 1024 or 2048 keys, for an even end: 16 single tokens over up to 51200 keys of 4 bits 131 -> 117 us.  With TILES the rows
+//   tell: as many as n_seq x max_q, then sequences are alike and more parts only cost (2 x 2048 queries over 12800 keys 790 us whole, 829 in two parts).
 Plan plan_of(const octo_attend_op* op, int cus) {
   Plan p{};
-  const long long rows = (long long)op->max_q * (op->q_heads / op->kv_heads), pairs = (long long)op->n_seq * op->kv_heads;
-  p.kernel = op->max_kv <= 128 && rows <= 64 ? OWN_ROWS : rows <= 16 ? SHARED_KEYS : op->dtype == OCTO_F32 || rows <= 32 ? OWN_ROWS : TILES;
-  if (getenv("OK")) p.kernel = atoi(getenv("OK"));
-  const int block_rows = p.kernel == TILES ? 128 : 16;
-  p.row_blocks = (int)((rows + block_rows - 1) / block_rows);
-  const long long blocks = p.kernel == OWN_ROWS ? (pairs * p.row_blocks + 3) / 4 : pairs * p.row_blocks;
-  long long target = 4ll * cus;
-  if (getenv("OT")) target = (long long)(atof(getenv("OT")) * cus);
-  long long keys = blocks >= target ? op->max_kv : (long long)op->max_kv * blocks / target;
-  const int least = p.kernel == OWN_ROWS ? 64 : 256, least2 = (op->max_kv + MAX_PARTS - 1) / MAX_PARTS;
-  if (keys < least) keys = least;
-  if (keys < least2) keys = least2;
-  if (getenv("OP")) keys = atoi(getenv("OP"));
-  p.part_keys = (int)((keys + 63) / 64 * 64);
-  p.n_split = (op->max_kv + p.part_keys - 1) / p.part_keys;
-  if (p.n_split < 1) p.n_split = 1;
+  const long long rows = (long long)op->max_q * (op->q_heads / op->kv_heads), pairs = (long long)op->n_seq * op->kv_heads, blocks16 = pairs * ((rows + 15) / 16);
+  const bool f32 = op->dtype == OCTO_F32, four_bits = op->kv_format == OCTO_KV_CACHE4;
+  const double work = (double)blocks16 * op->max_kv / cus;
+  if (blocks16 >= 4ll * cus && (f32 ? op->max_kv <= 512 : four_bits ? op->max_kv <= 512 && rows <= 48 : op->max_kv <= 128 && rows <= 32)) p.kernel = OWN_ROWS;
+  else if (f32 || rows <= 16 || work <= (four_bits ? 5500 : rows <= 32 ? 1700 : 600)) p.kernel = SHARED_KEYS;
+  else p.kernel = TILES;
+  const bool tiles = p.kernel == TILES;
+  p.row_blocks = (int)(tiles ? (rows + 127) / 128 : (rows + 15) / 16);
+  const long long blocks = p.kernel == OWN_ROWS ? (blocks16 + 3) / 4 : pairs * p.row_blocks;
+  const bool alike = tiles && op->n_q >= (long long)op->n_seq * op->max_q * 15 / 16;
+  auto parts = [&](int target, int least) { return blocks > 0 ? std::min<long long>((long long)target * cus / blocks, op->max_kv / least) : 1; };
+  long long n = parts(tiles ? 3 : p.kernel == SHARED_KEYS ? 2 : 4, 256);
+  if (!alike) n = std::max(n, parts(8, tiles ? 2048 : 1024));
+  n = std::max(1ll, std::min<long long>(n, MAX_PARTS));
+  p.part_keys = (int)((op->max_kv + n * 64 - 1) / (n * 64)) * 64;
+  p.n_split = op->max_kv > p.part_keys ? (op->max_kv + p.part_keys - 1) / p.part_keys : 1;
   return p;
 }
 
@@ -173,6 +184,8 @@ octo_status octo_op_attend(const octo_attend_op* op, void* hip_stream, int32_t* 
   hipStream_t s = (hipStream_t)hip_stream;
   a.part_keys = p.part_keys;
   a.row_blocks = p.row_blocks;
+  const long long sets = (long long)op->n_seq * op->kv_heads * p.n_split;
+  a.by_die = p.row_blocks > 1 && (sets % 8 == 0 || sets >= 64);
   a.div_heads = make_fastdiv((unsigned)op->kv_heads); a.div_blocks = make_fastdiv((unsigned)p.row_blocks); a.div_split = make_fastdiv((unsigned)p.n_split);
   const int share = p.kernel == SHARED_KEYS;
   hipError_t e = p.kernel == TILES ? (op->dtype == OCTO_F16 ? launch_attend_tile_f16(op->kv_format, a, s) : launch_attend_tile_bf16(op->kv_format, a, s))

@@ -30,16 +30,16 @@ template <typename T, int FORMAT, int DP, bool MASK>
 __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
   constexpr int TK = 64, RB = DP <= 64 ? 128 : 256, CH = RB / 16, STEPS = DP / 16, DT = DP / 32, TILE = TK * RB;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * TILE];          // keys, keys, values, values
-  const Piece pc = piece_of(a, blockIdx.x);
+  const Piece pc = piece_of(a, blockIdx.x, a.by_die);
   const int b = pc.seq, kv_head = pc.head, part = pc.part;
   Span sp;
-  if (!span_of(a, b, &sp)) return;
+  if (b >= a.n_seq || !span_of(a, b, &sp)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
   const int rows = sp.n_q * a.group;
   if (pc.block * 128 >= rows || part >= parts_of(a, sp.n_kv)) return;
   const bool whole = sp.n_kv <= a.part_keys;
   const int row = pc.block * 128 + wave * 32 + l32;
-  const bool has_row = row < rows;
+  const bool has_row = row < rows, busy = pc.block * 128 + wave * 32 < rows;      // a wavefront without rows loads and waits with the others
   const int qi = (int)fast_div((unsigned)row, a.div_group), head = kv_head * a.group + row - qi * a.group;
   const long long q_row = sp.q0 + qi;
 
@@ -155,6 +155,7 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
       load_mask(t + 2);
     }
     const unsigned char* const vs = smem + 2 * TILE + stage * TILE;
+    if (busy) {
     if (seen != ~0ull) {
       const unsigned lo = (unsigned)seen >> (4 * half), hi = (unsigned)(seen >> 32) >> (4 * half);
 #pragma unroll
@@ -198,10 +199,11 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
         const u32x2 w0 = __builtin_bit_cast(u32x2, v0), w1 = __builtin_bit_cast(u32x2, v1);
         acc[d] = Elem<T>::mfma(u32x4{w0[0], w0[1], w1[0], w1[1]}, p[k], acc[d]);
       }
+    if constexpr (more()) { st[0] = nx[0]; st[1] = nx[1]; }
+    }
     if constexpr (more()) {
       place_tile(stage, false);
       place_tile(stage ^ 1, true);
-      st[0] = nx[0]; st[1] = nx[1];
     }
     seen = seen_next;
   };
@@ -249,7 +251,7 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
 
 template <typename T, int FORMAT, int DP>
 hipError_t launch_tile(const AttendArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)a.n_seq * a.kv_heads * a.row_blocks * a.n_split);
+  const dim3 grid(piece_blocks(a));
   if (a.mask) hipLaunchKernelGGL((attend_tile_kernel<T, FORMAT, DP, true>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((attend_tile_kernel<T, FORMAT, DP, false>), grid, dim3(256), 0, s, a);
   return hipGetLastError();

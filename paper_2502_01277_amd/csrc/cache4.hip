@@ -2,7 +2,8 @@
 //
 // The bound is memory.  A lane takes eight values of a group of 32, four lanes the group: the largest magnitude comes from two
 // exchanges between neighbours, the exponent from its bits, the codes from the conversion instructions (E2M1 with a power-of-two scale, round to
-// nearest even, saturating).  Loads and stores are 16 and 4 bytes a lane, in the order of the states.
+// nearest even, saturating).  Loads and stores are 16 and 4 bytes a lane, in the order of the states.  What is read back from the cache goes past the
+// caches' reuse order (51200 tokens: 83 -> 57 us), what is stored does not (its lines are filled by several wavefronts).
 #include <cmath>
 #include <cstring>
 
@@ -45,14 +46,7 @@ __device__ __forceinline__ bool chunk_of(const Cache4Args& a, int* k, int* tok, 
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void cache4_store_kernel(Cache4Args a) {
-  int k, tok, head, chunk;
-  // the four lanes of a group come and go together: a group is one token and head
-  if (!chunk_of(a, &k, &tok, &head, &chunk)) return;
-  const long long slot = a.slots[tok];
-  if (slot < 0 || slot >= a.rows) return;
-  float v[8];
-  read8((const T*)a.x[k] + (long long)tok * a.token[k] + (long long)head * a.head[k] + chunk * 8, v);
+__device__ __forceinline__ void store_group(const octo_cache4_plane& p, const float* v, long long slot, int head, int chunk) {
   unsigned most = 0;                              // magnitudes compare as integers, infinities and NaN above all others
 #pragma unroll
   for (int e = 0; e < 8; ++e) most = max(most, __float_as_uint(v[e]) & 0x7FFFFFFFu);
@@ -67,9 +61,25 @@ __global__ __launch_bounds__(256) void cache4_store_kernel(Cache4Args a) {
   w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2], v[3], scale, 1);
   w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4], v[5], scale, 2);
   w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6], v[7], scale, 3);
-  const octo_cache4_plane& p = a.plane[k];
   *(unsigned*)(p.d_codes + slot * p.code_row + head * p.code_head + chunk * 4) = w;
   if ((chunk & 3) == 0) p.d_exps[slot * p.exp_row + head * p.exp_head + chunk / 4] = (uint8_t)(most >= 0x7F800000u ? 255 : e);
+}
+
+// A thread of the 16-bit types stores its chunk of both tensors: two loads in flight, one look at the slot (51200 tokens of 8 heads of 128, fp16:
+// 75 -> 64 us); in fp32 a chunk is two loads already, and one thread per tensor is the faster (34 us : 35 for 29498 tokens of 8 heads of 64).
+template <typename T>
+__global__ __launch_bounds__(256) void cache4_store_kernel(Cache4Args a) {
+  constexpr int BOTH = sizeof(T) == 2 ? 2 : 1;
+  int k, tok, head, chunk;
+  // the four lanes of a group come and go together: a group is one token and head
+  if (!chunk_of(a, &k, &tok, &head, &chunk)) return;
+  const long long slot = a.slots[tok];
+  float v[BOTH][8];
+#pragma unroll
+  for (int i = 0; i < BOTH; ++i) read8((const T*)a.x[k + i] + (long long)tok * a.token[k + i] + (long long)head * a.head[k + i] + chunk * 8, v[i]);
+  if (slot < 0 || slot >= a.rows) return;
+#pragma unroll
+  for (int i = 0; i < BOTH; ++i) store_group<T>(a.plane[k + i], v[i], slot, head, chunk);
 }
 
 template <typename T>
@@ -86,8 +96,8 @@ __global__ __launch_bounds__(256) void cache4_load_kernel(Cache4Args a) {
     typedef float floatx2 __attribute__((ext_vector_type(2)));
     const floatx2 f0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0), f1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 1);
     const floatx2 f2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 2), f3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 3);
-    *(floatx4*)y = floatx4{f0[0], f0[1], f1[0], f1[1]};
-    *(floatx4*)(y + 4) = floatx4{f2[0], f2[1], f3[0], f3[1]};
+    __builtin_nontemporal_store(floatx4{f0[0], f0[1], f1[0], f1[1]}, (floatx4*)y);
+    __builtin_nontemporal_store(floatx4{f2[0], f2[1], f3[0], f3[1]}, (floatx4*)(y + 4));
   } else {
     u32x4 o;
     if constexpr (std::is_same<T, _Float16>::value) {
@@ -101,7 +111,7 @@ __global__ __launch_bounds__(256) void cache4_load_kernel(Cache4Args a) {
       o[2] = __builtin_bit_cast(unsigned, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2));
       o[3] = __builtin_bit_cast(unsigned, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
     }
-    *(u32x4*)y = o;
+    __builtin_nontemporal_store(o, (u32x4*)y);
   }
 }
 
@@ -139,7 +149,7 @@ octo_status octo_op_cache4_store(const octo_cache4_op* op, void* hip_stream) {
   Cache4Args a{};
   const octo_status st = cache4_args(op, &a);
   if (st != OCTO_OK || !a.total) return st;
-  const dim3 grid((a.total + 255) / 256, 2);
+  const dim3 grid((a.total + 255) / 256, op->dtype == OCTO_F32 ? 2 : 1);
   hipStream_t s = (hipStream_t)hip_stream;
   if (op->dtype == OCTO_F32) hipLaunchKernelGGL(cache4_store_kernel<float>, grid, dim3(256), 0, s, a);
   else if (op->dtype == OCTO_F16) hipLaunchKernelGGL(cache4_store_kernel<_Float16>, grid, dim3(256), 0, s, a);

@@ -1,10 +1,10 @@
 // octo_op_rotate: norm of every head and rotation by the token's positions, queries and keys in one launch.
 //
-// The bound is memory: every value is read and written once, against some ten operations.  The angles depend on the token and
-// the pair alone, so a block of four wavefronts takes a few tokens, makes their cosines and sines once (one or two pairs a thread)
-// in LDS and then walks over the heads of both tensors, 64 / lanes-per-head heads of one token per wavefront and step, four steps'
-// loads at a time.  A lane holds VEC pairs, both elements of each: a rotation needs no exchange between lanes, a norm only
-// the sum over the lanes of a head.
+// The bound is memory: every value is read and written once, against some ten operations.  The heads of both tensors and all tokens are one
+// list of rows; a lane holds VEC pairs of a row, both elements of each (a rotation then needs no exchange between lanes, a norm only the sum over
+// the lanes of a row), a wavefront as many rows at a time as its lanes hold, and it walks over `items` such groups with the
+// loads of four in flight.  The angles depend on token and pair alone: the wavefront makes the cosines and sines of its few tokens
+// once, in LDS, while its first loads are on their way.  Wavefronts are independent of each other.
 //
 // An angle is pos * f / 2 pi revolutions.  The product is taken in fp64 and only its fraction goes to fp32 and to the sine and
 // cosine instructions, whose argument is in revolutions (1.3e-7 off at most on [0, 1)): positions of any size lose nothing, where an fp32 angle at
@@ -16,6 +16,8 @@
 
 namespace octo {
 namespace {
+
+constexpr int TURNS = 512;           // cosines and sines a wavefront can hold
 
 struct RotateArgs {
   const void* x[2]; void* y[2]; const float* w[2];
@@ -29,81 +31,121 @@ struct RotateArgs {
   double log2_base;
   const int* pos;
   float eps, inv_dim;
-  int lanes;                         // per head, a power of two >= dim / 2 / VEC
-  int steps;                         // per token: heads / (64 / lanes), rounded up
+  int w_aligned;                     // weights on 16 bytes
+  int lanes, rows;                   // per row: dim / 2 / VEC; rows at a time: 64 / lanes
+  int items;                         // groups of rows of a wavefront
   int table;                         // pairs, rounded up to a power of two
-  int tokens;                        // per block
+  unsigned total;                    // rows in all
+  FastDiv div_heads, div_lanes;
 };
 
 template <typename T, int N> struct alignas(sizeof(T) * N) Pack { T v[N]; };
+// Results go past the caches' reuse order: nothing here reads them again (51200 tokens of 32 + 8 heads of 128, bf16: 255 -> 246 us; 300
+// regions of 49 tokens, 8 + 8 heads of 64, fp16: 18.0 -> 16.8; the same for loads made it slower).
+template <typename P> __device__ __forceinline__ void store_once(P* p, const P& v) {
+  if constexpr (sizeof(P) == 16) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4*)p);
+  else *p = v;
+}
+
+// Sum over the lanes of a row, the same in each; `at` is the lane's place in its row.
+__device__ __forceinline__ float row_sum(float v, int lanes, int at, int lane) {
+  if ((lanes & (lanes - 1)) == 0) {
+    for (int d = 1; d < lanes; d *= 2) v += __shfl_xor(v, d);
+    return v;
+  }
+  for (int left = lanes; left > 1;) {
+    const int h = (left + 1) / 2;
+    const float o = __shfl(v, (lane + h) & 63);
+    if (at + h < left) v += o;
+    left = h;
+  }
+  return __shfl(v, lane - at);
+}
 
 template <typename T, int VEC>
 __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a) {
   constexpr int DEPTH = 4;
-  __shared__ float2 turn[512];           // [token of the block][pair]
-  __shared__ float weight[2][256];
-  const int n = a.n_dyn ? min(max(*a.n_dyn, 0), a.n) : a.n;
-  const int token0 = blockIdx.x * a.tokens;
-  if (token0 >= n) return;
-  const int here = min(a.tokens, n - token0);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int part_lane = lane & (a.lanes - 1), head_in_step = lane / a.lanes, per_step = 64 / a.lanes;
-  const int half = a.dim / 2, p0 = part_lane * VEC;
-  const bool works = p0 < half;
+  __shared__ float2 turns[4][TURNS];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  float2* const turn = turns[wave];                     // [token of the wavefront][pair]
+  const unsigned total = a.n_dyn ? (unsigned)min(max(*a.n_dyn, 0), a.n) * (unsigned)a.heads : a.total;
+  const unsigned per_wave = (unsigned)(a.items * a.rows), r0 = (blockIdx.x * 4 + wave) * per_wave;
+  if (r0 >= total) return;
+  const unsigned r_end = min(total, r0 + per_wave);
+  const int row_of_lane = (int)fast_div((unsigned)lane, a.div_lanes), at = lane - row_of_lane * a.lanes;
+  const int half = a.dim / 2, p0 = at * VEC;
+  const bool works = row_of_lane < a.rows;
   // elements of the lane's pairs: VEC from i0 and VEC from i1 (split), or 2 VEC from i0
   int i0, i1;
   if (!a.split) { i0 = 2 * p0; i1 = i0 + VEC; }
   else if (p0 < a.pairs) { i0 = p0; i1 = p0 + a.pairs; }
   else { i0 = a.pairs + p0; i1 = i0 + half - a.pairs; }
-  const int items = here * a.steps;
   typedef Pack<T, VEC> P;
 
   P in[DEPTH][2];
-  auto place = [&](int item, int* tok, int* head) {
-    *tok = item / a.steps;
-    *head = (item - *tok * a.steps) * per_step + head_in_step;
-    return works && item < items && *head < a.heads;
-  };
-  auto load = [&](int first_item) {
+  auto load = [&](unsigned first) {
 #pragma unroll
     for (int s = 0; s < DEPTH; ++s) {
-      int tok, head;
-      if (!place(first_item + 4 * s, &tok, &head)) continue;
+      const unsigned r = first + s * a.rows + row_of_lane;
+      if (!works || r >= r_end) continue;
+      const unsigned tok = fast_div(r, a.div_heads);
+      int head = (int)(r - tok * (unsigned)a.heads);
       const int k = head >= a.heads0;
-      const T* x = (const T*)a.x[k] + (long long)(token0 + tok) * a.x_token[k] + (long long)(head - (k ? a.heads0 : 0)) * a.x_head[k];
+      head -= k ? a.heads0 : 0;
+      const T* x = (const T*)a.x[k] + tok * a.x_token[k] + head * a.x_head[k];
       in[s][0] = *(const P*)(x + i0);
       in[s][1] = *(const P*)(x + i1);
     }
   };
-  load(wave);
+  load(r0);
 
-  for (int i = threadIdx.x; i < 2 * a.dim; i += 256) {
-    const int k = i >= a.dim, d = k ? i - a.dim : i;
-    if (a.w[k]) weight[k][d] = a.w[k][d];
-  }
-  if (a.pairs) {
-    const int p = threadIdx.x & (a.table - 1);
+  const unsigned tok0 = fast_div(r0, a.div_heads);
+  const int tokens = (int)(fast_div(r_end - 1, a.div_heads) - tok0) + 1;
+  for (int p = lane & (a.table - 1); p < a.pairs; p += 64) {
     int axis = 0;
     while (axis + 1 < a.n_axes && p >= a.first[axis + 1]) ++axis;
-    const int count = a.shared ? a.pairs : a.first[axis + 1] - a.first[axis];
+    const int count = a.shared ? a.pairs : a.first[axis + 1] - a.first[axis], step = a.table < 64 ? 64 / a.table : 1;
     const double f = exp2(-(double)(a.shared ? p : p - a.first[axis]) / count * a.log2_base) * 0.15915494309189533577;
-    if (p < a.pairs)
-      for (int t = threadIdx.x / a.table; t < here; t += 256 / a.table) {
-        const double rev = (double)a.pos[(size_t)(token0 + t) * a.n_axes + axis] * f;
-        const float r = (float)(rev - floor(rev));
-        turn[t * a.table + p] = make_float2(__builtin_amdgcn_cosf(r), __builtin_amdgcn_sinf(r));
-      }
+    for (int t = a.table < 64 ? lane / a.table : 0; t < tokens; t += step) {
+      const double rev = (double)a.pos[(size_t)(tok0 + t) * a.n_axes + axis] * f;
+      const float r = (float)(rev - floor(rev));
+      turn[t * a.pairs + p] = make_float2(__builtin_amdgcn_cosf(r), __builtin_amdgcn_sinf(r));
+    }
   }
-  __syncthreads();
+  float weight[2][2 * VEC];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    if (!a.w[k]) continue;                              // not used then
+    const float* w0 = a.w[k] + (works ? i0 : 0);
+    const float* w1 = a.w[k] + (works ? i1 : 0);
+    if (VEC % 4 == 0 && a.w_aligned) {
+#pragma unroll
+      for (int e = 0; e < VEC; e += 4) {
+        const floatx4 f0 = *(const floatx4*)(w0 + e), f1 = *(const floatx4*)(w1 + e);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) { weight[k][e + c] = f0[c]; weight[k][VEC + e + c] = f1[c]; }
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) { weight[k][e] = w0[e]; weight[k][VEC + e] = w1[e]; }
+    }
+  }
+  // the cosines and sines are read by other lanes of this wavefront: its LDS accesses stay in order
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 
-  for (int first_item = wave; first_item < items; first_item += 4 * DEPTH) {
-    if (first_item != wave) load(first_item);
+  for (unsigned first = r0; first < r_end; first += DEPTH * a.rows) {
+    if (first != r0) load(first);
 #pragma unroll
     for (int s = 0; s < DEPTH; ++s) {
-      int tok, head;
-      const bool any = place(first_item + 4 * s, &tok, &head);
-      if (first_item + 4 * s >= items) break;                     // the same for the whole wavefront
-      const int k = any && head >= a.heads0;
+      if (first + s * a.rows >= r_end) break;                     // the same for the whole wavefront
+      const unsigned r = first + s * a.rows + row_of_lane;
+      const bool any = works && r < r_end;
+      const unsigned tok = fast_div(any ? r : r0, a.div_heads);
+      int head = any ? (int)(r - tok * (unsigned)a.heads) : 0;
+      const int k = head >= a.heads0;
+      head -= k ? a.heads0 : 0;
       float u[2 * VEC];
 #pragma unroll
       for (int e = 0; e < VEC; ++e) { u[e] = any ? (float)in[s][0].v[e] : 0.f; u[VEC + e] = any ? (float)in[s][1].v[e] : 0.f; }
@@ -111,42 +153,39 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a) {
         float sum = 0.f;
 #pragma unroll
         for (int e = 0; e < 2 * VEC; ++e) sum += u[e] * u[e];
-        for (int d = 1; d < a.lanes; d *= 2) sum += __shfl_xor(sum, d);
-        if (a.w[k]) {
-          const float r = 1.0f / sqrtf(sum * a.inv_dim + a.eps);
-          if (works) {
+        sum = row_sum(sum, a.lanes, at, lane);
+        const float f = 1.0f / sqrtf(sum * a.inv_dim + a.eps);
+        if (k ? a.w[1] : a.w[0]) {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) { u[e] *= r * weight[k][i0 + e]; u[VEC + e] *= r * weight[k][i1 + e]; }
-          }
+          for (int e = 0; e < 2 * VEC; ++e) u[e] *= f * (k ? weight[1][e] : weight[0][e]);
         }
       }
       if (!any) continue;
       if (p0 < a.pairs) {
-        const float2* c = turn + tok * a.table + p0;
+        const float2* c = turn + (tok - tok0) * a.pairs + p0;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-          const int first = a.split ? e : 2 * e, second = a.split ? VEC + e : 2 * e + 1;
           if (p0 + e < a.pairs) {
             const float2 t = c[e];
-            const float x1 = u[first], x2 = u[second];
-            u[first] = x1 * t.x - x2 * t.y;
-            u[second] = x2 * t.x + x1 * t.y;
+            const float x1 = a.split ? u[e] : u[2 * e], x2 = a.split ? u[VEC + e] : u[2 * e + 1];
+            const float y1 = x1 * t.x - x2 * t.y, y2 = x2 * t.x + x1 * t.y;
+            if (a.split) { u[e] = y1; u[VEC + e] = y2; } else { u[2 * e] = y1; u[2 * e + 1] = y2; }
           }
         }
       }
-      T* y = (T*)a.y[k] + (long long)(token0 + tok) * a.y_token[k] + (long long)(head - (k ? a.heads0 : 0)) * a.y_head[k];
+      T* y = (T*)a.y[k] + tok * a.y_token[k] + head * a.y_head[k];
       P o0, o1;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) { o0.v[e] = (T)u[e]; o1.v[e] = (T)u[VEC + e]; }
-      *(P*)(y + i0) = o0;
-      *(P*)(y + i1) = o1;
+      store_once((P*)(y + i0), o0);
+      store_once((P*)(y + i1), o1);
     }
   }
 }
 
 template <typename T, int VEC>
 hipError_t launch_vec(const RotateArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((rotate_kernel<T, VEC>), dim3((a.n + a.tokens - 1) / a.tokens), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((rotate_kernel<T, VEC>), dim3((unsigned)(((unsigned long long)a.total + 4ull * a.items * a.rows - 1) / (4ull * a.items * a.rows))), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 template <typename T>
@@ -185,6 +224,7 @@ extern "C" octo_status octo_op_rotate(const octo_rotate_op* op, void* hip_stream
     if (p.d_weight && !(op->eps >= 0)) return OCTO_EINVAL;
     if (((uintptr_t)p.d_x | (uintptr_t)p.d_y) % es || ((uintptr_t)p.d_weight & 3)) return OCTO_EINVAL;
     align |= (uintptr_t)p.d_x / es | (uintptr_t)p.d_y / es | (unsigned long long)(p.x_token | p.x_head | p.y_token | p.y_head);
+    a.w_aligned = (k == 0 || a.w_aligned) && ((uintptr_t)p.d_weight & 15) == 0;
     a.x[k] = p.d_x; a.y[k] = p.d_y; a.w[k] = p.d_weight;
     a.x_token[k] = p.x_token; a.x_head[k] = p.x_head; a.y_token[k] = p.y_token; a.y_head[k] = p.y_head;
     if (!k) a.heads0 = p.heads;
@@ -193,16 +233,18 @@ extern "C" octo_status octo_op_rotate(const octo_rotate_op* op, void* hip_stream
   int vec = 16 / es;
   while (vec > 1 && align % vec) vec /= 2;
   if (half > 64 * vec) return OCTO_EINVAL;
-  a.lanes = 1;
-  while (a.lanes * vec < half) a.lanes *= 2;
-  a.steps = (a.heads + 64 / a.lanes - 1) / (64 / a.lanes);
+  a.lanes = half / vec;
+  a.rows = 64 / a.lanes;
   a.table = 1;
   while (a.table < a.pairs) a.table *= 2;
-  // Tokens of a block: as many as give each wavefront two rounds of loads, unless that leaves fewer than eight blocks per compute unit.
-  const int most = 512 / a.table < 16 ? 512 / a.table : 16;
-  a.tokens = (32 + a.steps - 1) / a.steps;
-  if (a.tokens > most) a.tokens = most;
-  while (a.tokens > 1 && (op->n_tokens + a.tokens - 1) / a.tokens < 2048) a.tokens = (a.tokens + 1) / 2;
+  const unsigned long long total = (unsigned long long)op->n_tokens * a.heads;
+  if (total > 0x7FFF0000ull) return OCTO_EINVAL;
+  a.total = (unsigned)total;
+  a.div_heads = make_fastdiv((unsigned)a.heads); a.div_lanes = make_fastdiv((unsigned)a.lanes);
+  // Groups of rows a wavefront: up to eight, as long as that leaves 4096 wavefronts and its tokens' turns fit (one group's always do).
+  const unsigned long long groups = (total + a.rows - 1) / a.rows;
+  a.items = groups / 4096 < 1 ? 1 : groups / 4096 > 8 ? 8 : (int)(groups / 4096);
+  while (a.items > 1 && ((a.items * a.rows + a.heads - 2) / a.heads + 1) * a.pairs > TURNS) --a.items;
   if (op->n_tokens == 0) return OCTO_OK;
   hipStream_t s = (hipStream_t)hip_stream;
   const hipError_t e = op->dtype == OCTO_F32 ? launch_type<float>(vec, a, s) : op->dtype == OCTO_F16 ? launch_type<_Float16>(vec, a, s) : launch_type<__bf16>(vec, a, s);
