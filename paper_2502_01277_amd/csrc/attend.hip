@@ -72,9 +72,11 @@ struct Plan { int kernel, row_blocks, n_split, part_keys; };
 //   SHARED_KEYS for up to 16 rows, for all else in fp32, and where the whole call is short, as its wavefronts are quickly done: 4 sequences of 400 keys, 128 rows
 //     8.1 us against 12.9 (TILES); 64 x 400, 32, 64 and 96 rows: 10.6, 15.0, 19.9 : 13.0, 14.1, 15.0; 4 x 24000, 32 and 40 rows: 29.2, 43.0 : 36.1, 37.4; from
 //     4 bits, where TILES has conversions to do first, up to three times as far: 64 x 3000, 64 and 96 rows: 38.8, 50.3 : 41.7, 47.2.
-//   TILES for the rest: 64 x 3000, 128 rows 69 us against 144; 512 x 400: 65 against 163.
-// Parts of the keys: as many as give every compute unit two (SHARED_KEYS), four or three blocks (TILES), of at least 256 keys, and, where sequences may
-//   differ in length, up to eight blocks of 1024 or 2048 keys, for an even end: 16 single tokens over up to 51200 keys of 4 bits 131 -> 117 us.  With TILES the rows
+//   TILES for the rest: 64 x 3000, 128 rows 69 us against 144; 512 x 400: 65 against 163; many short ones: 137 sequences of 4084 rows and 37 keys 89 us
+//     against 205.
+// Parts of the keys: as many as give every compute unit two blocks (TILES and fp32, which take longer for a key: three; OWN_ROWS: four), of at least 256 keys, and, where sequences may
+//   differ in length, up to sixteen blocks of 2048 keys, for an even end: 16 single tokens over up to 51200 keys of 4 bits 131 -> 117 us, 17 questions
+//   of up to 96 tokens over up to 20440 keys 486 -> 453.  With TILES the rows
 //   tell: as many as n_seq x max_q, then sequences are alike and more parts only cost (2 x 2048 queries over 12800 keys 790 us whole, 829 in two parts).
 Plan plan_of(const octo_attend_op* op, int cus) {
   Plan p{};
@@ -82,15 +84,15 @@ Plan plan_of(const octo_attend_op* op, int cus) {
   const bool f32 = op->dtype == OCTO_F32, four_bits = op->kv_format == OCTO_KV_CACHE4;
   const double work = (double)blocks16 * op->max_kv / cus;
   if (blocks16 >= 4ll * cus && (f32 ? op->max_kv <= 512 : four_bits ? op->max_kv <= 512 && rows <= 48 : op->max_kv <= 128 && rows <= 32)) p.kernel = OWN_ROWS;
-  else if (f32 || rows <= 16 || work <= (four_bits ? 5500 : rows <= 32 ? 1700 : 600)) p.kernel = SHARED_KEYS;
+  else if (f32 || rows <= 16 || ((blocks16 < 4ll * cus || op->max_kv >= 384) && work <= (four_bits ? 5500 : rows <= 32 ? 1700 : 600))) p.kernel = SHARED_KEYS;
   else p.kernel = TILES;
   const bool tiles = p.kernel == TILES;
   p.row_blocks = (int)(tiles ? (rows + 127) / 128 : (rows + 15) / 16);
   const long long blocks = p.kernel == OWN_ROWS ? (blocks16 + 3) / 4 : pairs * p.row_blocks;
   const bool alike = tiles && op->n_q >= (long long)op->n_seq * op->max_q * 15 / 16;
   auto parts = [&](int target, int least) { return blocks > 0 ? std::min<long long>((long long)target * cus / blocks, op->max_kv / least) : 1; };
-  long long n = parts(tiles ? 3 : p.kernel == SHARED_KEYS ? 2 : 4, 256);
-  if (!alike) n = std::max(n, parts(8, tiles ? 2048 : 1024));
+  long long n = parts(p.kernel == OWN_ROWS ? 4 : f32 || tiles ? 3 : 2, 256);
+  if (!alike) n = std::max(n, parts(16, 2048));
   n = std::max(1ll, std::min<long long>(n, MAX_PARTS));
   p.part_keys = (int)((op->max_kv + n * 64 - 1) / (n * 64)) * 64;
   p.n_split = op->max_kv > p.part_keys ? (op->max_kv + p.part_keys - 1) / p.part_keys : 1;
