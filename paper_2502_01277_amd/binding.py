@@ -820,7 +820,7 @@ _PLANE = "PPqqqq"
 _ROTATE = struct.Struct("@12id2fPP" + "PPPqqqqii" * MAX_ROTATE_PARTS)
 _CACHE4 = struct.Struct("@4iq" + 2 * _PLANE + "PP4qPP")
 _ATTEND = struct.Struct("@9ifqPqqPPqqqq" + 2 * _PLANE + "5PPqqPPN")
-_NO_PART, _NO_PLANE, _NO_KV = (0,) * 9, (0,) * 6, (0,) * 6
+_NO_PART, _NO_PLANE, _NO_KV, _NO_SECTIONS = {1: (0,) * 9, 2: ()}, (0,) * 6, (0,) * 6, (0,) * MAX_AXES
 
 
 class _Codes(dict):
@@ -861,34 +861,36 @@ def op_rotate(parts, pos, sections, base=10000.0, pairs="split", ladder="axis", 
     (octo_rotate_op in octo.h).  pos: int32 [tokens][axes]; sections: pairs of each axis, () for no rotation (pos None);
     n: int32 device tensor with the number of tokens present, or None."""
     t = _torch()
-    axes = len(sections)
-    if not 1 <= len(parts) <= MAX_ROTATE_PARTS or axes > MAX_AXES:
+    axes, count = len(sections), len(parts)
+    if not 1 <= count <= MAX_ROTATE_PARTS or axes > MAX_AXES:
         _refuse("one or two parts, up to %d axes" % MAX_AXES)
-    if axes and (pos is None or pos.dim() != 2 or pos.shape[1] != axes):
-        _refuse("positions are [tokens][axes]")
-    kind, packed = parts[0].x.dtype, ()
-    tokens = dim = None
+    x0 = parts[0].x
+    kind, shape0 = x0.dtype, x0.shape
+    if len(shape0) != 3:
+        _refuse("x and y of a part are [tokens][heads][dim]")
+    tokens, _, dim = shape0
+    packed = ()
     for p in parts:
-        x, y = p.x, p.y
+        x, y, w = p.x, p.y, p.weight
         shape, xs, ys = x.shape, x.stride(), y.stride()
-        if len(shape) != 3 or y.shape != shape:
-            _refuse("x and y of a part are [tokens][heads][dim]")
-        if tokens is None:
-            tokens, _, dim = shape
-        if shape[0] != tokens or shape[2] != dim or not (x.is_cuda and y.is_cuda) or x.dtype is not kind or y.dtype is not kind:
-            _refuse("parts are device tensors of one type, with the same tokens and dim")
-        if dim > 1 and (xs[2] != 1 or ys[2] != 1):
-            _refuse("dim is contiguous")
-        packed += (x.data_ptr(), y.data_ptr(), _optional(p.weight, t.float32, "weight is fp32 [dim] on the device", dim), xs[0], xs[1], ys[0], ys[1], shape[1], 0)
-    if len(parts) == 1:
-        packed += _NO_PART
-    if axes and pos.shape[0] != tokens:
-        _refuse("positions are [tokens][axes]")
-    op = _ROTATE.pack(_CODE[kind], tokens, dim, axes, *sections, *(0,) * (MAX_AXES - axes), PAIRS[pairs], LADDERS[ladder], len(parts), 0, base, eps, 0.0,
-                      _optional(pos, t.int32, "positions are int32, dense, on the device", 0) if axes else 0, _optional(n, t.int32, "n is int32 on the device"), *packed)
+        if len(shape) != 3 or y.shape != shape or shape[0] != tokens or shape[2] != dim:
+            _refuse("x and y of a part are [tokens][heads][dim], tokens and dim the same in all")
+        if not (x.is_cuda and y.is_cuda and x.dtype is kind and y.dtype is kind) or (dim > 1 and (xs[2] != 1 or ys[2] != 1)):
+            _refuse("parts are device tensors of one type, dim contiguous")
+        packed += (x.data_ptr(), y.data_ptr(), 0 if w is None else _optional(w, t.float32, "weight is fp32 [dim] on the device", dim), xs[0], xs[1], ys[0], ys[1], shape[1], 0)
+    d_pos = 0
+    if axes:
+        if pos is None or pos.shape != (tokens, axes):
+            _refuse("positions are [tokens][axes]")
+        d_pos = _optional(pos, t.int32, "positions are int32, dense, on the device", 0)
+    op = _ROTATE.pack(_CODE[kind], tokens, dim, axes, *sections, *_NO_SECTIONS[axes:], PAIRS[pairs], LADDERS[ladder], count, 0, base, eps, 0.0, d_pos,
+                      0 if n is None else _optional(n, t.int32, "n is int32 on the device"), *packed, *_NO_PART[count])
     if tokens:
-        _order(stream)
-        _st(lib().octo_op_rotate(op, _stream_ptr(stream)))
+        if stream is not None:
+            _order(stream)
+        st = lib().octo_op_rotate(op, _stream_ptr(stream))
+        if st:
+            _st(st)
 
 
 class Cache4:
@@ -909,40 +911,52 @@ class Cache4:
     def pack(self):
         """(heads, rows, dim, fields of the two planes), after a look at the shapes."""
         u8 = _torch().uint8
-        h, r, b = self.k_codes.shape
-        planes = ()
-        for codes, exps in ((self.k_codes, self.k_exps), (self.v_codes, self.v_exps)):
-            cs, es = codes.stride(), exps.stride()
-            if not (codes.is_cuda and exps.is_cuda and codes.dtype is u8 and exps.dtype is u8 and codes.shape == (h, r, b) and exps.shape == (h, r, b // 16)) or cs[2] != 1 or (es[2] != 1 and b > 16):
-                _refuse("codes are uint8 [heads][rows][dim / 2], exponents uint8 [heads][rows][dim / 32], on the device")
-            planes += (codes.data_ptr(), exps.data_ptr(), cs[1], cs[0], es[1], es[0])
-        return h, r, 2 * b, planes
+        kc, ke, vc, ve = self.k_codes, self.k_exps, self.v_codes, self.v_exps
+        shape, exp_shape = kc.shape, ke.shape
+        h, r, b = shape
+        s0, s1, s2, s3 = kc.stride(), ke.stride(), vc.stride(), ve.stride()
+        if (vc.shape != shape or ve.shape != exp_shape or exp_shape != (h, r, b // 16) or not (kc.is_cuda and ke.is_cuda and vc.is_cuda and ve.is_cuda)
+                or not (kc.dtype is u8 and ke.dtype is u8 and vc.dtype is u8 and ve.dtype is u8) or s0[2] != 1 or s2[2] != 1 or (b > 16 and (s1[2] != 1 or s3[2] != 1))):
+            _refuse("codes are uint8 [heads][rows][dim / 2], exponents uint8 [heads][rows][dim / 32], on the device")
+        return h, r, 2 * b, (kc.data_ptr(), ke.data_ptr(), s0[1], s0[0], s1[1], s1[0], vc.data_ptr(), ve.data_ptr(), s2[1], s2[0], s3[1], s3[0])
 
 
-def _cache4_call(name, cache, k, v, slots, n, stream):
+def _cache4_pack(cache, k, v, slots, n):
+    """The fields of a store or load, None where there are no tokens."""
     t = _torch()
     heads, rows, dim, planes = cache.pack()
-    shape, ks, vs = k.shape, k.stride(), v.stride()
-    if len(shape) != 3 or v.shape != shape or shape[1] != heads or shape[2] != dim or not (k.is_cuda and v.is_cuda) or k.dtype is not v.dtype or ks[2] != 1 or vs[2] != 1:
+    shape, ks, vs, kind = k.shape, k.stride(), v.stride(), k.dtype
+    if len(shape) != 3 or v.shape != shape or shape[1] != heads or shape[2] != dim or not (k.is_cuda and v.is_cuda) or kind is not v.dtype or ks[2] != 1 or vs[2] != 1:
         _refuse("k and v are [tokens][heads][dim] of one type, dim contiguous")
-    if slots.shape != shape[:1]:
+    tokens = shape[0]
+    if slots.shape != (tokens,):
         _refuse("one slot a token")
-    if not shape[0]:
-        return
-    op = _CACHE4.pack(_CODE[k.dtype], shape[0], heads, dim, rows, *planes, k.data_ptr(), v.data_ptr(), ks[0], ks[1], vs[0], vs[1],
-                      _optional(slots, t.int64, "slots are int64, dense, on the device"), _optional(n, t.int32, "n is int32 on the device"))
-    _order(stream)
-    _st(getattr(lib(), name)(op, _stream_ptr(stream)))
+    if not tokens:
+        return None
+    return _CACHE4.pack(_CODE[kind], tokens, heads, dim, rows, *planes, k.data_ptr(), v.data_ptr(), ks[0], ks[1], vs[0], vs[1],
+                        _optional(slots, t.int64, "slots are int64, dense, on the device"), 0 if n is None else _optional(n, t.int32, "n is int32 on the device"))
 
 
 def op_cache4_store(cache: Cache4, k, v, slots, n=None, stream=None):
     """Tokens k, v [tokens][heads][dim] into rows slots[i] (int64; outside the cache: skipped) of a cache of 4 bits a value."""
-    _cache4_call("octo_op_cache4_store", cache, k, v, slots, n, stream)
+    op = _cache4_pack(cache, k, v, slots, n)
+    if op is not None:
+        if stream is not None:
+            _order(stream)
+        st = lib().octo_op_cache4_store(op, _stream_ptr(stream))
+        if st:
+            _st(st)
 
 
 def op_cache4_load(cache: Cache4, slots, k, v, n=None, stream=None):
     """What the rows slots[i] hold, into k, v [tokens][heads][dim] (zeros for a slot outside the cache)."""
-    _cache4_call("octo_op_cache4_load", cache, k, v, slots, n, stream)
+    op = _cache4_pack(cache, k, v, slots, n)
+    if op is not None:
+        if stream is not None:
+            _order(stream)
+        st = lib().octo_op_cache4_load(op, _stream_ptr(stream))
+        if st:
+            _st(st)
 
 
 def _attend_pack(q, held, out, q_start, kv_start, kv_len, scale, max_q, max_kv, key_mask, lse, n_seq):
@@ -970,9 +984,9 @@ def _attend_pack(q, held, out, q_start, kv_start, kv_len, scale, max_q, max_kv, 
     return n, rows, (_CODE[kind], fmt, dim, heads, kv_heads, n, rows, rows if max_q is None else max_q, min(kv_rows, 0x7FFFFF00) if max_kv is None else max_kv,
                      dim ** -0.5 if scale is None else scale, kv_rows, q.data_ptr(), qs[0], qs[1], *kv,
                      _optional(q_start, t.int32, "q_start is int32 on the device"), _optional(kv_start, t.int64, "kv_start is int64 on the device", 0),
-                     _optional(kv_len, t.int32, "kv_len is int32 on the device", 0), _optional(n_seq, t.int32, "n_seq is int32 on the device"),
-                     _optional(key_mask, t.uint8, "key_mask is uint8 [rows of the pool] on the device", kv_rows), out.data_ptr(), os_[0], os_[1],
-                     _optional(lse, t.float32, "lse is fp32 [rows][heads] on the device", rows * heads))
+                     _optional(kv_len, t.int32, "kv_len is int32 on the device", 0), 0 if n_seq is None else _optional(n_seq, t.int32, "n_seq is int32 on the device"),
+                     0 if key_mask is None else _optional(key_mask, t.uint8, "key_mask is uint8 [rows of the pool] on the device", kv_rows), out.data_ptr(), os_[0], os_[1],
+                     0 if lse is None else _optional(lse, t.float32, "lse is fp32 [rows][heads] on the device", rows * heads))
 
 
 def op_attend(q, held, out, q_start, kv_start, kv_len, scale=None, max_q=None, max_kv=None, key_mask=None, lse=None, n_seq=None, workspace=None, stream=None) -> int:
@@ -993,9 +1007,12 @@ def op_attend(q, held, out, q_start, kv_start, kv_len, scale=None, max_q=None, m
             workspace = _torch().empty(need, dtype=_torch().uint8, device=q.device)
             scratch = (workspace,)
         op = _ATTEND.pack(*fields, workspace.data_ptr(), workspace.numel())
-    _order(stream, *scratch)
+    if stream is not None:
+        _order(stream, *scratch)
     kid = C.c_int32(0)
-    _st(L.octo_op_attend(op, _stream_ptr(stream), C.byref(kid)))
+    st = L.octo_op_attend(op, _stream_ptr(stream), C.byref(kid))
+    if st:
+        _st(st)
     return kid.value
 
 

@@ -157,11 +157,16 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
     const unsigned char* const vs = smem + 2 * TILE + stage * TILE;
     if (busy) {
     if (seen != ~0ull) {
-      const unsigned lo = (unsigned)seen >> (4 * half), hi = (unsigned)(seen >> 32) >> (4 * half);
+      // score i of half h belongs to key 32 h + 8 (i / 4) + i % 4 in lanes 0 .. 31 and to the key four further on in the others: which lanes keep it is made of
+      // two bits by the scalar unit (three vector instructions a score otherwise)
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) st[h][i] = (h ? hi : lo) >> (8 * (i / 4) + i % 4) & 1 ? st[h][i] : -INFINITY;
+        for (int i = 0; i < 16; ++i) {
+          const int bit = 8 * (i / 4) + i % 4, bits = (int)(h ? seen >> 32 : seen);
+          const unsigned long long keep = (unsigned)((bits << (31 - bit)) >> 31) | (unsigned long long)(unsigned)((bits << (27 - bit)) >> 31) << 32;
+          st[h][i] = __builtin_amdgcn_inverse_ballot_w64(keep) ? st[h][i] : -INFINITY;
+        }
     }
     float top = st[0][0];
 #pragma unroll
