@@ -181,6 +181,9 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
 #pragma unroll
       for (int d = 0; d < DT; ++d) acc[d] *= alpha;
     }
+    // From here to the end of the products the wavefront goes before the other of its SIMD, which is then at its loads and comparisons or waits
+    // (2 x 2048 queries over 12800 keys 777 -> 762 us, 732 together with the line drawn between exponentials and values below).
+    __builtin_amdgcn_s_setprio(1);
     const float refc = ref == -INFINITY ? 0.f : ref * c;
     floatx16 nx[2];
     if constexpr (more()) scores(smem + (stage ^ 1) * TILE, nx);
@@ -195,6 +198,7 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
       store4<T>((T*)&p[k] + 4, floatx4{w[4], w[5], w[6], w[7]});
     }
     sum += add[0] + add[1];
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
@@ -205,6 +209,7 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
         acc[d] = Elem<T>::mfma(u32x4{w0[0], w0[1], w1[0], w1[1]}, p[k], acc[d]);
       }
     if constexpr (more()) { st[0] = nx[0]; st[1] = nx[1]; }
+    __builtin_amdgcn_s_setprio(0);
     }
     if constexpr (more()) {
       place_tile(stage, false);
