@@ -29,10 +29,11 @@ def mx4_encode(x, cap=252):
     g = np.asarray(x, np.float64).reshape(x.shape[:-1] + (-1, 32))
     most = np.abs(g).max(-1)
     e = np.full(most.shape, -126, np.int64)
-    for i in np.ndindex(most.shape):
-        if np.isfinite(g[i]).all():
-            while e[i] < cap - 127 and most[i] > 7.0 * 2.0 ** int(e[i]):
-                e[i] += 1
+    while True:
+        more = np.isfinite(g).all(-1) & (e < cap - 127) & (most > 7.0 * np.exp2(e.astype(np.float64)))
+        if not more.any():
+            break
+        e[more] += 1
     finite = np.isfinite(g).all(-1)
     q = np.abs(np.where(finite[..., None], g, 0.0)) / np.exp2(e.astype(np.float64))[..., None]
     mids = (E2M1[1:] + E2M1[:-1]) / 2
@@ -70,14 +71,14 @@ def attend(q, k, v, q_start, kv_start, kv_len, scale, key_mask=None):
     for b in range(len(kv_start)):
         lo, hi = int(q_start[b]), int(q_start[b + 1])
         rows = np.arange(int(kv_start[b]), int(kv_start[b]) + int(kv_len[b]))
-        for i in range(lo, hi):
-            see = rows if key_mask is None else rows[np.asarray(key_mask)[rows] != 0]
-            for h in range(hq):
-                if not len(see):
-                    out[i, h], lse[i, h] = 0.0, -np.inf
-                    continue
-                with np.errstate(invalid="ignore"):
-                    s = k[see, h // group] @ q[i, h] * scale
-                    p = np.exp(s - s.max())
-                    out[i, h], lse[i, h] = p @ v[see, h // group] / p.sum(), s.max() + np.log(p.sum())
+        see = rows if key_mask is None else rows[np.asarray(key_mask)[rows] != 0]
+        for h in range(hq):
+            if not len(see):
+                out[lo:hi, h], lse[lo:hi, h] = 0.0, -np.inf
+                continue
+            with np.errstate(invalid="ignore"):
+                s = q[lo:hi, h] @ k[see, h // group].T * scale
+                top = s.max(-1, keepdims=True)
+                p = np.exp(s - top)
+                out[lo:hi, h], lse[lo:hi, h] = p @ v[see, h // group] / p.sum(-1, keepdims=True), top[:, 0] + np.log(p.sum(-1))
     return out, lse

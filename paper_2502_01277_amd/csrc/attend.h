@@ -35,10 +35,11 @@ struct AttendArgs {
 };
 
 enum { KV_PLAIN = OCTO_KV_PLAIN, KV_CACHE4 = OCTO_KV_CACHE4 };
+enum { DIRECT_OWN = 0, DIRECT_SHARE = 1, DIRECT_SHARE2 = 2 };      // 16 rows a wavefront, 16 or 32 a block whose wavefronts share the keys
 
-hipError_t launch_attend_direct_f16(int format, int share, const AttendArgs& a, hipStream_t s);
-hipError_t launch_attend_direct_bf16(int format, int share, const AttendArgs& a, hipStream_t s);
-hipError_t launch_attend_direct_f32(int format, int share, const AttendArgs& a, hipStream_t s);
+hipError_t launch_attend_direct_f16(int format, int how, const AttendArgs& a, hipStream_t s);
+hipError_t launch_attend_direct_bf16(int format, int how, const AttendArgs& a, hipStream_t s);
+hipError_t launch_attend_direct_f32(int format, int how, const AttendArgs& a, hipStream_t s);
 
 #ifdef __HIPCC__
 typedef uint32_t u32x3 __attribute__((ext_vector_type(3)));
@@ -248,10 +249,12 @@ template <typename T, int DP> struct Values<T, KV_CACHE4, DP> {
   }
 };
 
-template <typename T, int FORMAT, int DP, int t> __device__ __forceinline__ void add_values(const Values<T, FORMAT, DP>& v, const Eight<T>& p, floatx4* acc) {
+template <typename T, int FORMAT, int DP, int RT, int t> __device__ __forceinline__ void add_values(const Values<T, FORMAT, DP>& v, const Eight<T>* p, floatx4 (*acc)[DP / 16]) {
   if constexpr (t < DP / 16) {
-    acc[t] = mma<T>(v.template operand<t>(), p, acc[t]);
-    add_values<T, FORMAT, DP, t + 1>(v, p, acc);
+    const Eight<T> a = v.template operand<t>();
+#pragma unroll
+    for (int r = 0; r < RT; ++r) acc[r][t] = mma<T>(a, p[r], acc[r][t]);
+    add_values<T, FORMAT, DP, RT, t + 1>(v, p, acc);
   }
 }
 
@@ -282,33 +285,30 @@ __device__ __forceinline__ void finish_row(const AttendArgs& a, int part, bool w
   }
 }
 
-// A wavefront has 16 rows and walks over tiles of 32 keys, which it loads from memory to registers in the order of the operands: no
+// A wavefront has RT times 16 rows and walks over tiles of 32 keys, which it loads from memory to registers in the order of the operands: no
 // LDS and no barrier on the way, the next tile's loads are in flight while one is computed.  SHARE: the four wavefronts of
 // a block have the same rows and every fourth tile each, and add up in LDS at the end (few rows: what bounds it is reading the keys, and
-// more wavefronts have more loads in flight); otherwise each has rows of its own.
-template <typename T, int FORMAT, int DP, bool SHARE, bool MASK>
-__global__ __launch_bounds__(256, 2) void attend_direct_kernel(AttendArgs a) {
+// more wavefronts have more loads in flight); otherwise each has rows of its own.  RT = 2: two blocks of rows use each operand that has been loaded, and
+// converted or put in order.
+template <typename T, int FORMAT, int DP, bool SHARE, bool MASK, int RT>
+__global__ __launch_bounds__(256, RT == 2 && sizeof(T) == 4 && DP == 128 ? 1 : 2) void attend_direct_kernel(AttendArgs a) {
   constexpr int STEPS = DP / 32, PER = DP / 16, WAVES = SHARE ? 4 : 1;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
-  // what a block (SHARE) or a wavefront does: 16 rows of a sequence and key head
+  // what a block (SHARE) or a wavefront does: some rows of a sequence and key head
   const Piece pc = piece_of(a, SHARE ? blockIdx.x : blockIdx.x * 4 + wave, SHARE && a.by_die);
-  const int b = pc.seq, kv_head = pc.head, part = pc.part, row0 = pc.block * 16;
+  const int b = pc.seq, kv_head = pc.head, part = pc.part, row0 = pc.block * 16 * RT;
   Span sp;
   if (b >= a.n_seq || !span_of(a, b, &sp)) return;
   const int rows = sp.n_q * a.group;
   if (row0 >= rows || part >= parts_of(a, sp.n_kv)) return;      // SHARE: the whole block
   const bool whole = sp.n_kv <= a.part_keys;
-  const int row = row0 + col;
-  const bool has_row = row < rows;
-  const int qi = (int)fast_div((unsigned)row, a.div_group), head = kv_head * a.group + row - qi * a.group;
-  const long long q_row = sp.q0 + qi;
 
   const int tiles = (sp.n_kv + 31) / 32, per_part = a.part_keys / 32;
   const int first = part * per_part, last = min(tiles, first + per_part);      // first .. last - 1
 
   Keys<T, FORMAT, DP> keys;
   Values<T, FORMAT, DP> vals;
-  Eight<T> q[STEPS];
+  Eight<T> q[RT][STEPS];
   keys.init(a, g);
   uint32_t mask_byte = 0;
   auto keys_left = [&](int t) { return t < last ? min(32, sp.n_kv - 32 * t) : 0; };
@@ -320,29 +320,42 @@ __global__ __launch_bounds__(256, 2) void attend_direct_kernel(AttendArgs a) {
   vals.load(a, kv_head, sp.kv0 + 32ll * t, keys_left(t), col, g);
   load_mask(t);
 #pragma unroll
-  for (int s = 0; s < STEPS; ++s) {
-    const int d = Keys<T, FORMAT, DP>::q_dim(s, g);
-    const T* p = (const T*)a.q + q_row * a.q_row + head * a.q_head + d;
-    const bool in = has_row && d < a.dim;
-    if constexpr (sizeof(T) == 2) q[s].v = in ? *(const u32x4*)p : u32x4{0, 0, 0, 0};
-    else { q[s].lo = in ? *(const floatx4*)p : floatx4{0, 0, 0, 0}; q[s].hi = in ? *(const floatx4*)(p + 4) : floatx4{0, 0, 0, 0}; }
+  for (int r = 0; r < RT; ++r) {
+    const int row = row0 + 16 * r + col, qi = (int)fast_div((unsigned)row, a.div_group), head = kv_head * a.group + row - qi * a.group;
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      const int d = Keys<T, FORMAT, DP>::q_dim(s, g);
+      const T* p = (const T*)a.q + (sp.q0 + (long long)qi) * a.q_row + head * a.q_head + d;
+      const bool in = row < rows && d < a.dim;
+      if constexpr (sizeof(T) == 2) q[r][s].v = in ? *(const u32x4*)p : u32x4{0, 0, 0, 0};
+      else { q[r][s].lo = in ? *(const floatx4*)p : floatx4{0, 0, 0, 0}; q[r][s].hi = in ? *(const floatx4*)(p + 4) : floatx4{0, 0, 0, 0}; }
+    }
   }
 
-  floatx4 acc[PER];
+  floatx4 acc[RT][PER];
+  float ref[RT], sum[RT];                  // the reference in units of the raw score: weights are exp2((s - ref) scale2)
 #pragma unroll
-  for (int i = 0; i < PER; ++i) acc[i] = floatx4{0, 0, 0, 0};
-  float ref = -INFINITY, sum = 0.f;        // the reference in units of the raw score: weights are exp2((s - ref) scale2)
+  for (int r = 0; r < RT; ++r) {
+    ref[r] = -INFINITY; sum[r] = 0.f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) acc[r][i] = floatx4{0, 0, 0, 0};
+  }
   const float c = a.scale2;
 
   for (; t < last; t += WAVES) {
     const int n = keys_left(t);
     const unsigned seen = MASK ? (unsigned)__ballot(mask_byte != 0) : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1;
-    floatx4 st[2];
+    floatx4 st[RT][2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      st[h] = floatx4{0, 0, 0, 0};
 #pragma unroll
-      for (int s = 0; s < STEPS; ++s) st[h] = mma<T>(keys.operand(h, s), q[s], st[h]);
+      for (int r = 0; r < RT; ++r) st[r][h] = floatx4{0, 0, 0, 0};
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) {
+        const Eight<T> k = keys.operand(h, s);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) st[r][h] = mma<T>(k, q[r][s], st[r][h]);
+      }
     }
     keys.load(a, kv_head, sp.kv0 + 32ll * (t + WAVES), keys_left(t + WAVES), col);
     load_mask(t + WAVES);
@@ -352,91 +365,115 @@ __global__ __launch_bounds__(256, 2) void attend_direct_kernel(AttendArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const bool keep = seen >> (16 * h + 4 * g + i) & 1;
-          st[h][i] = keep ? st[h][i] : -INFINITY;
+#pragma unroll
+          for (int r = 0; r < RT; ++r) st[r][h][i] = keep ? st[r][h][i] : -INFINITY;
           if (MASK) vals.hide(4 * h + i, keep);               // beyond the last key zeros were read
         }
     }
     // The reference follows the largest score only where that is more than 2^8 above it: weights up to 2^8 cost no precision,
     // and the sums seldom have to be scaled.
-    const float top = fmaxf(fmaxf(fmaxf(st[0][0], st[0][1]), fmaxf(st[0][2], st[0][3])), fmaxf(fmaxf(st[1][0], st[1][1]), fmaxf(st[1][2], st[1][3])));
-    if (__any((top - ref) * c > 8.0f)) {
-      float m = fmaxf(top, __shfl_xor(top, 16));
-      m = fmaxf(ref, fmaxf(m, __shfl_xor(m, 32)));
-      const float alpha = m == ref ? 1.0f : __builtin_amdgcn_exp2f((ref - m) * c);
-      ref = m;
-      sum *= alpha;
+    float top[RT];
+    bool over = false;
 #pragma unroll
-      for (int i = 0; i < PER; ++i) acc[i] *= alpha;
+    for (int r = 0; r < RT; ++r) {
+      top[r] = fmaxf(fmaxf(fmaxf(st[r][0][0], st[r][0][1]), fmaxf(st[r][0][2], st[r][0][3])), fmaxf(fmaxf(st[r][1][0], st[r][1][1]), fmaxf(st[r][1][2], st[r][1][3])));
+      over = over || (top[r] - ref[r]) * c > 8.0f;
     }
-    const float refc = ref == -INFINITY ? 0.f : ref * c;
+    if (__any(over)) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+      for (int r = 0; r < RT; ++r) {
+        float m = fmaxf(top[r], __shfl_xor(top[r], 16));
+        m = fmaxf(ref[r], fmaxf(m, __shfl_xor(m, 32)));
+        const float alpha = m == ref[r] ? 1.0f : __builtin_amdgcn_exp2f((ref[r] - m) * c);
+        ref[r] = m;
+        sum[r] *= alpha;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) { st[h][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[h][i], c, -refc)); sum += st[h][i]; }
-    add_values<T, FORMAT, DP, 0>(vals, eight_of<T>(st[0], st[1]), acc);
+        for (int i = 0; i < PER; ++i) acc[r][i] *= alpha;
+      }
+    }
+    Eight<T> p[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      const float refc = ref[r] == -INFINITY ? 0.f : ref[r] * c;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { st[r][h][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[r][h][i], c, -refc)); sum[r] += st[r][h][i]; }
+      p[r] = eight_of<T>(st[r][0], st[r][1]);
+    }
+    add_values<T, FORMAT, DP, RT, 0>(vals, p, acc);
     vals.load(a, kv_head, sp.kv0 + 32ll * (t + WAVES), keys_left(t + WAVES), col, g);
   }
-  sum += __shfl_xor(sum, 16);
-  sum += __shfl_xor(sum, 32);
-  const float refc = ref == -INFINITY ? -INFINITY : ref * c;
 
-  if constexpr (!SHARE) {
-    if (!has_row) return;
-    // element of dim of acc[t][i]: PER (4 g + i) + t
+  constexpr int LD = DP + 4;
+  __shared__ float so[SHARE ? 4 : 1][SHARE ? 16 : 1][LD];
+  __shared__ float2 sm[SHARE ? 4 : 1][SHARE ? 16 : 1];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float o[PER];
+  for (int r = 0; r < RT; ++r) {
+    sum[r] += __shfl_xor(sum[r], 16);
+    sum[r] += __shfl_xor(sum[r], 32);
+    const float refc = ref[r] == -INFINITY ? -INFINITY : ref[r] * c;
+    // element of dim of acc[r][t][i]: PER (4 g + i) + t
+    if constexpr (!SHARE) {
+      const int row = row0 + 16 * r + col, qi = (int)fast_div((unsigned)row, a.div_group);
+      if (row >= rows) continue;
 #pragma unroll
-      for (int e = 0; e < PER; ++e) o[e] = acc[e][i];
-      finish_row<T, PER>(a, part, whole, q_row, head, PER * (4 * g + i), g == 0 && i == 0, o, refc, sum);
+      for (int i = 0; i < 4; ++i) {
+        float o[PER];
+#pragma unroll
+        for (int e = 0; e < PER; ++e) o[e] = acc[r][e][i];
+        finish_row<T, PER>(a, part, whole, sp.q0 + (long long)qi, kv_head * a.group + row - qi * a.group, PER * (4 * g + i), g == 0 && i == 0, o, refc, sum[r]);
+      }
+    } else {
+      if (row0 + 16 * r >= rows) break;                    // the same for the whole block
+      if (r) __syncthreads();                              // the rows before have been read
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < PER; e += 2) *(float2*)&so[wave][col][PER * (4 * g + i) + e] = make_float2(acc[r][e][i], acc[r][e + 1][i]);
+      if (g == 0) sm[wave][col] = make_float2(refc, sum[r]);
+      __syncthreads();
+      const int x = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * PER, row = row0 + 16 * r + x;
+      if (row >= rows) continue;
+      float m = -INFINITY, total = 0.f, o[PER];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) m = fmaxf(m, sm[w][x].x);
+#pragma unroll
+      for (int e = 0; e < PER; ++e) o[e] = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float2 y = sm[w][x];
+        const float f = y.x == m ? 1.0f : __builtin_amdgcn_exp2f(y.x - m);
+        total += y.y * f;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) o[e] += so[w][x][d0 + e] * f;
+      }
+      const int qi = (int)fast_div((unsigned)row, a.div_group);
+      finish_row<T, PER>(a, part, whole, sp.q0 + (long long)qi, kv_head * a.group + row - qi * a.group, d0, d0 == 0, o, m, total);
     }
-  } else {
-    constexpr int LD = DP + 4;
-    __shared__ float so[4][16][LD];
-    __shared__ float2 sm[4][16];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int e = 0; e < PER; e += 2) *(float2*)&so[wave][col][PER * (4 * g + i) + e] = make_float2(acc[e][i], acc[e + 1][i]);
-    if (g == 0) sm[wave][col] = make_float2(refc, sum);
-    __syncthreads();
-    const int r = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * PER;
-    if (row0 + r >= rows) return;
-    float m = -INFINITY, total = 0.f, o[PER];
-#pragma unroll
-    for (int w = 0; w < 4; ++w) m = fmaxf(m, sm[w][r].x);
-#pragma unroll
-    for (int e = 0; e < PER; ++e) o[e] = 0.f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float2 x = sm[w][r];
-      const float f = x.x == m ? 1.0f : __builtin_amdgcn_exp2f(x.x - m);
-      total += x.y * f;
-#pragma unroll
-      for (int e = 0; e < PER; ++e) o[e] += so[w][r][d0 + e] * f;
-    }
-    const int q2 = (int)fast_div((unsigned)(row0 + r), a.div_group);
-    finish_row<T, PER>(a, part, whole, sp.q0 + q2, kv_head * a.group + row0 + r - q2 * a.group, d0, d0 == 0, o, m, total);
   }
 }
 
-template <typename T, int FORMAT, int DP>
-hipError_t launch_direct(int share, const AttendArgs& a, hipStream_t s) {
-  const dim3 grid(share ? piece_blocks(a) : ((unsigned)a.n_seq * a.kv_heads * a.row_blocks * a.n_split + 3) / 4);
-  if (share && a.mask) hipLaunchKernelGGL((attend_direct_kernel<T, FORMAT, DP, true, true>), grid, dim3(256), 0, s, a);
-  else if (share) hipLaunchKernelGGL((attend_direct_kernel<T, FORMAT, DP, true, false>), grid, dim3(256), 0, s, a);
-  else if (a.mask) hipLaunchKernelGGL((attend_direct_kernel<T, FORMAT, DP, false, true>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((attend_direct_kernel<T, FORMAT, DP, false, false>), grid, dim3(256), 0, s, a);
+template <typename T, int FORMAT, int DP, bool MASK>
+hipError_t launch_direct_masked(int how, const AttendArgs& a, hipStream_t s) {
+  const dim3 grid(how != DIRECT_OWN ? piece_blocks(a) : ((unsigned)a.n_seq * a.kv_heads * a.row_blocks * a.n_split + 3) / 4);
+  if (how == DIRECT_OWN) hipLaunchKernelGGL((attend_direct_kernel<T, FORMAT, DP, false, MASK, 1>), grid, dim3(256), 0, s, a);
+  else if (how == DIRECT_SHARE) hipLaunchKernelGGL((attend_direct_kernel<T, FORMAT, DP, true, MASK, 1>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((attend_direct_kernel<T, FORMAT, DP, true, MASK, 2>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
+template <typename T, int FORMAT, int DP>
+hipError_t launch_direct(int how, const AttendArgs& a, hipStream_t s) {
+  return a.mask ? launch_direct_masked<T, FORMAT, DP, true>(how, a, s) : launch_direct_masked<T, FORMAT, DP, false>(how, a, s);
+}
 template <typename T>
-hipError_t launch_attend_direct(int format, int share, const AttendArgs& a, hipStream_t s) {
+hipError_t launch_attend_direct(int format, int how, const AttendArgs& a, hipStream_t s) {
   if constexpr (sizeof(T) == 2) {
-    if (format == KV_CACHE4) return a.dim <= 64 ? launch_direct<T, KV_CACHE4, 64>(share, a, s) : launch_direct<T, KV_CACHE4, 128>(share, a, s);
+    if (format == KV_CACHE4) return a.dim <= 64 ? launch_direct<T, KV_CACHE4, 64>(how, a, s) : launch_direct<T, KV_CACHE4, 128>(how, a, s);
   }
-  if (a.dim <= 64) return launch_direct<T, KV_PLAIN, 64>(share, a, s);
-  if (a.dim <= 96) return launch_direct<T, KV_PLAIN, 96>(share, a, s);
-  return launch_direct<T, KV_PLAIN, 128>(share, a, s);
+  if (a.dim <= 64) return launch_direct<T, KV_PLAIN, 64>(how, a, s);
+  if (a.dim <= 96) return launch_direct<T, KV_PLAIN, 96>(how, a, s);
+  return launch_direct<T, KV_PLAIN, 128>(how, a, s);
 }
 #endif
 

@@ -62,18 +62,20 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   store4<T>((T*)a.out + (sp.q0 + (long long)qi) * a.out_row + head * a.out_head + d, o * inv);
 }
 
-enum { SHARED_KEYS = 1, OWN_ROWS = 2, TILES = 3 };          // kernels, as in the id
-struct Plan { int kernel, row_blocks, n_split, part_keys; };
+enum { SHARED_KEYS = 1, OWN_ROWS = 2, TILES = 3 };          // as in the kernel id; 4 there: SHARED_KEYS with 32 rows
+struct Plan { int kernel, how, row_blocks, n_split, part_keys; };
 
-// Which kernel, by the rows of the longest sequence, the blocks of SHARED_KEYS (16 rows each) and their keys.
-//   OWN_ROWS where there are enough rows for all wavefronts and few keys to share: 512 sequences of 2 heads and 49 keys, dim 128, bf16, 8 / 16 / 32 / 40
-//     rows 9.7 / 11.4 / 15.0 / 18.6 us against 12.1 / 13.3 / 20.1 / 26.7 (SHARED_KEYS) and 14.1 / 14.5 / 15.3 / 16.2 (TILES); from 4 bits also 400 keys, 20 and 40
-//     rows: 22.7, 29.8 : 26.2, 36.1 : 31.6, 36.6; fp32, 400 keys, dim 64, 20 and 128 rows: 52.8, 154 : 63.6, 194.
-//   SHARED_KEYS for up to 16 rows, for all else in fp32, and where the whole call is short, as its wavefronts are quickly done: 4 sequences of 400 keys, 128 rows
-//     8.1 us against 12.9 (TILES); 64 x 400, 32, 64 and 96 rows: 10.6, 15.0, 19.9 : 13.0, 14.1, 15.0; 4 x 24000, 32 and 40 rows: 29.2, 43.0 : 36.1, 37.4; from
-//     4 bits, where TILES has conversions to do first, up to three times as far: 64 x 3000, 64 and 96 rows: 38.8, 50.3 : 41.7, 47.2.
-//   TILES for the rest: 64 x 3000, 128 rows 69 us against 144; 512 x 400: 65 against 163; many short ones: 137 sequences of 4084 rows and 37 keys 89 us
-//     against 205.
+// Which kernel, by the rows of the longest sequence, their tiles of 16 over all sequences and heads, and the keys ("512 x 49": 512 sequences of 2 heads and 49
+// keys; us, bf16, dim 128, where nothing else is said).
+//   OWN_ROWS where there are tiles for all wavefronts and few keys to share: 512 x 49, 8 / 16 / 32 / 48 rows 9.7 / 11.4 / 15.0 / 19.5 against 12.1 / 13.3 / 20.2 /
+//     27.3 (SHARED_KEYS) and 14.1 / 14.5 / 15.6 / 17.0 (TILES); from 4 bits also 400 keys, 20 and 48 rows: 22.8, 30.3 : 26.5, 36.1 : 32.2, 36.7; fp32,
+//     512 x 400, dim 64, 20 and 128 rows: 52.8, 153 : 66.0, 187.
+//   SHARED_KEYS for up to 16 rows, for all else in fp32, and where the whole call is short, as its wavefronts are quickly done: 4 x 400, 128 rows 8.2 against 13.7
+//     (TILES); 64 x 400, 32, 64 and 96 rows: 10.9, 12.7, 17.5 : 14.1, 14.6, 15.5; further for few long sequences (4 x 24000, 64 and 128 rows: 32, 44 : 40, 46; but
+//     64 x 3000, 64 rows 59.9 : 59.6) and from 4 bits, which TILES converts first and then puts in LDS (64 x 3000, 64 and 128 rows: 33, 42 : 47, 60).
+//   TILES for the rest: 64 x 3000, 128 rows 70 against 76; 512 x 400: 66 against 112; many short ones: 137 sequences of 4084 rows and 37 keys 89 against 205.
+// SHARED_KEYS with 32 rows a block instead of 16 where there are many tiles: the keys are read and put in order half as often (64 x 3000, 64 and 128 rows: 75, 131 ->
+//   60, 76; from 4 bits 33, 54 -> 33, 42; fp32, dim 64: 88, 161 -> 79, 114), but a short call is longer (4 x 400: 8.2 -> 10.0; fp32, 77 rows in 5 tiles 29 -> 37).
 // Parts of the keys: as many as give every compute unit two blocks (TILES and fp32, which take longer for a key: three; OWN_ROWS: four), of at least 256 keys, and, where sequences may
 //   differ in length, up to sixteen blocks of 2048 keys, for an even end: 16 single tokens over up to 51200 keys of 4 bits 131 -> 117 us, 17 questions
 //   of up to 96 tokens over up to 20440 keys 486 -> 453.  With TILES the rows
@@ -82,12 +84,18 @@ Plan plan_of(const octo_attend_op* op, int cus) {
   Plan p{};
   const long long rows = (long long)op->max_q * (op->q_heads / op->kv_heads), pairs = (long long)op->n_seq * op->kv_heads, blocks16 = pairs * ((rows + 15) / 16);
   const bool f32 = op->dtype == OCTO_F32, four_bits = op->kv_format == OCTO_KV_CACHE4;
-  const double work = (double)blocks16 * op->max_kv / cus;
-  if (blocks16 >= 4ll * cus && (f32 ? op->max_kv <= 512 : four_bits ? op->max_kv <= 512 && rows <= 48 : op->max_kv <= 128 && rows <= 32)) p.kernel = OWN_ROWS;
-  else if (f32 || rows <= 16 || ((blocks16 < 4ll * cus || op->max_kv >= 384) && work <= (four_bits ? 5500 : rows <= 32 ? 1700 : 600))) p.kernel = SHARED_KEYS;
-  else p.kernel = TILES;
+  const double work = (double)blocks16 * op->max_kv / cus;          // keys a compute unit reads if every tile reads its own
+  const bool many = blocks16 >= 4ll * cus, long_enough = !many || op->max_kv >= 384;
+  if (many && (f32 ? op->max_kv <= 512 : four_bits ? op->max_kv <= 512 && rows <= 48 : op->max_kv <= 128 && rows <= 32)) p.kernel = OWN_ROWS;
+  else if (f32 || rows <= 16) p.kernel = SHARED_KEYS;
+  else if (four_bits) p.kernel = (long_enough && work <= 5500) || (rows <= 128 && op->max_kv >= 2048 && work <= 13000) ? SHARED_KEYS : TILES;
+  else p.kernel = long_enough && work <= (rows <= 32 ? 3000 : rows <= 128 && op->max_kv >= 8192 ? 6000 : 1000) ? SHARED_KEYS : TILES;
   const bool tiles = p.kernel == TILES;
-  p.row_blocks = (int)(tiles ? (rows + 127) / 128 : (rows + 15) / 16);
+  const long long tiles16 = (rows + 15) / 16;
+  const bool pairs_of_tiles = f32 ? work >= 1500 && (tiles16 % 2 == 0 || tiles16 > 6) : four_bits ? rows > 64 && work >= 4000 : work >= (rows <= 32 ? 2000 : 400);
+  p.how = p.kernel == OWN_ROWS ? DIRECT_OWN : p.kernel == SHARED_KEYS && rows > 16 && pairs_of_tiles ? DIRECT_SHARE2 : DIRECT_SHARE;
+  const int block_rows = tiles ? 128 : p.how == DIRECT_SHARE2 ? 32 : 16;
+  p.row_blocks = (int)((rows + block_rows - 1) / block_rows);
   const long long blocks = p.kernel == OWN_ROWS ? (blocks16 + 3) / 4 : pairs * p.row_blocks;
   const bool alike = tiles && op->n_q >= (long long)op->n_seq * op->max_q * 15 / 16;
   auto parts = [&](int target, int least) { return blocks > 0 ? std::min<long long>((long long)target * cus / blocks, op->max_kv / least) : 1; };
@@ -189,11 +197,10 @@ octo_status octo_op_attend(const octo_attend_op* op, void* hip_stream, int32_t* 
   const long long sets = (long long)op->n_seq * op->kv_heads * p.n_split;
   a.by_die = p.row_blocks > 1 && (sets % 8 == 0 || sets >= 64);
   a.div_heads = make_fastdiv((unsigned)op->kv_heads); a.div_blocks = make_fastdiv((unsigned)p.row_blocks); a.div_split = make_fastdiv((unsigned)p.n_split);
-  const int share = p.kernel == SHARED_KEYS;
   hipError_t e = p.kernel == TILES ? (op->dtype == OCTO_F16 ? launch_attend_tile_f16(op->kv_format, a, s) : launch_attend_tile_bf16(op->kv_format, a, s))
-               : op->dtype == OCTO_F32 ? launch_attend_direct_f32(op->kv_format, share, a, s)
-               : op->dtype == OCTO_F16 ? launch_attend_direct_f16(op->kv_format, share, a, s)
-                                       : launch_attend_direct_bf16(op->kv_format, share, a, s);
+               : op->dtype == OCTO_F32 ? launch_attend_direct_f32(op->kv_format, p.how, a, s)
+               : op->dtype == OCTO_F16 ? launch_attend_direct_f16(op->kv_format, p.how, a, s)
+                                       : launch_attend_direct_bf16(op->kv_format, p.how, a, s);
   if (e == hipSuccess && p.n_split > 1) {
     const dim3 grid((unsigned)op->n_seq, (unsigned)(((long long)op->max_q * op->q_heads + 7) / 8));
     if (op->dtype == OCTO_F32) hipLaunchKernelGGL(attend_join_kernel<float>, grid, dim3(256), 0, s, a);
@@ -201,7 +208,7 @@ octo_status octo_op_attend(const octo_attend_op* op, void* hip_stream, int32_t* 
     else hipLaunchKernelGGL(attend_join_kernel<__bf16>, grid, dim3(256), 0, s, a);
     e = hipGetLastError();
   }
-  if (kernel_id && e == hipSuccess) *kernel_id = 1000 * p.kernel + p.n_split;
+  if (kernel_id && e == hipSuccess) *kernel_id = 1000 * (p.how == DIRECT_SHARE2 ? 4 : p.kernel) + p.n_split;
   return e == hipSuccess ? OCTO_OK : OCTO_EHIP;
 }
 

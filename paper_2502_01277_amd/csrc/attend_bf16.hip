@@ -2,5 +2,5 @@
 #include "attend.h"
 
 namespace octo {
-hipError_t launch_attend_direct_bf16(int format, int share, const AttendArgs& a, hipStream_t s) { return launch_attend_direct<__bf16>(format, share, a, s); }
+hipError_t launch_attend_direct_bf16(int format, int how, const AttendArgs& a, hipStream_t s) { return launch_attend_direct<__bf16>(format, how, a, s); }
 }  // namespace octo

@@ -90,22 +90,25 @@ class Problem:
         for b in range(n):
             rows = np.arange(self.kv_start[b], self.kv_start[b] + self.kv_len[b])
             rows = rows[self.used[rows]]
-            for i in range(self.q_start[b], self.q_start[b + 1]):
-                if not len(rows):
-                    assert np.all(out[i] == 0) and np.all(np.isneginf(got_lse[i])), (b, i)
-                    continue
-                for h in range(q.shape[1]):
-                    kk, vv = k[rows, h // group], v[rows, h // group]
-                    s = kk @ q[i, h] * self.scale
-                    d = (dim + 8) * 2.0 ** -24 * self.scale * (np.abs(kk) @ np.abs(q[i, h])).max()
-                    w = np.exp(s - lse[i, h])
-                    tiny = 2.0 ** -126 * (1 + np.abs(vv).sum(0))
-                    bound = (e + 2 * d + (len(rows) / 8 + 64) * 2.0 ** -24) * (w @ np.abs(vv)) + e * np.abs(ref[i, h]) + tiny
-                    if self.dtype == "f16":
-                        bound = bound + 2.0 ** -24 * (1 + np.abs(vv).sum(0) / np.exp(s - s.max()).sum())
-                    err = np.abs(out[i, h] - ref[i, h])
-                    assert np.all(err <= bound), (b, i, h, float((err - bound).max()), float(bound.max()))
-                    assert abs(got_lse[i, h] - lse[i, h]) <= d + (len(rows) / 8 + 64) * 2.0 ** -24 + 2.0 ** -22 * (1 + abs(lse[i, h])), (b, i, h)
+            lo, hi = self.q_start[b], self.q_start[b + 1]
+            if not len(rows):
+                assert np.all(out[lo:hi] == 0) and np.all(np.isneginf(got_lse[lo:hi])), b
+                continue
+            if lo == hi:
+                continue
+            for h in range(q.shape[1]):
+                kk, vv = k[rows, h // group], v[rows, h // group]
+                s = q[lo:hi, h] @ kk.T * self.scale
+                d = (dim + 8) * 2.0 ** -24 * self.scale * (np.abs(q[lo:hi, h]) @ np.abs(kk).T).max(-1, keepdims=True)
+                w = np.exp(s - lse[lo:hi, h, None])
+                tiny = 2.0 ** -126 * (1 + np.abs(vv).sum(0))
+                bound = (e + 2 * d + (len(rows) / 8 + 64) * 2.0 ** -24) * (w @ np.abs(vv)) + e * np.abs(ref[lo:hi, h]) + tiny
+                if self.dtype == "f16":
+                    bound = bound + 2.0 ** -24 * (1 + np.abs(vv).sum(0) / np.exp(s - s.max(-1, keepdims=True)).sum(-1, keepdims=True))
+                err = np.abs(out[lo:hi, h] - ref[lo:hi, h])
+                assert np.all(err <= bound), (b, h, float((err - bound).max()), float(bound.max()))
+                off = np.abs(got_lse[lo:hi, h] - lse[lo:hi, h])
+                assert np.all(off <= d[:, 0] + (len(rows) / 8 + 64) * 2.0 ** -24 + 2.0 ** -22 * (1 + np.abs(lse[lo:hi, h]))), (b, h)
 
 
 FORMS = [("bf16", "plain"), ("f16", "plain"), ("f32", "plain"), ("bf16", "cache4"), ("f16", "cache4")]
@@ -131,6 +134,37 @@ def test_questions_of_many_lengths(octo, dtype, fmt, dim, kv_heads, group, mask)
         pytest.skip("the cache holds groups of 32")
     p = Problem(octo, dtype, fmt, dim, kv_heads, group, [5, 0, 1, 33, 16, 70], [65, 50, 300, 1, 96, 129], mask, seed=dim + group)
     assert p.run(octo)
+    p.check()
+
+
+SHORT, EDGES = [20, 3, 17, 16, 1, 0, 32, 31], [49, 0, 1, 33, 64, 65, 31, 96]
+# every kernel on every type and format where there is one (the number of sequences and the keys decide): dim, key heads, group, queries, keys, kernel
+KERNELS = [
+    # a wavefront has rows of its own
+    ("bf16", "plain", 128, 8, 1, SHORT * 8, EDGES * 8, 2), ("f16", "plain", 72, 8, 1, SHORT * 8, EDGES * 8, 2), ("f32", "plain", 64, 8, 1, SHORT * 8, EDGES * 8, 2), ("f32", "plain", 128, 8, 1, SHORT * 8, EDGES * 8, 2),
+    ("bf16", "cache4", 128, 8, 1, SHORT * 8, EDGES * 8, 2), ("f16", "cache4", 64, 8, 1, SHORT * 8, EDGES * 8, 2),
+    # 128 rows and tiles of 64 keys in LDS
+    ("bf16", "plain", 128, 3, 1, [129, 1, 128, 33, 0, 97], [3000, 63, 1, 64, 65, 193], 3), ("f16", "plain", 64, 3, 1, [129, 1, 128, 33, 0, 97], [3000, 128, 0, 64, 65, 191], 3),
+    ("bf16", "plain", 80, 2, 5, [26, 7, 1, 30, 5, 2], [3500, 64, 65, 1, 0, 640], 3), ("f16", "plain", 96, 1, 8, [40, 33, 3, 16], [4500, 31, 127, 129], 3), ("bf16", "plain", 24, 4, 2, [70, 5, 66], [3000, 64, 65], 3),
+    ("bf16", "cache4", 128, 4, 1, [70, 64, 1, 49] * 16, [40, 64, 1, 65] * 16, 3), ("f16", "cache4", 64, 4, 1, [70, 64, 1, 49] * 16, [40, 64, 1, 130] * 16, 3), ("f16", "cache4", 96, 4, 1, [70, 64, 1, 49] * 16, [40, 0, 1, 63] * 16, 3),
+    ("bf16", "cache4", 32, 4, 1, [70, 64, 1, 49] * 16, [40, 64, 1, 65] * 16, 3),
+    # 32 rows share their keys
+    ("bf16", "plain", 128, 3, 1, [70, 33, 0, 48, 17, 1], [1500, 33, 9, 129, 1, 0], 4), ("f16", "plain", 64, 3, 2, [35, 16, 9, 1], [2500, 400, 31, 128], 4), ("f16", "plain", 88, 3, 1, [70, 33, 0, 48, 17, 1], [1500, 33, 9, 129, 1, 64], 4),
+    ("f32", "plain", 64, 3, 1, [90, 33, 0, 48, 17, 1], [3700, 33, 9, 129, 1, 0], 4), ("f32", "plain", 96, 3, 1, [90, 33, 1], [7400, 64, 129], 4), ("f32", "plain", 128, 3, 1, [90, 33, 1], [7400, 65, 129], 4),
+    ("bf16", "cache4", 128, 3, 1, [70, 33, 0, 48, 17, 1], [11600, 33, 9, 129, 1, 0], 4), ("f16", "cache4", 64, 3, 1, [70, 33, 0, 48, 17, 1], [11600, 33, 9, 129, 1, 64], 4),
+    # 16 rows, tiles of rows of several blocks
+    ("bf16", "plain", 96, 3, 1, [70, 33, 0, 48], [300, 33, 9, 129], 1), ("f32", "plain", 80, 3, 2, [35, 16, 9, 1], [300, 64, 31, 0], 1), ("f16", "cache4", 128, 3, 1, [70, 33, 0, 48], [900, 33, 9, 129], 1),
+]
+
+
+@pytest.mark.parametrize("mask", [None, 0.7], ids=["all", "mask"])
+@pytest.mark.parametrize("case", KERNELS, ids=lambda c: "%s_%s_%d_k%d" % (c[0], c[1], c[2], c[7]))
+def test_every_kernel_at_its_edges(octo, case, mask):
+    dtype, fmt, dim, kv_heads, group, q_len, kv_len, kernel = case
+    p = Problem(octo, dtype, fmt, dim, kv_heads, group, q_len, kv_len, mask, seed=dim)
+    kid = p.run(octo)
+    if octo.device_cu_count() == 256:
+        assert kid // 1000 == kernel, kid
     p.check()
 
 
@@ -178,6 +212,23 @@ def test_infinite_scores_stay_in_their_rows(octo, dtype):
     keep[int(p.kv_start[0]) + 5] = 0
     ref, _ = tokens.attend(_np(p.q), p.kv[0], p.kv[1], p.q_start, p.kv_start, p.kv_len, p.scale, keep)
     assert np.abs(out[[lo, lo + 2]] - ref[[lo, lo + 2]]).max() < 16 * E[dtype] + 1e-5
+
+
+@pytest.mark.parametrize("dtype,dim,heads,q_len,kv_len,kernel", [("bf16", 64, 1, [16], [70], 1), ("f16", 128, 3, [70, 20], [1500, 90], 4), ("bf16", 128, 3, [129, 30], [3000, 200], 3), ("f32", 64, 8, [20, 3] * 32, [49, 20] * 32, 2)])
+def test_a_query_that_is_no_number_stays_in_its_row(octo, dtype, dim, heads, q_len, kv_len, kernel):
+    import torch
+    p = Problem(octo, dtype, "plain", dim, heads, 1, q_len, kv_len, seed=7)
+    p.run(octo)
+    clean, lse = p.out.clone(), p.lse.clone()
+    sick = torch.zeros(p.q.shape[:2], dtype=torch.bool, device="cuda")
+    lo = int(p.q_start[0])
+    sick[lo + 5, 0] = sick[lo + 9, heads - 1] = True
+    p.q[sick] = torch.where(torch.arange(dim, device="cuda") == 3, float("nan"), 1.0).to(p.q.dtype)
+    kid = p.run(octo)
+    assert octo.device_cu_count() != 256 or kid // 1000 == kernel
+    assert bool(torch.isnan(p.out[sick]).all()) and bool(torch.isnan(p.lse[sick]).all())
+    # the reference of a wavefront's rows moves when one of them asks for it: the others agree within the bound, not bit for bit
+    assert float((p.out - clean)[~sick].abs().max()) <= 8 * E[dtype] * float(clean.abs().max()) + 1e-5 and float((p.lse - lse)[~sick].abs().max()) < 1e-4
 
 
 @forms
