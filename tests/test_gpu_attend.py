@@ -214,7 +214,7 @@ def test_infinite_scores_stay_in_their_rows(octo, dtype):
     assert np.abs(out[[lo, lo + 2]] - ref[[lo, lo + 2]]).max() < 16 * E[dtype] + 1e-5
 
 
-@pytest.mark.parametrize("dtype,dim,heads,q_len,kv_len,kernel", [("bf16", 64, 1, [16], [70], 1), ("f16", 128, 3, [70, 20], [1500, 90], 4), ("bf16", 128, 3, [129, 30], [3000, 200], 3), ("f32", 64, 8, [20, 3] * 32, [49, 20] * 32, 2)])
+@pytest.mark.parametrize("dtype,dim,heads,q_len,kv_len,kernel", [("bf16", 64, 1, [16], [70], 1), ("f16", 128, 3, [70, 33, 0, 48, 17, 1], [1500, 33, 9, 129, 1, 0], 4), ("bf16", 128, 3, [129, 1, 128, 33, 0, 97], [3000, 63, 1, 64, 65, 193], 3), ("f32", 64, 8, [20, 3] * 32, [49, 20] * 32, 2)])
 def test_a_query_that_is_no_number_stays_in_its_row(octo, dtype, dim, heads, q_len, kv_len, kernel):
     import torch
     p = Problem(octo, dtype, "plain", dim, heads, 1, q_len, kv_len, seed=7)
