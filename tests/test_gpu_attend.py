@@ -228,7 +228,7 @@ def test_a_query_that_is_no_number_stays_in_its_row(octo, dtype, dim, heads, q_l
     assert octo.device_cu_count() != 256 or kid // 1000 == kernel
     assert bool(torch.isnan(p.out[sick]).all()) and bool(torch.isnan(p.lse[sick]).all())
     # the reference of a wavefront's rows moves when one of them asks for it: the others agree within the bound, not bit for bit
-    assert float((p.out - clean)[~sick].abs().max()) <= 8 * E[dtype] * float(clean.abs().max()) + 1e-5 and float((p.lse - lse)[~sick].abs().max()) < 1e-4
+    assert float((p.out - clean)[~sick].abs().max()) <= 8 * E[dtype] * float(clean.abs().max()) + 1e-5 and bool(torch.isclose(p.lse, lse, rtol=0, atol=1e-4)[~sick].all())
 
 
 @forms
