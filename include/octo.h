@@ -654,7 +654,8 @@ octo_status octo_dequantize_mx4(const uint8_t* codes, const uint8_t* exps, size_
  * d_workspace: octo_op_attend_workspace_bytes(op) bytes, 16-byte aligned (NULL where that is 0), for this call alone until it is done:
  * long key sequences are split over the compute units and joined in a fixed order.  The same call on the same inputs gives the same bits.
  * *kernel_id (may be NULL): 0 nothing to do, else 1000 * kernel + the number of parts the keys were split into; kernel 1 and 4: the
- * wavefronts of a block share the keys of 16 and 32 rows (queries x q_heads / kv_heads), 2: a wavefront for 16 rows, 3: a block for 128 rows. */
+ * wavefronts of a block share the keys of 16 and 32 rows (queries x q_heads / kv_heads), 2: a wavefront for 16 rows, 3 and 5: a
+ * block for 128 rows (5: parts cut on the device by the lengths there, the number is the most a sequence can have). */
 typedef enum { OCTO_KV_PLAIN = 0, OCTO_KV_CACHE4 = 1 } octo_kv_format;
 typedef struct octo_attend_op {
   int32_t dtype, kv_format, dim, q_heads, kv_heads;

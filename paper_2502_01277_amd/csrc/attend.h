@@ -32,6 +32,8 @@ struct AttendArgs {
   int row_blocks;                                                      // of the kernel's rows, of the longest sequence
   FastDiv div_heads, div_blocks, div_split;                            // kv_heads, row_blocks, n_split
   int by_die;                                                          // blocks that read the same keys run on one die
+  int cut, slots;                                                      // attend_tile_kernel cuts its pieces itself, for so many blocks at a time;
+  int* cut_tiles;                                                      // what it took as the length of a part, for attend_join_kernel
 };
 
 enum { KV_PLAIN = OCTO_KV_PLAIN, KV_CACHE4 = OCTO_KV_CACHE4 };
@@ -64,7 +66,12 @@ __host__ inline unsigned piece_blocks(const AttendArgs& a) {
 }
 
 struct Span { int q0, n_q, n_kv; long long kv0; };
-__device__ __forceinline__ int parts_of(const AttendArgs& a, int n_kv) { return n_kv > a.part_keys ? (n_kv + a.part_keys - 1) / a.part_keys : 1; }
+__device__ __forceinline__ int parts_of(int n_kv, int part_keys) { return n_kv > part_keys ? (n_kv + part_keys - 1) / part_keys : 1; }
+// A sequence's part where parts are cut to `most` tiles of 64 keys: as many parts as that takes, of equal length.
+__device__ __forceinline__ int even_part(int n_kv, int most) {
+  const int tiles = (n_kv + 63) / 64, n = tiles > most ? (tiles + most - 1) / most : 1;
+  return 64 * (tiles ? (tiles + n - 1) / n : 1);
+}
 // The rows and keys of sequence b, cut to what the host stated; false: no such sequence, or no queries.
 __device__ __forceinline__ bool span_of(const AttendArgs& a, int b, Span* s) {
   if (a.n_dyn && b >= *a.n_dyn) return false;
@@ -300,7 +307,7 @@ __global__ __launch_bounds__(256, RT == 2 && sizeof(T) == 4 && DP == 128 ? 1 : 2
   Span sp;
   if (b >= a.n_seq || !span_of(a, b, &sp)) return;
   const int rows = sp.n_q * a.group;
-  if (row0 >= rows || part >= parts_of(a, sp.n_kv)) return;      // SHARE: the whole block
+  if (row0 >= rows || part >= parts_of(sp.n_kv, a.part_keys)) return;      // SHARE: the whole block
   const bool whole = sp.n_kv <= a.part_keys;
 
   const int tiles = (sp.n_kv + 31) / 32, per_part = a.part_keys / 32;

@@ -15,7 +15,7 @@ template <typename T>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   Span sp;
   if (!span_of(a, blockIdx.x, &sp)) return;
-  const int parts = parts_of(a, sp.n_kv), r = blockIdx.y * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31, d = lane * 4;
+  const int parts = parts_of(sp.n_kv, a.cut ? even_part(sp.n_kv, *a.cut_tiles) : a.part_keys), r = blockIdx.y * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31, d = lane * 4;
   if (parts == 1 || r >= sp.n_q * a.q_heads) return;
   const long long at = (long long)sp.q0 * a.q_heads + r, step = (long long)a.n_q * a.q_heads;
   // the first parts' sums are on their way while the references are compared; memory of all n_split parts is there, used or not
@@ -62,8 +62,8 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   store4<T>((T*)a.out + (sp.q0 + (long long)qi) * a.out_row + head * a.out_head + d, o * inv);
 }
 
-enum { SHARED_KEYS = 1, OWN_ROWS = 2, TILES = 3 };          // as in the kernel id; 4 there: SHARED_KEYS with 32 rows
-struct Plan { int kernel, how, row_blocks, n_split, part_keys; };
+enum { SHARED_KEYS = 1, OWN_ROWS = 2, TILES = 3 };          // as in the kernel id; 4 there: SHARED_KEYS with 32 rows, 5: TILES with parts cut on the device
+struct Plan { int kernel, how, row_blocks, n_split, part_keys, cut, slots; };
 
 // Which kernel, by the rows of the longest sequence, their tiles of 16 over all sequences and heads, and the keys ("512 x 49": 512 sequences of 2 heads and 49
 // keys; us, bf16, dim 128, where nothing else is said).
@@ -80,6 +80,8 @@ struct Plan { int kernel, how, row_blocks, n_split, part_keys; };
 //   differ in length, up to sixteen blocks of 2048 keys, for an even end: 16 single tokens over up to 51200 keys of 4 bits 131 -> 117 us, 17 questions
 //   of up to 96 tokens over up to 20440 keys 486 -> 453.  With TILES the rows
 //   tell: as many as n_seq x max_q, then sequences are alike and more parts only cost (2 x 2048 queries over 12800 keys 790 us whole, 829 in two parts).
+// A long call of up to 256 sequences on TILES cuts its parts on the device, where the lengths are (cut_piece; n_split is then the most a sequence can have): 24 tiles for every place a
+//   block can have at least, as looking at all lengths takes a block 5 us.
 Plan plan_of(const octo_attend_op* op, int cus) {
   Plan p{};
   const long long rows = (long long)op->max_q * (op->q_heads / op->kv_heads), pairs = (long long)op->n_seq * op->kv_heads, blocks16 = pairs * ((rows + 15) / 16);
@@ -104,6 +106,8 @@ Plan plan_of(const octo_attend_op* op, int cus) {
   n = std::max(1ll, std::min<long long>(n, MAX_PARTS));
   p.part_keys = (int)((op->max_kv + n * 64 - 1) / (n * 64)) * 64;
   p.n_split = op->max_kv > p.part_keys ? (op->max_kv + p.part_keys - 1) / p.part_keys : 1;
+  p.slots = cus * (op->dim <= 64 ? 3 : 2);                 // blocks of attend_tile_kernel at a time
+  p.cut = tiles && p.n_split > 1 && op->n_seq <= 256 && (double)blocks * ((op->max_kv + 63) / 64) >= 24.0 * p.slots;
   return p;
 }
 
@@ -132,8 +136,8 @@ bool sizes_ok(const octo_attend_op* op) {
   // pieces of work (sequences x key heads x 16 rows; x parts only where they are few) are numbered in 31 bits
   return (double)op->n_seq * op->kv_heads * (op->max_q * (double)(op->q_heads / op->kv_heads) / 16 + 1) < 2e9;
 }
-size_t part_bytes(const octo_attend_op* op, int n_split) {
-  return n_split > 1 ? (size_t)n_split * op->n_q * op->q_heads * ((size_t)op->dim * 4 + 8) : 0;
+size_t part_bytes(const octo_attend_op* op, const Plan& p) {
+  return p.n_split > 1 ? (size_t)p.n_split * op->n_q * op->q_heads * ((size_t)op->dim * 4 + 8) + 16 : 0;
 }
 bool stride_ok(long long elems, int es) { return elems >= 0 && (elems * es & 15) == 0; }
 constexpr long long MOST_ROW = 16 << 20;      // bytes between rows: 32 of them stay inside a buffer's 31 bits
@@ -148,7 +152,7 @@ extern "C" {
 size_t octo_op_attend_workspace_bytes(const octo_attend_op* op) {
   if (!sizes_ok(op) || !op->n_seq || !op->max_q) return 0;
   const int cus = cu_count();
-  return part_bytes(op, plan_of(op, cus > 0 ? cus : 256).n_split);
+  return part_bytes(op, plan_of(op, cus > 0 ? cus : 256));
 }
 
 octo_status octo_op_attend(const octo_attend_op* op, void* hip_stream, int32_t* kernel_id) {
@@ -177,7 +181,7 @@ octo_status octo_op_attend(const octo_attend_op* op, void* hip_stream, int32_t* 
   const int cus = cu_count();
   if (cus < 1) return OCTO_EHIP;
   const Plan p = plan_of(op, cus);
-  const size_t need = part_bytes(op, p.n_split);
+  const size_t need = part_bytes(op, p);
   if (need && (!op->d_workspace || ((uintptr_t)op->d_workspace & 15))) return OCTO_EINVAL;
   if (need > op->workspace_bytes) return OCTO_ENOMEM;
   a.q = op->d_q; a.q_row = op->q_row; a.q_head = op->q_head;
@@ -190,9 +194,12 @@ octo_status octo_op_attend(const octo_attend_op* op, void* hip_stream, int32_t* 
   if (need) {
     a.part_o = (float*)op->d_workspace;
     a.part_ml = (float2*)(a.part_o + (size_t)p.n_split * op->n_q * op->q_heads * op->dim);
+    a.cut_tiles = (int*)(a.part_ml + (size_t)p.n_split * op->n_q * op->q_heads);
   }
   hipStream_t s = (hipStream_t)hip_stream;
   a.part_keys = p.part_keys;
+  a.cut = p.cut;
+  a.slots = p.slots;
   a.row_blocks = p.row_blocks;
   const long long sets = (long long)op->n_seq * op->kv_heads * p.n_split;
   a.by_die = p.row_blocks > 1 && (sets % 8 == 0 || sets >= 64);
@@ -208,7 +215,7 @@ octo_status octo_op_attend(const octo_attend_op* op, void* hip_stream, int32_t* 
     else hipLaunchKernelGGL(attend_join_kernel<__bf16>, grid, dim3(256), 0, s, a);
     e = hipGetLastError();
   }
-  if (kernel_id && e == hipSuccess) *kernel_id = 1000 * (p.how == DIRECT_SHARE2 ? 4 : p.kernel) + p.n_split;
+  if (kernel_id && e == hipSuccess) *kernel_id = 1000 * (p.how == DIRECT_SHARE2 ? 4 : p.cut ? 5 : p.kernel) + p.n_split;
   return e == hipSuccess ? OCTO_OK : OCTO_EHIP;
 }
 

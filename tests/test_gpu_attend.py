@@ -148,6 +148,9 @@ KERNELS = [
     ("bf16", "plain", 80, 2, 5, [26, 7, 1, 30, 5, 2], [3500, 64, 65, 1, 0, 640], 3), ("f16", "plain", 96, 1, 8, [40, 33, 3, 16], [4500, 31, 127, 129], 3), ("bf16", "plain", 24, 4, 2, [70, 5, 66], [3000, 64, 65], 3),
     ("bf16", "cache4", 128, 4, 1, [70, 64, 1, 49] * 16, [40, 64, 1, 65] * 16, 3), ("f16", "cache4", 64, 4, 1, [70, 64, 1, 49] * 16, [40, 64, 1, 130] * 16, 3), ("f16", "cache4", 96, 4, 1, [70, 64, 1, 49] * 16, [40, 0, 1, 63] * 16, 3),
     ("bf16", "cache4", 32, 4, 1, [70, 64, 1, 49] * 16, [40, 64, 1, 65] * 16, 3),
+    # the same, with parts cut by the lengths on the device
+    ("bf16", "plain", 128, 3, 1, [129, 1, 128, 33, 0, 97], [22000, 63, 1, 64, 65, 193], 5), ("f16", "plain", 64, 4, 5, [1, 30, 0, 26, 13], [0, 33100, 64, 30000, 127], 5),
+    ("f16", "cache4", 128, 3, 1, [1, 129, 128, 33, 0, 97], [0, 22000, 1, 6400, 65, 12289], 5), ("bf16", "cache4", 64, 2, 3, [40, 90, 7, 1, 43, 0, 90, 3, 50, 88], [25000, 1, 63, 64, 65, 9, 24999, 128, 2000, 0], 5),
     # 32 rows share their keys
     ("bf16", "plain", 128, 3, 1, [70, 33, 0, 48, 17, 1], [1500, 33, 9, 129, 1, 0], 4), ("f16", "plain", 64, 3, 2, [35, 16, 9, 1], [2500, 400, 31, 128], 4), ("f16", "plain", 88, 3, 1, [70, 33, 0, 48, 17, 1], [1500, 33, 9, 129, 1, 64], 4),
     ("f32", "plain", 64, 3, 1, [90, 33, 0, 48, 17, 1], [3700, 33, 9, 129, 1, 0], 4), ("f32", "plain", 96, 3, 1, [90, 33, 1], [7400, 64, 129], 4), ("f32", "plain", 128, 3, 1, [90, 33, 1], [7400, 65, 129], 4),
@@ -252,6 +255,37 @@ def test_counts_and_lengths_on_the_device_are_cut_to_what_the_host_stated(octo, 
     p.dev[0][0], p.dev[0][4] = -100, 2 ** 30
     p.run(octo)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("fmt", ["plain", "cache4"])
+def test_parts_cut_on_the_device_follow_its_counts(octo, fmt):
+    """A long call with fewer sequences present, lengths beyond what the host stated, starts outside the pool, and the same bits twice."""
+    import torch
+    p = Problem(octo, "bf16", fmt, 128, 3, 1, [129, 40, 0, 128, 1, 2], [22000, 900, 70, 9000, 5, 6], 0.8, seed=12)
+    kw = dict(n_seq=torch.tensor([3], dtype=torch.int32, device="cuda"))
+    need = octo.attend_workspace_bytes(p.q, p.held, p.out, *p.dev, max_q=129, max_kv=22000)
+    kid = p.run(octo, workspace=torch.full((need,), 255, dtype=torch.uint8, device="cuda"), **kw)
+    assert octo.device_cu_count() != 256 or kid // 1000 == 5
+    p.check(3)
+    first = p.out.clone()
+    p.out.fill_(7)
+    p.run(octo, **kw)
+    assert torch.equal(p.out, first)
+    p.out.fill_(7), p.lse.fill_(7)
+    p.dev[1][3], p.dev[2][1] = -1, 2 ** 31 - 1
+    p.kv_len[3] = 0
+    p.kv_len[1] = min(22000, p.rows - int(p.kv_start[1]))
+    p.used[int(p.kv_start[1]):int(p.kv_start[1]) + int(p.kv_len[1])] &= p.mask[int(p.kv_start[1]):int(p.kv_start[1]) + int(p.kv_len[1])] != 0
+    if fmt == "plain":                          # rows between the sequences hold NaN: hide what the long sequence newly reads of them
+        p.mask[np.isnan(_np(p.held[0]).sum((1, 2)))] = 0
+        p.dmask.copy_(torch.from_numpy(p.mask))
+    else:
+        p.mask[(p.held.k_exps == 255).any(2).any(0).cpu().numpy()] = 0
+        p.dmask.copy_(torch.from_numpy(p.mask))
+    seen = np.arange(p.rows)
+    p.used = (p.mask != 0) & (seen >= 0)
+    p.run(octo)
+    p.check()
 
 
 @forms
