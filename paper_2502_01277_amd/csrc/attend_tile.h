@@ -341,7 +341,7 @@ hipError_t launch_tile(const AttendArgs& a, hipStream_t s) {
 }
 template <typename T>
 hipError_t launch_attend_tile(int format, const AttendArgs& a, hipStream_t s) {
-  if (format == KV_CACHE4) return a.dim <= 64 ? launch_tile<T, KV_CACHE4, 64>(a, s) : launch_tile<T, KV_CACHE4, 128>(a, s);
+  if (format == KV_CACHE4) return a.dim <= 64 ? launch_tile<T, KV_CACHE4, 64>(a, s) : a.dim <= 96 ? launch_tile<T, KV_CACHE4, 96>(a, s) : launch_tile<T, KV_CACHE4, 128>(a, s);
   if (a.dim <= 64) return launch_tile<T, KV_PLAIN, 64>(a, s);
   if (a.dim <= 96) return launch_tile<T, KV_PLAIN, 96>(a, s);
   return launch_tile<T, KV_PLAIN, 128>(a, s);

@@ -150,6 +150,7 @@ KERNELS = [
     ("bf16", "cache4", 32, 4, 1, [70, 64, 1, 49] * 16, [40, 64, 1, 65] * 16, 3),
     # the same, with parts cut by the lengths on the device
     ("bf16", "plain", 128, 3, 1, [129, 1, 128, 33, 0, 97], [22000, 63, 1, 64, 65, 193], 5), ("f16", "plain", 64, 4, 5, [1, 30, 0, 26, 13], [0, 33100, 64, 30000, 127], 5),
+    ("bf16", "cache4", 96, 3, 1, [1, 129, 128, 33, 0, 97], [0, 22000, 1, 6400, 65, 193], 5),
     ("f16", "cache4", 128, 3, 1, [1, 129, 128, 33, 0, 97], [0, 22000, 1, 6400, 65, 12289], 5), ("bf16", "cache4", 64, 2, 3, [40, 90, 7, 1, 43, 0, 90, 3, 50, 88], [25000, 1, 63, 64, 65, 9, 24999, 128, 2000, 0], 5),
     # 32 rows share their keys
     ("bf16", "plain", 128, 3, 1, [70, 33, 0, 48, 17, 1], [1500, 33, 9, 129, 1, 0], 4), ("f16", "plain", 64, 3, 2, [35, 16, 9, 1], [2500, 400, 31, 128], 4), ("f16", "plain", 88, 3, 1, [70, 33, 0, 48, 17, 1], [1500, 33, 9, 129, 1, 64], 4),
