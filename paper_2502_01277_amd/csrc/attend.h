@@ -32,6 +32,7 @@ struct AttendArgs {
   int row_blocks;                                                      // of the kernel's rows, of the longest sequence
   FastDiv div_heads, div_blocks, div_split;                            // kv_heads, row_blocks, n_split
   int by_die;                                                          // blocks that read the same keys run on one die
+  int even_tiles;                                                      // what cut takes as the length of a part where all sequences are alike, 0: nothing
   int cut, slots;                                                      // attend_tile_kernel cuts its pieces itself, for so many blocks at a time;
   int* cut_tiles;                                                      // what it took as the length of a part, for attend_join_kernel
 };

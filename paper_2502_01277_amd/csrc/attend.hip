@@ -63,7 +63,25 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
 }
 
 enum { SHARED_KEYS = 1, OWN_ROWS = 2, TILES = 3 };          // as in the kernel id; 4 there: SHARED_KEYS with 32 rows, 5: TILES with parts cut on the device
-struct Plan { int kernel, how, row_blocks, n_split, part_keys, cut, slots; };
+struct Plan { int kernel, how, row_blocks, n_split, part_keys, cut, slots, even_tiles; };
+
+// The number of parts with the least estimated end for blocks of equal length on TILES, `at_once` of them on a compute unit: the unit with the most blocks takes them in
+// rounds, alone a block has 1 / 1.6 of what the unit does with two or three, and its start and end are as long as six tiles;
+// the join as twelve, and for every part 0.6 and 0.4 for a million values written and read.
+// Fitted to 66 drawn calls of 1 to 24 parts: what it takes is 1 % off the best in the mean, three blocks a unit were 9 % off.
+long long even_parts(long long blocks, double outputs, int max_kv, int cus, int at_once) {
+  const int tiles = std::max(1, (max_kv + 63) / 64);
+  if (blocks > 65536) return 1;                             // over a hundred rounds: the last one is nothing
+  double best = 1e30;
+  long long n = 1;
+  for (int k = 1; k <= std::max(1, std::min(MAX_PARTS, max_kv / 256)); ++k) {
+    const int part = (tiles + k - 1) / k;
+    const long long parts = (tiles + part - 1) / part, most = (blocks * parts + cus - 1) / cus, last = most % at_once;
+    const double end = (most / at_once * at_once / 1.6 + (last > 1 ? last / 1.6 : last)) * (part + 6) + (parts > 1 ? 12 + parts * (0.6 + 4e-7 * outputs) : 0);
+    if (end < best) { best = end; n = parts; }
+  }
+  return n;
+}
 
 // Which kernel, by the rows of the longest sequence, their tiles of 16 over all sequences and heads, and the keys ("512 x 49": 512 sequences of 2 heads and 49
 // keys; us, bf16, dim 128, where nothing else is said).
@@ -79,9 +97,10 @@ struct Plan { int kernel, how, row_blocks, n_split, part_keys, cut, slots; };
 // Parts of the keys: as many as give every compute unit two blocks (TILES and fp32, which take longer for a key: three; OWN_ROWS: four), of at least 256 keys, and, where sequences may
 //   differ in length, up to sixteen blocks of 2048 keys, for an even end: 16 single tokens over up to 51200 keys of 4 bits 131 -> 117 us, 17 questions
 //   of up to 96 tokens over up to 20440 keys 486 -> 453.  With TILES the rows
-//   tell: as many as n_seq x max_q, then sequences are alike and more parts only cost (2 x 2048 queries over 12800 keys 790 us whole, 829 in two parts).
+//   tell: as many as n_seq x max_q, then sequences are alike, and even_parts has it: 64 x 3000, 128 rows 71 -> 59 us, 4 x 1600, 900 rows 55 -> 40,
+//   13 questions of 475 rows over 42138 keys of 4 bits 718 -> 498.
 // A long call of up to 256 sequences on TILES cuts its parts on the device, where the lengths are (cut_piece; n_split is then the most a sequence can have): 24 tiles for every place a
-//   block can have at least, as looking at all lengths takes a block 5 us.
+//   block can have at least, as looking at all lengths takes a block 5 us.  Where it finds them alike it takes even_parts's length.
 Plan plan_of(const octo_attend_op* op, int cus) {
   Plan p{};
   const long long rows = (long long)op->max_q * (op->q_heads / op->kv_heads), pairs = (long long)op->n_seq * op->kv_heads, blocks16 = pairs * ((rows + 15) / 16);
@@ -103,11 +122,18 @@ Plan plan_of(const octo_attend_op* op, int cus) {
   auto parts = [&](int target, int least) { return blocks > 0 ? std::min<long long>((long long)target * cus / blocks, op->max_kv / least) : 1; };
   long long n = parts(p.kernel == OWN_ROWS ? 4 : f32 || tiles ? 3 : 2, 256);
   if (!alike) n = std::max(n, parts(16, 2048));
-  n = std::max(1ll, std::min<long long>(n, MAX_PARTS));
-  p.part_keys = (int)((op->max_kv + n * 64 - 1) / (n * 64)) * 64;
-  p.n_split = op->max_kv > p.part_keys ? (op->max_kv + p.part_keys - 1) / p.part_keys : 1;
-  p.slots = cus * (op->dim <= 64 ? 3 : 2);                 // blocks of attend_tile_kernel at a time
+  const int at_once = op->dim <= 64 ? 3 : 2;
+  const long long even = alike ? even_parts(blocks, (double)op->n_q * op->q_heads * op->dim, op->max_kv, cus, at_once) : 1;
+  auto split = [&](long long n) {
+    n = std::max(1ll, std::min<long long>(n, MAX_PARTS));
+    p.part_keys = (int)((op->max_kv + n * 64 - 1) / (n * 64)) * 64;
+    p.n_split = op->max_kv > p.part_keys ? (op->max_kv + p.part_keys - 1) / p.part_keys : 1;
+  };
+  split(std::max(n, even));
+  p.slots = cus * at_once;                                 // blocks of attend_tile_kernel at a time
   p.cut = tiles && p.n_split > 1 && op->n_seq <= 256 && (double)blocks * ((op->max_kv + 63) / 64) >= 24.0 * p.slots;
+  p.even_tiles = alike ? (int)(((op->max_kv + 63) / 64 + even - 1) / even) : 0;
+  if (alike && !p.cut) split(even);
   return p;
 }
 
@@ -198,7 +224,7 @@ octo_status octo_op_attend(const octo_attend_op* op, void* hip_stream, int32_t* 
   }
   hipStream_t s = (hipStream_t)hip_stream;
   a.part_keys = p.part_keys;
-  a.cut = p.cut;
+  a.cut = p.cut; a.even_tiles = p.even_tiles;
   a.slots = p.slots;
   a.row_blocks = p.row_blocks;
   const long long sets = (long long)op->n_seq * op->kv_heads * p.n_split;

@@ -30,6 +30,7 @@ template <int RB> __device__ __forceinline__ int swizzle_v(int row) { return RB 
 // parts at all -, and finds its sequence by a running sum.  With parts of a fixed number of keys ragged sequences leave a last round half empty:
 // 60 drawn calls of more than 1000 keys take 4 to 5 % less in the mean, ragged ones up to a third (9 questions of up to 79 tokens over up to 22497 keys of 4 bits 193 -> 134 us, 29 texts of
 // up to 1053 tokens over up to 7029 keys 420 -> 336), single ones more (136 x 258 over up to 10341 321 -> 375).
+// Where the sequences turn out to be of equal length, the host's number of parts stands (even_tiles).
 struct CutPiece { int seq, head, block, part, part_keys, q0, n_q, n_kv; long long kv0; };
 constexpr float CUT_ROUNDS[3] = {0.85f, 1.85f, 2.85f};       // what of the last round may be lost to sequences shorter than a part
 __device__ __forceinline__ bool cut_piece(const AttendArgs& a, CutPiece* piece, float (*red)[8], int* ends) {
@@ -65,6 +66,7 @@ __device__ __forceinline__ bool cut_piece(const AttendArgs& a, CutPiece* piece, 
     const float n = (red[0][3 + c] + red[1][3 + c] + red[2][3 + c] + red[3][3 + c]) * a.kv_heads, end = ceilf(n / slots) * (most[c] + 3.f) + 4.f;
     if (end < best) { best = end; part = most[c]; }
   }
+  if (a.even_tiles > 0 && work >= whole * longest * (15.f / 16.f) && whole >= (float)a.n_seq * a.row_blocks * a.kv_heads * (15.f / 16.f)) part = max(least, a.even_tiles);
   if (blockIdx.x == 0 && i == 0) *a.cut_tiles = part;
   // whose piece is it
   const int part_keys = even_part(has ? sp.n_kv : 0, part), mine = has ? blocks * a.kv_heads * parts_of(sp.n_kv, part_keys) : 0;

@@ -289,6 +289,31 @@ def test_parts_cut_on_the_device_follow_its_counts(octo, fmt):
     p.check()
 
 
+@pytest.mark.parametrize("dtype,fmt,dim,heads,group,q_len,kv_len,kernel", [
+    ("bf16", "plain", 128, 6, 4, [64, 64, 64], [22000, 22000, 21990], 5), ("f16", "cache4", 96, 6, 4, [64, 64, 64], [22000, 22000, 21990], 5),
+    # the host takes them to be alike and they are not
+    ("f16", "plain", 72, 6, 4, [64, 64, 64], [22000, 0, 700], 5), ("bf16", "plain", 64, 2, 1, [128] * 16, [3000] * 15 + [1], 3),
+    ("bf16", "plain", 128, 3, 2, [300, 300], [2000, 2000], 3),
+], ids=lambda v: str(v) if not isinstance(v, list) else "")
+def test_parts_of_sequences_of_equal_length(octo, dtype, fmt, dim, heads, group, q_len, kv_len, kernel):
+    p = Problem(octo, dtype, fmt, dim, heads, group, q_len, kv_len, None, seed=14)
+    kid = p.run(octo)
+    p.check()
+    assert octo.device_cu_count() != 256 or (kid // 1000 == kernel and kid % 1000 > 1)
+    first = p.out.clone()
+    p.out.fill_(7)
+    p.run(octo)
+    import torch
+    assert torch.equal(p.out, first)
+
+
+def test_no_keys_for_many_equal_rows(octo):
+    """max_kv of zero with the rows of a long call."""
+    p = Problem(octo, "bf16", "plain", 64, 2, 1, [513] * 200, [0] * 200, None, seed=15)
+    p.run(octo)
+    p.check()
+
+
 @forms
 def test_strided_tensors_and_another_stream(octo, dtype, fmt):
     """Queries as slices of a wider projection, heads of the pool outermost, the result into a wider buffer."""
