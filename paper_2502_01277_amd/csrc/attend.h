@@ -10,8 +10,8 @@
 #pragma once
 #include <cfloat>
 
+#include "attend_choice.h"
 #include "mfma_common.h"
-#include "octo_internal.h"
 
 namespace octo {
 
@@ -33,12 +33,11 @@ struct AttendArgs {
   FastDiv div_heads, div_blocks, div_split;                            // kv_heads, row_blocks, n_split
   int by_die;                                                          // blocks that read the same keys run on one die
   int even_tiles;                                                      // what cut takes as the length of a part where all sequences are alike, 0: nothing
-  int cut, slots;                                                      // attend_tile_kernel cuts its pieces itself, for so many blocks at a time;
+  int cut, slots;                                                      // not 0: attend_tile_kernel cuts its pieces itself, in `cut` blocks, `slots` of them at a time;
   int* cut_tiles;                                                      // what it took as the length of a part, for attend_join_kernel
 };
 
 enum { KV_PLAIN = OCTO_KV_PLAIN, KV_CACHE4 = OCTO_KV_CACHE4 };
-enum { DIRECT_OWN = 0, DIRECT_SHARE = 1, DIRECT_SHARE2 = 2 };      // 16 rows a wavefront, 16 or 32 a block whose wavefronts share the keys
 
 hipError_t launch_attend_direct_f16(int format, int how, const AttendArgs& a, hipStream_t s);
 hipError_t launch_attend_direct_bf16(int format, int how, const AttendArgs& a, hipStream_t s);
@@ -67,12 +66,6 @@ __host__ inline unsigned piece_blocks(const AttendArgs& a) {
 }
 
 struct Span { int q0, n_q, n_kv; long long kv0; };
-__device__ __forceinline__ int parts_of(int n_kv, int part_keys) { return n_kv > part_keys ? (n_kv + part_keys - 1) / part_keys : 1; }
-// A sequence's part where parts are cut to `most` tiles of 64 keys: as many parts as that takes, of equal length.
-__device__ __forceinline__ int even_part(int n_kv, int most) {
-  const int tiles = (n_kv + 63) / 64, n = tiles > most ? (tiles + most - 1) / most : 1;
-  return 64 * (tiles ? (tiles + n - 1) / n : 1);
-}
 // The rows and keys of sequence b, cut to what the host stated; false: no such sequence, or no queries.
 __device__ __forceinline__ bool span_of(const AttendArgs& a, int b, Span* s) {
   if (a.n_dyn && b >= *a.n_dyn) return false;

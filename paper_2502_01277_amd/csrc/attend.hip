@@ -1,4 +1,4 @@
-// octo_op_attend: arguments, the choice of kernel and of the number of parts, and the kernel that joins parts.
+// octo_op_attend: arguments, and the kernel that joins parts.
 #include <algorithm>
 #include <cmath>
 #include <mutex>
@@ -10,7 +10,6 @@ namespace {
 
 // Adds up the parts of a row: sum_p 2^(ref_p - m) (o_p, sum_p), m the largest reference, in the order of the parts.  Half a wavefront has a
 // row: its lanes take references and sums of 32 parts at a time, then four elements of dim each.
-constexpr int MAX_PARTS = 128;
 template <typename T>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   Span sp;
@@ -60,81 +59,6 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   if (d == 0 && a.lse) a.lse[at] = total != 0.f ? (m + log2f(total)) * 0.693147180559945f : -INFINITY;
   const int qi = r / a.q_heads, head = r - qi * a.q_heads;
   store4<T>((T*)a.out + (sp.q0 + (long long)qi) * a.out_row + head * a.out_head + d, o * inv);
-}
-
-enum { SHARED_KEYS = 1, OWN_ROWS = 2, TILES = 3 };          // as in the kernel id; 4 there: SHARED_KEYS with 32 rows, 5: TILES with parts cut on the device
-struct Plan { int kernel, how, row_blocks, n_split, part_keys, cut, slots, even_tiles; };
-
-// The number of parts with the least estimated end for blocks of equal length on TILES, `at_once` of them on a compute unit: the unit with the most blocks takes them in
-// rounds, alone a block has 1 / 1.6 of what the unit does with two or three, and its start and end are as long as six tiles;
-// the join as twelve, and for every part 0.6 and 0.4 for a million values written and read.
-// Fitted to 66 drawn calls of 1 to 24 parts: what it takes is 1 % off the best in the mean, three blocks a unit were 9 % off.
-long long even_parts(long long blocks, double outputs, int max_kv, int cus, int at_once) {
-  const int tiles = std::max(1, (max_kv + 63) / 64);
-  if (blocks > 65536) return 1;                             // over a hundred rounds: the last one is nothing
-  double best = 1e30;
-  long long n = 1;
-  for (int k = 1; k <= std::max(1, std::min(MAX_PARTS, max_kv / 256)); ++k) {
-    const int part = (tiles + k - 1) / k;
-    const long long parts = (tiles + part - 1) / part, most = (blocks * parts + cus - 1) / cus, last = most % at_once;
-    const double end = (most / at_once * at_once / 1.6 + (last > 1 ? last / 1.6 : last)) * (part + 6) + (parts > 1 ? 12 + parts * (0.6 + 4e-7 * outputs) : 0);
-    if (end < best) { best = end; n = parts; }
-  }
-  return n;
-}
-
-// Which kernel, by the rows of the longest sequence, their tiles of 16 over all sequences and heads, and the keys ("512 x 49": 512 sequences of 2 heads and 49
-// keys; us, bf16, dim 128, where nothing else is said).
-//   OWN_ROWS where there are tiles for all wavefronts and few keys to share: 512 x 49, 8 / 16 / 32 / 48 rows 9.7 / 11.4 / 15.0 / 19.5 against 12.1 / 13.3 / 20.2 /
-//     27.3 (SHARED_KEYS) and 14.1 / 14.5 / 15.6 / 17.0 (TILES); from 4 bits also 400 keys, 20 and 48 rows: 22.8, 30.3 : 26.5, 36.1 : 32.2, 36.7; fp32,
-//     512 x 400, dim 64, 20 and 128 rows: 52.8, 153 : 66.0, 187.
-//   SHARED_KEYS for up to 16 rows, for all else in fp32, and where the whole call is short, as its wavefronts are quickly done: 4 x 400, 128 rows 8.2 against 13.7
-//     (TILES); 64 x 400, 32, 64 and 96 rows: 10.9, 12.7, 17.5 : 14.1, 14.6, 15.5; further for few long sequences (4 x 24000, 64 and 128 rows: 32, 44 : 40, 46; but
-//     64 x 3000, 64 rows 59.9 : 59.6) and from 4 bits, which TILES converts first and then puts in LDS (64 x 3000, 64 and 128 rows: 33, 42 : 47, 60).
-//   TILES for the rest: 64 x 3000, 128 rows 70 against 76; 512 x 400: 66 against 112; many short ones: 137 sequences of 4084 rows and 37 keys 89 against 205.
-// SHARED_KEYS with 32 rows a block instead of 16 where there are many tiles: the keys are read and put in order half as often (64 x 3000, 64 and 128 rows: 75, 131 ->
-//   60, 76; from 4 bits 33, 54 -> 33, 42; fp32, dim 64: 88, 161 -> 79, 114), but a short call is longer (4 x 400: 8.2 -> 10.0; fp32, 77 rows in 5 tiles 29 -> 37).
-// Parts of the keys: as many as give every compute unit two blocks (TILES and fp32, which take longer for a key: three; OWN_ROWS: four), of at least 256 keys, and, where sequences may
-//   differ in length, up to sixteen blocks of 2048 keys, for an even end: 16 single tokens over up to 51200 keys of 4 bits 131 -> 117 us, 17 questions
-//   of up to 96 tokens over up to 20440 keys 486 -> 453.  With TILES the rows
-//   tell: as many as n_seq x max_q, then sequences are alike, and even_parts has it: 64 x 3000, 128 rows 71 -> 59 us, 4 x 1600, 900 rows 55 -> 40,
-//   13 questions of 475 rows over 42138 keys of 4 bits 718 -> 498.
-// A long call of up to 256 sequences on TILES cuts its parts on the device, where the lengths are (cut_piece; n_split is then the most a sequence can have): 24 tiles for every place a
-//   block can have at least, as looking at all lengths takes a block 5 us.  Where it finds them alike it takes even_parts's length.
-Plan plan_of(const octo_attend_op* op, int cus) {
-  Plan p{};
-  const long long rows = (long long)op->max_q * (op->q_heads / op->kv_heads), pairs = (long long)op->n_seq * op->kv_heads, blocks16 = pairs * ((rows + 15) / 16);
-  const bool f32 = op->dtype == OCTO_F32, four_bits = op->kv_format == OCTO_KV_CACHE4;
-  const double work = (double)blocks16 * op->max_kv / cus;          // keys a compute unit reads if every tile reads its own
-  const bool many = blocks16 >= 4ll * cus, long_enough = !many || op->max_kv >= 384;
-  if (many && (f32 ? op->max_kv <= 512 : four_bits ? op->max_kv <= 512 && rows <= 48 : op->max_kv <= 128 && rows <= 32)) p.kernel = OWN_ROWS;
-  else if (f32 || rows <= 16) p.kernel = SHARED_KEYS;
-  else if (four_bits) p.kernel = (long_enough && work <= 5500) || (rows <= 128 && op->max_kv >= 2048 && work <= 13000) ? SHARED_KEYS : TILES;
-  else p.kernel = long_enough && work <= (rows <= 32 ? 3000 : rows <= 128 && op->max_kv >= 8192 ? 6000 : 1000) ? SHARED_KEYS : TILES;
-  const bool tiles = p.kernel == TILES;
-  const long long tiles16 = (rows + 15) / 16;
-  const bool pairs_of_tiles = f32 ? work >= 1500 && (tiles16 % 2 == 0 || tiles16 > 6) : four_bits ? rows > 64 && work >= 4000 : work >= (rows <= 32 ? 2000 : 400);
-  p.how = p.kernel == OWN_ROWS ? DIRECT_OWN : p.kernel == SHARED_KEYS && rows > 16 && pairs_of_tiles ? DIRECT_SHARE2 : DIRECT_SHARE;
-  const int block_rows = tiles ? 128 : p.how == DIRECT_SHARE2 ? 32 : 16;
-  p.row_blocks = (int)((rows + block_rows - 1) / block_rows);
-  const long long blocks = p.kernel == OWN_ROWS ? (blocks16 + 3) / 4 : pairs * p.row_blocks;
-  const bool alike = tiles && op->n_q >= (long long)op->n_seq * op->max_q * 15 / 16;
-  auto parts = [&](int target, int least) { return blocks > 0 ? std::min<long long>((long long)target * cus / blocks, op->max_kv / least) : 1; };
-  long long n = parts(p.kernel == OWN_ROWS ? 4 : f32 || tiles ? 3 : 2, 256);
-  if (!alike) n = std::max(n, parts(16, 2048));
-  const int at_once = op->dim <= 64 ? 3 : 2;
-  const long long even = alike ? even_parts(blocks, (double)op->n_q * op->q_heads * op->dim, op->max_kv, cus, at_once) : 1;
-  auto split = [&](long long n) {
-    n = std::max(1ll, std::min<long long>(n, MAX_PARTS));
-    p.part_keys = (int)((op->max_kv + n * 64 - 1) / (n * 64)) * 64;
-    p.n_split = op->max_kv > p.part_keys ? (op->max_kv + p.part_keys - 1) / p.part_keys : 1;
-  };
-  split(std::max(n, even));
-  p.slots = cus * at_once;                                 // blocks of attend_tile_kernel at a time
-  p.cut = tiles && p.n_split > 1 && op->n_seq <= 256 && (double)blocks * ((op->max_kv + 63) / 64) >= 24.0 * p.slots;
-  p.even_tiles = alike ? (int)(((op->max_kv + 63) / 64 + even - 1) / even) : 0;
-  if (alike && !p.cut) split(even);
-  return p;
 }
 
 constexpr int MAX_DEVICES = 64;
@@ -224,7 +148,7 @@ octo_status octo_op_attend(const octo_attend_op* op, void* hip_stream, int32_t* 
   }
   hipStream_t s = (hipStream_t)hip_stream;
   a.part_keys = p.part_keys;
-  a.cut = p.cut; a.even_tiles = p.even_tiles;
+  a.cut = p.cut ? (int)cut_blocks(p, (long long)op->n_seq * op->kv_heads * p.row_blocks, op->max_kv) : 0; a.even_tiles = p.even_tiles;
   a.slots = p.slots;
   a.row_blocks = p.row_blocks;
   const long long sets = (long long)op->n_seq * op->kv_heads * p.n_split;

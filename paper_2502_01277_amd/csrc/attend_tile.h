@@ -32,7 +32,6 @@ template <int RB> __device__ __forceinline__ int swizzle_v(int row) { return RB 
 // up to 1053 tokens over up to 7029 keys 420 -> 336), single ones more (136 x 258 over up to 10341 321 -> 375).
 // Where the sequences turn out to be of equal length, the host's number of parts stands (even_tiles).
 struct CutPiece { int seq, head, block, part, part_keys, q0, n_q, n_kv; long long kv0; };
-constexpr float CUT_ROUNDS[3] = {0.85f, 1.85f, 2.85f};       // what of the last round may be lost to sequences shorter than a part
 __device__ __forceinline__ bool cut_piece(const AttendArgs& a, CutPiece* piece, float (*red)[8], int* ends) {
   const int i = threadIdx.x, lane = i & 63, wave = i >> 6;
   Span sp;
@@ -46,27 +45,22 @@ __device__ __forceinline__ bool cut_piece(const AttendArgs& a, CutPiece* piece, 
   work = (red[0][0] + red[1][0] + red[2][0] + red[3][0]) * a.kv_heads;
   whole = (red[0][1] + red[1][1] + red[2][1] + red[3][1]) * a.kv_heads;
   longest = fmaxf(fmaxf(red[0][2], red[1][2]), fmaxf(red[2][2], red[3][2]));
+  const CutSums sums{work, whole, longest};
   const float slots = (float)a.slots;
-  const int least = max(4, ((int)longest + a.n_split - 1) / a.n_split);
+  const int least = cut_least(sums, a.n_split);
   int most[3];
   float pieces[3];
 #pragma unroll
   for (int c = 0; c < 3; ++c) {
-    most[c] = max(least, (int)ceilf(work / (slots * CUT_ROUNDS[c])));
+    most[c] = cut_most(sums, slots, least, c);
     pieces[c] = (float)(blocks * (tiles > most[c] ? (tiles + most[c] - 1) / most[c] : 1));
     for (int d = 1; d < 64; d *= 2) pieces[c] += __shfl_xor(pieces[c], d);
     if (lane == 0) red[wave][3 + c] = pieces[c];
   }
   __syncthreads();
-  // in tiles: a block's start and end are as long as three, the join as four; without parts the longest sequence may come last
-  int part = max(1, (int)longest);
-  float best = whole <= slots ? longest + 3.f : work / slots + longest + 3.f;
 #pragma unroll
-  for (int c = 0; c < 3; ++c) {
-    const float n = (red[0][3 + c] + red[1][3 + c] + red[2][3 + c] + red[3][3 + c]) * a.kv_heads, end = ceilf(n / slots) * (most[c] + 3.f) + 4.f;
-    if (end < best) { best = end; part = most[c]; }
-  }
-  if (a.even_tiles > 0 && work >= whole * longest * (15.f / 16.f) && whole >= (float)a.n_seq * a.row_blocks * a.kv_heads * (15.f / 16.f)) part = max(least, a.even_tiles);
+  for (int c = 0; c < 3; ++c) pieces[c] = (red[0][3 + c] + red[1][3 + c] + red[2][3 + c] + red[3][3 + c]) * a.kv_heads;
+  const int part = cut_tiles(sums, most, pieces, slots, least, a.even_tiles, (float)a.n_seq * a.row_blocks * a.kv_heads, (float)a.cut);
   if (blockIdx.x == 0 && i == 0) *a.cut_tiles = part;
   // whose piece is it
   const int part_keys = even_part(has ? sp.n_kv : 0, part), mine = has ? blocks * a.kv_heads * parts_of(sp.n_kv, part_keys) : 0;
@@ -335,8 +329,7 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
 
 template <typename T, int FORMAT, int DP>
 hipError_t launch_tile(const AttendArgs& a, hipStream_t s) {
-  // cut on the device: no more pieces than CUT_ROUNDS rounds and a last part of every sequence
-  const dim3 grid(a.cut ? (unsigned)(3 * a.slots + a.n_seq * a.kv_heads * a.row_blocks) : piece_blocks(a));
+  const dim3 grid(a.cut ? (unsigned)a.cut : piece_blocks(a));
   if (a.mask) hipLaunchKernelGGL((attend_tile_kernel<T, FORMAT, DP, true>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((attend_tile_kernel<T, FORMAT, DP, false>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
