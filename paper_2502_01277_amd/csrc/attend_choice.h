@@ -14,7 +14,7 @@ enum { SHARED_KEYS = 1, OWN_ROWS = 2, TILES = 3 };          // as in the kernel 
 
 struct Plan { int kernel, how, row_blocks, n_split, part_keys, cut, slots, even_tiles; };
 
-__host__ __device__ inline int parts_of(int n_kv, int part_keys) { return n_kv > part_keys ? (n_kv + part_keys - 1) / part_keys : 1; }
+__host__ __device__ inline int parts_of(int n_kv, int part_keys) { return n_kv > part_keys ? (n_kv - 1) / part_keys + 1 : 1; }
 // A sequence's part where parts are cut to `most` tiles of 64 keys: as many parts as that takes, of equal length.
 __host__ __device__ inline int even_part(int n_kv, int most) {
   const int tiles = (n_kv + 63) / 64, n = tiles > most ? (tiles + most - 1) / most : 1;
@@ -119,7 +119,7 @@ inline Plan plan_of(const octo_attend_op* op, int cus) {
   auto split = [&](long long n) {
     n = std::max(1ll, std::min<long long>(n, MAX_PARTS));
     p.part_keys = (int)((op->max_kv + n * 64 - 1) / (n * 64)) * 64;
-    p.n_split = op->max_kv > p.part_keys ? (op->max_kv + p.part_keys - 1) / p.part_keys : 1;
+    p.n_split = parts_of(op->max_kv, p.part_keys);
   };
   split(std::max(n, even));
   p.slots = cus * at_once;                                 // blocks of attend_tile_kernel at a time

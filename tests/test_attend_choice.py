@@ -113,3 +113,13 @@ def test_calls_of_more_than_three_rounds_of_pieces(ask):
         ("f16", True, 128, 32, 8, 17, 96, 20440), ("f16", True, 128, 32, 8, 5, 197, 49903), ("f16", False, 80, 16, 8, 6, 642, 21877), ("bf16", True, 128, 17, 1, 171, 1, 51200)]]
     for call, (tiles, cut, pieces, blocks, parts, room) in zip(calls, ask(calls)):
         assert tiles and cut and parts > 1 and pieces <= blocks and parts <= room, (call[:5], pieces, blocks, parts, room)
+
+
+@pytest.mark.parametrize("long", [False, True], ids=["stated", "there"])
+def test_as_many_keys_as_are_taken(ask, long):
+    """The largest number of keys that a call may state, with short sequences and with such a one."""
+    most = 0x7FFFFF00
+    calls = [(dtype, four, dim, 4 * hk, hk, [q] * n, [most if long else 700] * n, (q, most), 256) for dtype, four, dim in (("bf16", False, 128), ("f32", False, 64), ("f16", True, 96))
+             for hk in (1, 8) for n in (1, 3, 30, 200, 300) for q in (1, 9, 40, 700)]
+    for call, (tiles, cut, pieces, blocks, parts, room) in zip(calls, ask(calls)):
+        assert 1 <= parts <= room <= 128 and (not cut or pieces <= blocks) and (parts == 1) == (not long or room == 1), (call[:5], len(call[5]), call[5][0], parts, room, pieces, blocks)

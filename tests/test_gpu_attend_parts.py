@@ -97,3 +97,12 @@ def test_nearly_equal_sequences(octo, dtype, fmt, dim, q_heads, kv_heads, q_len,
     kid = p.run(octo)
     assert octo.device_cu_count() != 256 or kid // 1000 == 5, kid
     p.check()
+
+
+@pytest.mark.parametrize("dtype,fmt,dim,q_len,kv_len", [("bf16", "plain", 128, [1, 2], [700, 33]), ("f32", "plain", 64, [40, 3], [300, 65]), ("f16", "cache4", 96, [7] * 40, [500] * 40), ("bf16", "plain", 72, [300, 299], [900, 64])])
+def test_no_limit_stated(octo, dtype, fmt, dim, q_len, kv_len):
+    """Sequences of a few keys where the host states the largest number that is taken."""
+    from test_gpu_attend import Problem
+    p = Problem(octo, dtype, fmt, dim, 2, 4, q_len, kv_len, 0.8, seed=5)
+    assert p.run(octo, max_kv=0x7FFFFF00) % 1000 > 1
+    p.check()
