@@ -22,11 +22,11 @@ __host__ __device__ inline int even_part(int n_kv, int most) {
 }
 
 // Parts cut on the device.  What the lengths there sum up to: blocks x tiles and blocks over all sequences and key heads, and the tiles of the longest sequence.
-struct CutSums { float work, whole, longest; };
+struct CutSums { float work, whole; int longest; };
 constexpr float CUT_ROUNDS[3] = {0.85f, 1.85f, 2.85f};       // what of the last round may be lost to sequences shorter than a part
 // No sequence may have more parts than the workspace holds.
 __host__ __device__ inline int cut_least(const CutSums& s, int n_split) {
-  const int n = ((int)s.longest + n_split - 1) / n_split;
+  const int n = (s.longest + n_split - 1) / n_split;
   return n > 4 ? n : 4;
 }
 __host__ __device__ inline int cut_most(const CutSums& s, float slots, int least, int c) {
@@ -37,16 +37,17 @@ __host__ __device__ inline int cut_most(const CutSums& s, float slots, int least
 // three, the join as four; without parts the longest sequence may come last.  Where the sequences are as long as each other and as the host stated (`stated` blocks), even_tiles,
 // if the `blocks` there are enough for its pieces.
 __host__ __device__ inline int cut_tiles(const CutSums& s, const int* most, const float* pieces, float slots, int least, int even_tiles, float stated, float blocks) {
-  int part = s.longest > 1.f ? (int)s.longest : 1;
-  float best = s.whole <= slots ? s.longest + 3.f : s.work / slots + s.longest + 3.f;
+  int part = s.longest > 1 ? s.longest : 1;
+  const float longest = (float)s.longest;
+  float best = s.whole <= slots ? longest + 3.f : s.work / slots + longest + 3.f;
 #pragma unroll
   for (int c = 0; c < 3; ++c) {
     const float end = ceilf(pieces[c] / slots) * (most[c] + 3.f) + 4.f;
     if (end < best) { best = end; part = most[c]; }
   }
-  if (even_tiles > 0 && s.work >= s.whole * s.longest * (15.f / 16.f) && s.whole >= stated * (15.f / 16.f)) {
+  if (even_tiles > 0 && s.work >= s.whole * longest * (15.f / 16.f) && s.whole >= stated * (15.f / 16.f)) {
     const int even = least > even_tiles ? least : even_tiles;
-    if (s.whole * (float)(((int)s.longest + even - 1) / even) <= blocks) part = even;
+    if (s.whole * (float)((s.longest + even - 1) / even) <= blocks) part = even;
   }
   return part;
 }

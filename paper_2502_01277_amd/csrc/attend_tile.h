@@ -38,13 +38,14 @@ __device__ __forceinline__ bool cut_piece(const AttendArgs& a, CutPiece* piece, 
   const bool has = i < a.n_seq && span_of(a, i, &sp);
   const int blocks = has ? (sp.n_q * a.group + 127) / 128 : 0, tiles = has ? (sp.n_kv + 63) / 64 : 0;
   if (i == 0) piece->seq = -1;
-  float work = (float)blocks * tiles, whole = (float)blocks, longest = (float)tiles;
-  for (int d = 1; d < 64; d *= 2) { work += __shfl_xor(work, d); whole += __shfl_xor(whole, d); longest = fmaxf(longest, __shfl_xor(longest, d)); }
-  if (lane == 0) { red[wave][0] = work; red[wave][1] = whole; red[wave][2] = longest; }
+  float work = (float)blocks * tiles, whole = (float)blocks;
+  int longest = tiles;
+  for (int d = 1; d < 64; d *= 2) { work += __shfl_xor(work, d); whole += __shfl_xor(whole, d); longest = max(longest, __shfl_xor(longest, d)); }
+  if (lane == 0) { red[wave][0] = work; red[wave][1] = whole; ends[wave] = longest; }
   __syncthreads();
   work = (red[0][0] + red[1][0] + red[2][0] + red[3][0]) * a.kv_heads;
   whole = (red[0][1] + red[1][1] + red[2][1] + red[3][1]) * a.kv_heads;
-  longest = fmaxf(fmaxf(red[0][2], red[1][2]), fmaxf(red[2][2], red[3][2]));
+  longest = max(max(ends[0], ends[1]), max(ends[2], ends[3]));      // ends: free again after the next barrier
   const CutSums sums{work, whole, longest};
   const float slots = (float)a.slots;
   const int least = cut_least(sums, a.n_split);

@@ -24,7 +24,7 @@ int main() {
     std::vector<long long> blocks(op.n_seq), tiles(op.n_seq);
     for (int i = 0; i < op.n_seq; ++i) {
       blocks[i] = ((long long)q[i] * group + 127) / 128; tiles[i] = q[i] ? ((long long)kv[i] + 63) / 64 : 0;
-      s.work += (float)blocks[i] * tiles[i] * op.kv_heads; s.whole += (float)blocks[i] * op.kv_heads; s.longest = std::max(s.longest, (float)tiles[i]);
+      s.work += (float)blocks[i] * tiles[i] * op.kv_heads; s.whole += (float)blocks[i] * op.kv_heads; s.longest = std::max(s.longest, (int)tiles[i]);
     }
     const long long there = p.cut ? cut_blocks(p, (long long)op.n_seq * op.kv_heads * p.row_blocks, op.max_kv) : 0;
     const int least = cut_least(s, p.n_split);
@@ -123,3 +123,11 @@ def test_as_many_keys_as_are_taken(ask, long):
              for hk in (1, 8) for n in (1, 3, 30, 200, 300) for q in (1, 9, 40, 700)]
     for call, (tiles, cut, pieces, blocks, parts, room) in zip(calls, ask(calls)):
         assert 1 <= parts <= room <= 128 and (not cut or pieces <= blocks) and (parts == 1) == (not long or room == 1), (call[:5], len(call[5]), call[5][0], parts, room, pieces, blocks)
+
+
+@pytest.mark.parametrize("keys", [2 ** 30 + 64, 2 ** 30 + 3 * 64 + 1, 2 ** 31 - 5 * 64, 2 ** 31 - 2 ** 24])
+def test_sequences_longer_than_fp32_counts(ask, keys):
+    """More than 2^24 tiles: no sequence may have more parts than the workspace."""
+    calls = [("bf16", False, 64, 17 * hk, hk, q, [keys] * len(q), (max(q), keys), 256) for hk in (1, 2) for q in ([1], [5], [300], [5, 1], [300, 2], [40, 1, 0])]
+    for call, (tiles, cut, pieces, blocks, parts, room) in zip(calls, ask(calls)):
+        assert tiles and cut and 1 <= parts <= room and pieces <= blocks, (call[3:6], parts, room, pieces, blocks)
