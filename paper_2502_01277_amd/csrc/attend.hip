@@ -83,7 +83,7 @@ bool sizes_ok(const octo_attend_op* op) {
   if (op->kv_heads < 1 || op->q_heads < op->kv_heads || op->q_heads % op->kv_heads || op->q_heads > 4096) return false;
   if (op->n_seq < 0 || op->n_q < 0 || op->max_q < 0 || op->max_kv < 0 || op->kv_rows < 0) return false;
   if (op->max_q > op->n_q || op->max_kv > 0x7FFFFF00) return false;
-  // pieces of work (sequences x key heads x 16 rows; x parts only where they are few) are numbered in 31 bits
+  if ((long long)op->max_q * op->q_heads > 0x7FFFFF00) return false;       // rows of a sequence are numbered in 31 bits
   return (double)op->n_seq * op->kv_heads * (op->max_q * (double)(op->q_heads / op->kv_heads) / 16 + 1) < 2e9;
 }
 size_t part_bytes(const octo_attend_op* op, const Plan& p) {

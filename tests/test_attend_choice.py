@@ -131,3 +131,15 @@ def test_sequences_longer_than_fp32_counts(ask, keys):
     calls = [("bf16", False, 64, 17 * hk, hk, q, [keys] * len(q), (max(q), keys), 256) for hk in (1, 2) for q in ([1], [5], [300], [5, 1], [300, 2], [40, 1, 0])]
     for call, (tiles, cut, pieces, blocks, parts, room) in zip(calls, ask(calls)):
         assert tiles and cut and 1 <= parts <= room and pieces <= blocks, (call[3:6], parts, room, pieces, blocks)
+
+
+@pytest.mark.parametrize("n_q,q_heads,kv_heads", [(2 ** 28, 8, 8), (2 ** 28, 8, 1), (2 ** 29 - 1, 5, 5), (2 ** 31 - 1, 1, 1), (2 ** 31 - 1, 4, 2), (2 ** 19, 4096, 4096)])
+def test_rows_that_32_bits_do_not_number(n_q, q_heads, kv_heads):
+    """Refused before any launch: a sequence's queries times heads are row numbers in the kernels."""
+    import ctypes as C
+
+    from paper_2502_01277_amd import binding
+    from test_tokens_host import _attend_op
+    op = _attend_op()
+    op.dim, op.n_seq, op.n_q, op.max_q, op.q_heads, op.kv_heads = 8, 1, n_q, n_q, q_heads, kv_heads
+    assert binding.lib().octo_op_attend(C.byref(op), None, None) == binding.EINVAL and binding.lib().octo_op_attend_workspace_bytes(C.byref(op)) == 0
