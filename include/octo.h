@@ -650,7 +650,7 @@ octo_status octo_dequantize_mx4(const uint8_t* codes, const uint8_t* exps, size_
  * pool less than 16 MiB apart.  d_q_start: int32 [n_seq + 1], ascending; d_kv_start: int64 [n_seq]; d_kv_len: int32 [n_seq]; all on the device,
  * as lengths and regions of a cascade are.  The host states what they do not exceed: n_q rows of q, kv_rows rows of the
  * pool, max_q and max_kv the longest sequence; what lies beyond is cut off (a sequence that starts outside the pool has no keys); max_q times q_heads
- * stays below 0x7FFFFF01.  d_n_seq: NULL, or the number of sequences present, on the device.  d_lse: NULL or fp32 [n_q][q_heads].
+ * stays below 0x7FFFFF01, and the blocks of a launch (n_seq x kv_heads x their rows in 16s to 128s) below 2^24.  d_n_seq: NULL, or the number of sequences present, on the device.  d_lse: NULL or fp32 [n_q][q_heads].
  * d_workspace: octo_op_attend_workspace_bytes(op) bytes, 16-byte aligned (NULL where that is 0), for this call alone until it is done:
  * long key sequences are split over the compute units and joined in a fixed order.  The same call on the same inputs gives the same bits.
  * *kernel_id (may be NULL): 0 nothing to do, else 1000 * kernel + the number of parts the keys were split into; kernel 1 and 4: the

@@ -33,7 +33,8 @@ struct AttendArgs {
   FastDiv div_heads, div_blocks, div_split;                            // kv_heads, row_blocks, n_split
   int by_die;                                                          // blocks that read the same keys run on one die
   int even_tiles;                                                      // what cut takes as the length of a part where all sequences are alike, 0: nothing
-  int cut, slots;                                                      // not 0: attend_tile_kernel cuts its pieces itself, in `cut` blocks, `slots` of them at a time;
+  int blocks;                                                          // to start
+  int cut, slots;                                                      // cut: attend_tile_kernel cuts its pieces itself, for so many blocks at a time;
   int* cut_tiles;                                                      // what it took as the length of a part, for attend_join_kernel
 };
 
@@ -59,12 +60,6 @@ __device__ __forceinline__ Piece piece_of(const AttendArgs& a, unsigned n, bool 
   p.block = (int)(q - r * (unsigned)a.row_blocks); p.head = (int)(w - y * (unsigned)a.kv_heads); p.part = (int)(y - z * (unsigned)a.n_split); p.seq = (int)z;
   return p;
 }
-// blocks to start for pieces of a block each
-__host__ inline unsigned piece_blocks(const AttendArgs& a) {
-  const unsigned sets = (unsigned)a.n_seq * a.kv_heads * a.n_split;
-  return (a.by_die ? (sets + 7) / 8 * 8 : sets) * a.row_blocks;
-}
-
 struct Span { int q0, n_q, n_kv; long long kv0; };
 // The rows and keys of sequence b, cut to what the host stated; false: no such sequence, or no queries.
 __device__ __forceinline__ bool span_of(const AttendArgs& a, int b, Span* s) {
@@ -457,7 +452,7 @@ __global__ __launch_bounds__(256, RT == 2 && sizeof(T) == 4 && DP == 128 ? 1 : 2
 
 template <typename T, int FORMAT, int DP, bool MASK>
 hipError_t launch_direct_masked(int how, const AttendArgs& a, hipStream_t s) {
-  const dim3 grid(how != DIRECT_OWN ? piece_blocks(a) : ((unsigned)a.n_seq * a.kv_heads * a.row_blocks * a.n_split + 3) / 4);
+  const dim3 grid((unsigned)a.blocks);
   if (how == DIRECT_OWN) hipLaunchKernelGGL((attend_direct_kernel<T, FORMAT, DP, false, MASK, 1>), grid, dim3(256), 0, s, a);
   else if (how == DIRECT_SHARE) hipLaunchKernelGGL((attend_direct_kernel<T, FORMAT, DP, true, MASK, 1>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((attend_direct_kernel<T, FORMAT, DP, true, MASK, 2>), grid, dim3(256), 0, s, a);

@@ -102,7 +102,8 @@ extern "C" {
 size_t octo_op_attend_workspace_bytes(const octo_attend_op* op) {
   if (!sizes_ok(op) || !op->n_seq || !op->max_q) return 0;
   const int cus = cu_count();
-  return part_bytes(op, plan_of(op, cus > 0 ? cus : 256));
+  const Plan p = plan_of(op, cus > 0 ? cus : 256);
+  return launch_blocks(op, p) > MOST_BLOCKS ? 0 : part_bytes(op, p);
 }
 
 octo_status octo_op_attend(const octo_attend_op* op, void* hip_stream, int32_t* kernel_id) {
@@ -129,8 +130,10 @@ octo_status octo_op_attend(const octo_attend_op* op, void* hip_stream, int32_t* 
   if (kernel_id) *kernel_id = 0;
   if (!op->n_seq || !op->max_q) return OCTO_OK;
   const int cus = cu_count();
+  const Plan p = plan_of(op, cus > 0 ? cus : 256);
+  const long long blocks = launch_blocks(op, p);
+  if (blocks > MOST_BLOCKS) return OCTO_EINVAL;
   if (cus < 1) return OCTO_EHIP;
-  const Plan p = plan_of(op, cus);
   const size_t need = part_bytes(op, p);
   if (need && (!op->d_workspace || ((uintptr_t)op->d_workspace & 15))) return OCTO_EINVAL;
   if (need > op->workspace_bytes) return OCTO_ENOMEM;
@@ -148,11 +151,11 @@ octo_status octo_op_attend(const octo_attend_op* op, void* hip_stream, int32_t* 
   }
   hipStream_t s = (hipStream_t)hip_stream;
   a.part_keys = p.part_keys;
-  a.cut = p.cut ? (int)cut_blocks(p, (long long)op->n_seq * op->kv_heads * p.row_blocks, op->max_kv) : 0; a.even_tiles = p.even_tiles;
+  a.cut = p.cut; a.even_tiles = p.even_tiles;
   a.slots = p.slots;
   a.row_blocks = p.row_blocks;
-  const long long sets = (long long)op->n_seq * op->kv_heads * p.n_split;
-  a.by_die = p.row_blocks > 1 && (sets % 8 == 0 || sets >= 64);
+  a.by_die = by_die(p, (long long)op->n_seq * op->kv_heads * p.n_split);
+  a.blocks = (int)blocks;
   a.div_heads = make_fastdiv((unsigned)op->kv_heads); a.div_blocks = make_fastdiv((unsigned)p.row_blocks); a.div_split = make_fastdiv((unsigned)p.n_split);
   hipError_t e = p.kernel == TILES ? (op->dtype == OCTO_F16 ? launch_attend_tile_f16(op->kv_format, a, s) : launch_attend_tile_bf16(op->kv_format, a, s))
                : op->dtype == OCTO_F32 ? launch_attend_direct_f32(op->kv_format, p.how, a, s)

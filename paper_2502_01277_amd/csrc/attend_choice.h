@@ -130,4 +130,15 @@ inline Plan plan_of(const octo_attend_op* op, int cus) {
   return p;
 }
 
+// Blocks that read the same keys run on one die, where the sets of keys share out evenly over the eight.
+inline bool by_die(const Plan& p, long long sets) { return p.row_blocks > 1 && (sets % 8 == 0 || sets >= 64); }
+// Blocks of the first launch.  HIP counts the threads of a launch, 256 a block, in 32 bits.
+constexpr long long MOST_BLOCKS = 0xFFFFFF;
+inline long long launch_blocks(const octo_attend_op* op, const Plan& p) {
+  const long long whole = (long long)op->n_seq * op->kv_heads * p.row_blocks, sets = (long long)op->n_seq * op->kv_heads * p.n_split;
+  if (p.cut) return cut_blocks(p, whole, op->max_kv);
+  if (p.kernel == OWN_ROWS) return (whole * p.n_split + 3) / 4;
+  return (by_die(p, sets) ? (sets + 7) / 8 * 8 : sets) * p.row_blocks;
+}
+
 }  // namespace octo

@@ -61,7 +61,7 @@ __device__ __forceinline__ bool cut_piece(const AttendArgs& a, CutPiece* piece, 
   __syncthreads();
 #pragma unroll
   for (int c = 0; c < 3; ++c) pieces[c] = (red[0][3 + c] + red[1][3 + c] + red[2][3 + c] + red[3][3 + c]) * a.kv_heads;
-  const int part = cut_tiles(sums, most, pieces, slots, least, a.even_tiles, (float)a.n_seq * a.row_blocks * a.kv_heads, (float)a.cut);
+  const int part = cut_tiles(sums, most, pieces, slots, least, a.even_tiles, (float)a.n_seq * a.row_blocks * a.kv_heads, (float)a.blocks);
   if (blockIdx.x == 0 && i == 0) *a.cut_tiles = part;
   // whose piece is it
   const int part_keys = even_part(has ? sp.n_kv : 0, part), mine = has ? blocks * a.kv_heads * parts_of(sp.n_kv, part_keys) : 0;
@@ -330,7 +330,7 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
 
 template <typename T, int FORMAT, int DP>
 hipError_t launch_tile(const AttendArgs& a, hipStream_t s) {
-  const dim3 grid(a.cut ? (unsigned)a.cut : piece_blocks(a));
+  const dim3 grid((unsigned)a.blocks);
   if (a.mask) hipLaunchKernelGGL((attend_tile_kernel<T, FORMAT, DP, true>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((attend_tile_kernel<T, FORMAT, DP, false>), grid, dim3(256), 0, s, a);
   return hipGetLastError();

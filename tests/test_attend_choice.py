@@ -26,7 +26,7 @@ int main() {
       blocks[i] = ((long long)q[i] * group + 127) / 128; tiles[i] = q[i] ? ((long long)kv[i] + 63) / 64 : 0;
       s.work += (float)blocks[i] * tiles[i] * op.kv_heads; s.whole += (float)blocks[i] * op.kv_heads; s.longest = std::max(s.longest, (int)tiles[i]);
     }
-    const long long there = p.cut ? cut_blocks(p, (long long)op.n_seq * op.kv_heads * p.row_blocks, op.max_kv) : 0;
+    const long long there = launch_blocks(&op, p);
     const int least = cut_least(s, p.n_split);
     int most[3];
     float pieces[3];
@@ -58,7 +58,7 @@ def ask(tmp_path_factory):
 
     def run(calls):
         """(type, 4 bits, dim, query heads, key heads, [lengths of queries], [of keys], what the host states as the longest of each, compute units): per call
-        (on attend_tile_kernel, cut on the device, pieces, blocks there if cut, most parts of a sequence, parts in the workspace)."""
+        (on attend_tile_kernel, cut on the device, pieces of 128 rows, blocks there, most parts of a sequence, parts in the workspace)."""
         text = []
         for dtype, four, dim, hq, hk, q, kv, (max_q, max_kv), cus in calls:
             text.append(" ".join(map(str, [TYPES[dtype], int(four), dim, hq, hk, len(q), max(sum(q), max_q), max_q, max_kv, cus] + [x for pair in zip(q, kv) for x in pair])))
@@ -143,3 +143,15 @@ def test_rows_that_32_bits_do_not_number(n_q, q_heads, kv_heads):
     op = _attend_op()
     op.dim, op.n_seq, op.n_q, op.max_q, op.q_heads, op.kv_heads = 8, 1, n_q, n_q, q_heads, kv_heads
     assert binding.lib().octo_op_attend(C.byref(op), None, None) == binding.EINVAL and binding.lib().octo_op_attend_workspace_bytes(C.byref(op)) == 0
+
+
+@pytest.mark.parametrize("n_seq,q_heads,kv_heads,max_q,max_kv", [(2 ** 21, 8, 8, 1, 600), (2 ** 24, 1, 1, 3, 9000), (2 ** 27, 1, 1, 3, 49), (2 ** 20, 64, 16, 1, 4096), (2 ** 22, 32, 4, 100, 64), (5, 4096, 1, 200000, 700)])
+def test_more_blocks_than_a_launch_takes(n_seq, q_heads, kv_heads, max_q, max_kv):
+    """Refused before any launch."""
+    import ctypes as C
+
+    from paper_2502_01277_amd import binding
+    from test_tokens_host import _attend_op
+    L, op = binding.lib(), _attend_op()
+    op.dim, op.n_seq, op.n_q, op.max_q, op.max_kv, op.q_heads, op.kv_heads = 8, n_seq, 2 ** 31 - 1, max_q, max_kv, q_heads, kv_heads
+    assert L.octo_op_attend(C.byref(op), None, None) == binding.EINVAL and L.octo_op_attend_workspace_bytes(C.byref(op)) == 0
