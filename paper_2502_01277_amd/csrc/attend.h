@@ -30,7 +30,7 @@ struct AttendArgs {
   float scale2;                                                        // scale * log2(e)
   int n_split, part_keys;                                              // parts of part_keys keys (a multiple of 64); sequences of one part are finished by its block
   int row_blocks;                                                      // of the kernel's rows, of the longest sequence
-  FastDiv div_heads, div_blocks, div_split;                            // kv_heads, row_blocks, n_split
+  FastDiv div_heads, div_blocks, div_split, div_seq;                   // kv_heads, row_blocks, n_split, n_seq (the join's)
   int by_die;                                                          // blocks that read the same keys run on one die
   int even_tiles;                                                      // what cut takes as the length of a part where all sequences are alike, 0: nothing
   int blocks;                                                          // to start

@@ -13,8 +13,9 @@ namespace {
 template <typename T>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   Span sp;
-  if (!span_of(a, blockIdx.x, &sp)) return;
-  const int parts = parts_of(sp.n_kv, a.cut ? even_part(sp.n_kv, *a.cut_tiles) : a.part_keys), r = blockIdx.y * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31, d = lane * 4;
+  const unsigned rows8 = fast_div(blockIdx.x, a.div_seq);             // neighbours: the same rows of different sequences
+  if (!span_of(a, (int)(blockIdx.x - rows8 * (unsigned)a.n_seq), &sp)) return;
+  const int parts = parts_of(sp.n_kv, a.cut ? even_part(sp.n_kv, *a.cut_tiles) : a.part_keys), r = (int)rows8 * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31, d = lane * 4;
   if (parts == 1 || r >= sp.n_q * a.q_heads) return;
   const long long at = (long long)sp.q0 * a.q_heads + r, step = (long long)a.n_q * a.q_heads;
   // the first parts' sums are on their way while the references are compared; memory of all n_split parts is there, used or not
@@ -162,7 +163,8 @@ octo_status octo_op_attend(const octo_attend_op* op, void* hip_stream, int32_t* 
                : op->dtype == OCTO_F16 ? launch_attend_direct_f16(op->kv_format, p.how, a, s)
                                        : launch_attend_direct_bf16(op->kv_format, p.how, a, s);
   if (e == hipSuccess && p.n_split > 1) {
-    const dim3 grid((unsigned)op->n_seq, (unsigned)(((long long)op->max_q * op->q_heads + 7) / 8));
+    a.div_seq = make_fastdiv((unsigned)op->n_seq);
+    const dim3 grid((unsigned)join_blocks(op));
     if (op->dtype == OCTO_F32) hipLaunchKernelGGL(attend_join_kernel<float>, grid, dim3(256), 0, s, a);
     else if (op->dtype == OCTO_F16) hipLaunchKernelGGL(attend_join_kernel<_Float16>, grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL(attend_join_kernel<__bf16>, grid, dim3(256), 0, s, a);

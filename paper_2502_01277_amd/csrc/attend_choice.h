@@ -141,4 +141,7 @@ inline long long launch_blocks(const octo_attend_op* op, const Plan& p) {
   return (by_die(p, sets) ? (sets + 7) / 8 * 8 : sets) * p.row_blocks;
 }
 
+// Blocks of attend_join_kernel, 8 rows of a sequence each; calls with parts are of so few blocks that these are far from MOST_BLOCKS.
+inline long long join_blocks(const octo_attend_op* op) { return op->n_seq * (((long long)op->max_q * op->q_heads + 7) / 8); }
+
 }  // namespace octo

@@ -43,6 +43,7 @@ int main() {
       parts = std::max(parts, n);
       needs += blocks[i] * op.kv_heads * n;
     }
+    if (p.n_split > 1 && join_blocks(&op) > MOST_BLOCKS) return 1;
     printf("%d %d %lld %lld %d %d\n", p.kernel == TILES, p.cut, needs, there, parts, p.n_split);
   }
 }

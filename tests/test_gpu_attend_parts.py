@@ -59,27 +59,31 @@ class Long:
             for h in range(self.heads):
                 k, v = (self.values(i, h, self.kv_starts[b], self.kv_starts[b] + n) for i in (0, 1))
                 mine = slice(h * group, (h + 1) * group)
-                q = self.q[lo:hi, mine].double().reshape(-1, self.dim)
                 kt = k.t().contiguous()
-                s = (q @ kt) * scale
-                d = (self.dim + 8) * 2.0 ** -24 * scale * (q.abs() @ kt.abs()).amax(1)
-                lse = torch.logsumexp(s, 1)
-                w = torch.exp(s - lse[:, None])
-                ref = w @ v
-                fp32 = (n / 8 + 64) * 2.0 ** -24
-                bound = (e + 2 * d + fp32)[:, None] * (w @ v.abs()) + e * ref.abs() + 2.0 ** -126 * (1 + v.abs().sum(0))
-                if self.dtype == "f16":
-                    bound += 2.0 ** -24 * (1 + v.abs().sum(0) * torch.exp(s.amax(1) - lse)[:, None])
-                err = (self.out[lo:hi, mine].double().reshape(-1, self.dim) - ref).abs()
-                assert bool((err <= bound).all()), (b, h, float((err - bound).nan_to_num(nan=math.inf).max()))
-                off = (self.lse[lo:hi, mine].double().reshape(-1) - lse).abs()
-                assert bool((off <= d + fp32 + 2.0 ** -22 * (1 + lse.abs())).all()), (b, h)
+                every = [x[lo:hi, mine].double().reshape((hi - lo) * group, -1) for x in (self.q, self.out, self.lse[:, :, None])]
+                for q, out, got in zip(*[x.split(16384) for x in every]):
+                    got = got[:, 0]
+                    s = (q @ kt) * scale
+                    d = (self.dim + 8) * 2.0 ** -24 * scale * (q.abs() @ kt.abs()).amax(1)
+                    lse = torch.logsumexp(s, 1)
+                    w = torch.exp(s - lse[:, None])
+                    ref = w @ v
+                    fp32 = (n / 8 + 64) * 2.0 ** -24
+                    bound = (e + 2 * d + fp32)[:, None] * (w @ v.abs()) + e * ref.abs() + 2.0 ** -126 * (1 + v.abs().sum(0))
+                    if self.dtype == "f16":
+                        bound += 2.0 ** -24 * (1 + v.abs().sum(0) * torch.exp(s.amax(1) - lse)[:, None])
+                    err = (out - ref).abs()
+                    assert bool((err <= bound).all()), (b, h, float((err - bound).nan_to_num(nan=math.inf).max()))
+                    off = (got - lse).abs()
+                    assert bool((off <= d + fp32 + 2.0 ** -22 * (1 + lse.abs())).all()), (b, h)
 
 
 @pytest.mark.parametrize("dtype,fmt,dim,q_heads,kv_heads,n,q_len,kv_len", [
     ("bf16", "plain", 128, 32, 8, 2, 2049, 12800), ("bf16", "plain", 72, 16, 1, 5, 900, 6400), ("f16", "plain", 32, 64, 2, 3, 520, 12800), ("f16", "plain", 80, 16, 8, 6, 642, 21877),
     ("bf16", "plain", 72, 40, 8, 36, 4, 16452), ("f16", "cache4", 128, 32, 8, 17, 96, 20440), ("bf16", "cache4", 96, 68, 4, 2, 520, 6400), ("f16", "cache4", 64, 64, 2, 3, 520, 12800),
-    ("bf16", "cache4", 64, 136, 8, 100, 1, 6400)])
+    ("bf16", "cache4", 64, 136, 8, 100, 1, 6400),
+    # 599552 rows to join
+    ("bf16", "plain", 8, 512, 8, 1, 1171, 12800)])
 def test_equal_sequences(octo, dtype, fmt, dim, q_heads, kv_heads, n, q_len, kv_len):
     p = Long(octo, dtype, fmt, dim, q_heads, kv_heads, [q_len] * n, [kv_len] * n)
     kid = p.run(octo)
