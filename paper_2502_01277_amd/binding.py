@@ -998,6 +998,8 @@ def op_attend(q, held, out, q_start, kv_start, kv_len, scale=None, max_q=None, m
     n, rows, fields = _attend_pack(q, held, out, q_start, kv_start, kv_len, scale, max_q, max_kv, key_mask, lse, n_seq)
     if not n or not rows:
         return 0
+    if workspace is not None:
+        _optional(workspace, _torch().uint8, "workspace is dense uint8 on the device", 0)
     L = lib()
     op = _ATTEND.pack(*fields, 0, 0)
     need = L.octo_op_attend_workspace_bytes(op)
