@@ -36,6 +36,7 @@ struct RotateArgs {
   int items;                         // groups of rows of a wavefront
   int table;                         // pairs, rounded up to a power of two
   unsigned total;                    // rows in all
+  int blocks;                        // to start
   FastDiv div_heads, div_lanes;
 };
 
@@ -185,7 +186,7 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a) {
 
 template <typename T, int VEC>
 hipError_t launch_vec(const RotateArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((rotate_kernel<T, VEC>), dim3((unsigned)(((unsigned long long)a.total + 4ull * a.items * a.rows - 1) / (4ull * a.items * a.rows))), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((rotate_kernel<T, VEC>), dim3((unsigned)a.blocks), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 template <typename T>
@@ -245,6 +246,9 @@ extern "C" octo_status octo_op_rotate(const octo_rotate_op* op, void* hip_stream
   const unsigned long long groups = (total + a.rows - 1) / a.rows;
   a.items = groups / 4096 < 1 ? 1 : groups / 4096 > 8 ? 8 : (int)(groups / 4096);
   while (a.items > 1 && ((a.items * a.rows + a.heads - 2) / a.heads + 1) * a.pairs > TURNS) --a.items;
+  const unsigned long long blocks = (total + 4ull * a.items * a.rows - 1) / (4ull * a.items * a.rows);
+  if (blocks > 0xFFFFFF) return OCTO_EINVAL;                // HIP counts the threads of a launch, 256 a block, in 32 bits
+  a.blocks = (int)blocks;
   if (op->n_tokens == 0) return OCTO_OK;
   hipStream_t s = (hipStream_t)hip_stream;
   const hipError_t e = op->dtype == OCTO_F32 ? launch_type<float>(vec, a, s) : op->dtype == OCTO_F16 ? launch_type<_Float16>(vec, a, s) : launch_type<__bf16>(vec, a, s);
