@@ -593,7 +593,7 @@ typedef struct {
  * rotation, NULL).  d_n: NULL, or the number of tokens present, on the device (clamped to n_tokens).  dtype: OCTO_F32, _F16 or
  * _BF16; arithmetic in fp32, one rounding at the end.  dim: even, at most 256, and dim / 2 at most 64 times the longest vector
  * (8, 4, 2 or 1 values of at most 16 bytes) that divides P and dim / 2 - P (split) or dim / 2 and to which all addresses and
- * strides are aligned.  Tokens times heads of all parts: below 2^28; more, up to 0x7FFF0000, where a launch takes them (wavefronts have more rows). */
+ * strides are aligned.  Tokens times heads of all parts: up to 2^27; more, up to 0x7FFF0000, where a launch takes them (wavefronts have more rows). */
 typedef struct octo_rotate_op {
   int32_t dtype, n_tokens, dim, n_axes;
   int32_t sections[OCTO_MAX_AXES];

@@ -51,9 +51,11 @@ class RegionReader:
 
     def _linear(self, layer, x):
         """[n][cin] -> [n][cout] by a 1x1 layer."""
-        y = x.new_empty(x.shape[0], 1, 1, layer.cout)
-        binding.op_conv(layer, x.view(x.shape[0], 1, 1, -1), y)
-        return y.view(x.shape[0], layer.cout)
+        n, cin = x.shape
+        y = x.new_empty(n, layer.cout)
+        if n:
+            binding.op_conv(layer, x.view(n, 1, 1, cin), y.view(n, 1, 1, layer.cout))
+        return y
 
     def look(self, frames, rois, first_frame=0):
         """Tokens of the regions `rois` (ROI records, as Pipeline.get_rois gives them) of `frames` into the cache.  Returns the numbers by which `ask` knows
