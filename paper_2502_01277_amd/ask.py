@@ -5,8 +5,8 @@
     text tokens -> queries (1x1 layer) -> head norms and rotation -> attention to one region's tokens each
                 -> output layer                                                                          RegionReader.ask
 
-Everything runs in the library's kernels on the caller's stream, nothing waits for the GPU.  The weights are random, as all of this
-package's: the module shows how the calls go together.
+The layers, norms, rotations, cache and attention run in the library's kernels, indices and copies in torch's, all on the current stream; nothing
+waits for the GPU.  The weights are random, as all of this package's: the module shows how the calls go together.
 
     python -m paper_2502_01277_amd.ask        # the tiny cascade's regions, one question each
 """
@@ -73,7 +73,9 @@ class RegionReader:
         binding.op_conv(self.patches, crops, tokens)
         kv = self._linear(self.to_kv, tokens.view(n * GRID * GRID, self.width)).view(-1, 2 * self.kv_heads, self.dim)
         pos = self.cells.repeat(n, 1, 1)
-        pos[:, :, 0] = torch.from_numpy(np.ascontiguousarray(rois["frame"])).to(pos.device)[:, None] + first_frame
+        # from pinned memory, so that the host goes on (torch keeps it until the copy is done)
+        frame = torch.from_numpy(np.ascontiguousarray(rois["frame"])).pin_memory()
+        pos[:, :, 0] = frame.to(pos.device, non_blocking=True)[:, None] + first_frame
         keys = kv[:, :self.kv_heads]
         binding.op_rotate([binding.RotatePart(keys, keys, self.k_weight)], pos.view(-1, 3), AXES)
         slots = (ids % self.capacity)[:, None] * (GRID * GRID) + torch.arange(GRID * GRID, device="cuda")
