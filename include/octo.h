@@ -641,11 +641,12 @@ octo_status octo_dequantize_mx4(const uint8_t* codes, const uint8_t* exps, size_
  * h / (q_heads / kv_heads).  Over the visible keys j (d_key_mask NULL, or its byte for the pool row not zero):
  *   out = sum_j exp(s_j) v_j / sum_j exp(s_j),  s_j = scale * (q . k_j),   lse = log sum_j exp(s_j)
  * No visible key: out 0, lse -infinity.  What hidden keys and values hold does not matter, NaN neither.  Rows of q outside every
- * sequence are not written.  Sums, maxima and products are in fp32; the weights exp(s_j - m), m a maximum of s so far, are rounded to the type of q
+ * sequence are not written.  d_out may not overlap d_q.  Sums, maxima and products are in fp32; the weights exp(s_j - m), m a maximum of s so far, are rounded to the type of q
  * before they multiply the values (fp32: not at all), their sum is taken before.
  *
  * dtype: type of q and out (fp32, fp16, bf16).  kv_format OCTO_KV_PLAIN: k and v of the same type; OCTO_KV_CACHE4: the planes that
- * octo_op_cache4_store fills (dtype fp16 or bf16; values beyond the range of dtype are infinities).  dim: a multiple of 8 up
+ * octo_op_cache4_store fills (dtype fp16 or bf16: values are converted to it; those beyond its range
+ * are infinities, those below fp16's smallest normal number, 2^-14, may lose bits).  dim: a multiple of 8 up
  * to 128 (OCTO_KV_CACHE4: of 32).  d_q, d_k, d_v, d_out 16-byte aligned, their strides multiples of 16 bytes; rows of the
  * pool less than 16 MiB apart.  d_q_start: int32 [n_seq + 1], ascending; d_kv_start: int64 [n_seq]; d_kv_len: int32 [n_seq]; all on the device,
  * as lengths and regions of a cascade are.  The host states what they do not exceed: n_q rows of q, kv_rows rows of the

@@ -61,7 +61,8 @@ inline long long cut_blocks(const Plan& p, long long whole, int max_kv) {
 // The number of parts with the least estimated end for blocks of equal length on TILES, `at_once` of them on a compute unit: the unit with the most blocks takes them in
 // rounds, alone a block has 1 / 1.6 of what the unit does with two or three, and its start and end are as long as six tiles;
 // the join as twelve, and for every part 0.6 and 0.4 for a million values written and read.
-// Fitted to 66 drawn calls of 1 to 24 parts: what it takes is 1 % off the best in the mean, three blocks a unit were 9 % off.
+// 79 calls of equal lengths, timed in turn: 3.3 % less in the mean than with three blocks a unit (5 x 197 queries over 49903 keys of 4 bits, 32 / 8 heads of 128, 1424 -> 903 us;
+// 6 x 642 over 21877, 16 / 8 heads of 80, 844 -> 630), single ones more (59 x 33 over 36264 of 4 bits, 2 heads of 64, 164 -> 230).
 inline long long even_parts(long long blocks, double outputs, int max_kv, int cus, int at_once) {
   const int tiles = std::max(1, (max_kv + 63) / 64);
   if (blocks > 65536) return 1;                             // over a hundred rounds: the last one is nothing
@@ -91,9 +92,10 @@ inline long long even_parts(long long blocks, double outputs, int max_kv, int cu
 //   differ in length, up to sixteen blocks of 2048 keys, for an even end: 16 single tokens over up to 51200 keys of 4 bits 131 -> 117 us, 17 questions
 //   of up to 96 tokens over up to 20440 keys 486 -> 453.  With TILES the rows
 //   tell: as many as n_seq x max_q, then sequences are alike, and even_parts has it: 64 x 3000, 128 rows 71 -> 59 us, 4 x 1600, 900 rows 55 -> 40,
-//   13 questions of 475 rows over 42138 keys of 4 bits 718 -> 498.
+//   13 questions of 475 rows (20 / 4 heads of 96) over 42138 keys of 4 bits 718 -> 498.
 // A long call of up to 256 sequences on TILES cuts its parts on the device, where the lengths are (cut_piece; n_split is then the most a sequence can have): 24 tiles for every place a
-//   block can have at least, as looking at all lengths takes a block 5 us.  Where it finds them alike it takes even_parts's length.
+//   block can have at least, as looking at all lengths takes a block 5 us.  Where it finds them alike it takes even_parts's length
+//   (0.7 % of the 3.3 there; 3.2 % over 16 calls of equal queries and ragged keys).
 inline Plan plan_of(const octo_attend_op* op, int cus) {
   Plan p{};
   const long long rows = (long long)op->max_q * (op->q_heads / op->kv_heads), pairs = (long long)op->n_seq * op->kv_heads, blocks16 = pairs * ((rows + 15) / 16);

@@ -263,6 +263,7 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
       float w[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) { w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[k / 2][8 * (k % 2) + i], c, -refc)); add[i & 1] += w[i]; }
+      // rounded to T, as in attend_direct_kernel
       store4<T>((T*)&p[k], floatx4{w[0], w[1], w[2], w[3]});
       store4<T>((T*)&p[k] + 4, floatx4{w[4], w[5], w[6], w[7]});
     }
