@@ -34,7 +34,7 @@ def test_look_does_not_wait_for_the_gpu(reader):
     reader.look(frames, _regions(3))
     torch.cuda.synchronize()
     busy = torch.cuda.Event()
-    torch.cuda._sleep(int(3e8))                                      # a tenth of a second and more
+    torch.cuda._sleep(int(1e9))                                      # some tenths of a second
     busy.record()
     reader.look(frames, _regions(3))
     waited = busy.query()
