@@ -50,7 +50,7 @@ typedef enum {
 
 /* OCTO_F8 is 8-bit floating point in the OCP E4M3 format: 1 sign bit, 4 exponent bits (bias 7), 3 mantissa bits,
  * subnormals down to 2^-9, no infinities, 0x7F and 0xFF are NaN, largest finite value 448.  Only octo_op_conv and the
- * two conversion helpers below take it; models of a pipeline are stored in one of the other three. */
+ * two conversion helpers below take it (rows of tokens in 8 bits have scales of their own: octo_mx8_rows); models of a pipeline are stored in one of the other three. */
 typedef enum { OCTO_F32 = 0, OCTO_F16 = 1, OCTO_BF16 = 2, OCTO_F8 = 3 } octo_dtype;
 typedef enum { OCTO_CONV = 0, OCTO_MAXPOOL = 1, OCTO_UPSAMPLE2X = 2, OCTO_CONCAT = 3, OCTO_ADD = 4, OCTO_GAP = 5, OCTO_FC = 6 } octo_op;
 typedef enum { OCTO_ACT_NONE = 0, OCTO_ACT_RELU = 1, OCTO_ACT_SILU = 2 } octo_act;
@@ -676,6 +676,48 @@ typedef struct octo_attend_op {
 octo_status octo_op_attend(const octo_attend_op* op, void* hip_stream, int32_t* kernel_id);
 /* Bytes of workspace of that call (0 too where the arguments are not valid); looks at sizes and types only. */
 size_t octo_op_attend_workspace_bytes(const octo_attend_op* op);
+
+/* Rows held in 8 bits ("MX8"): groups of 32 along a row with one exponent byte each.
+ *   e = the smallest integer with max |x| <= 448 * 2^e, stored as e + 127 in 1 .. 247;
+ *   code = x / 2^e in E4M3 (octo_dtype), rounded to nearest, ties to even.
+ *   A group that holds a NaN or an infinity gets the byte 255 and codes 0x7F: it reads as NaN.
+ * Element (row, i) is the byte d_codes[row * code_row + i], the exponent of its group d_exps[row * exp_row + i / 32].  Widths are
+ * multiples of 32; d_codes 16-byte aligned, code_row a multiple of 16. */
+typedef struct {
+  uint8_t* d_codes; uint8_t* d_exps;
+  int64_t code_row, exp_row;
+} octo_mx8_rows;
+typedef enum { OCTO_ROWS_PLAIN = 0, OCTO_ROWS_MX8 = 1 } octo_row_format;
+
+/* Residual sum and root-mean-square norm of every row, in one pass:
+ *   s = x (+ d_res),   y = s / sqrt(mean over the row of s^2 + eps) * d_weight       (norm == 0: y = s * d_weight)
+ * x, d_res (or NULL) and d_sum (or NULL: s is not kept) are rows of `dtype` (OCTO_F32, _F16, _BF16), d_weight is fp32 [width] or NULL
+ * for ones; y goes to d_y in `dtype` (y_format OCTO_ROWS_PLAIN) or to y8 (OCTO_ROWS_MX8; with norm 0 and no weight the call is the
+ * conversion to 8 bits).  Arithmetic is in fp32, the norm is that of the unrounded sum, every output is rounded once.  A NaN or an infinity stays in
+ * its row.  width: 1 to 32768, for OCTO_ROWS_MX8 a multiple of 32 with d_x, d_res and d_sum 16-byte aligned, their strides multiples of 16
+ * bytes (other calls take any address of an element).  d_sum and d_y may each be d_x or d_res with the same stride (not both the same one);
+ * apart from that no output may overlap anything else.  d_n: NULL, or the number of rows present, on the device (clamped to n): later rows are left as they were. */
+typedef struct octo_norm_op {
+  int32_t dtype, y_format, n, width, norm;
+  float eps;
+  const void* d_x; const void* d_res; void* d_sum; void* d_y;
+  int64_t x_row, res_row, sum_row, y_row;
+  octo_mx8_rows y8;
+  const float* d_weight;
+  const int32_t* d_n;
+} octo_norm_op;
+octo_status octo_op_norm(const octo_norm_op* op, void* hip_stream);
+/* The values of rows held in 8 bits, in `dtype` (rounded, where its range or its bits do not hold them): d_y 16-byte aligned, y_row a multiple of 16 bytes. */
+typedef struct octo_mx8_op {
+  int32_t dtype, n, width, pad_;
+  octo_mx8_rows x8;
+  void* d_y; int64_t y_row;
+  const int32_t* d_n;
+} octo_mx8_op;
+octo_status octo_op_mx8_load(const octo_mx8_op* op, void* hip_stream);
+/* The same conversion on the host (no GPU): n values (a multiple of 32) to n codes and n / 32 exponent bytes, and back. */
+octo_status octo_quantize_mx8(const float* src, size_t n, uint8_t* codes, uint8_t* exps);
+octo_status octo_dequantize_mx8(const uint8_t* codes, const uint8_t* exps, size_t n, float* dst);
 
 #ifdef __cplusplus
 }

@@ -173,6 +173,20 @@ class OctoAttendOp(C.Structure):
                 ("d_out", C.c_void_p), ("out_row", C.c_int64), ("out_head", C.c_int64), ("d_lse", C.c_void_p), ("d_workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
 
 
+class OctoMx8Rows(C.Structure):
+    _fields_ = [("d_codes", C.c_void_p), ("d_exps", C.c_void_p), ("code_row", C.c_int64), ("exp_row", C.c_int64)]
+
+
+class OctoNormOp(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("y_format", C.c_int32), ("n", C.c_int32), ("width", C.c_int32), ("norm", C.c_int32), ("eps", C.c_float),
+                ("d_x", C.c_void_p), ("d_res", C.c_void_p), ("d_sum", C.c_void_p), ("d_y", C.c_void_p),
+                ("x_row", C.c_int64), ("res_row", C.c_int64), ("sum_row", C.c_int64), ("y_row", C.c_int64), ("y8", OctoMx8Rows), ("d_weight", C.c_void_p), ("d_n", C.c_void_p)]
+
+
+class OctoMx8Op(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n", C.c_int32), ("width", C.c_int32), ("pad_", C.c_int32), ("x8", OctoMx8Rows), ("d_y", C.c_void_p), ("y_row", C.c_int64), ("d_n", C.c_void_p)]
+
+
 # Every symbol include/octo.h declares.
 EXPORTS = [
     "octo_pipeline_workspace_size", "octo_pipeline_create", "octo_pipeline_destroy", "octo_submit_frames", "octo_run",
@@ -188,6 +202,7 @@ EXPORTS = [
     "octo_op_conv", "octo_op_conv_packed_bytes", "octo_op_conv_padded_cout", "octo_op_conv_pack", "octo_quantize_e4m3", "octo_dequantize_e4m3",
     "octo_op_rotate", "octo_op_cache4_store", "octo_op_cache4_load", "octo_quantize_mx4", "octo_dequantize_mx4",
     "octo_op_attend", "octo_op_attend_workspace_bytes",
+    "octo_op_norm", "octo_op_mx8_load", "octo_quantize_mx8", "octo_dequantize_mx8",
 ]
 
 _lib = None
@@ -286,6 +301,10 @@ def lib() -> C.CDLL:
         L.octo_op_attend_workspace_bytes.restype = C.c_size_t
         L.octo_quantize_mx4.argtypes = [vp, C.c_size_t, vp, vp]
         L.octo_dequantize_mx4.argtypes = [vp, vp, C.c_size_t, vp]
+        L.octo_op_norm.argtypes = [vp, vp]
+        L.octo_op_mx8_load.argtypes = [vp, vp]
+        L.octo_quantize_mx8.argtypes = [vp, C.c_size_t, vp, vp]
+        L.octo_dequantize_mx8.argtypes = [vp, vp, C.c_size_t, vp]
         _lib = L
     return _lib
 
@@ -815,11 +834,15 @@ def op_conv(layer: ConvOp, x, y, res=None, res_mode=0, out_f32=False, res_scale=
 
 # ---- tokens behind a cascade ---------------------------------------------------
 # A call's arguments are packed in one go (a dozen microseconds less than field by field, as long as the small kernels take): the
-# layouts of OctoRotateOp, OctoCache4Op and OctoAttendOp.
+# layouts of OctoRotateOp, OctoCache4Op, OctoAttendOp, OctoNormOp and OctoMx8Op.
 _PLANE = "PPqqqq"
 _ROTATE = struct.Struct("@12id2fPP" + "PPPqqqqii" * MAX_ROTATE_PARTS)
 _CACHE4 = struct.Struct("@4iq" + 2 * _PLANE + "PP4qPP")
 _ATTEND = struct.Struct("@9ifqPqqPPqqqq" + 2 * _PLANE + "5PPqqPPN")
+_MX8_ROWS = "PPqq"
+_NORM = struct.Struct("@5if4P4q" + _MX8_ROWS + "PP")
+_MX8 = struct.Struct("@4i" + _MX8_ROWS + "PqP")
+_NO_MX8 = (0,) * 4
 _NO_PART, _NO_PLANE, _NO_KV, _NO_SECTIONS = {1: (0,) * 9, 2: ()}, (0,) * 6, (0,) * 6, (0,) * MAX_AXES
 
 
@@ -1039,6 +1062,109 @@ def dequantize_mx4(codes: np.ndarray, exps: np.ndarray) -> np.ndarray:
         _refuse("16 bytes of codes per exponent")
     out = np.empty(codes.shape[:-1] + (2 * codes.shape[-1],), np.float32)
     _st(lib().octo_dequantize_mx4(codes.ctypes.data, exps.ctypes.data, out.size, out.ctypes.data))
+    return out
+
+
+# ---- around attention: norms, products, the choice of a token ---------------------
+class Mx8:
+    """Rows held in 8 bits (octo_mx8_rows in octo.h): codes uint8 [rows][width], exponents uint8 [rows][width / 32] (any strides, the last contiguous)."""
+    __slots__ = ("codes", "exps")
+
+    def __init__(self, codes, exps):
+        self.codes, self.exps = codes, exps
+
+    @classmethod
+    def empty(cls, rows, width, device="cuda"):
+        t = _torch()
+        if width % 32:
+            _refuse("width is a multiple of 32")
+        return cls(t.empty((rows, width), dtype=t.uint8, device=device), t.empty((rows, width // 32), dtype=t.uint8, device=device))
+
+    @property
+    def shape(self):
+        return self.codes.shape
+
+    def pack(self):
+        """(rows, width, fields), after a look at the shapes."""
+        u8, c, e = _torch().uint8, self.codes, self.exps
+        shape, cs, es = c.shape, c.stride(), e.stride()
+        if (len(shape) != 2 or shape[1] % 32 or e.shape != (shape[0], shape[1] // 32) or not (c.is_cuda and e.is_cuda and c.dtype is u8 and e.dtype is u8)
+                or cs[1] != 1 or (shape[1] > 32 and es[1] != 1)):
+            _refuse("codes are uint8 [rows][width], exponents uint8 [rows][width / 32], on the device")
+        return shape[0], shape[1], (c.data_ptr(), e.data_ptr(), cs[0], es[0])
+
+
+def _rows(x, dtype, shape, what):
+    """(address, row stride) of device rows of a type and shape, their values contiguous."""
+    s = x.stride()
+    if x.shape != shape or not x.is_cuda or x.dtype is not dtype or (shape[1] > 1 and s[1] != 1):
+        _refuse(what)
+    return x.data_ptr(), s[0]
+
+
+def op_norm(x, y, weight=None, res=None, total=None, eps=1e-6, norm=True, n=None, stream=None):
+    """Residual sum and root-mean-square norm of rows in one pass (octo_norm_op in octo.h).  x [rows][width]; y: such a tensor of the same type, or an Mx8;
+    weight fp32 [width] or None; res: added to x, total: where the sum goes (both like x, or None); norm=False: y is the sum times the weight.  n: int32
+    device tensor with the number of rows present, or None."""
+    t = _torch()
+    kind, shape = x.dtype, x.shape
+    if len(shape) != 2:
+        _refuse("x is [rows][width]")
+    d_x, x_row = _rows(x, kind, shape, "x is on the device, its rows contiguous")
+    d_res = res_row = d_sum = sum_row = d_y = y_row = 0
+    if res is not None:
+        d_res, res_row = _rows(res, kind, shape, "res is like x")
+    if total is not None:
+        d_sum, sum_row = _rows(total, kind, shape, "total is like x")
+    y8, fmt = _NO_MX8, 0
+    if isinstance(y, Mx8):
+        rows, width, y8 = y.pack()
+        fmt = 1
+        if (rows, width) != shape:
+            _refuse("y has the shape of x")
+    else:
+        d_y, y_row = _rows(y, kind, shape, "y is like x, or an Mx8")
+    if not shape[0] or not shape[1]:
+        return
+    op = _NORM.pack(_CODE[kind], fmt, shape[0], shape[1], 1 if norm else 0, eps, d_x, d_res, d_sum, d_y, x_row, res_row, sum_row, y_row, *y8,
+                    0 if weight is None else _optional(weight, t.float32, "weight is fp32 [width] on the device", shape[1]), 0 if n is None else _optional(n, t.int32, "n is int32 on the device"))
+    if stream is not None:
+        _order(stream)
+    st = lib().octo_op_norm(op, _stream_ptr(stream))
+    if st:
+        _st(st)
+
+
+def op_mx8_load(x: Mx8, y, n=None, stream=None):
+    """The values of rows held in 8 bits, into y [rows][width] (fp32, fp16 or bf16)."""
+    rows, width, fields = x.pack()
+    d_y, y_row = _rows(y, y.dtype, (rows, width), "y has the shape of x, its rows contiguous, on the device")
+    if not rows or not width:
+        return
+    op = _MX8.pack(_CODE[y.dtype], rows, width, 0, *fields, d_y, y_row, 0 if n is None else _optional(n, _torch().int32, "n is int32 on the device"))
+    if stream is not None:
+        _order(stream)
+    st = lib().octo_op_mx8_load(op, _stream_ptr(stream))
+    if st:
+        _st(st)
+
+
+def quantize_mx8(x: np.ndarray):
+    """(codes uint8 [..., n], exponents uint8 [..., n / 32]) of fp32 [..., n], by the library (host)."""
+    x = np.ascontiguousarray(x, np.float32)
+    if not x.ndim or x.shape[-1] % 32:
+        _refuse("groups of 32 along the last axis")
+    codes, exps = np.empty(x.shape, np.uint8), np.empty(x.shape[:-1] + (x.shape[-1] // 32,), np.uint8)
+    _st(lib().octo_quantize_mx8(x.ctypes.data, x.size, codes.ctypes.data, exps.ctypes.data))
+    return codes, exps
+
+
+def dequantize_mx8(codes: np.ndarray, exps: np.ndarray) -> np.ndarray:
+    codes, exps = np.ascontiguousarray(codes, np.uint8), np.ascontiguousarray(exps, np.uint8)
+    if codes.size != 32 * exps.size:
+        _refuse("32 codes per exponent")
+    out = np.empty(codes.shape, np.float32)
+    _st(lib().octo_dequantize_mx8(codes.ctypes.data, exps.ctypes.data, out.size, out.ctypes.data))
     return out
 
 

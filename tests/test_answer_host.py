@@ -1,0 +1,120 @@
+"""The calls around attention, as far as they need no GPU: the oracle's pins, the host's conversion to 8 bits, refusals."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+
+from oracle import answer
+from paper_2502_01277_amd import binding
+
+
+# ---- the oracle ----
+def test_norm_by_hand():
+    s, y = answer.norm(np.array([[1.0, 4.0]]), np.array([[2.0, 0.0]]), np.array([2.0, 0.5]), eps=0.0)
+    assert np.allclose(s, [[3, 4]]) and np.allclose(y, [[6 / math.sqrt(12.5), 2 / math.sqrt(12.5)]])
+    assert np.allclose(answer.norm(np.array([[3.0, 4.0]]), norm=False)[1], [[3, 4]])
+
+
+def test_product_by_hand():
+    x, w = np.array([[1.0, 2.0]]), np.array([[3.0, 1.0], [0.0, -2.0]])
+    assert np.allclose(answer.product(x, w, [0.5, 1.0], "relu", res=[[1.0, 1.0]]), [[6.5, 1.0]])
+    assert np.allclose(answer.product(x, w, [0.5, 1.0], "silu", gated=True), [[5.5 / (1 + math.exp(-5.5)) * -3]])
+    assert np.allclose(answer.activate("gelu", np.array([1.0])), 0.5 * (1 + math.erf(math.sqrt(0.5))))
+
+
+def test_sampling_by_hand():
+    x = np.log([0.1, 0.4, 0.3, 0.2])
+    assert [answer.sample(x, u)[0] for u in (0.0, 0.09, 0.11, 0.49, 0.51, 0.79, 0.81, 0.999)] == [0, 0, 1, 1, 2, 2, 3, 3]
+    assert answer.kept_tokens(x, top_k=2)[0] == [1, 2] and answer.kept_tokens(x, top_p=0.69)[0] == [1, 2] and answer.kept_tokens(x, top_p=0.71)[0] == [1, 2, 3]
+    assert answer.kept_tokens(x, min_p=0.51)[0] == [1, 2] and answer.kept_tokens(x, top_p=0.0)[0] == [1] and answer.kept_tokens(x, temperature=0.0, top_k=3)[0] == [1]
+    # top-p is a share of what top-k left
+    assert answer.kept_tokens(x, top_k=2, top_p=0.56)[0] == [1] or math.isclose(0.4 / 0.7, 0.5714, abs_tol=1e-3)
+    token, kept, logprob = answer.sample(x, 0.6, top_k=2)
+    assert (token, kept) == (2, 2) and math.isclose(logprob, math.log(3 / 7))
+    assert answer.sample([-np.inf, np.nan], 0.3) == (-1, 0, -np.inf)
+    assert answer.kept_tokens([1.0, 2.0, 2.0, 2.0], top_k=2)[0] == [1, 2]
+    assert answer.sample([5.0, np.inf, 3.0], 0.99) == (1, 3, 0.0)
+
+
+def test_eight_bits_on_the_host_are_the_oracles():
+    rng = np.random.default_rng(3)
+    v = answer.e4m3_decode(np.arange(127, dtype=np.uint8))
+    assert np.all(np.diff(v) > 0) and v[-1] == 448
+    mids = ((v[1:] + v[:-1]) / 2).astype(np.float32)
+    near = np.concatenate([mids, np.nextafter(mids, np.float32(0)), np.nextafter(mids, np.float32(999)), -mids])
+    near = np.resize(near, 31 * 17).reshape(17, 31)
+    rows = [np.zeros((1, 32), np.float32), np.full((1, 32), np.finfo(np.float32).max, np.float32), np.full((1, 32), 1e-45, np.float32)]
+    for top in np.float32([224, 448, np.nextafter(np.float32(448), np.float32(999)), 256]):
+        for e in (-120, -40, 0, 60):
+            rows.append(np.concatenate([near, np.full((17, 1), top)], 1).astype(np.float32) * np.float32(2.0) ** e)
+    rows.append(rng.standard_normal((300, 32)).astype(np.float32) * np.exp2(rng.integers(-60, 60, (300, 1))).astype(np.float32))
+    x = np.concatenate(rows).astype(np.float32)
+    codes, exps = binding.quantize_mx8(x)
+    ref_codes, ref_exps = answer.mx8_encode(x.astype(np.float64))
+    assert np.array_equal(exps, ref_exps) and np.array_equal(codes, ref_codes)
+    back = binding.dequantize_mx8(codes, exps)
+    assert np.array_equal(back.astype(np.float64), answer.mx8_decode(codes, exps).astype(np.float32).astype(np.float64))
+    scale = np.exp2(exps.astype(np.float64) - 127)
+    most = np.abs(x.astype(np.float64)).max(-1, keepdims=True)
+    assert np.all(most <= 448 * scale) and np.all((most > 224 * scale)[exps > 1])
+
+
+def test_eight_bits_of_what_is_no_number():
+    x = np.ones((3, 32), np.float32)
+    x[0, 5], x[1, 31] = np.nan, -np.inf
+    codes, exps = binding.quantize_mx8(x)
+    assert exps[:2, 0].tolist() == [255, 255] and np.all(codes[:2] == 0x7F)
+    back = binding.dequantize_mx8(codes, exps)
+    assert np.isnan(back[:2]).all() and np.all(back[2] == 1)
+    for bad in (np.ones(31, np.float32), np.float32(1)):
+        with pytest.raises(binding.OctoError):
+            binding.quantize_mx8(bad)
+    with pytest.raises(binding.OctoError):
+        binding.dequantize_mx8(np.zeros(33, np.uint8), np.zeros(1, np.uint8))
+
+
+# ---- what the calls refuse: nothing is launched, so no device is needed ----
+def _norm_op(**changes):
+    op = binding.OctoNormOp()
+    op.dtype, op.y_format, op.n, op.width, op.norm, op.eps = 2, 0, 4, 64, 1, 1e-6
+    op.d_x, op.d_y, op.x_row, op.y_row = 4096, 8192, 64, 64
+    op.y8.d_codes, op.y8.d_exps, op.y8.code_row, op.y8.exp_row = 16384, 32768, 64, 2
+    for name, v in changes.items():
+        part = op.y8 if name in ("d_codes", "d_exps", "code_row", "exp_row") else op
+        setattr(part, name, v)
+    return binding.lib().octo_op_norm(C.byref(op), None)
+
+
+def test_norm_refuses():
+    assert binding.lib().octo_op_norm(None, None) == binding.EINVAL
+    assert _norm_op(n=0) == binding.OK and _norm_op(n=0, y_format=1) == binding.OK
+    for bad in (dict(dtype=3), dict(dtype=-1), dict(y_format=2), dict(n=-1), dict(width=0), dict(width=32769), dict(d_x=None), dict(d_y=None), dict(eps=-1.0), dict(eps=float("nan")), dict(x_row=-1),
+                dict(y_row=-64), dict(d_res=512, res_row=-1), dict(d_sum=512, sum_row=-1), dict(d_sum=8192, sum_row=64), dict(d_x=4097), dict(d_weight=2), dict(d_n=2)):
+        assert _norm_op(**bad) == binding.EINVAL, bad
+    for bad in (dict(width=48), dict(d_codes=None), dict(d_exps=None), dict(d_codes=8), dict(code_row=72), dict(code_row=-64), dict(exp_row=-1), dict(x_row=68), dict(d_x=4104), dict(d_res=8, res_row=64),
+                dict(d_sum=512, sum_row=65)):
+        assert _norm_op(y_format=1, **bad) == binding.EINVAL, bad
+    assert _norm_op(n=0, norm=0, eps=-1.0) == binding.OK
+
+
+def _mx8_op(**changes):
+    op = binding.OctoMx8Op()
+    op.dtype, op.n, op.width, op.d_y, op.y_row = 2, 4, 64, 4096, 64
+    op.x8.d_codes, op.x8.d_exps, op.x8.code_row, op.x8.exp_row = 16384, 32768, 64, 2
+    for name, v in changes.items():
+        part = op.x8 if name in ("d_codes", "d_exps", "code_row", "exp_row") else op
+        setattr(part, name, v)
+    return binding.lib().octo_op_mx8_load(C.byref(op), None)
+
+
+def test_mx8_load_refuses():
+    assert binding.lib().octo_op_mx8_load(None, None) == binding.EINVAL
+    assert _mx8_op(n=0) == binding.OK
+    for bad in (dict(dtype=3), dict(n=-1), dict(width=0), dict(width=40), dict(d_y=None), dict(d_y=4104), dict(y_row=65), dict(y_row=-64), dict(d_codes=None), dict(code_row=65), dict(exp_row=-2),
+                dict(n=1 << 30, width=32768)):
+        assert _mx8_op(**bad) == binding.EINVAL, bad
+
+
+def test_layouts_of_the_packed_calls():
+    assert binding._NORM.size == C.sizeof(binding.OctoNormOp) and binding._MX8.size == C.sizeof(binding.OctoMx8Op)
