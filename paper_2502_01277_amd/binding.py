@@ -187,6 +187,13 @@ class OctoMx8Op(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("n", C.c_int32), ("width", C.c_int32), ("pad_", C.c_int32), ("x8", OctoMx8Rows), ("d_y", C.c_void_p), ("y_row", C.c_int64), ("d_n", C.c_void_p)]
 
 
+class OctoProductOp(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("x_format", C.c_int32), ("y_format", C.c_int32), ("out_f32", C.c_int32), ("n", C.c_int32), ("k", C.c_int32), ("cols", C.c_int32),
+                ("act", C.c_int32), ("gated", C.c_int32), ("pad_", C.c_int32), ("d_x", C.c_void_p), ("d_w", C.c_void_p), ("x_row", C.c_int64), ("w_row", C.c_int64),
+                ("x8", OctoMx8Rows), ("w8", OctoMx8Rows), ("d_bias", C.c_void_p), ("d_res", C.c_void_p), ("d_y", C.c_void_p), ("res_row", C.c_int64), ("y_row", C.c_int64),
+                ("y8", OctoMx8Rows), ("d_n", C.c_void_p)]
+
+
 # Every symbol include/octo.h declares.
 EXPORTS = [
     "octo_pipeline_workspace_size", "octo_pipeline_create", "octo_pipeline_destroy", "octo_submit_frames", "octo_run",
@@ -202,7 +209,7 @@ EXPORTS = [
     "octo_op_conv", "octo_op_conv_packed_bytes", "octo_op_conv_padded_cout", "octo_op_conv_pack", "octo_quantize_e4m3", "octo_dequantize_e4m3",
     "octo_op_rotate", "octo_op_cache4_store", "octo_op_cache4_load", "octo_quantize_mx4", "octo_dequantize_mx4",
     "octo_op_attend", "octo_op_attend_workspace_bytes",
-    "octo_op_norm", "octo_op_mx8_load", "octo_quantize_mx8", "octo_dequantize_mx8",
+    "octo_op_norm", "octo_op_mx8_load", "octo_quantize_mx8", "octo_dequantize_mx8", "octo_op_product",
 ]
 
 _lib = None
@@ -303,6 +310,7 @@ def lib() -> C.CDLL:
         L.octo_dequantize_mx4.argtypes = [vp, vp, C.c_size_t, vp]
         L.octo_op_norm.argtypes = [vp, vp]
         L.octo_op_mx8_load.argtypes = [vp, vp]
+        L.octo_op_product.argtypes = [vp, vp, vp]
         L.octo_quantize_mx8.argtypes = [vp, C.c_size_t, vp, vp]
         L.octo_dequantize_mx8.argtypes = [vp, vp, C.c_size_t, vp]
         _lib = L
@@ -834,7 +842,7 @@ def op_conv(layer: ConvOp, x, y, res=None, res_mode=0, out_f32=False, res_scale=
 
 # ---- tokens behind a cascade ---------------------------------------------------
 # A call's arguments are packed in one go (a dozen microseconds less than field by field, as long as the small kernels take): the
-# layouts of OctoRotateOp, OctoCache4Op, OctoAttendOp, OctoNormOp and OctoMx8Op.
+# layouts of OctoRotateOp, OctoCache4Op, OctoAttendOp, OctoNormOp, OctoMx8Op and OctoProductOp.
 _PLANE = "PPqqqq"
 _ROTATE = struct.Struct("@12id2fPP" + "PPPqqqqii" * MAX_ROTATE_PARTS)
 _CACHE4 = struct.Struct("@4iq" + 2 * _PLANE + "PP4qPP")
@@ -842,7 +850,9 @@ _ATTEND = struct.Struct("@9ifqPqqPPqqqq" + 2 * _PLANE + "5PPqqPPN")
 _MX8_ROWS = "PPqq"
 _NORM = struct.Struct("@5if4P4q" + _MX8_ROWS + "PP")
 _MX8 = struct.Struct("@4i" + _MX8_ROWS + "PqP")
-_NO_MX8 = (0,) * 4
+_PRODUCT = struct.Struct("@10iPPqq" + 2 * _MX8_ROWS + "PPPqq" + _MX8_ROWS + "P")
+_ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
+_NO_MX8, _NO_ROWS = (0,) * 4, (0,) * 8
 _NO_PART, _NO_PLANE, _NO_KV, _NO_SECTIONS = {1: (0,) * 9, 2: ()}, (0,) * 6, (0,) * 6, (0,) * MAX_AXES
 
 
@@ -1147,6 +1157,58 @@ def op_mx8_load(x: Mx8, y, n=None, stream=None):
     st = lib().octo_op_mx8_load(op, _stream_ptr(stream))
     if st:
         _st(st)
+
+
+def op_product(x, w, y, bias=None, act="none", gated=False, res=None, n=None, stream=None) -> int:
+    """y = act(x w^T + bias) (+ res), gated: the first half of w's rows, activated, times the second (octo_product_op in octo.h).  x [tokens][k] and w [rows][k]: tensors of
+    one type, or Mx8 both; y [tokens][cols]: a tensor of x's type or fp32 (of any type where x is Mx8), or an Mx8; bias fp32 [rows of w]; res like y;
+    act: "none", "relu", "silu" or "gelu".  n: int32 device tensor with the number of tokens present, or None.  Returns the id of the kernel that ran."""
+    t = _torch()
+    if isinstance(x, Mx8):
+        if not isinstance(w, Mx8):
+            _refuse("x and w are both tensors or both Mx8")
+        (tokens, k, x8), (rows, wk, w8) = x.pack(), w.pack()
+        x_fields, x_fmt, kind = (0, 0, 0, 0) + x8 + w8, 1, None
+    else:
+        if isinstance(w, Mx8) or len(x.shape) != 2 or len(w.shape) != 2:
+            _refuse("x is [tokens][k], w [rows][k], both tensors or both Mx8")
+        (tokens, k), (rows, wk), kind = x.shape, w.shape, x.dtype
+        d_x, x_row = _rows(x, kind, x.shape, "x is on the device, its rows contiguous")
+        d_w, w_row = _rows(w, kind, w.shape, "w is of the type of x, on the device, its rows contiguous")
+        x_fields, x_fmt = (d_x, d_w, x_row, w_row) + _NO_ROWS, 0
+    cols = rows // 2 if gated else rows
+    if wk != k or (gated and rows % 2) or act not in _ACTS:
+        _refuse("w has the k of x, a gated layer's w an even number of rows, act is one of %s" % ", ".join(_ACTS))
+    d_res = res_row = d_y = y_row = out_f32 = 0
+    y8, y_fmt = _NO_MX8, 0
+    if isinstance(y, Mx8):
+        y_tokens, y_cols, y8 = y.pack()
+        y_fmt = 1
+        if (y_tokens, y_cols) != (tokens, cols) or res is not None:
+            _refuse("y is [tokens][cols]; one of 8 bits takes no residual")
+        code = 2 if kind is None else _CODE[kind]
+    else:
+        d_y, y_row = _rows(y, y.dtype, (tokens, cols), "y is [tokens][cols] on the device, its rows contiguous")
+        if kind is None or y.dtype is kind:
+            code = _CODE[y.dtype]
+        elif y.dtype is t.float32:
+            code, out_f32 = _CODE[kind], 1
+        else:
+            _refuse("y is of the type of x, or fp32")
+        if res is not None:
+            d_res, res_row = _rows(res, y.dtype, (tokens, cols), "res is like y")
+    if not tokens or not cols:
+        return 0
+    op = _PRODUCT.pack(code, x_fmt, y_fmt, out_f32, tokens, k, cols, _ACTS[act], 1 if gated else 0, 0, *x_fields,
+                       0 if bias is None else _optional(bias, t.float32, "bias is fp32 [rows of w] on the device", rows), d_res, d_y, res_row, y_row, *y8,
+                       0 if n is None else _optional(n, t.int32, "n is int32 on the device"))
+    if stream is not None:
+        _order(stream)
+    kid = C.c_int32(0)
+    st = lib().octo_op_product(op, _stream_ptr(stream), C.byref(kid))
+    if st:
+        _st(st)
+    return kid.value
 
 
 def quantize_mx8(x: np.ndarray):

@@ -1,0 +1,522 @@
+// octo_op_product: rows times weights with bias, activation or gate, and residual.
+//
+//   y[i][j] = act(sum_k x[i][k] w[j][k] + b[j]) + r[i][j],     gated: act(z[i][j]) z[i][cols + j] + r[i][j], z the sums of all 2 cols rows of w
+//
+// Rows of w and of x are alike: both are read along k, 16 bytes a lane, and go into the matrix instructions as they lie in memory.  w is the first operand, so a lane gets
+// results of neighbouring outputs of one token.
+#pragma once
+#include "mx8.h"
+#include "octo_internal.h"
+
+namespace octo {
+
+enum { PRODUCT_Y_F32 = 0, PRODUCT_Y_F16 = 1, PRODUCT_Y_BF16 = 2, PRODUCT_Y_MX8 = 3 };
+enum { PRODUCT_ACT_NONE = 0, PRODUCT_ACT_RELU = 1, PRODUCT_ACT_SILU = 2, PRODUCT_ACT_GELU = 3 };
+
+struct ProductArgs {
+  const char* x; const char* w;                       // rows of k_bytes, x_row and w_row bytes apart
+  const uint8_t* xe; const uint8_t* we;               // exponents of rows in 8 bits
+  long long x_row, w_row, xe_row, we_row;
+  const float* bias; const void* res; void* y;
+  long long res_row, y_row;                           // in elements
+  octo_mx8_rows y8;
+  const int* n_dyn;
+  int n, k_bytes, cols, gated, act, y_kind;
+  int y_vec, res_vec, bias_vec;                       // four values at a multiple of four outputs are one aligned vector
+  int exp_words;                                      // the exponents of 128 values of k are one aligned word
+  int tiles_n, tiles_m;
+};
+
+typedef __attribute__((address_space(3))) unsigned char LdsBytes;
+
+__device__ __forceinline__ float product_act(int act, float v) {
+  if (act == PRODUCT_ACT_RELU) return fmaxf(v, 0.f);
+  if (act == PRODUCT_ACT_SILU) return silu(v);
+  if (act == PRODUCT_ACT_GELU) return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f));
+  return v;
+}
+
+template <typename T> __device__ __forceinline__ void product_read4(const void* p, long long at, int have, int vec, float* v) {
+  const T* r = (const T*)p + at;
+  if (vec && have == 4) {
+    const floatx4 f = load4(r);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += f[e];
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) if (e < have) v[e] += (float)r[e];
+  }
+}
+template <typename T> __device__ __forceinline__ void product_write4(void* p, long long at, int have, int vec, const float* v) {
+  T* y = (T*)p + at;
+  if (vec && have == 4) {
+    store4<T>(y, floatx4{v[0], v[1], v[2], v[3]});
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) if (e < have) y[e] = (T)v[e];
+  }
+}
+
+// The sums of outputs j .. j + 3 (a multiple of four) of token i become results: z, and up where the layer is gated.  Where they go to 8 bits, the eight lanes of a group of 32
+// outputs call it together.  `on`: the token is there.
+__device__ __forceinline__ void product_finish4(const ProductArgs& a, bool on, int i, int j, floatx4 z, floatx4 up) {
+  const int have = min(4, a.cols - j);
+  on = on && have > 0;
+  float v[4] = {z[0], z[1], z[2], z[3]};
+  if (a.bias && on) product_read4<float>(a.bias, j, have, a.bias_vec, v);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = product_act(a.act, v[e]);
+  if (a.gated) {
+    float u[4] = {up[0], up[1], up[2], up[3]};
+    if (a.bias && on) product_read4<float>(a.bias, (long long)a.cols + j, have, a.bias_vec, u);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] *= u[e];
+  }
+  if (a.y_kind == PRODUCT_Y_MX8) {
+    unsigned most = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) most = max(most, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+    if (!on) most = 0;
+#pragma unroll
+    for (int d = 1; d < 8; d *= 2) most = max(most, (unsigned)__shfl_xor((int)most, d));
+    if (!on) return;
+    const bool none = most >= 0x7F800000u;
+    const int ex = mx8_exp(most);
+    *(unsigned*)(a.y8.d_codes + i * a.y8.code_row + j) = none ? MX8_NAN4 : mx8_pack4(floatx4{v[0], v[1], v[2], v[3]}, mx8_inverse(ex));
+    if (j % 32 == 0) a.y8.d_exps[i * a.y8.exp_row + j / 32] = (uint8_t)(none ? 255 : ex);
+    return;
+  }
+  if (!on) return;
+  const long long ry = i * a.res_row + j, wy = i * a.y_row + j;
+  if (a.y_kind == PRODUCT_Y_F32) {
+    if (a.res) product_read4<float>(a.res, ry, have, a.res_vec, v);
+    product_write4<float>(a.y, wy, have, a.y_vec, v);
+  } else if (a.y_kind == PRODUCT_Y_F16) {
+    if (a.res) product_read4<_Float16>(a.res, ry, have, a.res_vec, v);
+    product_write4<_Float16>(a.y, wy, have, a.y_vec, v);
+  } else {
+    if (a.res) product_read4<__bf16>(a.res, ry, have, a.res_vec, v);
+    product_write4<__bf16>(a.y, wy, have, a.y_vec, v);
+  }
+}
+
+// Two operands of 32 rows and 64 values of k in 8 bits: a lane (row l % 32, half l / 32) gives bytes 16 half .. + 15 of the first and of the second block of 32, and the
+// exponent of block number `half` of its row, byte 2 KK of a word that is shifted by 8 half.
+template <int KK>
+__device__ __forceinline__ floatx16 mfma_mx8(u32x4 a0, u32x4 a1, u32x4 b0, u32x4 b1, floatx16 c, int ea, int eb) {
+  const i32x8 a = {(int)a0[0], (int)a0[1], (int)a0[2], (int)a0[3], (int)a1[0], (int)a1[1], (int)a1[2], (int)a1[3]};
+  const i32x8 b = {(int)b0[0], (int)b0[1], (int)b0[2], (int)b0[3], (int)b1[0], (int)b1[1], (int)b1[2], (int)b1[3]};
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 2 * KK, ea, 2 * KK, eb);
+}
+
+// Sixteen values of 8 bits in bf16, which holds them and their power of two exactly; `e`: their exponent byte.
+__device__ __forceinline__ void widen_mx8(u32x4 v, unsigned e, u32x4* lo, u32x4* hi) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const float scale = __uint_as_float(e << 23);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const unsigned a = __builtin_bit_cast(unsigned, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)v[i], scale, false));
+    const unsigned b = __builtin_bit_cast(unsigned, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)v[i], scale, true));
+    if (i < 2) { (*lo)[2 * i] = a; (*lo)[2 * i + 1] = b; }
+    else { (*hi)[2 * i - 4] = a; (*hi)[2 * i - 3] = b; }
+  }
+}
+
+// ---- many tokens: tiles in LDS -----------------------------------------------------------------------------------------
+// A block makes BN rows of w times BM tokens; its WN x WM wavefronts take TN x TM blocks of 32 x 32 each.  A step covers 128 bytes of k of all rows.  Loads go straight
+// to LDS, two steps deep: once all wavefronts have read their last operands of step t, its place is given to step t + 2, whose loads then have a whole step's products to
+// arrive in.  Operands of the next products are read from LDS while the present ones run, also across steps, so a step costs one barrier in the middle of
+// products.  The 16-byte chunks of a row lie at their number xor the row's, which spreads the rows that eight lanes read together over all banks.
+//
+// Rows of 8 bits: the 8-bit matrix instructions add products in groups of eight at the weight of the group's largest and drop what lies 2^13 below it (measured: 1 + 2^-13 comes
+// out, 1 + 2^-14 does not), 2^-14 of a sum's size in the mean.  Results that are rounded to 16 or 8 bits can bear that; for fp32 results (EXACT) the values are widened to bf16,
+// whose products are exact and added in fp32, at half the rate.
+template <typename T, bool EXACT, int TN, int TM, int WN, int WM, int MINB>
+__global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(ProductArgs a) {
+  constexpr bool MX = std::is_same<T, f8>::value;
+  constexpr int NW = WN * WM, BN = WN * TN * 32, BM = WM * TM * 32, ROWS = BN + BM, STAGE = ROWS * 128, LW = BN / 8 / NW, LX = BM / 8 / NW;
+  constexpr int KQ = MX ? 2 : 4, FV = MX ? 2 : 1;                    // products of k within a step, 16-byte vectors of an operand
+  constexpr int HT = TM < 2 ? 1 : 2, UNIT = HT * 32 * TN * 32 * 4;    // sums of a wavefront on their way out, of 32 or 64 tokens
+  constexpr int MAIN = 2 * STAGE + (MX ? 4 * ROWS * 4 : 0), LDS = MAIN > NW * UNIT ? MAIN : NW * UNIT;
+  static_assert(BN / 8 % NW == 0 && BM / 8 % NW == 0 && TN % 2 == 0 && NW % 4 == 0, "whole loads a wavefront, pairs of blocks");
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[LDS];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
+  const int wn = wave % WN, wm = wave / WN;
+  const int n = a.n_dyn ? min(max(*a.n_dyn, 0), a.n) : a.n;
+
+  // Tiles in groups of eight along the tokens, all outputs of a group one after the other, and an eighth of that list to each die (block b runs on die b % 8): the
+  // blocks of a die share rows of w and x in its L2.
+  int tn, tm;
+  {
+    const int tiles = a.tiles_n * a.tiles_m, die = blockIdx.x % 8, i = blockIdx.x / 8, base = tiles / 8, more = tiles % 8;
+    const int id = die * base + min(die, more) + i;
+    const int group = id / (8 * a.tiles_n), first = group * 8, tall = min(8, a.tiles_m - first), in = id - group * 8 * a.tiles_n;
+    tm = first + in % tall; tn = in / tall;
+  }
+  const int m0 = tm * BM, n0 = tn * (a.gated ? BN / 2 : BN);         // the tile's first token and output
+  if (m0 >= n) return;
+
+  const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(LdsBytes*)smem);
+  const int chunk = (lane & 7) ^ (lane >> 3);
+  int woff[LW], xoff[LX];
+#pragma unroll
+  for (int i = 0; i < LW; ++i) {
+    const int row = (i * NW + wave) * 8 + (lane >> 3);
+    const int col = a.gated ? row / 64 * 32 + row % 32 : row;
+    woff[i] = n0 + col < a.cols ? col * (int)a.w_row + chunk * 16 : OOB;
+  }
+#pragma unroll
+  for (int i = 0; i < LX; ++i) {
+    const int row = (i * NW + wave) * 8 + (lane >> 3);
+    xoff[i] = m0 + row < n ? row * (int)a.x_row + chunk * 16 : OOB;
+  }
+  const char* const w0 = a.w + n0 * a.w_row;
+  const char* const w1 = w0 + (a.gated ? a.cols * a.w_row : 0);
+  const char* const x0 = a.x + m0 * a.x_row;
+  const int nk = (a.k_bytes + 127) / 128;
+
+  // exponents: a thread takes row threadIdx.x, and those NW * 64 further on
+  constexpr int NE = MX ? (ROWS + NW * 64 - 1) / (NW * 64) : 1;
+  unsigned exps[NE];
+  auto exp_row = [&](int r, bool* there) -> const uint8_t* {
+    if (r < BN) {
+      const int col = a.gated ? r / 64 * 32 + r % 32 : r;
+      *there = n0 + col < a.cols;
+      return a.we + ((a.gated && r / 32 % 2 ? a.cols : 0) + n0 + col) * a.we_row;
+    }
+    *there = r < ROWS && m0 + r - BN < n;
+    return a.xe + (m0 + r - BN) * a.xe_row;
+  };
+  auto load_exps = [&](int t) __attribute__((always_inline)) {
+    if constexpr (MX) {
+#pragma unroll
+      for (int i = 0; i < NE; ++i) {
+        bool there;
+        const uint8_t* p = exp_row(i * NW * 64 + (int)threadIdx.x, &there) + 4 * t;
+        exps[i] = 0;
+        if (!there || t >= nk) continue;
+        if (a.exp_words) { exps[i] = *(const unsigned*)p; continue; }
+#pragma unroll
+        for (int b = 0; b < 4; ++b) if (t * 128 + b * 32 < a.k_bytes) exps[i] |= (unsigned)p[b] << (8 * b);
+      }
+    }
+  };
+  auto place_exps = [&](int t) __attribute__((always_inline)) {
+    if constexpr (MX) {
+#pragma unroll
+      for (int i = 0; i < NE; ++i) {
+        const int r = i * NW * 64 + (int)threadIdx.x;
+        if (r < ROWS) *(unsigned*)(smem + 2 * STAGE + ((t & 3) * ROWS + r) * 4) = exps[i];
+      }
+    }
+  };
+  auto issue = [&](int t) __attribute__((always_inline)) {
+    const int beyond = chunk * 16 + t * 128 >= a.k_bytes ? OOB : 0;   // the end of a row inside a step
+    const unsigned to = lds + (t & 1) * STAGE + wave * 1024;
+    const __amdgpu_buffer_rsrc_t rw0 = __builtin_amdgcn_make_buffer_rsrc((void*)(w0 + t * 128), 0, 0x7FFFFFFF, BUF_FLAGS);
+    const __amdgpu_buffer_rsrc_t rw1 = __builtin_amdgcn_make_buffer_rsrc((void*)(w1 + t * 128), 0, 0x7FFFFFFF, BUF_FLAGS);
+    const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc((void*)(x0 + t * 128), 0, 0x7FFFFFFF, BUF_FLAGS);
+#pragma unroll
+    for (int i = 0; i < LW; ++i) {
+      // blocks of 32 rows alternate between the two halves of a gated layer: rows i NW 8 + 8 wave ..
+      const bool second = NW == 4 ? i & 1 : (wave >> 2) & 1;
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(to + i * NW * 1024), "v"(woff[i] | beyond), "s"(second ? rw1 : rw0) : "memory");
+    }
+#pragma unroll
+    for (int i = 0; i < LX; ++i)
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(to + BN * 128 + i * NW * 1024), "v"(xoff[i] | beyond), "s"(rx) : "memory");
+  };
+
+  u32x4 fw[2][TN][FV], fx[2][TM][FV];
+  int ew[2][TN], ex[2][TM];
+  const int wrow = (wn * TN * 32 + l32) * 128, xrow = (BN + wm * TM * 32 + l32) * 128;
+  auto frags = [&](int set, int t, int kq) __attribute__((always_inline)) {
+    const unsigned char* const p = smem + (t & 1) * STAGE;
+#pragma unroll
+    for (int h = 0; h < FV; ++h) {
+      const int c = ((MX ? 4 * kq + 2 * h + half : 2 * kq + half) ^ (lane & 7)) * 16;
+#pragma unroll
+      for (int i = 0; i < TN; ++i) fw[set][i][h] = *(const u32x4*)(p + wrow + i * 4096 + c);
+#pragma unroll
+      for (int j = 0; j < TM; ++j) fx[set][j][h] = *(const u32x4*)(p + xrow + j * 4096 + c);
+    }
+  };
+  auto scales = [&](int set, int t) __attribute__((always_inline)) {
+    if constexpr (MX) {
+      const unsigned char* const p = smem + 2 * STAGE + (t & 3) * ROWS * 4;
+#pragma unroll
+      for (int i = 0; i < TN; ++i) ew[set][i] = *(const unsigned*)(p + (wn * TN * 32 + i * 32 + l32) * 4) >> (EXACT ? 0 : 8 * half);
+#pragma unroll
+      for (int j = 0; j < TM; ++j) ex[set][j] = *(const unsigned*)(p + (BN + wm * TM * 32 + j * 32 + l32) * 4) >> (EXACT ? 0 : 8 * half);
+    }
+  };
+
+  floatx16 acc[TN][TM];
+#pragma unroll
+  for (int i = 0; i < TN; ++i)
+#pragma unroll
+    for (int j = 0; j < TM; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+
+  load_exps(0); place_exps(0);
+  load_exps(1); place_exps(1);
+  issue(0);
+  issue(1);
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(LW + LX) : "memory");
+  __builtin_amdgcn_s_barrier();
+  load_exps(2);
+  frags(0, 0, 0);
+  scales(0, 0);
+
+  // Loads and reads beyond the last step are of nothing (zeros go to LDS): the loop has no branches.
+#pragma nounroll
+  for (int t = 0; t < nk; ++t) {
+#pragma unroll
+    for (int kq = 0; kq < KQ; ++kq) {
+      const int cur = kq & 1;
+      if (kq < KQ - 1) {
+        frags(cur ^ 1, t, kq + 1);
+      } else {
+        place_exps(t + 2);
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        issue(t + 2);
+        load_exps(t + 3);
+        frags(cur ^ 1, t + 1, 0);
+        scales(1, t + 1);
+      }
+      if constexpr (MX && EXACT) {
+#pragma unroll
+        for (int h = 0; h < FV; ++h) {
+          u32x4 w[TN][2], x[TM][2];
+#pragma unroll
+          for (int i = 0; i < TN; ++i) widen_mx8(fw[cur][i][h], (unsigned)ew[0][i] >> (16 * kq + 8 * h) & 255, &w[i][0], &w[i][1]);
+#pragma unroll
+          for (int j = 0; j < TM; ++j) widen_mx8(fx[cur][j][h], (unsigned)ex[0][j] >> (16 * kq + 8 * h) & 255, &x[j][0], &x[j][1]);
+#pragma unroll
+          for (int i = 0; i < TN; ++i)
+#pragma unroll
+            for (int j = 0; j < TM; ++j) acc[i][j] = Elem<__bf16>::mfma(w[i][1], x[j][1], Elem<__bf16>::mfma(w[i][0], x[j][0], acc[i][j]));
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+#pragma unroll
+          for (int j = 0; j < TM; ++j) {
+            if constexpr (MX) {
+              if (kq == 0) acc[i][j] = mfma_mx8<0>(fw[cur][i][0], fw[cur][i][1], fx[cur][j][0], fx[cur][j][1], acc[i][j], ew[0][i], ex[0][j]);
+              else acc[i][j] = mfma_mx8<1>(fw[cur][i][0], fw[cur][i][1], fx[cur][j][0], fx[cur][j][1], acc[i][j], ew[0][i], ex[0][j]);
+            } else {
+              acc[i][j] = Elem<T>::mfma(fw[cur][i][0], fx[cur][j][0], acc[i][j]);
+            }
+          }
+      }
+    }
+    if constexpr (MX) {
+#pragma unroll
+      for (int i = 0; i < TN; ++i) ew[0][i] = ew[1][i];
+#pragma unroll
+      for (int j = 0; j < TM; ++j) ex[0][j] = ex[1][j];
+    }
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+
+  // Sums leave through LDS, up to 64 tokens of a wavefront at a time, in a place of its own: lanes then hold four neighbouring outputs of a token.  Chunks of four lie at their
+  // number xor the token's, as above.
+  __syncthreads();
+  float* const out = (float*)(smem + wave * UNIT);
+  const int lpt = a.gated ? TN * 4 : TN * 8;                         // lanes of a token
+#pragma unroll
+  for (int h = 0; h < TM; h += HT) {
+#pragma unroll
+    for (int j = 0; j < HT; ++j)
+#pragma unroll
+      for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const floatx16& c = acc[i][h + j];
+          *(floatx4*)(out + ((j * 32 + l32) * TN * 8 + ((8 * i + 2 * q + half) ^ (lane & 7))) * 4) = floatx4{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
+        }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    const int token0 = m0 + (wm * TM + h) * 32;
+#pragma nounroll
+    for (int p = lane; p < HT * 32 * lpt; p += 64) {
+      const int tok = p / lpt, o4 = p % lpt;                         // both powers of two
+      const int c4 = a.gated ? o4 / 8 * 16 + o4 % 8 : o4;            // the chunk of its sums; those it is a gate of lie eight further on
+      const float* const row = out + tok * TN * 32;
+      const floatx4 z = *(const floatx4*)(row + (c4 ^ (tok & 7)) * 4), up = *(const floatx4*)(row + ((a.gated ? c4 + 8 : c4) ^ (tok & 7)) * 4);
+      product_finish4(a, token0 + tok < n, token0 + tok, n0 + wn * (lpt * 4) + o4 * 4, z, up);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  }
+}
+
+template <typename T, bool EXACT, int TN, int TM, int WN, int WM, int MINB>
+hipError_t launch_product_tile(ProductArgs a, hipStream_t s) {
+  constexpr int BN = WN * TN * 32, BM = WM * TM * 32;
+  const int outs = a.gated ? BN / 2 : BN;
+  a.tiles_n = (a.cols + outs - 1) / outs; a.tiles_m = (a.n + BM - 1) / BM;
+  hipLaunchKernelGGL((product_tile_kernel<T, EXACT, TN, TM, WN, WM, MINB>), dim3((unsigned)(a.tiles_n * a.tiles_m)), dim3(WN * WM * 64), 0, s, a);
+  return hipGetLastError();
+}
+
+// ---- few tokens: operands straight from memory ---------------------------------------------------------------------------
+// The bound is memory: every weight goes into one or a few products.  A block makes TILES x 16 rows of w times TB x 16 tokens; its wavefronts take steps of 128 bytes of k in turn, load
+// their operands from memory straight into registers, several steps in flight, and add up their sums in LDS at the end, in a fixed order.  A gated block has gates in the first
+// half of its tiles and what they are a gate of in the second.
+template <typename T, int TILES, int TB>
+__global__ __launch_bounds__(512, TILES * TB > 4 ? 1 : 2) void product_few_kernel(ProductArgs a) {
+  constexpr bool MX = std::is_same<T, f8>::value;
+  constexpr int W = 8, U = TILES + TB <= 3 ? 4 : 2;
+  __shared__ __attribute__((aligned(16))) floatx4 red[W][TILES][TB][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
+  const int n = a.n_dyn ? min(max(*a.n_dyn, 0), a.n) : a.n;
+  const int outs = a.gated ? TILES * 8 : TILES * 16;
+  const int tn = blockIdx.x % a.tiles_n, tm = blockIdx.x / a.tiles_n;
+  const int m0 = tm * TB * 16, n0 = tn * outs;
+  if (m0 >= n) return;
+  const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc((void*)(a.x + m0 * a.x_row), 0, 0x7FFFFFFF, BUF_FLAGS);
+  const char* const w0 = a.w + n0 * a.w_row;
+  const __amdgpu_buffer_rsrc_t rw[2] = {__builtin_amdgcn_make_buffer_rsrc((void*)w0, 0, 0x7FFFFFFF, BUF_FLAGS),
+                                        __builtin_amdgcn_make_buffer_rsrc((void*)(w0 + (a.gated ? a.cols * a.w_row : 0)), 0, 0x7FFFFFFF, BUF_FLAGS)};
+  __amdgpu_buffer_rsrc_t re[2], rxe;
+  if constexpr (MX) {
+    const uint8_t* const e0 = a.we + n0 * a.we_row;
+    re[0] = __builtin_amdgcn_make_buffer_rsrc((void*)e0, 0, 0x7FFFFFFF, BUF_FLAGS);
+    re[1] = __builtin_amdgcn_make_buffer_rsrc((void*)(e0 + (a.gated ? a.cols * a.we_row : 0)), 0, 0x7FFFFFFF, BUF_FLAGS);
+    rxe = __builtin_amdgcn_make_buffer_rsrc((void*)(a.xe + m0 * a.xe_row), 0, 0x7FFFFFFF, BUF_FLAGS);
+  }
+  int woff[TILES], weoff[TILES], xoff[TB], xeoff[TB];
+#pragma unroll
+  for (int i = 0; i < TILES; ++i) {
+    const int col = (a.gated ? i % (TILES > 1 ? TILES / 2 : 1) : i) * 16 + r16;
+    woff[i] = n0 + col < a.cols ? col * (int)a.w_row + g * 16 : OOB;
+    weoff[i] = n0 + col < a.cols ? col * (int)a.we_row + g / 2 : OOB;
+  }
+#pragma unroll
+  for (int j = 0; j < TB; ++j) {
+    const bool there = m0 + j * 16 + r16 < n;
+    xoff[j] = there ? (j * 16 + r16) * (int)a.x_row + g * 16 : OOB;
+    xeoff[j] = there ? (j * 16 + r16) * (int)a.xe_row + g / 2 : OOB;
+  }
+  const int nk = (a.k_bytes + 127) / 128;
+  floatx4 acc[TILES][TB];
+#pragma unroll
+  for (int i = 0; i < TILES; ++i)
+#pragma unroll
+    for (int j = 0; j < TB; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+  for (int t0 = wave; t0 < nk; t0 += W * U) {
+    u32x4 fw[U][TILES][2], fx[U][TB][2];
+    unsigned ew[U][TILES][2], ex[U][TB][2];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int t = t0 + u * W;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        // chunks g and g + 4 of the step; beyond the row's end, and for steps beyond the last, zeros that no memory is asked for
+        const int beyond = t * 128 + h * 64 + g * 16 >= a.k_bytes ? OOB : 0;
+#pragma unroll
+        for (int i = 0; i < TILES; ++i)
+          fw[u][i][h] = __builtin_amdgcn_raw_buffer_load_b128(rw[a.gated && i >= TILES / 2], (woff[i] | beyond) + t * 128 + h * 64, 0, 0);
+#pragma unroll
+        for (int j = 0; j < TB; ++j) fx[u][j][h] = __builtin_amdgcn_raw_buffer_load_b128(rx, (xoff[j] | beyond) + t * 128 + h * 64, 0, 0);
+        if constexpr (MX) {
+#pragma unroll
+          for (int i = 0; i < TILES; ++i) ew[u][i][h] = __builtin_amdgcn_raw_buffer_load_b8(re[a.gated && i >= TILES / 2], (weoff[i] | beyond) + t * 4 + h * 2, 0, 0);
+#pragma unroll
+          for (int j = 0; j < TB; ++j) ex[u][j][h] = __builtin_amdgcn_raw_buffer_load_b8(rxe, (xeoff[j] | beyond) + t * 4 + h * 2, 0, 0);
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if constexpr (MX) {
+          u32x4 w[TILES][2], x[TB][2];
+#pragma unroll
+          for (int i = 0; i < TILES; ++i) widen_mx8(fw[u][i][h], ew[u][i][h], &w[i][0], &w[i][1]);
+#pragma unroll
+          for (int j = 0; j < TB; ++j) widen_mx8(fx[u][j][h], ex[u][j][h], &x[j][0], &x[j][1]);
+#pragma unroll
+          for (int i = 0; i < TILES; ++i)
+#pragma unroll
+            for (int j = 0; j < TB; ++j) acc[i][j] = mfma16<__bf16>(w[i][1], x[j][1], mfma16<__bf16>(w[i][0], x[j][0], acc[i][j]));
+        } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+          for (int i = 0; i < TILES; ++i)
+#pragma unroll
+            for (int j = 0; j < TB; ++j) {
+              const floatx4 w = __builtin_bit_cast(floatx4, fw[u][i][h]), x = __builtin_bit_cast(floatx4, fx[u][j][h]);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[e], x[e], acc[i][j], 0, 0, 0);
+            }
+        } else {
+#pragma unroll
+          for (int i = 0; i < TILES; ++i)
+#pragma unroll
+            for (int j = 0; j < TB; ++j) acc[i][j] = mfma16<T>(fw[u][i][h], fx[u][j][h], acc[i][j]);
+        }
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < TILES; ++i)
+#pragma unroll
+    for (int j = 0; j < TB; ++j) red[wave][i][j][lane] = acc[i][j];
+  __syncthreads();
+  // token l % 16 and rows 4 (l / 16) .. + 3 of a tile are lane l's
+  const int quads = outs / 4;
+  for (int p = threadIdx.x; p < quads * TB * 16; p += 512) {
+    const int tok = p / quads, q = p % quads, at = (q & 3) * 16 + (tok & 15);
+    floatx4 z = red[0][q >> 2][tok >> 4][at], up = z;
+    for (int w = 1; w < W; ++w) z += red[w][q >> 2][tok >> 4][at];
+    if (a.gated) {
+      const int second = (q >> 2) + TILES / 2;
+      up = red[0][second % TILES][tok >> 4][at];
+      for (int w = 1; w < W; ++w) up += red[w][second % TILES][tok >> 4][at];
+    }
+    product_finish4(a, m0 + tok < n, m0 + tok, n0 + q * 4, z, up);
+  }
+}
+
+template <typename T, int TILES, int TB>
+hipError_t launch_product_few(ProductArgs a, hipStream_t s) {
+  const int outs = a.gated ? TILES * 8 : TILES * 16;
+  a.tiles_n = (a.cols + outs - 1) / outs; a.tiles_m = (a.n + TB * 16 - 1) / (TB * 16);
+  hipLaunchKernelGGL((product_few_kernel<T, TILES, TB>), dim3((unsigned)(a.tiles_n * a.tiles_m)), dim3(512), 0, s, a);
+  return hipGetLastError();
+}
+
+template <typename T> hipError_t launch_product(int variant, const ProductArgs& a, hipStream_t s);
+
+#ifdef OCTO_PRODUCT_TYPE
+template <> hipError_t launch_product<OCTO_PRODUCT_TYPE>(int variant, const ProductArgs& a, hipStream_t s) {
+  typedef OCTO_PRODUCT_TYPE T;
+  if constexpr (std::is_same<T, f8>::value) {
+    if (a.y_kind == PRODUCT_Y_F32) {
+      if (variant == 1 || variant == 2) return launch_product_tile<T, true, 2, 2, 2, 2, 2>(a, s);
+      if (variant == 3) return launch_product_tile<T, true, 2, 1, 2, 2, 2>(a, s);
+    }
+  }
+  switch (variant) {
+    case 1: return launch_product_tile<T, false, 4, 4, 2, 2, 1>(a, s);
+    case 2: return launch_product_tile<T, false, 2, 2, 2, 2, 2>(a, s);
+    case 3: return launch_product_tile<T, false, 2, 1, 2, 2, 2>(a, s);
+    case 11: return launch_product_few<T, 1, 1>(a, s);
+    case 21: return launch_product_few<T, 2, 1>(a, s);
+    case 22: return launch_product_few<T, 2, 2>(a, s);
+    case 24: return launch_product_few<T, 2, 4>(a, s);
+    case 41: return launch_product_few<T, 4, 1>(a, s);
+    case 42: return launch_product_few<T, 4, 2>(a, s);
+  }
+  return hipErrorInvalidValue;
+}
+#endif
+
+}  // namespace octo

@@ -1,0 +1,54 @@
+// octo_op_product: arguments, their checks and the choice of a kernel.
+#include "product.h"
+#include "product_choice.h"
+
+using namespace octo;
+
+namespace {
+bool rows_near(long long bytes) { return bytes >= 0 && bytes <= 8 << 20; }        // 255 of them stay within 31 bits
+}  // namespace
+
+extern "C" octo_status octo_op_product(const octo_product_op* op, void* hip_stream, int32_t* kernel_id) {
+  if (kernel_id) *kernel_id = 0;
+  if (!op || (op->dtype != OCTO_F32 && op->dtype != OCTO_F16 && op->dtype != OCTO_BF16)) return OCTO_EINVAL;
+  if (op->x_format < OCTO_ROWS_PLAIN || op->x_format > OCTO_ROWS_MX8 || op->y_format < OCTO_ROWS_PLAIN || op->y_format > OCTO_ROWS_MX8) return OCTO_EINVAL;
+  if (op->n < 0 || op->k < 1 || op->cols < 1 || op->cols > 0x20000000 || op->act < OCTO_ACT_NONE || op->act > OCTO_ACT_GELU) return OCTO_EINVAL;
+  const bool x8 = op->x_format == OCTO_ROWS_MX8, y8 = op->y_format == OCTO_ROWS_MX8;
+  const int es = op->dtype == OCTO_F32 ? 4 : 2;
+  ProductArgs a{};
+  if (x8) {
+    if (op->k % 32 || !mx8_ok(op->x8) || !mx8_ok(op->w8) || op->x8.exp_row > 8 << 20 || op->w8.exp_row > 8 << 20) return OCTO_EINVAL;
+    a.x = (const char*)op->x8.d_codes; a.w = (const char*)op->w8.d_codes; a.x_row = op->x8.code_row; a.w_row = op->w8.code_row;
+    a.xe = op->x8.d_exps; a.we = op->w8.d_exps; a.xe_row = op->x8.exp_row; a.we_row = op->w8.exp_row;
+    a.k_bytes = op->k;
+    a.exp_words = op->k % 128 == 0 && !(((uintptr_t)a.xe | (uintptr_t)a.we | (uintptr_t)a.xe_row | (uintptr_t)a.we_row) & 3);
+  } else {
+    if (!op->d_x || !op->d_w || (((uintptr_t)op->d_x | (uintptr_t)op->d_w) & 15) || op->k > 0x7FFFFF00 / es || op->k * es % 16) return OCTO_EINVAL;
+    if (op->x_row < 0 || op->w_row < 0 || op->x_row > 8 << 20 || op->w_row > 8 << 20 || (op->x_row * es & 15) || (op->w_row * es & 15)) return OCTO_EINVAL;
+    a.x = (const char*)op->d_x; a.w = (const char*)op->d_w; a.x_row = op->x_row * es; a.w_row = op->w_row * es;
+    a.k_bytes = op->k * es;
+  }
+  if (!rows_near(a.x_row) || !rows_near(a.w_row)) return OCTO_EINVAL;
+  const int ys = op->out_f32 ? 4 : es;
+  if (y8) {
+    if (op->out_f32 || op->d_res || op->cols % 32 || !mx8_ok(op->y8)) return OCTO_EINVAL;
+  } else if (!op->d_y || op->y_row < 0 || ((uintptr_t)op->d_y | (uintptr_t)op->d_res) % ys || (op->d_res && op->res_row < 0)) {
+    return OCTO_EINVAL;
+  }
+  if (((uintptr_t)op->d_bias & 3) || ((uintptr_t)op->d_n & 3)) return OCTO_EINVAL;
+  a.bias = op->d_bias; a.res = op->d_res; a.y = op->d_y; a.res_row = op->res_row; a.y_row = op->y_row; a.y8 = op->y8;
+  a.n_dyn = op->d_n; a.n = op->n; a.cols = op->cols; a.gated = op->gated != 0; a.act = op->act;
+  a.y_kind = y8 ? PRODUCT_Y_MX8 : op->out_f32 || op->dtype == OCTO_F32 ? PRODUCT_Y_F32 : op->dtype == OCTO_F16 ? PRODUCT_Y_F16 : PRODUCT_Y_BF16;
+  a.y_vec = !((uintptr_t)op->d_y % (4 * ys)) && op->y_row % 4 == 0;
+  a.res_vec = !((uintptr_t)op->d_res % (4 * ys)) && op->res_row % 4 == 0;
+  a.bias_vec = !((uintptr_t)op->d_bias & 15) && (!a.gated || op->cols % 4 == 0);
+  if (!op->n) return OCTO_OK;
+  const ProductChoice c = product_choice(op->n, a.cols, a.gated, y8, x8 && a.y_kind == PRODUCT_Y_F32);
+  if (c.blocks > 0x7FFFFF) return OCTO_EINVAL;                       // HIP counts the threads of a launch, up to 512 a block, in 32 bits
+  hipStream_t s = (hipStream_t)hip_stream;
+  const hipError_t e = x8 ? launch_product<f8>(c.variant, a, s) : op->dtype == OCTO_F32 ? launch_product<float>(c.variant, a, s)
+                     : op->dtype == OCTO_F16 ? launch_product<_Float16>(c.variant, a, s) : launch_product<__bf16>(c.variant, a, s);
+  if (e != hipSuccess) return OCTO_EHIP;
+  if (kernel_id) *kernel_id = c.variant;
+  return OCTO_OK;
+}

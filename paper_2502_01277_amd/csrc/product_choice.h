@@ -1,0 +1,24 @@
+// Which kernel octo_op_product runs.  Host arithmetic only: no HIP header is needed to compile this file.
+#pragma once
+
+namespace octo {
+
+struct ProductChoice { int variant; long long blocks; };
+
+// variant: 1, 2, 3: tiles in LDS of 256 x 256, 128 x 128 and 128 x 64 (rows of w x tokens); 10 R + T: operands straight from memory, R x 16 rows of w and T x 16 tokens a block.
+// to8: results in 8 bits, whose groups of 32 outputs one block holds.  exact8: rows of 8 bits that go through bf16, which has no tiles of 256 x 256.
+inline ProductChoice product_choice(int n, int cols, bool gated, bool to8, bool exact8) {
+  const long long rows = gated ? 2ll * cols : cols;
+  auto blocks = [&](int bn, int bm) { return (rows + bn - 1) / bn * ((n + bm - 1) / bm); };
+  auto few = [&](int r, int t) { const int outs = gated ? 8 * r : 16 * r; return ProductChoice{10 * r + t, (cols + outs - 1ll) / outs * ((n + 16ll * t - 1) / (16 * t))}; };
+  if (n <= 64 || blocks(128, 64) < 128) {
+    const int t = n <= 16 ? 1 : n <= 32 || (gated && to8) ? 2 : 4;
+    if (gated && to8) return few(4, t);
+    return few(gated || to8 || t > 1 || rows > 16 * 512 ? 2 : 1, t);
+  }
+  if (!exact8 && blocks(256, 256) >= 256) return {1, blocks(256, 256)};
+  if (blocks(128, 128) >= 256) return {2, blocks(128, 128)};
+  return {3, blocks(128, 64)};
+}
+
+}  // namespace octo

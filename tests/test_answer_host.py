@@ -118,3 +118,39 @@ def test_mx8_load_refuses():
 
 def test_layouts_of_the_packed_calls():
     assert binding._NORM.size == C.sizeof(binding.OctoNormOp) and binding._MX8.size == C.sizeof(binding.OctoMx8Op)
+
+
+def _product_op(**changes):
+    op = binding.OctoProductOp()
+    op.dtype, op.x_format, op.y_format, op.n, op.k, op.cols = 2, 0, 0, 4, 64, 96
+    op.d_x, op.d_w, op.x_row, op.w_row, op.d_y, op.y_row, op.res_row = 4096, 8192, 64, 64, 65536, 96, 96
+    for rows, at in ((op.x8, 1), (op.w8, 2), (op.y8, 3)):
+        rows.d_codes, rows.d_exps, rows.code_row, rows.exp_row = at << 20, (at << 20) + 65536, 96, 3
+    for name, v in changes.items():
+        part = op
+        for p in name.split("__")[:-1]:
+            part = getattr(part, p)
+        setattr(part, name.split("__")[-1], v)
+    kid = C.c_int32(7)
+    st = binding.lib().octo_op_product(C.byref(op), None, C.byref(kid))
+    assert kid.value == 0
+    return st
+
+
+def test_product_refuses():
+    assert binding.lib().octo_op_product(None, None, None) == binding.EINVAL
+    assert _product_op(n=0) == binding.OK and _product_op(n=0, x_format=1, y_format=1) == binding.OK and _product_op(n=0, gated=1, act=3, d_res=512) == binding.OK
+    for bad in (dict(dtype=3), dict(dtype=-1), dict(x_format=2), dict(y_format=-1), dict(n=-1), dict(k=0), dict(cols=0), dict(cols=0x20000001), dict(act=4), dict(act=-1), dict(d_x=None), dict(d_w=None),
+                dict(d_x=4104), dict(d_w=8200), dict(k=60), dict(k=2147483640), dict(x_row=60), dict(w_row=-8), dict(x_row=(8 << 20) // 2 + 8), dict(w_row=1 << 60), dict(d_y=None), dict(d_y=65537), dict(y_row=-1),
+                dict(d_res=1), dict(d_res=512, res_row=-1), dict(d_bias=2), dict(d_n=2), dict(out_f32=1, d_y=65538)):
+        assert _product_op(**bad) == binding.EINVAL, bad
+    for bad in (dict(k=48), dict(x8__d_codes=None), dict(w8__d_exps=None), dict(x8__d_codes=8), dict(w8__code_row=72), dict(x8__code_row=-96), dict(w8__exp_row=-1), dict(x8__code_row=(8 << 20) + 16),
+                dict(x8__exp_row=1 << 40)):
+        assert _product_op(x_format=1, **bad) == binding.EINVAL, bad
+    for bad in (dict(cols=100), dict(out_f32=1), dict(d_res=512), dict(y8__d_codes=None), dict(y8__code_row=100), dict(y8__exp_row=-1)):
+        assert _product_op(y_format=1, **bad) == binding.EINVAL, bad
+    assert _product_op(n=0x7FFFFFFF, cols=0x20000000) == binding.EINVAL       # more blocks than a launch takes
+
+
+def test_layout_of_the_packed_product():
+    assert binding._PRODUCT.size == C.sizeof(binding.OctoProductOp)
