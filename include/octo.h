@@ -743,6 +743,27 @@ typedef struct octo_product_op {
 } octo_product_op;
 octo_status octo_op_product(const octo_product_op* op, void* hip_stream, int32_t* kernel_id);
 
+/* One token of each row of logits, by a given random number.  In the order of descending logits, equal ones by ascending index, with w = exp((logit - largest) / temperature):
+ *   top_k > 0 keeps the first top_k tokens; top_p < 1 the shortest beginning of what that left whose weights reach top_p of all of its (at least one); min_p > 0 those with w >= min_p
+ *   (and the first).  What all three keep is drawn from in the order of indices: the first token at which the sum of kept weights exceeds u times all of them.
+ * temperature <= 0 (or NaN): the first in order.  -infinity and NaN are tokens that may not be drawn; +infinity is the only one drawn where it occurs.  A row without any token: d_token -1, d_kept
+ * 0, d_logprob -infinity.  A NaN among top_p and min_p keeps all; u is taken as 0 .. 1 - 2^-24.
+ * Weights are computed in 64 bits and added up as integers, multiples of 2^-(62 - log2 vocab) (2^-50 at most) of the largest: same inputs, same token, on any device.
+ * d_logits: rows of `dtype` (OCTO_F32, _F16, _BF16), `row` elements apart, at any address of an element, vocab up to OCTO_MAX_VOCAB.  d_u: fp32 [n], in [0, 1).  d_temperature,
+ * d_top_k, d_top_p, d_min_p: one for each row, on the device, or NULL: the number beside it for all.  d_token: int32 [n]; d_logprob: NULL or fp32 [n], the logarithm of the token's share
+ * of the kept weights; d_kept: NULL or int32 [n], how many were kept.  d_n: NULL, or the number of rows present, on the device: later rows are left as they were. */
+#define OCTO_MAX_VOCAB (1 << 19)
+typedef struct octo_sample_op {
+  int32_t dtype, n, vocab, pad_;
+  const void* d_logits; int64_t row;
+  const float* d_u;
+  const float* d_temperature; const int32_t* d_top_k; const float* d_top_p; const float* d_min_p;
+  float temperature; int32_t top_k; float top_p, min_p;
+  int32_t* d_token; float* d_logprob; int32_t* d_kept;
+  const int32_t* d_n;
+} octo_sample_op;
+octo_status octo_op_sample(const octo_sample_op* op, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

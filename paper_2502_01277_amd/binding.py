@@ -194,6 +194,13 @@ class OctoProductOp(C.Structure):
                 ("y8", OctoMx8Rows), ("d_n", C.c_void_p)]
 
 
+class OctoSampleOp(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n", C.c_int32), ("vocab", C.c_int32), ("pad_", C.c_int32), ("d_logits", C.c_void_p), ("row", C.c_int64), ("d_u", C.c_void_p),
+                ("d_temperature", C.c_void_p), ("d_top_k", C.c_void_p), ("d_top_p", C.c_void_p), ("d_min_p", C.c_void_p),
+                ("temperature", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float),
+                ("d_token", C.c_void_p), ("d_logprob", C.c_void_p), ("d_kept", C.c_void_p), ("d_n", C.c_void_p)]
+
+
 # Every symbol include/octo.h declares.
 EXPORTS = [
     "octo_pipeline_workspace_size", "octo_pipeline_create", "octo_pipeline_destroy", "octo_submit_frames", "octo_run",
@@ -209,7 +216,7 @@ EXPORTS = [
     "octo_op_conv", "octo_op_conv_packed_bytes", "octo_op_conv_padded_cout", "octo_op_conv_pack", "octo_quantize_e4m3", "octo_dequantize_e4m3",
     "octo_op_rotate", "octo_op_cache4_store", "octo_op_cache4_load", "octo_quantize_mx4", "octo_dequantize_mx4",
     "octo_op_attend", "octo_op_attend_workspace_bytes",
-    "octo_op_norm", "octo_op_mx8_load", "octo_quantize_mx8", "octo_dequantize_mx8", "octo_op_product",
+    "octo_op_norm", "octo_op_mx8_load", "octo_quantize_mx8", "octo_dequantize_mx8", "octo_op_product", "octo_op_sample",
 ]
 
 _lib = None
@@ -311,6 +318,7 @@ def lib() -> C.CDLL:
         L.octo_op_norm.argtypes = [vp, vp]
         L.octo_op_mx8_load.argtypes = [vp, vp]
         L.octo_op_product.argtypes = [vp, vp, vp]
+        L.octo_op_sample.argtypes = [vp, vp]
         L.octo_quantize_mx8.argtypes = [vp, C.c_size_t, vp, vp]
         L.octo_dequantize_mx8.argtypes = [vp, vp, C.c_size_t, vp]
         _lib = L
@@ -842,7 +850,7 @@ def op_conv(layer: ConvOp, x, y, res=None, res_mode=0, out_f32=False, res_scale=
 
 # ---- tokens behind a cascade ---------------------------------------------------
 # A call's arguments are packed in one go (a dozen microseconds less than field by field, as long as the small kernels take): the
-# layouts of OctoRotateOp, OctoCache4Op, OctoAttendOp, OctoNormOp, OctoMx8Op and OctoProductOp.
+# layouts of OctoRotateOp, OctoCache4Op, OctoAttendOp, OctoNormOp, OctoMx8Op, OctoProductOp and OctoSampleOp.
 _PLANE = "PPqqqq"
 _ROTATE = struct.Struct("@12id2fPP" + "PPPqqqqii" * MAX_ROTATE_PARTS)
 _CACHE4 = struct.Struct("@4iq" + 2 * _PLANE + "PP4qPP")
@@ -851,6 +859,7 @@ _MX8_ROWS = "PPqq"
 _NORM = struct.Struct("@5if4P4q" + _MX8_ROWS + "PP")
 _MX8 = struct.Struct("@4i" + _MX8_ROWS + "PqP")
 _PRODUCT = struct.Struct("@10iPPqq" + 2 * _MX8_ROWS + "PPPqq" + _MX8_ROWS + "P")
+_SAMPLE = struct.Struct("@4iPqP4PfiffPPPP")
 _ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 _NO_MX8, _NO_ROWS = (0,) * 4, (0,) * 8
 _NO_PART, _NO_PLANE, _NO_KV, _NO_SECTIONS = {1: (0,) * 9, 2: ()}, (0,) * 6, (0,) * 6, (0,) * MAX_AXES
@@ -1209,6 +1218,32 @@ def op_product(x, w, y, bias=None, act="none", gated=False, res=None, n=None, st
     if st:
         _st(st)
     return kid.value
+
+
+def op_sample(logits, u, token, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, logprob=None, kept=None, n=None, stream=None):
+    """One token of each row of logits [rows][vocab] by random numbers u fp32 [rows] (octo_sample_op in octo.h), into token int32 [rows].  temperature, top_k, top_p,
+    min_p: a number for all rows, or a device tensor with one for each (fp32, top_k int32); logprob fp32 and kept int32 [rows] or None.  n: int32 device tensor with the
+    number of rows present, or None."""
+    t = _torch()
+    shape, stride = logits.shape, logits.stride()
+    if len(shape) != 2 or not logits.is_cuda or (shape[1] > 1 and stride[1] != 1):
+        _refuse("logits are [rows][vocab] on the device, the words of a row contiguous")
+    rows = shape[0]
+    at, alone = [], []
+    for x, kind, none, what in ((temperature, t.float32, 1.0, "temperature"), (top_k, t.int32, 0, "top_k"), (top_p, t.float32, 1.0, "top_p"), (min_p, t.float32, 0.0, "min_p")):
+        each = isinstance(x, t.Tensor)
+        at.append(_optional(x, kind, "%s is a number or %s [rows] on the device" % (what, kind), rows) if each else 0)
+        alone.append(none if each or x is None else x)
+    if not rows or not shape[1]:
+        return
+    op = _SAMPLE.pack(_CODE[logits.dtype], rows, shape[1], 0, logits.data_ptr(), stride[0], _optional(u, t.float32, "u is fp32 [rows] on the device", rows), *at, *alone,
+                      _optional(token, t.int32, "token is int32 [rows] on the device", rows), 0 if logprob is None else _optional(logprob, t.float32, "logprob is fp32 [rows] on the device", rows),
+                      0 if kept is None else _optional(kept, t.int32, "kept is int32 [rows] on the device", rows), 0 if n is None else _optional(n, t.int32, "n is int32 on the device"))
+    if stream is not None:
+        _order(stream)
+    st = lib().octo_op_sample(op, _stream_ptr(stream))
+    if st:
+        _st(st)
 
 
 def quantize_mx8(x: np.ndarray):

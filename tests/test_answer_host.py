@@ -154,3 +154,24 @@ def test_product_refuses():
 
 def test_layout_of_the_packed_product():
     assert binding._PRODUCT.size == C.sizeof(binding.OctoProductOp)
+
+
+def _sample_op(**changes):
+    op = binding.OctoSampleOp()
+    op.dtype, op.n, op.vocab, op.d_logits, op.row, op.d_u, op.d_token = 2, 4, 100, 4096, 100, 8192, 16384
+    op.temperature, op.top_p = 1.0, 1.0
+    for name, v in changes.items():
+        setattr(op, name, v)
+    return binding.lib().octo_op_sample(C.byref(op), None)
+
+
+def test_sample_refuses():
+    assert binding.lib().octo_op_sample(None, None) == binding.EINVAL
+    assert _sample_op(n=0) == binding.OK and _sample_op(n=0, d_logits=4098, row=0) == binding.OK
+    for bad in (dict(dtype=3), dict(n=-1), dict(n=1 << 22), dict(vocab=0), dict(vocab=(1 << 19) + 1), dict(d_logits=None), dict(d_logits=4097), dict(dtype=0, d_logits=4098), dict(row=-1), dict(d_u=None),
+                dict(d_token=None), dict(d_u=8194), dict(d_token=2), dict(d_temperature=1), dict(d_top_k=2), dict(d_top_p=3), dict(d_min_p=2), dict(d_logprob=1), dict(d_kept=2), dict(d_n=2)):
+        assert _sample_op(**bad) == binding.EINVAL, bad
+
+
+def test_layout_of_the_packed_sample():
+    assert binding._SAMPLE.size == C.sizeof(binding.OctoSampleOp)
