@@ -5,6 +5,9 @@
 // Rows of w and of x are alike: both are read along k, 16 bytes a lane, and go into the matrix instructions as they lie in memory.  w is the first operand, so a lane gets
 // results of neighbouring outputs of one token.
 #pragma once
+#ifndef OCTO_SPREAD
+#define OCTO_SPREAD 1
+#endif
 #include "mx8.h"
 #include "octo_internal.h"
 
@@ -23,7 +26,9 @@ struct ProductArgs {
   const int* n_dyn;
   int n, k_bytes, cols, gated, act, y_kind;
   int y_vec, res_vec, bias_vec;                       // four values at a multiple of four outputs are one aligned vector
+  int vec;                                            // all of them are (or are not there), and outputs are whole vectors, not in 8 bits
   int exp_words;                                      // the exponents of 128 values of k are one aligned word
+  int direct;                                         // results of 16 bits, eight of them one aligned vector, or of 8 bits, activations that take few instructions
   int tiles_n, tiles_m;
 };
 
@@ -100,6 +105,51 @@ __device__ __forceinline__ void product_finish4(const ProductArgs& a, bool on, i
   }
 }
 
+// The same for B pieces of four outputs at once, whose residuals and biases are in flight together.  Only where `a.vec`: all of it in aligned vectors of four.
+template <typename Y, int B>
+__device__ __forceinline__ void product_finish_vec(const ProductArgs& a, const bool* on, const int* i, const int* j, floatx4* z, floatx4* up) {
+  floatx4 res[B];
+  if (a.bias) {
+    floatx4 b0[B], b1[B];
+#pragma unroll
+    for (int b = 0; b < B; ++b) b0[b] = on[b] ? *(const floatx4*)(a.bias + j[b]) : floatx4{0.f, 0.f, 0.f, 0.f};
+    if (a.gated) {
+#pragma unroll
+      for (int b = 0; b < B; ++b) b1[b] = on[b] ? *(const floatx4*)(a.bias + a.cols + j[b]) : floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+#pragma unroll
+    for (int b = 0; b < B; ++b) { z[b] += b0[b]; if (a.gated) up[b] += b1[b]; }
+  }
+  if (a.res) {
+#pragma unroll
+    for (int b = 0; b < B; ++b) if (on[b]) res[b] = load4((const Y*)a.res + i[b] * a.res_row + j[b]);
+  }
+  auto act = [&](auto f) __attribute__((always_inline)) {
+#pragma unroll
+    for (int b = 0; b < B; ++b)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) z[b][e] = f(z[b][e]);
+  };
+  if (a.act == PRODUCT_ACT_SILU) act([](float v) { return silu(v); });
+  else if (a.act == PRODUCT_ACT_RELU) act([](float v) { return fmaxf(v, 0.f); });
+  else if (a.act == PRODUCT_ACT_GELU) act([](float v) { return product_act(PRODUCT_ACT_GELU, v); });
+  if (a.gated) {
+#pragma unroll
+    for (int b = 0; b < B; ++b)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) z[b][e] *= up[b][e];
+  }
+#pragma unroll
+  for (int b = 0; b < B; ++b) {
+    if (!on[b]) continue;
+    if (a.res) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) z[b][e] += res[b][e];
+    }
+    store4((Y*)a.y + i[b] * a.y_row + j[b], z[b]);
+  }
+}
+
 // Two operands of 32 rows and 64 values of k in 8 bits: a lane (row l % 32, half l / 32) gives bytes 16 half .. + 15 of the first and of the second block of 32, and the
 // exponent of block number `half` of its row, byte 2 KK of a word that is shifted by 8 half.
 template <int KK>
@@ -122,11 +172,128 @@ __device__ __forceinline__ void widen_mx8(u32x4 v, unsigned e, u32x4* lo, u32x4*
   }
 }
 
+// A wavefront's sums, blocks of 32 rows of w (of a gated layer: gate, gated, gate ...) times 32 tokens, straight from its registers: a lane has rows 8 q + 4 (l / 32) .. + 3 of
+// token l % 32.  Exchanges between lanes make 16 bytes of neighbouring outputs a lane, 64 bytes a token of every store (swap_rows16).  For results of 16 or 8 bits whose rows are
+// aligned (`a.direct`).
+struct DirectMx8 {};
+template <typename Y, int TN, int TM, bool GATED>
+__device__ __forceinline__ void finish_direct_as(const ProductArgs& a, floatx16 (&acc)[TN][TM], int n, int tok0, int col0, int lane) {
+  constexpr bool TO8 = std::is_same<Y, DirectMx8>::value;
+  constexpr int STEP = GATED ? 2 : 1;
+  typedef typename std::conditional<TO8, __bf16, Y>::type Y16;
+  const int l32 = lane & 31, half = lane >> 5, turned = (lane >> 4 & 1) * 2 + (lane >> 5);      // the chunk of eight outputs that swap_rows16 leaves in a lane
+#pragma unroll
+  for (int i = 0; i < TN; i += STEP) {
+    const int col = col0 + i / STEP * 32;
+    if (col >= a.cols) return;
+    u32x4 res[TM][2];
+    if (!TO8 && a.res) {
+#pragma unroll
+      for (int j = 0; j < TM; ++j)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int tok = tok0 + j * 32 + h * 16 + (lane & 15), c = col + turned * 8;
+          res[j][h] = u32x4{0, 0, 0, 0};
+          if (tok < n && c < a.cols) res[j][h] = *(const u32x4*)((const Y16*)a.res + tok * a.res_row + c);
+        }
+    }
+    floatx4 b0[4], b1[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int c = col + 8 * q + 4 * half;
+      b0[q] = a.bias && c < a.cols ? *(const floatx4*)(a.bias + c) : floatx4{0.f, 0.f, 0.f, 0.f};
+      b1[q] = GATED && a.bias && c < a.cols ? *(const floatx4*)(a.bias + a.cols + c) : floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+      // the sums of the largest tiles fill one half of the registers and are taken out of it block by block, here and not before
+      if constexpr (TN * TM >= 16) {
+        asm volatile("" : "+a"(acc[i][j]));
+        if constexpr (GATED) asm volatile("" : "+a"(acc[i + 1][j]));
+      }
+      floatx4 v[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[q][e] = acc[i][j][4 * q + e] + b0[q][e];
+      auto each = [&](auto f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[q][e] = f(v[q][e]);
+      };
+      if (a.act == PRODUCT_ACT_SILU) each([](float z) { return silu(z); });
+      else if (a.act == PRODUCT_ACT_RELU) each([](float z) { return fmaxf(z, 0.f); });
+      if constexpr (GATED) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[q][e] *= acc[i + 1][j][4 * q + e] + b1[q][e];
+      }
+      if constexpr (TO8) {
+        unsigned most = 0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) most = max(most, __float_as_uint(v[q][e]) & 0x7FFFFFFFu);
+        most = max(most, (unsigned)__shfl_xor((int)most, 32));
+        const bool none = most >= 0x7F800000u;
+        const int ex = mx8_exp(most);
+        const float inverse = mx8_inverse(ex);
+        unsigned w[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) w[q] = none ? MX8_NAN4 : mx8_pack4(v[q], inverse);
+        const auto s0 = __builtin_amdgcn_permlane32_swap(w[0], w[1], false, false), s1 = __builtin_amdgcn_permlane32_swap(w[2], w[3], false, false);
+        const int tok = tok0 + j * 32 + l32;
+        if (tok < n) {
+          uint8_t* const y = a.y8.d_codes + tok * a.y8.code_row + col + 8 * half;
+          *(u32x2*)y = u32x2{s0[0], s0[1]};
+          *(u32x2*)(y + 16) = u32x2{s1[0], s1[1]};
+          if (!half) a.y8.d_exps[tok * a.y8.exp_row + col / 32] = (uint8_t)(none ? 255 : ex);
+        }
+      } else {
+        if (a.res) {
+          swap_rows16(res[j][0], res[j][1]);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const auto s0 = __builtin_amdgcn_permlane32_swap(res[j][h][0], res[j][h][2], false, false), s1 = __builtin_amdgcn_permlane32_swap(res[j][h][1], res[j][h][3], false, false);
+            const u32x2 x = {s0[0], s1[0]}, z = {s0[1], s1[1]};
+            const floatx4 rx = load4((const Y16*)&x), rz = load4((const Y16*)&z);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { v[2 * h][e] += rx[e]; v[2 * h + 1][e] += rz[e]; }
+          }
+        }
+        u32x4 o[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          u32x2 x, z;
+          store4<Y16>((Y16*)&x, v[2 * h]);
+          store4<Y16>((Y16*)&z, v[2 * h + 1]);
+          const auto s0 = __builtin_amdgcn_permlane32_swap(x[0], z[0], false, false), s1 = __builtin_amdgcn_permlane32_swap(x[1], z[1], false, false);
+          o[h] = u32x4{s0[0], s1[0], s0[1], s1[1]};
+        }
+        swap_rows16(o[0], o[1]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int tok = tok0 + j * 32 + h * 16 + (lane & 15), c = col + turned * 8;
+          if (tok < n && c < a.cols) *(u32x4*)((Y16*)a.y + tok * a.y_row + c) = o[h];
+        }
+      }
+    }
+  }
+}
+template <typename Y, int TN, int TM>
+__device__ __forceinline__ void finish_direct(const ProductArgs& a, floatx16 (&acc)[TN][TM], int n, int tok0, int col0, int lane) {
+  if (a.gated) finish_direct_as<Y, TN, TM, true>(a, acc, n, tok0, col0, lane);
+  else finish_direct_as<Y, TN, TM, false>(a, acc, n, tok0, col0, lane);
+}
+
 // ---- many tokens: tiles in LDS -----------------------------------------------------------------------------------------
 // A block makes BN rows of w times BM tokens; its WN x WM wavefronts take TN x TM blocks of 32 x 32 each.  A step covers 128 bytes of k of all rows.  Loads go straight
 // to LDS, two steps deep: once all wavefronts have read their last operands of step t, its place is given to step t + 2, whose loads then have a whole step's products to
 // arrive in.  Operands of the next products are read from LDS while the present ones run, also across steps, so a step costs one barrier in the middle of
-// products.  The 16-byte chunks of a row lie at their number xor the row's, which spreads the rows that eight lanes read together over all banks.
+// products.  The 16-byte chunks of a row lie at their number xor half
+// the row's, which spreads the rows that sixteen lanes read together over all banks.
 //
 // Rows of 8 bits: the 8-bit matrix instructions add products in groups of eight at the weight of the group's largest and drop what lies 2^13 below it (measured: 1 + 2^-13 comes
 // out, 1 + 2^-14 does not), 2^-14 of a sum's size in the mean.  Results that are rounded to 16 or 8 bits can bear that; for fp32 results (EXACT) the values are widened to bf16,
@@ -136,6 +303,8 @@ __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(Produc
   constexpr bool MX = std::is_same<T, f8>::value;
   constexpr int NW = WN * WM, BN = WN * TN * 32, BM = WM * TM * 32, ROWS = BN + BM, STAGE = ROWS * 128, LW = BN / 8 / NW, LX = BM / 8 / NW;
   constexpr int KQ = MX ? 2 : 4, FV = MX ? 2 : 1;                    // products of k within a step, 16-byte vectors of an operand
+  constexpr int L = LW + LX, R = (TN + TM) * FV, M = TN * TM;        // loads of a step, reads and products of a part of one
+  constexpr int SPREAD = MX ? 1 : OCTO_SPREAD, L0 = MX && EXACT ? L : L / (SPREAD + 1);     // parts of the next step that loads are issued in, loads behind the barrier
   constexpr int HT = TM < 2 ? 1 : 2, UNIT = HT * 32 * TN * 32 * 4;    // sums of a wavefront on their way out, of 32 or 64 tokens
   constexpr int MAIN = 2 * STAGE + (MX ? 4 * ROWS * 4 : 0), LDS = MAIN > NW * UNIT ? MAIN : NW * UNIT;
   static_assert(BN / 8 % NW == 0 && BM / 8 % NW == 0 && TN % 2 == 0 && NW % 4 == 0, "whole loads a wavefront, pairs of blocks");
@@ -157,89 +326,98 @@ __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(Produc
   if (m0 >= n) return;
 
   const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(LdsBytes*)smem);
-  const int chunk = (lane & 7) ^ (lane >> 3);
+  // Load q of a wavefront brings rows 8 (LW wave + q) .. + 7 of the tile (of x: LX wave + ..), 1024 bytes behind load q - 1.  The places in LDS of four loads differ by the instructions' offset
+  // alone, which is taken off the addresses again: each write of m0 holds the wavefront up for some twenty cycles (16 a step: 2460 cycles for 2048 of products).
+  const int row8 = lane >> 3;
   int woff[LW], xoff[LX];
 #pragma unroll
   for (int i = 0; i < LW; ++i) {
-    const int row = (i * NW + wave) * 8 + (lane >> 3);
+    const int row = (wave * LW + i) * 8 + row8, chunk = (lane & 7) ^ (row >> 1 & 7);
     const int col = a.gated ? row / 64 * 32 + row % 32 : row;
-    woff[i] = n0 + col < a.cols ? col * (int)a.w_row + chunk * 16 : OOB;
+    woff[i] = n0 + col < a.cols ? col * (int)a.w_row + chunk * 16 + 4096 - i % 4 * 1024 : OOB;
   }
 #pragma unroll
   for (int i = 0; i < LX; ++i) {
-    const int row = (i * NW + wave) * 8 + (lane >> 3);
-    xoff[i] = m0 + row < n ? row * (int)a.x_row + chunk * 16 : OOB;
+    const int row = (wave * LX + i) * 8 + row8, chunk = (lane & 7) ^ (row >> 1 & 7);
+    xoff[i] = m0 + row < n ? row * (int)a.x_row + chunk * 16 + 4096 - i % 4 * 1024 : OOB;
   }
   const char* const w0 = a.w + n0 * a.w_row;
   const char* const w1 = w0 + (a.gated ? a.cols * a.w_row : 0);
   const char* const x0 = a.x + m0 * a.x_row;
   const int nk = (a.k_bytes + 127) / 128;
 
-  // exponents: a thread takes row threadIdx.x, and those NW * 64 further on
+  // Exponents, a word for each row and step, four steps deep: a thread has row threadIdx.x and those NW * 64 further on.  Whole words go straight to LDS.  Otherwise bytes are
+  // taken one by one to registers, since what lies behind a row's end may read as NaN, and placed a step later.
   constexpr int NE = MX ? (ROWS + NW * 64 - 1) / (NW * 64) : 1;
+  const uint8_t* exp_at[NE];
   unsigned exps[NE];
-  auto exp_row = [&](int r, bool* there) -> const uint8_t* {
-    if (r < BN) {
-      const int col = a.gated ? r / 64 * 32 + r % 32 : r;
-      *there = n0 + col < a.cols;
-      return a.we + ((a.gated && r / 32 % 2 ? a.cols : 0) + n0 + col) * a.we_row;
+  if constexpr (MX) {
+#pragma unroll
+    for (int i = 0; i < NE; ++i) {
+      const int r = i * NW * 64 + (int)threadIdx.x;
+      const int col = min(n0 + (a.gated ? r / 64 * 32 + r % 32 : r), a.cols - 1), tok = min(m0 + max(r - BN, 0), n - 1);      // of a row that is not there: any row's
+      exp_at[i] = r < BN ? a.we + ((a.gated && r / 32 % 2 ? (long long)a.cols : 0) + col) * a.we_row : a.xe + tok * a.xe_row;
     }
-    *there = r < ROWS && m0 + r - BN < n;
-    return a.xe + (m0 + r - BN) * a.xe_row;
-  };
-  auto load_exps = [&](int t) __attribute__((always_inline)) {
+  }
+  auto load_exps = [&](int t) __attribute__((always_inline)) {       // bytes
     if constexpr (MX) {
+      if (!a.exp_words) {
 #pragma unroll
-      for (int i = 0; i < NE; ++i) {
-        bool there;
-        const uint8_t* p = exp_row(i * NW * 64 + (int)threadIdx.x, &there) + 4 * t;
-        exps[i] = 0;
-        if (!there || t >= nk) continue;
-        if (a.exp_words) { exps[i] = *(const unsigned*)p; continue; }
+        for (int i = 0; i < NE; ++i) {
+          exps[i] = 0;
 #pragma unroll
-        for (int b = 0; b < 4; ++b) if (t * 128 + b * 32 < a.k_bytes) exps[i] |= (unsigned)p[b] << (8 * b);
+          for (int b = 0; b < 4; ++b) if (t * 128 + b * 32 < a.k_bytes) exps[i] |= (unsigned)exp_at[i][4 * t + b] << (8 * b);
+        }
       }
     }
   };
   auto place_exps = [&](int t) __attribute__((always_inline)) {
     if constexpr (MX) {
+      if (!a.exp_words) {
 #pragma unroll
-      for (int i = 0; i < NE; ++i) {
-        const int r = i * NW * 64 + (int)threadIdx.x;
-        if (r < ROWS) *(unsigned*)(smem + 2 * STAGE + ((t & 3) * ROWS + r) * 4) = exps[i];
+        for (int i = 0; i < NE; ++i) {
+          const int r = i * NW * 64 + (int)threadIdx.x;
+          if (r < ROWS) *(unsigned*)(smem + 2 * STAGE + ((t & 3) * ROWS + r) * 4) = exps[i];
+        }
       }
     }
   };
-  auto issue = [&](int t) __attribute__((always_inline)) {
-    const int beyond = chunk * 16 + t * 128 >= a.k_bytes ? OOB : 0;   // the end of a row inside a step
-    const unsigned to = lds + (t & 1) * STAGE + wave * 1024;
-    const __amdgpu_buffer_rsrc_t rw0 = __builtin_amdgcn_make_buffer_rsrc((void*)(w0 + t * 128), 0, 0x7FFFFFFF, BUF_FLAGS);
-    const __amdgpu_buffer_rsrc_t rw1 = __builtin_amdgcn_make_buffer_rsrc((void*)(w1 + t * 128), 0, 0x7FFFFFFF, BUF_FLAGS);
-    const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc((void*)(x0 + t * 128), 0, 0x7FFFFFFF, BUF_FLAGS);
+  auto issue_exps = [&](int t) __attribute__((always_inline)) {      // words
+    if constexpr (MX) {
+      if (a.exp_words) {
 #pragma unroll
-    for (int i = 0; i < LW; ++i) {
-      // blocks of 32 rows alternate between the two halves of a gated layer: rows i NW 8 + 8 wave ..
-      const bool second = NW == 4 ? i & 1 : (wave >> 2) & 1;
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(to + i * NW * 1024), "v"(woff[i] | beyond), "s"(second ? rw1 : rw0) : "memory");
+        for (int i = 0; i < NE; ++i)
+          if ((i * NW + wave) * 64 < ROWS)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
+                         :: "s"(lds + 2 * STAGE + ((t & 3) * ROWS + (i * NW + wave) * 64) * 4), "v"(exp_at[i] + 4 * min(t, nk - 1)) : "memory");
+      }
     }
-#pragma unroll
-    for (int i = 0; i < LX; ++i)
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(to + BN * 128 + i * NW * 1024), "v"(xoff[i] | beyond), "s"(rx) : "memory");
+  };
+  // load q of step t: LW of w, then LX of x.  Addresses are 4096 too large, for the offsets, and buffers start as much earlier.
+  auto issue = [&](int t, int q, auto whole) __attribute__((always_inline)) {
+    const bool is_w = q < LW;
+    const int i = is_w ? q : q - LW, off = is_w ? woff[is_w ? i : 0] : xoff[is_w ? 0 : i];
+    const int part = (lane & 7) ^ (((is_w ? wave * LW : wave * LX) + i) * 4 + (lane >> 4) & 7);          // the lane's chunk
+    const int beyond = !whole() && part * 16 + t * 128 >= a.k_bytes ? OOB : 0;         // the end of a row inside a step, and steps beyond the last
+    // rows of a gated layer alternate between its halves, 32 at a time
+    const bool second = is_w && ((LW % 8 == 0 ? i / 4 : (wave * LW + i) / 4) & 1);
+    const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc((void*)((is_w ? second ? w1 : w0 : x0) + t * 128 - 4096), 0, 0x7FFFFFFF, BUF_FLAGS);
+    const unsigned to = lds + (t & 1) * STAGE + (is_w ? wave * LW * 1024 : BN * 128 + wave * LX * 1024) + i / 4 * 4096;
+    if (i % 4 == 0) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(to), "v"(off | beyond), "s"(rc) : "memory");
+    else if (i % 4 == 1) asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:1024 lds" :: "v"(off | beyond), "s"(rc) : "memory");
+    else if (i % 4 == 2) asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:2048 lds" :: "v"(off | beyond), "s"(rc) : "memory");
+    else asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:3072 lds" :: "v"(off | beyond), "s"(rc) : "memory");
   };
 
   u32x4 fw[2][TN][FV], fx[2][TM][FV];
   int ew[2][TN], ex[2][TM];
   const int wrow = (wn * TN * 32 + l32) * 128, xrow = (BN + wm * TM * 32 + l32) * 128;
-  auto frags = [&](int set, int t, int kq) __attribute__((always_inline)) {
+  // read r of an operand set, in the order in which the products want them: the first row of w, all of x, the other rows of w
+  auto frag = [&](int set, int t, int kq, int r) __attribute__((always_inline)) {
     const unsigned char* const p = smem + (t & 1) * STAGE;
-#pragma unroll
-    for (int h = 0; h < FV; ++h) {
-      const int c = ((MX ? 4 * kq + 2 * h + half : 2 * kq + half) ^ (lane & 7)) * 16;
-#pragma unroll
-      for (int i = 0; i < TN; ++i) fw[set][i][h] = *(const u32x4*)(p + wrow + i * 4096 + c);
-#pragma unroll
-      for (int j = 0; j < TM; ++j) fx[set][j][h] = *(const u32x4*)(p + xrow + j * 4096 + c);
-    }
+    const int o = r / FV, h = r % FV, c = ((MX ? 4 * kq + 2 * h + half : 2 * kq + half) ^ (lane >> 1 & 7)) * 16;
+    if (o >= 1 && o <= TM) fx[set][o - 1][h] = *(const u32x4*)(p + xrow + (o - 1) * 4096 + c);
+    else fw[set][o ? o - TM : 0][h] = *(const u32x4*)(p + wrow + (o ? o - TM : 0) * 4096 + c);
   };
   auto scales = [&](int set, int t) __attribute__((always_inline)) {
     if constexpr (MX) {
@@ -261,29 +439,31 @@ __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(Produc
 
   load_exps(0); place_exps(0);
   load_exps(1); place_exps(1);
-  issue(0);
-  issue(1);
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(LW + LX) : "memory");
+  issue_exps(0);
+  issue_exps(1);
+#pragma unroll
+  for (int q = 0; q < L; ++q) issue(0, q, std::false_type{});
+#pragma unroll
+  for (int q = 0; q < L0; ++q) issue(1, q, std::false_type{});
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(L0) : "memory");
   __builtin_amdgcn_s_barrier();
   load_exps(2);
-  frags(0, 0, 0);
+#pragma unroll
+  for (int r = 0; r < R; ++r) frag(0, 0, 0, r);
   scales(0, 0);
 
-  // Loads and reads beyond the last step are of nothing (zeros go to LDS): the loop has no branches.
-#pragma nounroll
-  for (int t = 0; t < nk; ++t) {
+  // Loads and reads beyond the last step are of nothing (zeros go to LDS): the loop has no branches.  While the steps that are loaded are whole ones, addresses take no arithmetic.  Reads and loads stand between the products, in the order below: a product
+  // keeps the matrix unit busy for 32 cycles or more, in which the wavefront issues what lies behind it.
+  auto step = [&](int t, auto whole) __attribute__((always_inline)) {
 #pragma unroll
     for (int kq = 0; kq < KQ; ++kq) {
       const int cur = kq & 1;
-      if (kq < KQ - 1) {
-        frags(cur ^ 1, t, kq + 1);
-      } else {
+      if (kq == KQ - 1) {
         place_exps(t + 2);
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
-        issue(t + 2);
         load_exps(t + 3);
-        frags(cur ^ 1, t + 1, 0);
+        issue_exps(t + 2);
         scales(1, t + 1);
       }
       if constexpr (MX && EXACT) {
@@ -299,18 +479,32 @@ __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(Produc
 #pragma unroll
             for (int j = 0; j < TM; ++j) acc[i][j] = Elem<__bf16>::mfma(w[i][1], x[j][1], Elem<__bf16>::mfma(w[i][0], x[j][0], acc[i][j]));
         }
+#pragma unroll
+        for (int r = 0; r < R; ++r) frag(cur ^ 1, kq == KQ - 1 ? t + 1 : t, kq == KQ - 1 ? 0 : kq + 1, r);
+        if (kq == KQ - 1) {
+#pragma unroll
+          for (int q = 0; q < L; ++q) issue(t + 2, q, whole);
+        }
       } else {
 #pragma unroll
-        for (int i = 0; i < TN; ++i)
-#pragma unroll
-          for (int j = 0; j < TM; ++j) {
-            if constexpr (MX) {
-              if (kq == 0) acc[i][j] = mfma_mx8<0>(fw[cur][i][0], fw[cur][i][1], fx[cur][j][0], fx[cur][j][1], acc[i][j], ew[0][i], ex[0][j]);
-              else acc[i][j] = mfma_mx8<1>(fw[cur][i][0], fw[cur][i][1], fx[cur][j][0], fx[cur][j][1], acc[i][j], ew[0][i], ex[0][j]);
-            } else {
-              acc[i][j] = Elem<T>::mfma(fw[cur][i][0], fx[cur][j][0], acc[i][j]);
-            }
+        for (int m = 0; m < M; ++m) {
+          const int i = m / TM, j = m % TM;
+          if constexpr (MX) {
+            if (kq == 0) acc[i][j] = mfma_mx8<0>(fw[cur][i][0], fw[cur][i][1], fx[cur][j][0], fx[cur][j][1], acc[i][j], ew[0][i], ex[0][j]);
+            else acc[i][j] = mfma_mx8<1>(fw[cur][i][0], fw[cur][i][1], fx[cur][j][0], fx[cur][j][1], acc[i][j], ew[0][i], ex[0][j]);
+          } else {
+            acc[i][j] = Elem<T>::mfma(fw[cur][i][0], fx[cur][j][0], acc[i][j]);
           }
+#pragma unroll
+          for (int r = 0; r < R; ++r) if (r * M / R == m) frag(cur ^ 1, kq == KQ - 1 ? t + 1 : t, kq == KQ - 1 ? 0 : kq + 1, r);
+          // the loads of step t + 2 behind the barrier and in the next step, all but its last parts
+#pragma unroll
+          for (int q = 0; q < L; ++q) {
+            if (kq == KQ - 1 && q < L0 && (M - 1 ? q * M / L0 | 1 : 0) == m) issue(t + 2, q, whole);
+            if (kq < SPREAD && q >= L0 && (M - 1 ? (q - L0) * SPREAD * M / (L - L0) | 1 : 0) == kq * M + m) issue(t + 1, q, whole);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
     }
     if constexpr (MX) {
@@ -319,14 +513,26 @@ __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(Produc
 #pragma unroll
       for (int j = 0; j < TM; ++j) ex[0][j] = ex[1][j];
     }
-  }
+  };
+  int t = 0;
+#pragma nounroll
+  for (; t + 2 < a.k_bytes / 128; ++t) step(t, std::true_type{});
+#pragma nounroll
+  for (; t < nk; ++t) step(t, std::false_type{});
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 
+  if (a.direct) {
+    const int col0 = n0 + (a.gated ? wn * TN * 16 : wn * TN * 32), tok0 = m0 + wm * TM * 32;
+    if (a.y_kind == PRODUCT_Y_MX8) finish_direct<DirectMx8, TN, TM>(a, acc, n, tok0, col0, lane);
+    else if (a.y_kind == PRODUCT_Y_F16) { if constexpr (!std::is_same<T, __bf16>::value && sizeof(T) < 4) finish_direct<_Float16, TN, TM>(a, acc, n, tok0, col0, lane); }
+    else if constexpr (!std::is_same<T, _Float16>::value && sizeof(T) < 4) finish_direct<__bf16, TN, TM>(a, acc, n, tok0, col0, lane);
+    return;
+  }
   // Sums leave through LDS, up to 64 tokens of a wavefront at a time, in a place of its own: lanes then hold four neighbouring outputs of a token.  Chunks of four lie at their
-  // number xor the token's, as above.
+  // number xor the token's.
   __syncthreads();
   float* const out = (float*)(smem + wave * UNIT);
-  const int lpt = a.gated ? TN * 4 : TN * 8;                         // lanes of a token
+  const int lpt_log2 = (TN == 4 ? 5 : 4) - a.gated, lpt = 1 << lpt_log2;      // lanes of a token
 #pragma unroll
   for (int h = 0; h < TM; h += HT) {
 #pragma unroll
@@ -336,19 +542,44 @@ __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(Produc
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const floatx16& c = acc[i][h + j];
-          *(floatx4*)(out + ((j * 32 + l32) * TN * 8 + ((8 * i + 2 * q + half) ^ (lane & 7))) * 4) = floatx4{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
+          *(floatx4*)(out + ((j * 32 + l32) * TN * 8 + ((8 * i + 2 * q + half) ^ (lane & 15))) * 4) = floatx4{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
         }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     const int token0 = m0 + (wm * TM + h) * 32;
-#pragma nounroll
-    for (int p = lane; p < HT * 32 * lpt; p += 64) {
-      const int tok = p / lpt, o4 = p % lpt;                         // both powers of two
+    auto piece = [&](int p, bool* on, int* i, int* j, floatx4* z, floatx4* up) __attribute__((always_inline)) {
+      const int tok = p >> lpt_log2, o4 = p & (lpt - 1);
       const int c4 = a.gated ? o4 / 8 * 16 + o4 % 8 : o4;            // the chunk of its sums; those it is a gate of lie eight further on
       const float* const row = out + tok * TN * 32;
-      const floatx4 z = *(const floatx4*)(row + (c4 ^ (tok & 7)) * 4), up = *(const floatx4*)(row + ((a.gated ? c4 + 8 : c4) ^ (tok & 7)) * 4);
-      product_finish4(a, token0 + tok < n, token0 + tok, n0 + wn * (lpt * 4) + o4 * 4, z, up);
+      *z = *(const floatx4*)(row + (c4 ^ (tok & 15)) * 4);
+      *up = a.gated ? *(const floatx4*)(row + ((c4 + 8) ^ (tok & 15)) * 4) : *z;
+      *i = token0 + tok; *j = n0 + wn * (lpt * 4) + o4 * 4; *on = *i < n && *j < a.cols;
+    };
+    constexpr int B = 4;
+    static_assert(HT * 32 * TN * 4 % (64 * B) == 0, "whole batches");
+    auto batches = [&](auto y) __attribute__((always_inline)) {
+#pragma nounroll
+      for (int p0 = lane; p0 < HT * 32 * lpt; p0 += 64 * B) {
+        bool on[B]; int i[B], j[B]; floatx4 z[B], up[B];
+#pragma unroll
+        for (int b = 0; b < B; ++b) piece(p0 + 64 * b, &on[b], &i[b], &j[b], &z[b], &up[b]);
+        product_finish_vec<decltype(y), B>(a, on, i, j, z, up);
+      }
+    };
+    if (!a.vec) {
+#pragma nounroll
+      for (int p = lane; p < HT * 32 * lpt; p += 64) {
+        bool on; int i, j; floatx4 z, up;
+        piece(p, &on, &i, &j, &z, &up);
+        product_finish4(a, i < n, i, j, z, up);
+      }
+    } else if (a.y_kind == PRODUCT_Y_F32) {
+      batches(float{});
+    } else if (a.y_kind == PRODUCT_Y_F16) {
+      batches(_Float16{});
+    } else {
+      batches(__bf16{});
     }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
