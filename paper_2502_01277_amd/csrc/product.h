@@ -5,9 +5,8 @@
 // Rows of w and of x are alike: both are read along k, 16 bytes a lane, and go into the matrix instructions as they lie in memory.  w is the first operand, so a lane gets
 // results of neighbouring outputs of one token.
 #pragma once
-#ifndef OCTO_SPREAD
-#define OCTO_SPREAD 1
-#endif
+#include <utility>
+
 #include "mx8.h"
 #include "octo_internal.h"
 
@@ -28,6 +27,7 @@ struct ProductArgs {
   int y_vec, res_vec, bias_vec;                       // four values at a multiple of four outputs are one aligned vector
   int vec;                                            // all of them are (or are not there), and outputs are whole vectors, not in 8 bits
   int exp_words;                                      // the exponents of 128 values of k are one aligned word
+  int exact8;                                         // rows of 8 bits go through bf16 also where tokens are many
   int direct;                                         // results of 16 bits, eight of them one aligned vector, or of 8 bits, activations that take few instructions
   int tiles_n, tiles_m;
 };
@@ -150,13 +150,24 @@ __device__ __forceinline__ void product_finish_vec(const ProductArgs& a, const b
   }
 }
 
-// Two operands of 32 rows and 64 values of k in 8 bits: a lane (row l % 32, half l / 32) gives bytes 16 half .. + 15 of the first and of the second block of 32, and the
-// exponent of block number `half` of its row, byte 2 KK of a word that is shifted by 8 half.
-template <int KK>
-__device__ __forceinline__ floatx16 mfma_mx8(u32x4 a0, u32x4 a1, u32x4 b0, u32x4 b1, floatx16 c, int ea, int eb) {
-  const i32x8 a = {(int)a0[0], (int)a0[1], (int)a0[2], (int)a0[3], (int)a1[0], (int)a1[1], (int)a1[2], (int)a1[3]};
-  const i32x8 b = {(int)b0[0], (int)b0[1], (int)b0[2], (int)b0[3], (int)b1[0], (int)b1[1], (int)b1[2], (int)b1[3]};
-  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 2 * KK, ea, 2 * KK, eb);
+// Products of 16 x 16 blocks: a lane (row l % 16, part g = l / 16) gives 16 bytes of its row of each operand and gets rows 4 g .. + 3 of column l % 16.  Under the power limit these run 14 % (8
+// bits: 8 %) faster than 32 x 32 blocks (bf16 registers alone 2113 TFLOP/s and 1849, 8 bits 4428 and 4096).
+template <typename T>
+__device__ __forceinline__ floatx4 mfma_part(u32x4 a, u32x4 b, floatx4 c) {
+  if constexpr (sizeof(T) == 4) {
+    const floatx4 w = __builtin_bit_cast(floatx4, a), x = __builtin_bit_cast(floatx4, b);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(w[e], x[e], c, 0, 0, 0);
+    return c;
+  } else {
+    return mfma16<T>(a, b, c);
+  }
+}
+// In 8 bits, 128 values of k: bytes 16 g .. + 15 of both halves, and the exponent of block g of its row.
+__device__ __forceinline__ floatx4 mfma_mx8(const u32x4* a, const u32x4* b, floatx4 c, int ea, int eb) {
+  typedef uint32_t u32x8 __attribute__((ext_vector_type(8)));
+  const u32x8 x = __builtin_shufflevector(a[0], a[1], 0, 1, 2, 3, 4, 5, 6, 7), y = __builtin_shufflevector(b[0], b[1], 0, 1, 2, 3, 4, 5, 6, 7);
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(__builtin_bit_cast(i32x8, x), __builtin_bit_cast(i32x8, y), c, 0, 0, 0, ea, 0, eb);
 }
 
 // Sixteen values of 8 bits in bf16, which holds them and their power of two exactly; `e`: their exponent byte.
@@ -172,121 +183,108 @@ __device__ __forceinline__ void widen_mx8(u32x4 v, unsigned e, u32x4* lo, u32x4*
   }
 }
 
-// A wavefront's sums, blocks of 32 rows of w (of a gated layer: gate, gated, gate ...) times 32 tokens, straight from its registers: a lane has rows 8 q + 4 (l / 32) .. + 3 of
-// token l % 32.  Exchanges between lanes make 16 bytes of neighbouring outputs a lane, 64 bytes a token of every store (swap_rows16).  For results of 16 or 8 bits whose rows are
-// aligned (`a.direct`).
+// A wavefront's sums, 2 TN x 2 TM blocks of 16 rows of w times 16 tokens (of a gated layer: two of gates, two of what they are gates of, ...), straight from its registers.  An
+// exchange between rows of 16 lanes makes 16 bytes of neighbouring outputs a lane, 64 bytes a token of every store: the lane's chunk of eight outputs is then {0, 2, 1, 3}[g].  For
+// results of 16 or 8 bits whose rows are aligned (`a.direct`).
 struct DirectMx8 {};
 template <typename Y, int TN, int TM, bool GATED>
-__device__ __forceinline__ void finish_direct_as(const ProductArgs& a, floatx16 (&acc)[TN][TM], int n, int tok0, int col0, int lane) {
+__device__ __forceinline__ void finish_direct_as(const ProductArgs& a, floatx4 (&acc)[2 * TN][2 * TM], int n, int tok0, int col0, int lane) {
   constexpr bool TO8 = std::is_same<Y, DirectMx8>::value;
-  constexpr int STEP = GATED ? 2 : 1;
+  constexpr int STEP = GATED ? 4 : 2;
   typedef typename std::conditional<TO8, __bf16, Y>::type Y16;
-  const int l32 = lane & 31, half = lane >> 5, turned = (lane >> 4 & 1) * 2 + (lane >> 5);      // the chunk of eight outputs that swap_rows16 leaves in a lane
+  const int g = lane >> 4, turned = (g & 1) * 2 + (g >> 1);
+  auto swap = [](u32x2& x, u32x2& z) __attribute__((always_inline)) {          // its own inverse
 #pragma unroll
-  for (int i = 0; i < TN; i += STEP) {
+    for (int e = 0; e < 2; ++e) {
+      const auto r = __builtin_amdgcn_permlane16_swap(x[e], z[e], false, false);
+      x[e] = r[0]; z[e] = r[1];
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < 2 * TN; i += STEP) {
     const int col = col0 + i / STEP * 32;
     if (col >= a.cols) return;
-    u32x4 res[TM][2];
+    const int c = col + turned * 8;
+    u32x4 res[2 * TM];
     if (!TO8 && a.res) {
 #pragma unroll
-      for (int j = 0; j < TM; ++j)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int tok = tok0 + j * 32 + h * 16 + (lane & 15), c = col + turned * 8;
-          res[j][h] = u32x4{0, 0, 0, 0};
-          if (tok < n && c < a.cols) res[j][h] = *(const u32x4*)((const Y16*)a.res + tok * a.res_row + c);
-        }
+      for (int j = 0; j < 2 * TM; ++j) {
+        const int tok = tok0 + j * 16 + (lane & 15);
+        res[j] = u32x4{0, 0, 0, 0};
+        if (tok < n && c < a.cols) res[j] = *(const u32x4*)((const Y16*)a.res + tok * a.res_row + c);
+      }
     }
-    floatx4 b0[4], b1[4];
+    floatx4 b0[2], b1[2];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int c = col + 8 * q + 4 * half;
-      b0[q] = a.bias && c < a.cols ? *(const floatx4*)(a.bias + c) : floatx4{0.f, 0.f, 0.f, 0.f};
-      b1[q] = GATED && a.bias && c < a.cols ? *(const floatx4*)(a.bias + a.cols + c) : floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int h = 0; h < 2; ++h) {
+      const int at = col + 16 * h + 4 * g;
+      b0[h] = a.bias && at < a.cols ? *(const floatx4*)(a.bias + at) : floatx4{0.f, 0.f, 0.f, 0.f};
+      b1[h] = GATED && a.bias && at < a.cols ? *(const floatx4*)(a.bias + a.cols + at) : floatx4{0.f, 0.f, 0.f, 0.f};
     }
 #pragma unroll
-    for (int j = 0; j < TM; ++j) {
+    for (int j = 0; j < 2 * TM; ++j) {
       // the sums of the largest tiles fill one half of the registers and are taken out of it block by block, here and not before
       if constexpr (TN * TM >= 16) {
-        asm volatile("" : "+a"(acc[i][j]));
-        if constexpr (GATED) asm volatile("" : "+a"(acc[i + 1][j]));
+#pragma unroll
+        for (int h = 0; h < STEP; ++h) asm volatile("" : "+a"(acc[i + h][j]));
       }
-      floatx4 v[4];
+      floatx4 v[2];
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[q][e] = acc[i][j][4 * q + e] + b0[q][e];
+      for (int h = 0; h < 2; ++h) v[h] = acc[i + h][j] + b0[h];
       auto each = [&](auto f) __attribute__((always_inline)) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[q][e] = f(v[q][e]);
+          for (int e = 0; e < 4; ++e) v[h][e] = f(v[h][e]);
       };
       if (a.act == PRODUCT_ACT_SILU) each([](float z) { return silu(z); });
       else if (a.act == PRODUCT_ACT_RELU) each([](float z) { return fmaxf(z, 0.f); });
       if constexpr (GATED) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[q][e] *= acc[i + 1][j][4 * q + e] + b1[q][e];
+        for (int h = 0; h < 2; ++h) v[h] *= acc[i + 2 + h][j] + b1[h];
       }
+      const int tok = tok0 + j * 16 + (lane & 15);
       if constexpr (TO8) {
         unsigned most = 0;
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) most = max(most, __float_as_uint(v[q][e]) & 0x7FFFFFFFu);
+          for (int e = 0; e < 4; ++e) most = max(most, __float_as_uint(v[h][e]) & 0x7FFFFFFFu);
+        most = max(most, (unsigned)__shfl_xor((int)most, 16));
         most = max(most, (unsigned)__shfl_xor((int)most, 32));
         const bool none = most >= 0x7F800000u;
         const int ex = mx8_exp(most);
         const float inverse = mx8_inverse(ex);
-        unsigned w[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) w[q] = none ? MX8_NAN4 : mx8_pack4(v[q], inverse);
-        const auto s0 = __builtin_amdgcn_permlane32_swap(w[0], w[1], false, false), s1 = __builtin_amdgcn_permlane32_swap(w[2], w[3], false, false);
-        const int tok = tok0 + j * 32 + l32;
+        const auto r = __builtin_amdgcn_permlane16_swap(none ? MX8_NAN4 : mx8_pack4(v[0], inverse), none ? MX8_NAN4 : mx8_pack4(v[1], inverse), false, false);
         if (tok < n) {
-          uint8_t* const y = a.y8.d_codes + tok * a.y8.code_row + col + 8 * half;
-          *(u32x2*)y = u32x2{s0[0], s0[1]};
-          *(u32x2*)(y + 16) = u32x2{s1[0], s1[1]};
-          if (!half) a.y8.d_exps[tok * a.y8.exp_row + col / 32] = (uint8_t)(none ? 255 : ex);
+          *(u32x2*)(a.y8.d_codes + tok * a.y8.code_row + c) = u32x2{r[0], r[1]};
+          if (!g) a.y8.d_exps[tok * a.y8.exp_row + col / 32] = (uint8_t)(none ? 255 : ex);
         }
       } else {
         if (a.res) {
-          swap_rows16(res[j][0], res[j][1]);
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const auto s0 = __builtin_amdgcn_permlane32_swap(res[j][h][0], res[j][h][2], false, false), s1 = __builtin_amdgcn_permlane32_swap(res[j][h][1], res[j][h][3], false, false);
-            const u32x2 x = {s0[0], s1[0]}, z = {s0[1], s1[1]};
-            const floatx4 rx = load4((const Y16*)&x), rz = load4((const Y16*)&z);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) { v[2 * h][e] += rx[e]; v[2 * h + 1][e] += rz[e]; }
-          }
+          u32x2 x = {res[j][0], res[j][1]}, z = {res[j][2], res[j][3]};
+          swap(x, z);
+          v[0] += load4((const Y16*)&x);
+          v[1] += load4((const Y16*)&z);
         }
-        u32x4 o[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          u32x2 x, z;
-          store4<Y16>((Y16*)&x, v[2 * h]);
-          store4<Y16>((Y16*)&z, v[2 * h + 1]);
-          const auto s0 = __builtin_amdgcn_permlane32_swap(x[0], z[0], false, false), s1 = __builtin_amdgcn_permlane32_swap(x[1], z[1], false, false);
-          o[h] = u32x4{s0[0], s1[0], s0[1], s1[1]};
-        }
-        swap_rows16(o[0], o[1]);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int tok = tok0 + j * 32 + h * 16 + (lane & 15), c = col + turned * 8;
-          if (tok < n && c < a.cols) *(u32x4*)((Y16*)a.y + tok * a.y_row + c) = o[h];
-        }
+        u32x2 x, z;
+        store4<Y16>((Y16*)&x, v[0]);
+        store4<Y16>((Y16*)&z, v[1]);
+        swap(x, z);
+        if (tok < n && c < a.cols) *(u32x4*)((Y16*)a.y + tok * a.y_row + c) = u32x4{x[0], x[1], z[0], z[1]};
       }
     }
   }
 }
 template <typename Y, int TN, int TM>
-__device__ __forceinline__ void finish_direct(const ProductArgs& a, floatx16 (&acc)[TN][TM], int n, int tok0, int col0, int lane) {
+__device__ __forceinline__ void finish_direct(const ProductArgs& a, floatx4 (&acc)[2 * TN][2 * TM], int n, int tok0, int col0, int lane) {
   if (a.gated) finish_direct_as<Y, TN, TM, true>(a, acc, n, tok0, col0, lane);
   else finish_direct_as<Y, TN, TM, false>(a, acc, n, tok0, col0, lane);
 }
+
+// f(integral_constant 0), .. f(integral_constant N - 1): loops whose bodies have other loops with bounds by their counter
+template <typename F, int... I> __device__ __forceinline__ void unrolled(F&& f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
+template <int N, typename F> __device__ __forceinline__ void unrolled(F&& f) { unrolled(f, std::make_integer_sequence<int, N>{}); }
 
 // ---- many tokens: tiles in LDS -----------------------------------------------------------------------------------------
 // A block makes BN rows of w times BM tokens; its WN x WM wavefronts take TN x TM blocks of 32 x 32 each.  A step covers 128 bytes of k of all rows.  Loads go straight
@@ -296,20 +294,19 @@ __device__ __forceinline__ void finish_direct(const ProductArgs& a, floatx16 (&a
 // the row's, which spreads the rows that sixteen lanes read together over all banks.
 //
 // Rows of 8 bits: the 8-bit matrix instructions add products in groups of eight at the weight of the group's largest and drop what lies 2^13 below it (measured: 1 + 2^-13 comes
-// out, 1 + 2^-14 does not), 2^-14 of a sum's size in the mean.  Results that are rounded to 16 or 8 bits can bear that; for fp32 results (EXACT) the values are widened to bf16,
-// whose products are exact and added in fp32, at half the rate.
+// out, 1 + 2^-14 does not), 2^-14 of a sum's size in the mean.  Results that are rounded to 16 or 8 bits can bear that; for fp32 results, and where exponents are no aligned words (EXACT), the
+// values are widened to bf16, whose products are exact and added in fp32, at half the rate.
 template <typename T, bool EXACT, int TN, int TM, int WN, int WM, int MINB>
 __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(ProductArgs a) {
   constexpr bool MX = std::is_same<T, f8>::value;
   constexpr int NW = WN * WM, BN = WN * TN * 32, BM = WM * TM * 32, ROWS = BN + BM, STAGE = ROWS * 128, LW = BN / 8 / NW, LX = BM / 8 / NW;
-  constexpr int KQ = MX ? 2 : 4, FV = MX ? 2 : 1;                    // products of k within a step, 16-byte vectors of an operand
-  constexpr int L = LW + LX, R = (TN + TM) * FV, M = TN * TM;        // loads of a step, reads and products of a part of one
-  constexpr int SPREAD = MX ? 1 : OCTO_SPREAD, L0 = MX && EXACT ? L : L / (SPREAD + 1);     // parts of the next step that loads are issued in, loads behind the barrier
+  constexpr int BW = 2 * TN, BX = 2 * TM, M = BW * BX, L = LW + LX;   // blocks of 16 rows of a wavefront, their products, loads of a step
   constexpr int HT = TM < 2 ? 1 : 2, UNIT = HT * 32 * TN * 32 * 4;    // sums of a wavefront on their way out, of 32 or 64 tokens
-  constexpr int MAIN = 2 * STAGE + (MX ? 4 * ROWS * 4 : 0), LDS = MAIN > NW * UNIT ? MAIN : NW * UNIT;
+  constexpr int NE = MX ? (ROWS + NW * 64 - 1) / (NW * 64) : 1, EXPS = NE * NW * 64;   // exponents of a step, whole loads
+  constexpr int RING = EXACT ? 4 : 2, MAIN = 2 * STAGE + (MX ? RING * EXPS * 4 : 0), LDS = MAIN > NW * UNIT ? MAIN : NW * UNIT;
   static_assert(BN / 8 % NW == 0 && BM / 8 % NW == 0 && TN % 2 == 0 && NW % 4 == 0, "whole loads a wavefront, pairs of blocks");
   __shared__ __attribute__((aligned(1024))) unsigned char smem[LDS];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
   const int wn = wave % WN, wm = wave / WN;
   const int n = a.n_dyn ? min(max(*a.n_dyn, 0), a.n) : a.n;
 
@@ -346,9 +343,8 @@ __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(Produc
   const char* const x0 = a.x + m0 * a.x_row;
   const int nk = (a.k_bytes + 127) / 128;
 
-  // Exponents, a word for each row and step, four steps deep: a thread has row threadIdx.x and those NW * 64 further on.  Whole words go straight to LDS.  Otherwise bytes are
-  // taken one by one to registers, since what lies behind a row's end may read as NaN, and placed a step later.
-  constexpr int NE = MX ? (ROWS + NW * 64 - 1) / (NW * 64) : 1;
+  // Exponents, a word for each row and step, two steps deep (EXACT: four): a thread has row threadIdx.x and those NW * 64 further on.  Whole words go straight to LDS.  Otherwise (EXACT
+  // alone) bytes are taken one by one to registers, since what lies behind a row's end may read as NaN, and placed a step later.
   const uint8_t* exp_at[NE];
   unsigned exps[NE];
   if constexpr (MX) {
@@ -360,7 +356,7 @@ __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(Produc
     }
   }
   auto load_exps = [&](int t) __attribute__((always_inline)) {       // bytes
-    if constexpr (MX) {
+    if constexpr (MX && EXACT) {
       if (!a.exp_words) {
 #pragma unroll
         for (int i = 0; i < NE; ++i) {
@@ -372,153 +368,183 @@ __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(Produc
     }
   };
   auto place_exps = [&](int t) __attribute__((always_inline)) {
-    if constexpr (MX) {
+    if constexpr (MX && EXACT) {
       if (!a.exp_words) {
 #pragma unroll
         for (int i = 0; i < NE; ++i) {
           const int r = i * NW * 64 + (int)threadIdx.x;
-          if (r < ROWS) *(unsigned*)(smem + 2 * STAGE + ((t & 3) * ROWS + r) * 4) = exps[i];
+          if (r < ROWS) *(unsigned*)(smem + 2 * STAGE + ((t & (RING - 1)) * EXPS + r) * 4) = exps[i];
         }
       }
     }
   };
   auto issue_exps = [&](int t) __attribute__((always_inline)) {      // words
     if constexpr (MX) {
-      if (a.exp_words) {
+      if (!EXACT || a.exp_words) {
 #pragma unroll
         for (int i = 0; i < NE; ++i)
-          if ((i * NW + wave) * 64 < ROWS)
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
-                         :: "s"(lds + 2 * STAGE + ((t & 3) * ROWS + (i * NW + wave) * 64) * 4), "v"(exp_at[i] + 4 * min(t, nk - 1)) : "memory");
+                         :: "s"(lds + 2 * STAGE + ((t & (RING - 1)) * EXPS + (i * NW + wave) * 64) * 4), "v"(exp_at[i] + 4 * min(t, nk - 1)) : "memory");
       }
     }
   };
+  // Lanes whose chunk of step t lies behind their row's end, of loads of even and odd number: they load nothing from there on.  (No branches in the loop: products would move across them.)
+  bool gone[2];
+  auto cut = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+    for (int odd = 0; odd < 2; ++odd) gone[odd] = ((lane & 7) ^ (odd * 4 + (lane >> 4))) * 16 + t * 128 >= a.k_bytes;
+  };
   // load q of step t: LW of w, then LX of x.  Addresses are 4096 too large, for the offsets, and buffers start as much earlier.
-  auto issue = [&](int t, int q, auto whole) __attribute__((always_inline)) {
+  auto issue = [&](int t, int stage, int q) __attribute__((always_inline)) {
     const bool is_w = q < LW;
-    const int i = is_w ? q : q - LW, off = is_w ? woff[is_w ? i : 0] : xoff[is_w ? 0 : i];
-    const int part = (lane & 7) ^ (((is_w ? wave * LW : wave * LX) + i) * 4 + (lane >> 4) & 7);          // the lane's chunk
-    const int beyond = !whole() && part * 16 + t * 128 >= a.k_bytes ? OOB : 0;         // the end of a row inside a step, and steps beyond the last
+    const int i = is_w ? q : q - LW;
+    int& off = is_w ? woff[is_w ? i : 0] : xoff[is_w ? 0 : i];
+    off = gone[i & 1] ? OOB : off;
     // rows of a gated layer alternate between its halves, 32 at a time
     const bool second = is_w && ((LW % 8 == 0 ? i / 4 : (wave * LW + i) / 4) & 1);
     const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc((void*)((is_w ? second ? w1 : w0 : x0) + t * 128 - 4096), 0, 0x7FFFFFFF, BUF_FLAGS);
-    const unsigned to = lds + (t & 1) * STAGE + (is_w ? wave * LW * 1024 : BN * 128 + wave * LX * 1024) + i / 4 * 4096;
-    if (i % 4 == 0) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(to), "v"(off | beyond), "s"(rc) : "memory");
-    else if (i % 4 == 1) asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:1024 lds" :: "v"(off | beyond), "s"(rc) : "memory");
-    else if (i % 4 == 2) asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:2048 lds" :: "v"(off | beyond), "s"(rc) : "memory");
-    else asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:3072 lds" :: "v"(off | beyond), "s"(rc) : "memory");
+    const unsigned to = lds + stage * STAGE + (is_w ? wave * LW * 1024 : BN * 128 + wave * LX * 1024) + i / 4 * 4096;
+    if (i % 4 == 0) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(to), "v"(off), "s"(rc) : "memory");
+    else if (i % 4 == 1) asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:1024 lds" :: "v"(off), "s"(rc) : "memory");
+    else if (i % 4 == 2) asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:2048 lds" :: "v"(off), "s"(rc) : "memory");
+    else asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:3072 lds" :: "v"(off), "s"(rc) : "memory");
   };
 
-  u32x4 fw[2][TN][FV], fx[2][TM][FV];
-  int ew[2][TN], ex[2][TM];
-  const int wrow = (wn * TN * 32 + l32) * 128, xrow = (BN + wm * TM * 32 + l32) * 128;
-  // read r of an operand set, in the order in which the products want them: the first row of w, all of x, the other rows of w
-  auto frag = [&](int set, int t, int kq, int r) __attribute__((always_inline)) {
-    const unsigned char* const p = smem + (t & 1) * STAGE;
-    const int o = r / FV, h = r % FV, c = ((MX ? 4 * kq + 2 * h + half : 2 * kq + half) ^ (lane >> 1 & 7)) * 16;
-    if (o >= 1 && o <= TM) fx[set][o - 1][h] = *(const u32x4*)(p + xrow + (o - 1) * 4096 + c);
-    else fw[set][o ? o - TM : 0][h] = *(const u32x4*)(p + wrow + (o ? o - TM : 0) * 4096 + c);
-  };
-  auto scales = [&](int set, int t) __attribute__((always_inline)) {
-    if constexpr (MX) {
-      const unsigned char* const p = smem + 2 * STAGE + (t & 3) * ROWS * 4;
+  floatx4 acc[BW][BX];
 #pragma unroll
-      for (int i = 0; i < TN; ++i) ew[set][i] = *(const unsigned*)(p + (wn * TN * 32 + i * 32 + l32) * 4) >> (EXACT ? 0 : 8 * half);
+  for (int i = 0; i < BW; ++i)
 #pragma unroll
-      for (int j = 0; j < TM; ++j) ex[set][j] = *(const unsigned*)(p + (BN + wm * TM * 32 + j * 32 + l32) * 4) >> (EXACT ? 0 : 8 * half);
-    }
+    for (int j = 0; j < BX; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+  const int wrow = (wn * TN * 32 + r16) * 128, xrow = (BN + wm * TM * 32 + r16) * 128;
+  // chunk c of the lane's row of block i of w or x, in one of the two stages
+  auto read = [&](bool is_x, int stage, int i, int c) __attribute__((always_inline)) -> u32x4 {
+    return *(const u32x4*)(smem + stage * STAGE + (is_x ? xrow : wrow) + i * 2048 + ((c ^ (r16 >> 1)) << 4));
   };
 
-  floatx16 acc[TN][TM];
-#pragma unroll
-  for (int i = 0; i < TN; ++i)
-#pragma unroll
-    for (int j = 0; j < TM; ++j)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+  // Loads of step t + 2 have places behind the products, from the barrier of step t on: place s of the 2 M up to the next barrier, the last quarter of which stays free for them to arrive.
+  auto load_place = [&](int t, int stage, auto place) __attribute__((always_inline)) {
+    constexpr int S = 3 * M / 2, first = (place() * L + S - 1) / S, last = ((place() + 1) * L + S - 1) / S;
+    unrolled<(last < L ? last : L) - (first < L ? first : L)>([&](auto q) __attribute__((always_inline)) { issue(t, stage, first + q()); });
+  };
+  constexpr int FIRST = (M * L + 3 * M / 2 - 1) / (3 * M / 2);        // loads with places before M
 
   load_exps(0); place_exps(0);
   load_exps(1); place_exps(1);
   issue_exps(0);
   issue_exps(1);
+  cut(0);
 #pragma unroll
-  for (int q = 0; q < L; ++q) issue(0, q, std::false_type{});
-#pragma unroll
-  for (int q = 0; q < L0; ++q) issue(1, q, std::false_type{});
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(L0) : "memory");
+  for (int q = 0; q < L; ++q) issue(0, 0, q);
+  cut(1);
+  unrolled<M>([&](auto p) __attribute__((always_inline)) { load_place(1, 1, p); });
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(FIRST) : "memory");
   __builtin_amdgcn_s_barrier();
   load_exps(2);
-#pragma unroll
-  for (int r = 0; r < R; ++r) frag(0, 0, 0, r);
-  scales(0, 0);
 
-  // Loads and reads beyond the last step are of nothing (zeros go to LDS): the loop has no branches.  While the steps that are loaded are whole ones, addresses take no arithmetic.  Reads and loads stand between the products, in the order below: a product
-  // keeps the matrix unit busy for 32 cycles or more, in which the wavefront issues what lies behind it.
-  auto step = [&](int t, auto whole) __attribute__((always_inline)) {
-#pragma unroll
-    for (int kq = 0; kq < KQ; ++kq) {
-      const int cur = kq & 1;
-      if (kq == KQ - 1) {
-        place_exps(t + 2);
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        load_exps(t + 3);
-        issue_exps(t + 2);
-        scales(1, t + 1);
-      }
-      if constexpr (MX && EXACT) {
-#pragma unroll
-        for (int h = 0; h < FV; ++h) {
-          u32x4 w[TN][2], x[TM][2];
-#pragma unroll
-          for (int i = 0; i < TN; ++i) widen_mx8(fw[cur][i][h], (unsigned)ew[0][i] >> (16 * kq + 8 * h) & 255, &w[i][0], &w[i][1]);
-#pragma unroll
-          for (int j = 0; j < TM; ++j) widen_mx8(fx[cur][j][h], (unsigned)ex[0][j] >> (16 * kq + 8 * h) & 255, &x[j][0], &x[j][1]);
-#pragma unroll
-          for (int i = 0; i < TN; ++i)
-#pragma unroll
-            for (int j = 0; j < TM; ++j) acc[i][j] = Elem<__bf16>::mfma(w[i][1], x[j][1], Elem<__bf16>::mfma(w[i][0], x[j][0], acc[i][j]));
-        }
-#pragma unroll
-        for (int r = 0; r < R; ++r) frag(cur ^ 1, kq == KQ - 1 ? t + 1 : t, kq == KQ - 1 ? 0 : kq + 1, r);
-        if (kq == KQ - 1) {
-#pragma unroll
-          for (int q = 0; q < L; ++q) issue(t + 2, q, whole);
-        }
-      } else {
-#pragma unroll
-        for (int m = 0; m < M; ++m) {
-          const int i = m / TM, j = m % TM;
-          if constexpr (MX) {
-            if (kq == 0) acc[i][j] = mfma_mx8<0>(fw[cur][i][0], fw[cur][i][1], fx[cur][j][0], fx[cur][j][1], acc[i][j], ew[0][i], ex[0][j]);
-            else acc[i][j] = mfma_mx8<1>(fw[cur][i][0], fw[cur][i][1], fx[cur][j][0], fx[cur][j][1], acc[i][j], ew[0][i], ex[0][j]);
-          } else {
-            acc[i][j] = Elem<T>::mfma(fw[cur][i][0], fx[cur][j][0], acc[i][j]);
-          }
-#pragma unroll
-          for (int r = 0; r < R; ++r) if (r * M / R == m) frag(cur ^ 1, kq == KQ - 1 ? t + 1 : t, kq == KQ - 1 ? 0 : kq + 1, r);
-          // the loads of step t + 2 behind the barrier and in the next step, all but its last parts
-#pragma unroll
-          for (int q = 0; q < L; ++q) {
-            if (kq == KQ - 1 && q < L0 && (M - 1 ? q * M / L0 | 1 : 0) == m) issue(t + 2, q, whole);
-            if (kq < SPREAD && q >= L0 && (M - 1 ? (q - L0) * SPREAD * M / (L - L0) | 1 : 0) == kq * M + m) issue(t + 1, q, whole);
-          }
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      }
-    }
-    if constexpr (MX) {
-#pragma unroll
-      for (int i = 0; i < TN; ++i) ew[0][i] = ew[1][i];
-#pragma unroll
-      for (int j = 0; j < TM; ++j) ex[0][j] = ex[1][j];
-    }
+  // Loads and reads beyond the last step are of nothing (zeros go to LDS).  Reads and loads stand between the products, in the order of the code: a product keeps the matrix unit busy for 16 cycles or more, in which the wavefront issues what lies behind it.
+  auto turn = [&](int t) __attribute__((always_inline)) {             // all are done with step t's place in LDS, and step t + 1 is there
+    place_exps(t + 2);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    load_exps(t + 3);
+    issue_exps(t + 2);
+    cut(t + 2);
   };
-  int t = 0;
+  if constexpr (MX && !EXACT) {
+    // A step is one product of k.  Its M products go through four quarters, (w low, x low), (w low, x high), (w high, x high), (w high, x low); each half of an operand is read
+    // again, for the next use, as soon as the quarter that needed it last is over, so one set of registers does.  Odd steps have x low and high the other way round.
+    u32x4 fw[BW][2], fx[BX][2];
+    int ew[BW], ex[BX];
+    auto fetch = [&](bool is_x, int stage, int high, int r) __attribute__((always_inline)) {      // read r of 3 TN or 3 TM of a half
+      const int i = high * (is_x ? TM : TN) + r / 3, h = r % 3, at = is_x ? BN + wm * TM * 32 : wn * TN * 32;
+      if (h == 2) {
+        (is_x ? ex[is_x ? i : 0] : ew[is_x ? 0 : i]) = *(const uint8_t*)(smem + 2 * STAGE + (stage * EXPS + at + i * 16 + r16) * 4 + g);
+      } else {
+        (is_x ? fx[is_x ? i : 0][h & 1] : fw[is_x ? 0 : i][h & 1]) = read(is_x, stage, i, g + 4 * h);
+      }
+    };
+#pragma unroll
+    for (int r = 0; r < 3 * TN; ++r) fetch(false, 0, 0, r);
+#pragma unroll
+    for (int r = 0; r < 3 * TM; ++r) fetch(true, 0, 0, r);
+    auto step = [&](int t, auto odd) __attribute__((always_inline)) {
+      constexpr int X = odd() ? 1 : 0;                                // the half of x that comes first, the stage of the step
+      unrolled<4>([&](auto quarter_) __attribute__((always_inline)) {
+        constexpr int quarter = quarter_(), MQ = TN * TM, wh = quarter / 2, xh = (quarter == 1 || quarter == 2) ? 1 - X : X, R = quarter == 0 || quarter == 3 ? 3 * TM : 3 * TN;
+        if constexpr (quarter == 2) turn(t);
+        unrolled<MQ>([&](auto m_) __attribute__((always_inline)) {
+          constexpr int m = m_(), i = wh * TN + m / TM, j = xh * TM + m % TM, first = (m * R + MQ - 1) / MQ, last = ((m + 1) * R + MQ - 1) / MQ;
+          acc[i][j] = mfma_mx8(fw[i], fx[j], acc[i][j], ew[i], ex[j]);
+          // quarter 0 reads the other half of x, 1 the other half of w, 2 the first half of w of the next step, 3 the half of x that the next step begins with
+          unrolled<last - first>([&](auto d) __attribute__((always_inline)) {
+            constexpr int r = first + d();
+            if constexpr (quarter == 0) fetch(true, X, 1 - X, r);
+            else if constexpr (quarter == 1) fetch(false, X, 1, r);
+            else if constexpr (quarter == 2) fetch(false, 1 - X, 0, r);
+            else fetch(true, 1 - X, 1 - X, r);
+          });
+          // the barrier lies between quarters 1 and 2
+          constexpr int place = (quarter * MQ + m + 2 * MQ) % (4 * MQ) * 2;
+          load_place(quarter >= 2 ? t + 2 : t + 1, quarter >= 2 ? X : 1 - X, std::integral_constant<int, place>{});
+          load_place(quarter >= 2 ? t + 2 : t + 1, quarter >= 2 ? X : 1 - X, std::integral_constant<int, place + 1>{});
+          __builtin_amdgcn_sched_barrier(0);
+        });
+      });
+    };
 #pragma nounroll
-  for (; t + 2 < a.k_bytes / 128; ++t) step(t, std::true_type{});
+    for (int t = 0; t < nk; t += 2) { step(t, std::false_type{}); step(t + 1, std::true_type{}); }
+  } else {
+    // A step is two products of k; two sets of operands.
+    constexpr int R = BW + BX;
+    u32x4 fw[2][BW], fx[2][BX];
+    unsigned ew[2][MX ? BW : 1], ex[2][MX ? BX : 1];
+    // read r of an operand set, in the order in which the products want them: the first row of w, all of x, the other rows of w
+    auto fetch = [&](int set, int t, int kq, int r) __attribute__((always_inline)) {
+      if (r >= 1 && r <= BX) fx[set][r - 1] = read(true, t & 1, r - 1, 4 * kq + g);
+      else fw[set][r ? r - BX : 0] = read(false, t & 1, r ? r - BX : 0, 4 * kq + g);
+    };
+    auto scales = [&](int set, int t) __attribute__((always_inline)) {
+      if constexpr (MX) {
+        const unsigned char* const p = smem + 2 * STAGE + (t & (RING - 1)) * EXPS * 4;
+#pragma unroll
+        for (int i = 0; i < BW; ++i) ew[set][i] = *(const unsigned*)(p + (wn * TN * 32 + i * 16 + r16) * 4);
+#pragma unroll
+        for (int j = 0; j < BX; ++j) ex[set][j] = *(const unsigned*)(p + (BN + wm * TM * 32 + j * 16 + r16) * 4);
+      }
+    };
+#pragma unroll
+    for (int r = 0; r < R; ++r) fetch(0, 0, 0, r);
+    scales(0, 0);
+    auto step = [&](int t) __attribute__((always_inline)) {
+      unrolled<2>([&](auto kq_) __attribute__((always_inline)) {
+        constexpr int kq = kq_();
+        if constexpr (kq == 1) { turn(t); scales(1, t + 1); }
+        u32x4 w8[MX ? BW : 1][2], x8[MX ? BX : 1][2];
+        if constexpr (MX) {
+#pragma unroll
+          for (int i = 0; i < BW; ++i) widen_mx8(fw[kq][i], ew[0][i] >> (16 * kq + 8 * (g >> 1)) & 255, &w8[i][0], &w8[i][1]);
+#pragma unroll
+          for (int j = 0; j < BX; ++j) widen_mx8(fx[kq][j], ex[0][j] >> (16 * kq + 8 * (g >> 1)) & 255, &x8[j][0], &x8[j][1]);
+        }
+        unrolled<M>([&](auto m_) __attribute__((always_inline)) {
+          constexpr int m = m_(), i = m / BX, j = m % BX, first = (m * R + M - 1) / M, last = ((m + 1) * R + M - 1) / M;
+          if constexpr (MX) acc[i][j] = mfma16<__bf16>(w8[i][1], x8[j][1], mfma16<__bf16>(w8[i][0], x8[j][0], acc[i][j]));
+          else acc[i][j] = mfma_part<T>(fw[kq][i], fx[kq][j], acc[i][j]);
+          unrolled<last - first>([&](auto d) __attribute__((always_inline)) { fetch(kq ^ 1, t + kq, kq ^ 1, first + d()); });
+          load_place(kq == 1 ? t + 2 : t + 1, kq == 1 ? t & 1 : ~t & 1, std::integral_constant<int, kq == 1 ? m : M + m>{});
+          __builtin_amdgcn_sched_barrier(0);
+        });
+      });
+      if constexpr (MX) {
+#pragma unroll
+        for (int i = 0; i < BW; ++i) ew[0][i] = ew[1][i];
+#pragma unroll
+        for (int j = 0; j < BX; ++j) ex[0][j] = ex[1][j];
+      }
+    };
 #pragma nounroll
-  for (; t < nk; ++t) step(t, std::false_type{});
+    for (int t = 0; t < nk; ++t) step(t);
+  }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 
   if (a.direct) {
@@ -536,14 +562,9 @@ __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(Produc
 #pragma unroll
   for (int h = 0; h < TM; h += HT) {
 #pragma unroll
-    for (int j = 0; j < HT; ++j)
+    for (int j = 0; j < 2 * HT; ++j)
 #pragma unroll
-      for (int i = 0; i < TN; ++i)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const floatx16& c = acc[i][h + j];
-          *(floatx4*)(out + ((j * 32 + l32) * TN * 8 + ((8 * i + 2 * q + half) ^ (lane & 15))) * 4) = floatx4{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
-        }
+      for (int i = 0; i < BW; ++i) *(floatx4*)(out + ((j * 16 + r16) * TN * 8 + ((4 * i + g) ^ r16)) * 4) = acc[i][2 * h + j];
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
@@ -730,7 +751,7 @@ template <typename T> hipError_t launch_product(int variant, const ProductArgs& 
 template <> hipError_t launch_product<OCTO_PRODUCT_TYPE>(int variant, const ProductArgs& a, hipStream_t s) {
   typedef OCTO_PRODUCT_TYPE T;
   if constexpr (std::is_same<T, f8>::value) {
-    if (a.y_kind == PRODUCT_Y_F32) {
+    if (a.exact8) {
       if (variant == 1 || variant == 2) return launch_product_tile<T, true, 2, 2, 2, 2, 2>(a, s);
       if (variant == 3) return launch_product_tile<T, true, 2, 1, 2, 2, 2>(a, s);
     }
