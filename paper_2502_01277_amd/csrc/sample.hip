@@ -3,11 +3,15 @@
 // With the tokens of a row in the order of their logits (equal ones by index) and w = exp((x - max) / temperature), top-k, top-p and min-p each keep a beginning of that order; what
 // they keep in common is one too, and is known by its last token.  The token is drawn in the order of indices: the first at which the sum of the kept weights passes u times all.
 //
-// A workgroup takes a row.  Sums of weights decide which token a border falls on, so they are made of integers: w is computed in fp64 (64 steps an octave from a table, the rest by a
-// polynomial, 1e-15 off) and rounded to multiples of 2^-shift of the largest, whose sums in 64 bits are the same in any order.  Borders are found by a histogram of
-// counts and weights over 64 octaves of w, 64 bins each; the tokens of the bin that holds the border are sorted.  Where they are too many (equal logits, say), bits of the
-// logits themselves make further histograms.
+// A workgroup takes a row.  Sums of weights decide which token a border falls on, so they are made of integers: w is computed in fp64 (1024 steps an octave from a table, the rest by a
+// polynomial, 2e-14 off) and rounded to multiples of 2^-shift of the largest, whose sums in 64 bits are the same in any order.  The bound is arithmetic, an exponential of twenty
+// instructions for each logit, so it is computed where it has to be:
+//   - top_k of up to LISTED: the k-th largest of the threads' own largest logits is no larger than the k-th largest of all; what is not below it, little more than k logits, is sorted in LDS.
+//   - bf16: a row has few different logits.  Codes of the 16 octaves below the largest magnitude are counted, 4096 of them, and all sums are those of counts times weights.
+//   - else borders are found by a histogram of counts and weights over 64 octaves of w, 64 bins each; the tokens of the bin that holds the border are sorted.  Where they are too
+//     many (equal logits, say), bits of the logits themselves make further histograms.  The same where the others do not fit (more equal logits than are sorted, borders in codes that are not counted).
 #include <cmath>
+#include <type_traits>
 
 #include "mfma_common.h"
 #include "octo_internal.h"
@@ -15,7 +19,7 @@
 namespace octo {
 namespace {
 
-constexpr int SAMPLE_THREADS = 1024, SAMPLE_WAVES = 16, BINS = 4096, SORTED = 2048;
+constexpr int SAMPLE_THREADS = 1024, SAMPLE_WAVES = 16, BINS = 4096, SORTED = 2048, LISTED = 512;
 typedef unsigned long long u64;
 
 struct SampleArgs {
@@ -27,39 +31,38 @@ struct SampleArgs {
   int vocab, shift;
 };
 
-// 2^(j / 64), j = 0 .. 63
-struct ExpTable { double v[64]; };
-ExpTable exp_table() {
-  ExpTable t;
-  for (int j = 0; j < 64; ++j) t.v[j] = std::exp2(j / 64.0);
-  return t;
-}
-
-// Floats as integers of the same order.
+// Floats as integers of the same order, both zeros alike.
 __device__ __forceinline__ unsigned ordered(float v) {
-  const unsigned b = __float_as_uint(v);
+  const unsigned b = __float_as_uint(v + 0.0f);
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
+__device__ __forceinline__ float unordered(unsigned k) { return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k); }
+
+constexpr int STEPS = 1024;    // of an octave
 struct Weigher {
-  const double* table;      // in LDS
+  const double* table;      // 2^(j / STEPS), in LDS
   double inverse;           // 1 / temperature
   float max;
   int shift;
-  // w of a logit in units of 2^-shift, its bin, and w itself
-  __device__ __forceinline__ u64 operator()(float v, int* bin, double* w) const {
-    double x = v == max ? 0.0 : ((double)v - (double)max) * inverse;
-    x = fmax(x, -50.0);                                              // e^-50 < 2^-72; also where it is no number (an infinite maximum, an infinite temperature)
-    const double kd = rint(x * 92.33248261689366);               // 64 / ln 2
-    const double r = fma(kd, -0.010830424696249145, x), r2 = fma(kd, -3.623510646634843e-19, r);
-    const int k = (int)kd;
-    double p = fma(r2, 1.0 / 120, 1.0 / 24);
-    p = fma(p, r2, 1.0 / 6); p = fma(p, r2, 0.5); p = fma(p, r2, 1.0); p = fma(p, r2, 1.0);
-    *w = ldexp(p * table[k & 63], k >> 6);
-    *bin = min(-k, BINS - 1);
-    // adding 2^52 leaves the nearest integer in the low bits
-    return (u64)__double_as_longlong(ldexp(*w, shift) + 4503599627370496.0) - 0x4330000000000000ull;
+  // (v - max) / temperature
+  __device__ __forceinline__ double exponent(float v) const {
+    const double x = v == max ? 0.0 : ((double)v - (double)max) * inverse;
+    return fmax(x, -50.0);                                           // e^-50 < 2^-72; also where it is no number (an infinite maximum, an infinite temperature)
   }
+  __device__ __forceinline__ int steps(double x) const { return (int)rint(x * 1477.3197218702985); }       // STEPS / ln 2
+  __device__ __forceinline__ int bin_of(int k) const { return min(-k >> 4, BINS - 1); }
+  __device__ __forceinline__ int bin(float v) const { return bin_of(steps(exponent(v))); }
+  // w times 2^shift
+  __device__ __forceinline__ double scaled(double x, int k) const {
+    const double r = fma((double)k, -0.0006769015435155716, x);      // ln 2 / STEPS; r is at most half of that
+    const double p = fma(fma(fma(r, 1.0 / 6, 0.5), r, 1.0), r, 1.0);
+    return ldexp(p * table[k & (STEPS - 1)], (k >> 10) + shift);
+  }
+  __device__ __forceinline__ double scaled(float v) const { const double x = exponent(v); return scaled(x, steps(x)); }
+  // the nearest integer: adding 2^52 leaves it in the low bits
+  static __device__ __forceinline__ u64 whole(double w) { return (u64)__double_as_longlong(w + 4503599627370496.0) - 0x4330000000000000ull; }
+  __device__ __forceinline__ u64 operator()(float v) const { return whole(scaled(v)); }
 };
 
 template <typename V> __device__ __forceinline__ V wave_sum(V v) {
@@ -74,32 +77,39 @@ template <typename V> __device__ __forceinline__ V wave_scan(V v, int lane) {   
 }
 
 struct SampleShared {
-  double table[64];
+  double table[STEPS];
   u64 weight[BINS];
   unsigned count[BINS];
   u64 list[SORTED];
   u64 wave_w[SAMPLE_WAVES];
   unsigned wave_c[SAMPLE_WAVES];
-  float wave_max[SAMPLE_WAVES];
-  int wave_at[SAMPLE_WAVES];
-  int listed, bin, token;
+  float wave_max[SAMPLE_WAVES], wave_big[SAMPLE_WAVES];
+  unsigned votes[2];
+  int listed, bin, token, cut;
   unsigned bin_count, key, at, before_c;
-  u64 before_w;
+  u64 before_w, tiny_w;
 };
 
+// The last token that is kept: all whose ordered logit is above `key`, and of those equal to it the ones up to index `at`.
+struct Last { unsigned key; int at; };
+
 template <typename T>
-__global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a, ExpTable table) {
+__global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
   constexpr int VEC = 16 / sizeof(T), DEPTH = 4;
   __shared__ SampleShared s;
   const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   if (a.n_dyn && row >= *a.n_dyn) return;
   const T* const x = (const T*)a.logits + row * a.row;
-  if (tid < 64) s.table[tid] = table.v[tid];
+  const float temperature = a.temperature ? a.temperature[row] : a.all_temperature;
+  const int top_k = a.top_k ? a.top_k[row] : a.all_top_k;
+  const float top_p = a.top_p ? a.top_p[row] : a.all_top_p, min_p = a.min_p ? a.min_p[row] : a.all_min_p;
+  const float u = fminf(fmaxf(a.u[row], 0.f), 0.99999994f);
 
   // Positions are indices plus the distance of the row's start from the last 16-byte border before it, so that vectors are aligned; a wavefront has a range of them, lanes have
   // neighbouring vectors.
   const int skew = (int)(((uintptr_t)x & 15) / sizeof(T)), end = a.vocab + skew;
   const int tiles = (end + SAMPLE_WAVES * 64 * VEC - 1) / (SAMPLE_WAVES * 64 * VEC);                 // vectors of a lane
+  const int range_len = tiles * 64 * VEC;                                                            // positions of a wavefront
   auto load = [&](int p) __attribute__((always_inline)) -> u32x4 {
     u32x4 v;
     if (p >= skew && p + VEC <= end) return *(const u32x4*)(x + (p - skew));
@@ -107,61 +117,67 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a, Ex
     for (int e = 0; e < VEC; ++e) ((T*)&v)[e] = p + e >= skew && p + e < end ? x[p + e - skew] : (T)-INFINITY;
     return v;
   };
-  // f(index, logit) of every token of the positions from, from + stride ... that may be drawn
-  auto each = [&](int from, int count, int stride, auto&& f) __attribute__((always_inline)) {
+  // f(position, vector) of the positions from, from + stride ...
+  auto vectors = [&](int from, int count, int stride, auto&& f) __attribute__((always_inline)) {
     for (int i0 = 0; i0 < count; i0 += DEPTH) {
       u32x4 v[DEPTH];
 #pragma unroll
       for (int d = 0; d < DEPTH; ++d) if (i0 + d < count) v[d] = load(from + (i0 + d) * stride);
 #pragma unroll
-      for (int d = 0; d < DEPTH; ++d) {
-        if (i0 + d >= count) break;
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          const float f32 = (float)((const T*)&v[d])[e];
-          if (f32 > -INFINITY) f(from + (i0 + d) * stride + e - skew, f32);          // neither -infinity nor NaN
-        }
-      }
+      for (int d = 0; d < DEPTH; ++d) if (i0 + d < count) f(from + (i0 + d) * stride, v[d]);
     }
   };
-  const int mine = wave * tiles * 64 * VEC + lane * VEC;
-  auto all = [&](auto&& f) __attribute__((always_inline)) { each(mine, tiles, 64 * VEC, f); };
-
-  // the best token, and how many there are
-  float best = -INFINITY; int best_at = 0x7FFFFFFF; unsigned there = 0;
-  all([&](int i, float v) { ++there; if (v > best || (v == best && i < best_at)) { best = v; best_at = i; } });
+  auto value = [&](const u32x4& v, int e) __attribute__((always_inline)) { return (float)((const T*)&v)[e]; };
+  // f(index, logit) of every token there that may be drawn
+  auto each = [&](int from, int count, int stride, auto&& f) __attribute__((always_inline)) {
+    vectors(from, count, stride, [&](int p, const u32x4& v) __attribute__((always_inline)) {
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const float v = __shfl_xor(best, d); const int i = __shfl_xor(best_at, d);
-    if (v > best || (v == best && i < best_at)) { best = v; best_at = i; }
-  }
-  there = wave_sum(there);
-  if (!lane) { s.wave_max[wave] = best; s.wave_at[wave] = best_at; s.wave_c[wave] = there; }
-  __syncthreads();
-  there = 0;
-  for (int w = 0; w < SAMPLE_WAVES; ++w) {
-    const float v = s.wave_max[w]; const int i = s.wave_at[w];
-    if (v > best || (v == best && i < best_at)) { best = v; best_at = i; }
-    there += s.wave_c[w];
-  }
-  __syncthreads();
+      for (int e = 0; e < VEC; ++e) {
+        const float f32 = value(v, e);
+        if (f32 > -INFINITY) f(p + e - skew, f32);                   // neither -infinity nor NaN
+      }
+    });
+  };
+  const int mine = wave * range_len + lane * VEC;
+  auto all = [&](auto&& f) __attribute__((always_inline)) { each(mine, tiles, 64 * VEC, f); };
+  auto answer = [&](int token, int kept, double logprob) {
+    a.token[row] = token;
+    if (a.kept) a.kept[row] = kept;
+    if (a.logprob) a.logprob[row] = (float)logprob;
+  };
 
-  const float temperature = a.temperature ? a.temperature[row] : a.all_temperature;
-  if (!there || !(temperature > 0)) {
-    if (!tid) {
-      a.token[row] = there ? best_at : -1;
-      if (a.kept) a.kept[row] = there ? 1 : 0;
-      if (a.logprob) a.logprob[row] = there ? 0.f : -INFINITY;
+  // the largest logit, of this thread and of all, and the largest magnitude
+  float own = -INFINITY, big = 0.f;
+  vectors(mine, tiles, 64 * VEC, [&](int, const u32x4& v) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      const float f = value(v, e);
+      own = fmaxf(own, f);                                           // the other one where one is NaN
+      if (sizeof(T) == 2) big = fmaxf(big, f > -INFINITY ? fabsf(f) : 0.f);
     }
+  });
+  float best = own;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) { best = fmaxf(best, __shfl_xor(best, d)); big = fmaxf(big, __shfl_xor(big, d)); }
+  if (!lane) { s.wave_max[wave] = best; s.wave_big[wave] = big; }
+  if (tid == 0) { s.listed = 0; s.at = 0x7FFFFFFF; s.token = -1; s.cut = 0x7FFFFFFF; s.tiny_w = 0; s.votes[0] = s.votes[1] = 0; }
+  if (tid < STEPS) s.table[tid] = exp2(tid * (1.0 / STEPS));
+  __syncthreads();
+  for (int w = 0; w < SAMPLE_WAVES; ++w) { best = fmaxf(best, s.wave_max[w]); big = fmaxf(big, s.wave_big[w]); }
+  if (!(best > -INFINITY)) {
+    if (!tid) answer(-1, 0, -INFINITY);
     return;
   }
-  const int top_k = a.top_k ? a.top_k[row] : a.all_top_k;
-  const float top_p = a.top_p ? a.top_p[row] : a.all_top_p, min_p = a.min_p ? a.min_p[row] : a.all_min_p;
+  if (!(temperature > 0) || top_k == 1 || top_p <= 0 || min_p > 1) {
+    // the first in order alone
+    all([&](int i, float v) { if (v == best) atomicMin(&s.at, (unsigned)i); });
+    __syncthreads();
+    if (!tid) answer((int)s.at, 1, 0.0);
+    return;
+  }
   const Weigher weigh{s.table, 1.0 / (double)temperature, best, a.shift};
-
-  // the last token that top-k and top-p keep: all whose ordered logit is above `last_key`, and of those equal to it the ones up to index `last_at`
-  unsigned last_key = 0; int last_at = 0x7FFFFFFF;
-  const bool by_k = top_k > 0 && (unsigned)top_k < there, by_p = top_p < 1.0f;
+  const bool by_p = top_p < 1.0f;
+  const double least = min_p > 0 ? ldexp((double)min_p, a.shift) : -1.0;               // of scaled weights; NaN: none
 
   // sums over the threads before this one and over all; ends with all threads past its use of LDS
   auto block_scan = [&](u64 w, unsigned c, u64* before_w, unsigned* before_c, u64* all_w, unsigned* all_c) __attribute__((always_inline)) {
@@ -176,213 +192,403 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a, Ex
     *before_w = bw + sw - w; *before_c = bc + sc - c; *all_w = aw; *all_c = ac;
     __syncthreads();
   };
+  auto sort_list = [&](int padded) {                                  // ascending
+    for (int k = 2; k <= padded; k *= 2)
+      for (int j = k / 2; j > 0; j /= 2) {
+        for (int p = tid; p < padded / 2; p += SAMPLE_THREADS) {
+          const int lo = 2 * j * (p / j) + p % j, hi = lo + j;
+          const u64 x0 = s.list[lo], x1 = s.list[hi];
+          if ((x0 > x1) == ((lo & k) == 0)) { s.list[lo] = x1; s.list[hi] = x0; }
+        }
+        __syncthreads();
+      }
+  };
+  auto logprob_of = [&](float v, u64 kept_w) { return weigh.exponent(v) - log(ldexp((double)kept_w, -a.shift)); };
 
-  u64 total = 0;                                                     // the weight that top-p takes a share of
-  if (by_k || by_p) {
-    // One border: the first token in order at which the count reaches `limit_c` (by_count), or the weight `limit_w`.  Its bin is looked for among the bins of w, then among bits of the logits, until
-    // few enough share it; those are sorted.  Returns the weight up to and with the token.
-    auto clear = [&]() { for (int b = tid; b < BINS; b += SAMPLE_THREADS) { s.weight[b] = 0; s.count[b] = 0; } __syncthreads(); };
-    auto find_bin = [&](bool by_count, unsigned limit_c, double limit_w, unsigned base_c, u64 base_w) {
-      // four bins a thread
-      u64 w = 0; unsigned c = 0;
-      for (int b = 0; b < 4; ++b) { w += s.weight[4 * tid + b]; c += s.count[4 * tid + b]; }
-      u64 bw, aw; unsigned bc, ac;
-      block_scan(w, c, &bw, &bc, &aw, &ac);
-      bw += base_w; bc += base_c;
-      if (!tid) s.bin = -1;
+  // ---- a short list -----------------------------------------------------------------------------------------------------
+  if (top_k > 0 && top_k <= LISTED) {
+    // the largest key that top_k threads reach with their own largest logit, bit by bit (0 where fewer have any)
+    unsigned floor_key = 0;
+    const unsigned own_key = own > -INFINITY ? ordered(own) : 0;
+    for (int bit = 31; bit >= 0; --bit) {
+      const unsigned probe = floor_key | 1u << bit;
+      const unsigned votes = (unsigned)__popcll(__ballot(own_key >= probe));
+      if (!lane && votes) atomicAdd(&s.votes[bit & 1], votes);
       __syncthreads();
-      const bool before = by_count ? bc < limit_c : !bc || (double)bw < limit_w, after = by_count ? bc + c >= limit_c : bc + c && (double)(bw + w) >= limit_w;
-      if (c && before && after) {
-        for (int b = 0; b < 4; ++b) {
-          const unsigned cb = s.count[4 * tid + b]; const u64 wb = s.weight[4 * tid + b];
-          if (cb && (by_count ? bc + cb >= limit_c : (double)(bw + wb) >= limit_w)) { s.bin = 4 * tid + b; s.bin_count = cb; s.before_c = bc; s.before_w = bw; break; }
-          bc += cb; bw += wb;
-        }
-      }
+      if (s.votes[bit & 1] >= (unsigned)top_k) floor_key = probe;
+      if (tid == 0) s.votes[~bit & 1] = 0;                            // the next one's: all are past it
       __syncthreads();
-    };
-    auto border = [&](bool by_count, unsigned limit_c, double limit_w) -> u64 {
-      // s.weight and s.count are over the bins of w here
-      find_bin(by_count, limit_c, limit_w, 0, 0);
-      const int w_bin = s.bin;
-      unsigned size = s.bin_count, base_c = s.before_c, mask = 0, bits = 0;
-      u64 base_w = s.before_w;
-      __syncthreads();
-      auto in_group = [&](float v, int* bin, double* w, u64* q) __attribute__((always_inline)) {
-        *q = weigh(v, bin, w);
-        return *bin == w_bin && (ordered(v) & mask) == bits;
-      };
-      for (int level = 0; size > SORTED && level < 3; ++level) {
-        const int down = level == 0 ? 20 : level == 1 ? 8 : 0, digits = level < 2 ? 4096 : 256;
-        clear();
-        all([&](int, float v) {
-          int bin; double w; u64 q;
-          if (in_group(v, &bin, &w, &q)) { const int d = digits - 1 - (int)(ordered(v) >> down & (digits - 1)); atomicAdd(&s.weight[d], q); atomicAdd(&s.count[d], 1u); }
-        });
-        __syncthreads();
-        find_bin(by_count, limit_c, limit_w, base_c, base_w);
-        bits |= (unsigned)(digits - 1 - s.bin) << down; mask |= (unsigned)(digits - 1) << down;
-        size = s.bin_count; base_c = s.before_c; base_w = s.before_w;
-        __syncthreads();
-      }
-      if (size > SORTED) {
-        // more equal logits than can be sorted: they are in the order of their indices, and all weigh the same
-        int bin; double wd;
-        const unsigned sign = bits & 0x80000000u ? bits & 0x7FFFFFFFu : ~bits;
-        const u64 q = weigh(__uint_as_float(sign), &bin, &wd);
-        unsigned m = 1;
-        if (by_count) m = limit_c - base_c;
-        else if (q) {
-          const double need = ceil((limit_w - (double)base_w) / (double)q);
-          m = need < 1 ? 1 : need > size ? size : (unsigned)need;
-        }
-        unsigned c = 0;
-        all([&](int, float v) { c += ordered(v) == bits; });
-        c = wave_sum(c);
-        u64 bw, aw; unsigned bc, ac;
-        block_scan(0, lane ? 0 : c, &bw, &bc, &aw, &ac);
-        bc = __shfl(bc, 0);
-        if (bc < m && bc + c >= m) {
-          // in this wavefront's range: vector by vector, in the order of the indices
-          for (int i = 0; i < tiles; ++i) {
-            unsigned here = 0;
-            each(mine + i * 64 * VEC, 1, 0, [&](int, float v) { here += ordered(v) == bits; });
-            const unsigned up = wave_scan(here, lane), last = __shfl(up, 63);
-            if (bc + last >= m) {
-              unsigned at = bc + up - here;
-              each(mine + i * 64 * VEC, 1, 0, [&](int index, float v) { if (ordered(v) == bits && ++at == m) s.at = (unsigned)index; });
-              break;
-            }
-            bc += last;
-          }
-        }
-        __syncthreads();
-        last_key = bits; last_at = (int)s.at;
-        __syncthreads();
-        return base_w + m * q;
-      }
-      if (!tid) s.listed = 0;
-      int padded = 2;
-      while (padded < (int)size) padded *= 2;
-      __syncthreads();
-      for (int i = tid; i < padded; i += SAMPLE_THREADS) s.list[i] = ~0ull;
-      __syncthreads();
+    }
+    if (own_key >= floor_key) {                                       // others have none
       all([&](int i, float v) {
-        int bin; double w; u64 q;
-        if (in_group(v, &bin, &w, &q)) s.list[atomicAdd(&s.listed, 1)] = (u64)~ordered(v) << 32 | (unsigned)i;      // ascending: larger logits first, equal ones by index
+        if (ordered(v) < floor_key) return;
+        const int at = atomicAdd(&s.listed, 1);
+        if (at < SORTED) s.list[at] = (u64)~ordered(v) << 32 | (unsigned)i;      // ascending: larger logits first, equal ones by index
+      });
+    }
+    __syncthreads();
+    const int listed = s.listed;
+    if (listed <= SORTED) {
+      int padded = 2;
+      while (padded < listed) padded *= 2;
+      for (int i = listed + tid; i < padded; i += SAMPLE_THREADS) s.list[i] = ~0ull;
+      __syncthreads();
+      sort_list(padded);
+      // an entry a thread
+      const int k = min(top_k, listed);
+      u64 entry = ~0ull, q = 0, bw, aw; unsigned bc, ac;
+      double w = 0.0;
+      if (tid < k) { entry = s.list[tid]; w = weigh.scaled(unordered(~(unsigned)(entry >> 32))); q = Weigher::whole(w); }
+      block_scan(q, 0, &bw, &bc, &aw, &ac);
+      const bool keep = tid < k && (!tid || ((!by_p || (double)bw < (double)top_p * (double)aw) && !(w < least)));
+      // what is kept is a beginning; in the order of the indices
+      const int kept = __syncthreads_count(keep);
+      padded = 2;
+      while (padded < kept) padded *= 2;
+      if (tid < kept) { s.list[tid] = entry << 32 | (unsigned)tid; s.weight[tid] = q; }
+      else if (tid < padded) s.list[tid] = ~0ull;
+      const unsigned key = ~(unsigned)(entry >> 32);
+      s.count[tid] = key;
+      __syncthreads();
+      sort_list(padded);
+      const u64 by_index = tid < kept ? s.list[tid] : 0;
+      const u64 qi = tid < kept ? s.weight[(unsigned)by_index] : 0;
+      block_scan(qi, 0, &bw, &bc, &aw, &ac);
+      const double target = (double)u * (double)aw;
+      if (qi && !((double)bw > target) && (double)(bw + qi) > target)
+        answer((int)(by_index >> 32), kept, logprob_of(unordered(s.count[(unsigned)by_index]), aw));
+      return;
+    }
+    __syncthreads();
+    if (!tid) s.listed = 0;
+    __syncthreads();
+  }
+
+  Last last{0, 0x7FFFFFFF};
+  u64 kept_w = 0; unsigned kept = 0;
+  bool counted = false;                                              // by the codes of bf16
+
+  // ---- codes of bf16 ------------------------------------------------------------------------------------------------------
+  // Entry j of the order: codes of positive logits from the largest down, 0 .. 2047, then of negative ones.  Codes of smaller magnitude than the 16 octaves ("tiny") lie between them; they are listed.
+  const int base = max((int)(__float_as_uint(big) >> 23) - 15, 0) << 7;         // the least code of the octaves
+  auto entry_of = [&](unsigned code) __attribute__((always_inline)) -> int {    // -1: tiny
+    const int off = (int)(code & 0x7FFF) - base;
+    return off < 0 ? -1 : code > 0x8000 ? 2048 + off : 2047 - off;              // both zeros are alike
+  };
+  auto code_of_entry = [&](int j) -> float { return __uint_as_float((unsigned)(j < 2048 ? base + 2047 - j : 0x8000 | (base + j - 2048)) << 16); };
+  unsigned ties = 0;                                                 // how many of the last code are kept
+  int last_entry = BINS;
+  u64 last_q = 0;
+  bool tiny_kept = true;
+  if constexpr (std::is_same<T, __bf16>::value) {
+    if (big < INFINITY) {
+      for (int b = tid; b < BINS; b += SAMPLE_THREADS) s.count[b] = 0;
+      __syncthreads();
+      vectors(mine, tiles, 64 * VEC, [&](int, const u32x4& v) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          const unsigned code = (e & 1 ? v[e / 2] >> 16 : v[e / 2] & 0xFFFF);
+          if ((code & 0x7FFF) > 0x7F80 || code == 0xFF80) continue;             // NaN, -infinity
+          const int j = entry_of(code);
+          if (j >= 0) { atomicAdd(&s.count[j], 1u); continue; }
+          const float t = __uint_as_float(code << 16);
+          const int at = atomicAdd(&s.listed, 1);
+          atomicAdd(&s.tiny_w, weigh(t));
+          if (at < SORTED) s.list[at] = ordered(t);
+        }
       });
       __syncthreads();
-      for (int k = 2; k <= padded; k *= 2)
-        for (int j = k / 2; j > 0; j /= 2) {
-          for (int p = tid; p < padded / 2; p += SAMPLE_THREADS) {
-            const int lo = 2 * j * (p / j) + p % j, hi = lo + j;
-            const u64 x0 = s.list[lo], x1 = s.list[hi];
-            if ((x0 > x1) == ((lo & k) == 0)) { s.list[lo] = x1; s.list[hi] = x0; }
+      const unsigned tiny_c = (unsigned)s.listed;
+      const u64 tiny_w = s.tiny_w;
+      // four entries a thread, and the tiny ones before those of thread 512
+      const int first = tid == 512 ? -1 : 0;
+      u64 q[4], w4 = tid == 512 ? tiny_w : 0; unsigned c[4], c4 = tid == 512 ? tiny_c : 0;
+      int cut = 0x7FFFFFFF;                                          // the first entry that min-p drops
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        c[e] = s.count[4 * tid + e];
+        const double w = c[e] ? weigh.scaled(code_of_entry(4 * tid + e)) : 0.0;
+        q[e] = Weigher::whole(w);
+        s.weight[4 * tid + e] = q[e];
+        w4 += q[e] * c[e]; c4 += c[e];
+        if (c[e] && w < least) cut = min(cut, 4 * tid + e);
+      }
+      if (least > 0) atomicMin(&s.cut, cut);
+      u64 bw, aw; unsigned bc, ac;
+      block_scan(w4, c4, &bw, &bc, &aw, &ac);
+      kept_w = aw; kept = ac;
+      bool fits = tiny_c <= SORTED;
+      // an entry at which the count or the weight reaches its limit becomes the last one, with as many of its tokens as that takes
+      auto border = [&](bool by_count, unsigned limit_c, double limit_w) {
+        if (!tid) s.bin = -2;
+        __syncthreads();
+        u64 w = bw; unsigned n = bc;
+        for (int e = first; e < 4; ++e) {
+          const unsigned ce = e < 0 ? tiny_c : c[e < 0 ? 0 : e];
+          const u64 all_e = e < 0 ? tiny_w : q[e < 0 ? 0 : e] * ce;
+          const bool before = by_count ? n < limit_c : !n || (double)w < limit_w, after = by_count ? n + ce >= limit_c : (double)(w + all_e) >= limit_w;
+          if (ce && before && after) { s.bin = e < 0 ? -1 : 4 * tid + e; s.before_c = n; s.before_w = w; }
+          n += ce; w += all_e;
+        }
+        __syncthreads();
+        const int j = s.bin;
+        const unsigned n0 = s.before_c; const u64 w0 = s.before_w;
+        __syncthreads();
+        if (j == -2) return;                                         // not reached: all are kept
+        if (j == -1) { fits = false; return; }
+        const unsigned ce = s.count[j]; const u64 qe = s.weight[j];
+        unsigned m = ce;
+        if (by_count) m = limit_c - n0;
+        else if (qe) {
+          const double need = ceil((limit_w - (double)w0) / (double)qe);
+          m = need < 1 ? 1 : need > ce ? ce : (unsigned)need;
+          while (m > 1 && (double)(w0 + (m - 1) * qe) >= limit_w) --m;
+          while (m < ce && (double)(w0 + m * qe) < limit_w) ++m;
+        }
+        if (j > last_entry || (j == last_entry && m >= ties)) return;
+        last_entry = j; ties = m; last_q = qe; kept_w = w0 + m * qe; kept = n0 + m;
+      };
+      if (top_k > 0) border(true, (unsigned)top_k, 0.0);
+      if (by_p) border(false, 0, (double)top_p * (double)kept_w);
+      if (least > 0) {
+        // tiny ones lie on both sides of the least weight, or all on one
+        int tiny_in = 0, tiny_out = 0;
+        for (int i = tid; i < (int)min(tiny_c, (unsigned)SORTED); i += SAMPLE_THREADS) { if (weigh.scaled(unordered((unsigned)s.list[i])) < least) tiny_out = 1; else tiny_in = 1; }
+        tiny_in = __syncthreads_or(tiny_in); tiny_out = __syncthreads_or(tiny_out);
+        const int j = min(s.cut, BINS);                              // the first counted entry that is dropped
+        if (tiny_out && tiny_in && last_entry >= 2048) fits = false;
+        const int stop = tiny_out && j > 2048 ? 2048 : j;
+        if (stop < BINS && stop <= last_entry) {
+          // everything before entry `stop` is kept
+          if (tid == stop / 4) {
+            u64 w = bw; unsigned n = bc;
+            if (tid == 512 && !tiny_out) { w += tiny_w; n += tiny_c; }
+            for (int e = 0; e < stop % 4; ++e) { w += q[e] * c[e]; n += c[e]; }
+            s.before_w = w; s.before_c = n;
           }
           __syncthreads();
+          kept_w = s.before_w; kept = s.before_c; last_entry = stop; ties = 0; last_q = 0;
+          __syncthreads();
         }
-      // two entries a thread
-      u64 q[2] = {0, 0}; unsigned c = 0;
-      for (int e = 0; e < 2; ++e) {
-        if (2 * tid + e >= (int)size) continue;
-        const unsigned key = ~(unsigned)(s.list[2 * tid + e] >> 32);
-        int bin; double w;
-        q[e] = weigh(__uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key), &bin, &w);
-        ++c;
+        if (tiny_out) tiny_kept = false;
       }
-      u64 bw, aw; unsigned bc, ac;
-      block_scan(q[0] + q[1], c, &bw, &bc, &aw, &ac);
-      bw += base_w; bc += base_c;
-      for (int e = 0; e < (int)c; ++e) {
-        const bool before = by_count ? bc < limit_c : !bc || (double)bw < limit_w;
-        ++bc; bw += q[e];
-        const bool after = by_count ? bc >= limit_c : (double)bw >= limit_w;
-        if (before && after) { s.key = ~(unsigned)(s.list[2 * tid + e] >> 32); s.at = (unsigned)s.list[2 * tid + e]; s.before_w = bw; }
+      if (last_entry < 2048) tiny_kept = false;
+      if (fits) {
+        // weights of what is not kept, and of the last code, whose tokens are counted, become none
+        for (int j = tid; j < BINS; j += SAMPLE_THREADS) if (j >= last_entry) s.weight[j] = 0;
+        counted = true;
       }
       __syncthreads();
-      last_key = s.key; last_at = (int)s.at;
-      const u64 sum = s.before_w;
-      __syncthreads();
-      return sum;
-    };
-    auto histogram = [&]() {
-      clear();
-      all([&](int, float v) {
-        int bin; double w;
-        const u64 q = weigh(v, &bin, &w);
-        atomicAdd(&s.weight[bin], q);
-        atomicAdd(&s.count[bin], 1u);
-      });
-      __syncthreads();
-    };
-    histogram();
-    {
-      u64 w = 0, bw; unsigned bc, ac;
-      for (int b = 0; b < 4; ++b) w += s.weight[4 * tid + b];
-      block_scan(w, 0, &bw, &bc, &total, &ac);
-    }
-    if (by_k) total = border(true, (unsigned)top_k, 0.0);
-    if (by_p) {
-      const unsigned k_key = last_key; const int k_at = last_at;
-      if (by_k) histogram();                                         // the border's own histograms may have taken their place
-      border(false, 0u, (double)top_p * (double)total);
-      // of two beginnings the shorter one
-      if (by_k && (k_key > last_key || (k_key == last_key && k_at < last_at))) { last_key = k_key; last_at = k_at; }
+      if (!fits) { kept_w = 0; kept = 0; if (!tid) s.listed = 0; __syncthreads(); }
     }
   }
 
-  // kept weights by ranges of positions
-  auto keeps = [&](int i, float v, double w) __attribute__((always_inline)) {
-    const unsigned key = ordered(v);
-    return (key > last_key || (key == last_key && i <= last_at)) && (!(w < (double)min_p) || i == best_at);
+  if (!counted) {
+    // ---- histograms of weights ------------------------------------------------------------------------------------------------
+    if (top_k > 0 || by_p) {
+      // One border: the first token in order at which the count reaches `limit_c` (by_count), or the weight `limit_w`.  Its bin is looked for among the bins of w, then among bits of the
+      // logits, until few enough share it; those are sorted.  Returns the weight up to and with the token; all of it where the limit is not reached.
+      auto clear = [&]() { for (int b = tid; b < BINS; b += SAMPLE_THREADS) { s.weight[b] = 0; s.count[b] = 0; } __syncthreads(); };
+      auto find_bin = [&](bool by_count, unsigned limit_c, double limit_w, unsigned base_c, u64 base_w) {
+        // four bins a thread
+        u64 w = 0; unsigned c = 0;
+        for (int b = 0; b < 4; ++b) { w += s.weight[4 * tid + b]; c += s.count[4 * tid + b]; }
+        u64 bw, aw; unsigned bc, ac;
+        block_scan(w, c, &bw, &bc, &aw, &ac);
+        bw += base_w; bc += base_c;
+        if (!tid) { s.bin = -1; s.before_w = aw; }
+        __syncthreads();
+        const bool before = by_count ? bc < limit_c : !bc || (double)bw < limit_w, after = by_count ? bc + c >= limit_c : bc + c && (double)(bw + w) >= limit_w;
+        if (c && before && after) {
+          for (int b = 0; b < 4; ++b) {
+            const unsigned cb = s.count[4 * tid + b]; const u64 wb = s.weight[4 * tid + b];
+            if (cb && (by_count ? bc + cb >= limit_c : (double)(bw + wb) >= limit_w)) { s.bin = 4 * tid + b; s.bin_count = cb; s.before_c = bc; s.before_w = bw; break; }
+            bc += cb; bw += wb;
+          }
+        }
+        __syncthreads();
+      };
+      auto border = [&](bool by_count, unsigned limit_c, double limit_w) -> u64 {
+        // s.weight and s.count are over the bins of w here
+        find_bin(by_count, limit_c, limit_w, 0, 0);
+        const int w_bin = s.bin;
+        unsigned size = s.bin_count, base_c = s.before_c, mask = 0, bits = 0;
+        u64 base_w = s.before_w;
+        __syncthreads();
+        if (w_bin < 0) return base_w;
+        auto in_group = [&](float v) __attribute__((always_inline)) { return (ordered(v) & mask) == bits && weigh.bin(v) == w_bin; };
+        for (int level = 0; size > SORTED && level < 3; ++level) {
+          const int down = level == 0 ? 20 : level == 1 ? 8 : 0, digits = level < 2 ? 4096 : 256;
+          clear();
+          all([&](int, float v) {
+            if (in_group(v)) { const int d = digits - 1 - (int)(ordered(v) >> down & (digits - 1)); atomicAdd(&s.weight[d], weigh(v)); atomicAdd(&s.count[d], 1u); }
+          });
+          __syncthreads();
+          find_bin(by_count, limit_c, limit_w, base_c, base_w);
+          bits |= (unsigned)(digits - 1 - s.bin) << down; mask |= (unsigned)(digits - 1) << down;
+          size = s.bin_count; base_c = s.before_c; base_w = s.before_w;
+          __syncthreads();
+        }
+        if (size > SORTED) {
+          // more equal logits than can be sorted: they are in the order of their indices, and all weigh the same
+          const u64 q = weigh(unordered(bits));
+          unsigned m = 1;
+          if (by_count) m = limit_c - base_c;
+          else if (q) {
+            const double need = ceil((limit_w - (double)base_w) / (double)q);
+            m = need < 1 ? 1 : need > size ? size : (unsigned)need;
+            while (m > 1 && (double)(base_w + (m - 1) * q) >= limit_w) --m;
+            while (m < size && (double)(base_w + m * q) < limit_w) ++m;
+          }
+          unsigned c = 0;
+          all([&](int, float v) { c += ordered(v) == bits; });
+          c = wave_sum(c);
+          u64 bw, aw; unsigned bc, ac;
+          block_scan(0, lane ? 0 : c, &bw, &bc, &aw, &ac);
+          bc = __shfl(bc, 0);
+          if (bc < m && bc + c >= m) {
+            // in this wavefront's range: vector by vector, in the order of the indices
+            for (int i = 0; i < tiles; ++i) {
+              unsigned here = 0;
+              each(mine + i * 64 * VEC, 1, 0, [&](int, float v) { here += ordered(v) == bits; });
+              const unsigned up = wave_scan(here, lane), sum = __shfl(up, 63);
+              if (bc + sum >= m) {
+                unsigned at = bc + up - here;
+                each(mine + i * 64 * VEC, 1, 0, [&](int index, float v) { if (ordered(v) == bits && ++at == m) s.at = (unsigned)index; });
+                break;
+              }
+              bc += sum;
+            }
+          }
+          __syncthreads();
+          last = Last{bits, (int)s.at};
+          __syncthreads();
+          return base_w + m * q;
+        }
+        if (!tid) s.listed = 0;
+        int padded = 2;
+        while (padded < (int)size) padded *= 2;
+        for (int i = tid; i < padded; i += SAMPLE_THREADS) s.list[i] = ~0ull;
+        __syncthreads();
+        all([&](int i, float v) { if (in_group(v)) s.list[atomicAdd(&s.listed, 1)] = (u64)~ordered(v) << 32 | (unsigned)i; });      // larger logits first, equal ones by index
+        __syncthreads();
+        sort_list(padded);
+        // two entries a thread
+        u64 q[2] = {0, 0}; unsigned c = 0;
+        for (int e = 0; e < 2; ++e) if (2 * tid + e < (int)size) { q[e] = weigh(unordered(~(unsigned)(s.list[2 * tid + e] >> 32))); ++c; }
+        u64 bw, aw; unsigned bc, ac;
+        block_scan(q[0] + q[1], c, &bw, &bc, &aw, &ac);
+        bw += base_w; bc += base_c;
+        for (int e = 0; e < (int)c; ++e) {
+          const bool before = by_count ? bc < limit_c : !bc || (double)bw < limit_w;
+          ++bc; bw += q[e];
+          const bool after = by_count ? bc >= limit_c : (double)bw >= limit_w;
+          if (before && after) { s.key = ~(unsigned)(s.list[2 * tid + e] >> 32); s.at = (unsigned)s.list[2 * tid + e]; s.before_w = bw; }
+        }
+        __syncthreads();
+        last = Last{s.key, (int)s.at};
+        const u64 sum = s.before_w;
+        __syncthreads();
+        return sum;
+      };
+      auto histogram = [&]() {
+        clear();
+        all([&](int, float v) {
+          const double e = weigh.exponent(v);
+          const int k = weigh.steps(e), bin = weigh.bin_of(k);
+          atomicAdd(&s.weight[bin], Weigher::whole(weigh.scaled(e, k)));
+          atomicAdd(&s.count[bin], 1u);
+        });
+        __syncthreads();
+      };
+      histogram();
+      u64 total = 0;                                                 // the weight that top-p takes a share of
+      if (top_k > 0) {
+        total = border(true, (unsigned)top_k, 0.0);
+      } else {
+        u64 w = 0, bw; unsigned bc, ac;
+        for (int b = 0; b < 4; ++b) w += s.weight[4 * tid + b];
+        block_scan(w, 0, &bw, &bc, &total, &ac);
+      }
+      if (by_p) {
+        const Last k_last = last;
+        if (top_k > 0) histogram();                                  // the border's own histograms may have taken their place
+        border(false, 0u, (double)top_p * (double)total);
+        // of two beginnings the shorter one
+        if (top_k > 0 && (k_last.key > last.key || (k_last.key == last.key && k_last.at < last.at))) last = k_last;
+      }
+    }
+  }
+
+  // ---- the draw -------------------------------------------------------------------------------------------------------------
+  // Weights of what is kept by ranges of positions; f(index, logit, weight) in a lane's own order.  Where codes were counted, tokens of the last code come with ~0 for their weight: the
+  // first `ties` of them by index are kept.
+  auto weights = [&](int from, int count, int stride, auto&& f) __attribute__((always_inline)) {
+    if constexpr (std::is_same<T, __bf16>::value) {
+      if (counted) {
+        vectors(from, count, stride, [&](int p, const u32x4& v) __attribute__((always_inline)) {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) {
+            const unsigned code = (e & 1 ? v[e / 2] >> 16 : v[e / 2] & 0xFFFF);
+            if ((code & 0x7FFF) > 0x7F80 || code == 0xFF80) continue;
+            const int j = entry_of(code);
+            const float value16 = __uint_as_float(code << 16);
+            if (j >= 0) f(p + e - skew, value16, j == last_entry ? ~0ull : s.weight[j]);
+            else if (tiny_kept) f(p + e - skew, value16, weigh(value16));
+          }
+        });
+        return;
+      }
+    }
+    each(from, count, stride, [&](int i, float v) __attribute__((always_inline)) {
+      const unsigned key = ordered(v);
+      if (key < last.key || (key == last.key && i > last.at)) return;
+      const double w = weigh.scaled(v);
+      if (!(w < least)) f(i, v, Weigher::whole(w));
+    });
   };
-  u64 sum = 0; unsigned count = 0;
-  all([&](int i, float v) {
-    int bin; double w;
-    const u64 q = weigh(v, &bin, &w);
-    if (keeps(i, v, w)) { sum += q; ++count; }
+  u64 sum = 0; unsigned count = 0;                                   // count: of what is kept, or of the last code
+  weights(mine, tiles, 64 * VEC, [&](int, float, u64 q) __attribute__((always_inline)) {
+    if (counted) { if (q == ~0ull) ++count; else sum += q; }
+    else { sum += q; ++count; }
   });
   sum = wave_sum(sum); count = wave_sum(count);
   if (!lane) { s.wave_w[wave] = sum; s.wave_c[wave] = count; }
   __syncthreads();
-  u64 kept_w = 0; unsigned kept = 0;
-  for (int w = 0; w < SAMPLE_WAVES; ++w) { kept_w += s.wave_w[w]; kept += s.wave_c[w]; }
-  const float u = fminf(fmaxf(a.u[row], 0.f), 0.99999994f);
+  if (!counted) for (int w = 0; w < SAMPLE_WAVES; ++w) { kept_w += s.wave_w[w]; kept += s.wave_c[w]; }
   const double target = (double)u * (double)kept_w;
-  u64 before = 0; int range = 0;
+  // weight up to a point: w of other tokens and n of the last code
+  auto weight_of = [&](u64 w, unsigned n) { return counted ? w + (u64)min(n, ties) * last_q : w; };
+  u64 before = 0; unsigned before_n = 0; int range = 0;
   for (; range < SAMPLE_WAVES - 1; ++range) {
-    if ((double)(before + s.wave_w[range]) > target) break;
-    before += s.wave_w[range];
+    const u64 w = before + s.wave_w[range]; const unsigned n = before_n + s.wave_c[range];
+    if ((double)weight_of(w, n) > target) break;
+    before = w; before_n = n;
   }
-  if (!tid) s.token = -1;
   __syncthreads();
   // the range that the target is in, in pieces of neighbouring vectors of all threads
-  for (int p0 = range * tiles * 64 * VEC; p0 < (range + 1) * tiles * 64 * VEC; p0 += SAMPLE_THREADS * VEC) {
-    const bool in = p0 + tid * VEC < (range + 1) * tiles * 64 * VEC;
-    u64 here = 0;
-    if (in) each(p0 + tid * VEC, 1, 0, [&](int i, float v) { int bin; double w; const u64 q = weigh(v, &bin, &w); if (keeps(i, v, w)) here += q; });
-    u64 bw, aw; unsigned bc, ac;
-    block_scan(here, 0, &bw, &bc, &aw, &ac);
-    bw += before;
-    if (in && here && !((double)bw > target) && (double)(bw + here) > target) {
+  for (int p0 = range * range_len; p0 < (range + 1) * range_len; p0 += SAMPLE_THREADS * VEC) {
+    const bool in = p0 + tid * VEC < (range + 1) * range_len;
+    u64 here = 0; unsigned here_n = 0;
+    if (in) weights(p0 + tid * VEC, 1, 0, [&](int, float, u64 q) { if (counted && q == ~0ull) ++here_n; else here += q; });
+    u64 bw, aw; unsigned bn, an;
+    block_scan(here, here_n, &bw, &bn, &aw, &an);
+    bw += before; bn += before_n;
+    if (in && !((double)weight_of(bw, bn) > target) && (double)weight_of(bw + here, bn + here_n) > target) {
       bool found = false;
-      each(p0 + tid * VEC, 1, 0, [&](int i, float v) {
-        int bin; double w;
-        const u64 q = weigh(v, &bin, &w);
-        if (!keeps(i, v, w) || found) return;
-        bw += q;
-        if ((double)bw > target) {
+      weights(p0 + tid * VEC, 1, 0, [&](int i, float v, u64 q) {
+        if (found) return;
+        if (counted && q == ~0ull) ++bn; else bw += q;
+        if ((double)weight_of(bw, bn) > target) {
           found = true;
           s.token = i;
-          a.token[row] = i;
-          if (a.kept) a.kept[row] = (int)kept;
-          if (a.logprob) a.logprob[row] = (float)((v == best ? 0.0 : ((double)v - (double)best) * weigh.inverse) - log(ldexp((double)kept_w, -a.shift)));
+          answer(i, (int)kept, logprob_of(v, kept_w));
         }
       });
     }
     __syncthreads();
     if (s.token >= 0) return;
-    before += aw;
+    before += aw; before_n += an;
   }
 }
 
@@ -406,11 +612,10 @@ extern "C" octo_status octo_op_sample(const octo_sample_op* op, void* hip_stream
   int bits = 0;
   while ((1 << bits) < op->vocab) ++bits;
   a.shift = 62 - bits < 50 ? 62 - bits : 50;                         // a sum of `vocab` weights of up to one stays within 63 bits
-  static const ExpTable table = exp_table();
   hipStream_t s = (hipStream_t)hip_stream;
   const dim3 grid((unsigned)op->n), block(SAMPLE_THREADS);
-  if (op->dtype == OCTO_F32) hipLaunchKernelGGL(sample_kernel<float>, grid, block, 0, s, a, table);
-  else if (op->dtype == OCTO_F16) hipLaunchKernelGGL(sample_kernel<_Float16>, grid, block, 0, s, a, table);
-  else hipLaunchKernelGGL(sample_kernel<__bf16>, grid, block, 0, s, a, table);
+  if (op->dtype == OCTO_F32) hipLaunchKernelGGL(sample_kernel<float>, grid, block, 0, s, a);
+  else if (op->dtype == OCTO_F16) hipLaunchKernelGGL(sample_kernel<_Float16>, grid, block, 0, s, a);
+  else hipLaunchKernelGGL(sample_kernel<__bf16>, grid, block, 0, s, a);
   return hipGetLastError() == hipSuccess ? OCTO_OK : OCTO_EHIP;
 }

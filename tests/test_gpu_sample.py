@@ -135,6 +135,42 @@ def test_a_long_flat_tail(octo):
         _check(_run(octo, logits, u, **settings), logits, u, settings)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_both_zeros_and_tiny_logits(octo, dtype):
+    """Zeros of both signs are equal logits; magnitudes far below the largest one's lie between positive and negative ones."""
+    import torch
+    g = torch.Generator().manual_seed(6)
+    n, vocab = 12, 5000
+    x = torch.randn(n, vocab, generator=g)
+    x[0::4] = torch.where(torch.rand(3, vocab, generator=g) < 0.5, 0.0, -0.0)
+    x[0::4, ::997] = 1.0
+    small = torch.randn(3, vocab, generator=g) * 2.0 ** -20
+    x[1::4] = torch.where(torch.rand(3, vocab, generator=g) < 0.3, small, x[1::4])
+    x[2::4] *= 2.0 ** -14                                       # all small: octaves follow the largest magnitude
+    x[3::4] = -x[3::4].abs() - 0.5
+    logits = x.to(_t(dtype)).cuda()
+    u = torch.rand(n, generator=g).cuda()
+    for settings in ({}, dict(top_k=700), dict(top_k=3000, top_p=0.9), dict(temperature=0.8, top_p=0.45), dict(top_p=0.62), dict(min_p=0.1), dict(min_p=0.999), dict(temperature=1e-3, top_p=0.97), dict(top_k=9), dict(top_k=2500, min_p=0.2)):
+        _check(_run(octo, logits, u, **settings), logits, u, settings)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("min_p", [0.02, 0.3, 0.9])
+def test_what_min_p_drops(octo, dtype, min_p):
+    """Borders of min-p at, above and below logits of no magnitude, alone and beside the others."""
+    import torch
+    base = [3.0, 1.5, 0.25, 2.0 ** -22, 0.0, -(2.0 ** -23), -0.25, -1.5, -4.0]
+    rows = [torch.tensor(base).repeat(400)] + [torch.tensor(base[i:]).repeat(400)[:2000] for i in (1, 2, 3, 4, 6)] + [torch.tensor([1.5, 2.0 ** -22, -1.5]).repeat(900)]
+    n = max(len(r) for r in rows)
+    logits = torch.full((len(rows), n), -math.inf)
+    for i, r in enumerate(rows):
+        logits[i, :len(r)] = r
+    logits = logits.to(_t(dtype)).cuda()
+    u = torch.linspace(0.03, 0.97, len(rows)).cuda()
+    for settings in (dict(min_p=min_p), dict(min_p=min_p, top_k=1100), dict(min_p=min_p, top_p=0.6), dict(min_p=min_p, top_k=1500, top_p=0.83, temperature=0.7)):
+        _check(_run(octo, logits, u, **settings), logits, u, settings)
+
+
 def test_infinities(octo):
     import torch
     x = torch.randn(4, 500).cuda()
