@@ -40,29 +40,43 @@ __device__ __forceinline__ unsigned ordered(float v) {
 __device__ __forceinline__ float unordered(unsigned k) { return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k); }
 
 constexpr int STEPS = 1024;    // of an octave
+// 2^(j / STEPS) by the exponential's series, rounded a few times
+struct Octave { double v[STEPS]; };
+constexpr Octave make_octave() {
+  Octave o{};
+  for (int j = 0; j < STEPS; ++j) {
+    const double x = j * (0.69314718055994530942 / STEPS);
+    double sum = 1.0;
+    for (int n = 24; n > 0; --n) sum = 1.0 + sum * x / n;
+    o.v[j] = sum;
+  }
+  return o;
+}
+__device__ const Octave octave = make_octave();
+// w of a logit in units of 2^-shift.  The exponent t is in steps of an octave, in fp64: its nearest integer picks w from the table, what is left, at most half a step, a factor 1 + eps that
+// fp32 holds to 2^-35 of w.
 struct Weigher {
   const double* table;      // 2^(j / STEPS), in LDS
-  double inverse;           // 1 / temperature
-  float max;
+  double best, factor;      // t = (v - best) factor
   int shift;
-  // (v - max) / temperature
-  __device__ __forceinline__ double exponent(float v) const {
-    const double x = v == max ? 0.0 : ((double)v - (double)max) * inverse;
-    return fmax(x, -50.0);                                           // e^-50 < 2^-72; also where it is no number (an infinite maximum, an infinite temperature)
+  static constexpr u64 ZERO = 0x4330000000000000ull;                 // 2^52: integers added to it lie in its low bits
+  __device__ __forceinline__ double steps(float v) const {
+    return fmax(((double)v - best) * factor, -73728.0);           // 72 octaves down nothing is left; also for what is no number (-infinity, NaN, at an infinite temperature too)
   }
-  __device__ __forceinline__ int steps(double x) const { return (int)rint(x * 1477.3197218702985); }       // STEPS / ln 2
-  __device__ __forceinline__ int bin_of(int k) const { return min(-k >> 4, BINS - 1); }
-  __device__ __forceinline__ int bin(float v) const { return bin_of(steps(exponent(v))); }
-  // w times 2^shift
-  __device__ __forceinline__ double scaled(double x, int k) const {
-    const double r = fma((double)k, -0.0006769015435155716, x);      // ln 2 / STEPS; r is at most half of that
-    const double p = fma(fma(fma(r, 1.0 / 6, 0.5), r, 1.0), r, 1.0);
-    return ldexp(p * table[k & (STEPS - 1)], (k >> 10) + shift);
+  __device__ __forceinline__ double scaled(double t, int* k) const {
+    const double m = t + 6755399441055744.0;                         // 1.5 * 2^52: the nearest integer is in the low bits
+    *k = (int)__double_as_longlong(m);
+    const float f = (float)(t - (m - 6755399441055744.0));
+    const float eps = f * fmaf(f, fmaf(f, 5.1696e-11f, 2.29097850e-7f), 6.76901543e-4f);         // 2^(f / STEPS) - 1, coefficients (ln 2 / STEPS)^n / n!
+    const double w = __longlong_as_double(__double_as_longlong(table[*k & (STEPS - 1)]) + ((long long)((*k >> 10) + shift) << 52));
+    return fma(w, (double)eps, w);
   }
-  __device__ __forceinline__ double scaled(float v) const { const double x = exponent(v); return scaled(x, steps(x)); }
-  // the nearest integer: adding 2^52 leaves it in the low bits
-  static __device__ __forceinline__ u64 whole(double w) { return (u64)__double_as_longlong(w + 4503599627370496.0) - 0x4330000000000000ull; }
+  __device__ __forceinline__ double scaled(float v) const { int k; return scaled(steps(v), &k); }
+  static __device__ __forceinline__ u64 bits(double w) { return (u64)__double_as_longlong(w + 4503599627370496.0); }      // ZERO + the nearest integer
+  static __device__ __forceinline__ u64 whole(double w) { return bits(w) - ZERO; }
   __device__ __forceinline__ u64 operator()(float v) const { return whole(scaled(v)); }
+  static __device__ __forceinline__ int bin_of(int k) { return min(-k >> 4, BINS - 1); }
+  __device__ __forceinline__ int bin(float v) const { return bin_of((int)__double_as_longlong(steps(v) + 6755399441055744.0)); }
 };
 
 template <typename V> __device__ __forceinline__ V wave_sum(V v) {
@@ -84,7 +98,7 @@ struct SampleShared {
   u64 wave_w[SAMPLE_WAVES];
   unsigned wave_c[SAMPLE_WAVES];
   float wave_max[SAMPLE_WAVES], wave_big[SAMPLE_WAVES];
-  unsigned votes[2];
+  unsigned votes[3];
   int listed, bin, token, cut;
   unsigned bin_count, key, at, before_c;
   u64 before_w, tiny_w;
@@ -110,11 +124,19 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
   const int skew = (int)(((uintptr_t)x & 15) / sizeof(T)), end = a.vocab + skew;
   const int tiles = (end + SAMPLE_WAVES * 64 * VEC - 1) / (SAMPLE_WAVES * 64 * VEC);                 // vectors of a lane
   const int range_len = tiles * 64 * VEC;                                                            // positions of a wavefront
+  bool odd = false;
   auto load = [&](int p) __attribute__((always_inline)) -> u32x4 {
     u32x4 v;
-    if (p >= skew && p + VEC <= end) return *(const u32x4*)(x + (p - skew));
+    if (p >= skew && p + VEC <= end) {
+      v = *(const u32x4*)(x + (p - skew));
+    } else {
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) ((T*)&v)[e] = p + e >= skew && p + e < end ? x[p + e - skew] : (T)-INFINITY;
+      for (int e = 0; e < VEC; ++e) ((T*)&v)[e] = p + e >= skew && p + e < end ? x[p + e - skew] : (T)-INFINITY;
+    }
+    if (odd) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) { const float f = (float)((T*)&v)[e]; ((T*)&v)[e] = (T)(f == INFINITY ? 0.f : f > -INFINITY ? -1.f : -INFINITY); }
+    }
     return v;
   };
   // f(position, vector) of the positions from, from + stride ...
@@ -146,6 +168,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
     if (a.logprob) a.logprob[row] = (float)logprob;
   };
 
+  s.table[tid] = octave.v[tid];
   // the largest logit, of this thread and of all, and the largest magnitude
   float own = -INFINITY, big = 0.f;
   vectors(mine, tiles, 64 * VEC, [&](int, const u32x4& v) __attribute__((always_inline)) {
@@ -160,8 +183,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) { best = fmaxf(best, __shfl_xor(best, d)); big = fmaxf(big, __shfl_xor(big, d)); }
   if (!lane) { s.wave_max[wave] = best; s.wave_big[wave] = big; }
-  if (tid == 0) { s.listed = 0; s.at = 0x7FFFFFFF; s.token = -1; s.cut = 0x7FFFFFFF; s.tiny_w = 0; s.votes[0] = s.votes[1] = 0; }
-  if (tid < STEPS) s.table[tid] = exp2(tid * (1.0 / STEPS));
+  if (tid == 0) { s.listed = 0; s.at = 0x7FFFFFFF; s.token = -1; s.cut = 0x7FFFFFFF; s.tiny_w = 0; s.votes[0] = s.votes[1] = s.votes[2] = 0; }
   __syncthreads();
   for (int w = 0; w < SAMPLE_WAVES; ++w) { best = fmaxf(best, s.wave_max[w]); big = fmaxf(big, s.wave_big[w]); }
   if (!(best > -INFINITY)) {
@@ -175,7 +197,11 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
     if (!tid) answer((int)s.at, 1, 0.0);
     return;
   }
-  const Weigher weigh{s.table, 1.0 / (double)temperature, best, a.shift};
+  // A row with infinite logits is one of zeros and ones: those weigh 1, the others that may be drawn nothing.
+  odd = best == INFINITY;
+  if (odd) { best = 0.f; own = own == INFINITY ? 0.f : own > -INFINITY ? -1.f : -INFINITY; }
+  const double factor = odd ? 1e6 : (double)STEPS * 1.4426950408889634 / (double)temperature;
+  const Weigher weigh{s.table, (double)best, factor, a.shift};
   const bool by_p = top_p < 1.0f;
   const double least = min_p > 0 ? ldexp((double)min_p, a.shift) : -1.0;               // of scaled weights; NaN: none
 
@@ -192,32 +218,33 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
     *before_w = bw + sw - w; *before_c = bc + sc - c; *all_w = aw; *all_c = ac;
     __syncthreads();
   };
-  auto sort_list = [&](int padded) {                                  // ascending
-    for (int k = 2; k <= padded; k *= 2)
-      for (int j = k / 2; j > 0; j /= 2) {
-        for (int p = tid; p < padded / 2; p += SAMPLE_THREADS) {
-          const int lo = 2 * j * (p / j) + p % j, hi = lo + j;
+  auto sort_list = [&](int log2_padded) {                             // ascending
+    for (int lk = 1; lk <= log2_padded; ++lk)
+      for (int lj = lk - 1; lj >= 0; --lj) {
+        for (int p = tid; p < 1 << (log2_padded - 1); p += SAMPLE_THREADS) {
+          const int lo = p >> lj << (lj + 1) | (p & ((1 << lj) - 1)), hi = lo + (1 << lj);
           const u64 x0 = s.list[lo], x1 = s.list[hi];
-          if ((x0 > x1) == ((lo & k) == 0)) { s.list[lo] = x1; s.list[hi] = x0; }
+          if ((x0 > x1) == ((lo >> lk & 1) == 0)) { s.list[lo] = x1; s.list[hi] = x0; }
         }
         __syncthreads();
       }
   };
-  auto logprob_of = [&](float v, u64 kept_w) { return weigh.exponent(v) - log(ldexp((double)kept_w, -a.shift)); };
+  auto logprob_of = [&](float v, u64 kept_w) { return weigh.steps(v) * (0.69314718055994530942 / STEPS) - log(ldexp((double)kept_w, -a.shift)); };
 
   // ---- a short list -----------------------------------------------------------------------------------------------------
   if (top_k > 0 && top_k <= LISTED) {
-    // the largest key that top_k threads reach with their own largest logit, bit by bit (0 where fewer have any)
+    // the largest key of 20 bits that top_k threads reach with their own largest logit, bit by bit (0 where fewer have any)
     unsigned floor_key = 0;
     const unsigned own_key = own > -INFINITY ? ordered(own) : 0;
-    for (int bit = 31; bit >= 0; --bit) {
+    for (int bit = 31, slot = 0; bit >= 12; --bit) {
       const unsigned probe = floor_key | 1u << bit;
       const unsigned votes = (unsigned)__popcll(__ballot(own_key >= probe));
-      if (!lane && votes) atomicAdd(&s.votes[bit & 1], votes);
+      if (!lane && votes) atomicAdd(&s.votes[slot], votes);
+      const int next = slot == 2 ? 0 : slot + 1;
       __syncthreads();
-      if (s.votes[bit & 1] >= (unsigned)top_k) floor_key = probe;
-      if (tid == 0) s.votes[~bit & 1] = 0;                            // the next one's: all are past it
-      __syncthreads();
+      if (s.votes[slot] >= (unsigned)top_k) floor_key = probe;
+      if (!tid) s.votes[next == 2 ? 0 : next + 1] = 0;                // two rounds on; all have read it
+      slot = next;
     }
     if (own_key >= floor_key) {                                       // others have none
       all([&](int i, float v) {
@@ -229,9 +256,44 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
     __syncthreads();
     const int listed = s.listed;
     if (listed <= SORTED) {
-      int padded = 2;
-      while (padded < listed) padded *= 2;
-      for (int i = listed + tid; i < padded; i += SAMPLE_THREADS) s.list[i] = ~0ull;
+      const double limit = by_p ? (double)top_p : 2.0;
+      if (listed <= 256) {
+        // Few: places in the order and sums before an entry are counted, four threads an entry.
+        const int i = tid & 255, part = tid >> 8;
+        const u64 entry = i < listed ? s.list[i] : ~0ull;
+        const float v = unordered(~(unsigned)(entry >> 32));
+        const double w = i < listed ? weigh.scaled(v) : 0.0;
+        const u64 q = i < listed ? Weigher::whole(w) : 0;
+        if (tid < 256) { s.weight[i] = q; s.weight[256 + i] = 0; s.count[i] = 0; }
+        __syncthreads();
+        unsigned place = 0; u64 before = 0;
+        for (int j = part; j < listed; j += 4) if (s.list[j] < entry) { ++place; before += s.weight[j]; }
+        if (place) { atomicAdd(&s.count[i], place); atomicAdd(&s.weight[256 + i], before); }
+        __syncthreads();
+        place = s.count[i]; before = s.weight[256 + i];
+        const bool chosen = tid < listed && place < (unsigned)top_k;
+        u64 sum = wave_sum(chosen ? q : 0);
+        if (!lane) s.wave_w[wave] = sum;
+        __syncthreads();
+        sum = s.wave_w[0] + s.wave_w[1] + s.wave_w[2] + s.wave_w[3];
+        const bool keep = chosen && (!place || ((double)before < limit * (double)sum && (!(w < least) || v == best)));
+        if (tid < 256) { s.weight[i] = keep ? q : 0; s.weight[256 + i] = 0; }
+        const int kept = __syncthreads_count(keep);
+        before = 0;
+        for (int j = part; j < listed; j += 4) if ((unsigned)s.list[j] < (unsigned)entry) before += s.weight[j];
+        if (before) atomicAdd(&s.weight[256 + i], before);
+        sum = wave_sum(keep ? q : 0);
+        if (!lane) s.wave_w[wave] = sum;
+        __syncthreads();
+        sum = s.wave_w[0] + s.wave_w[1] + s.wave_w[2] + s.wave_w[3];
+        before = s.weight[256 + i];
+        const double target = (double)u * (double)sum;
+        if (keep && !((double)before > target) && (double)(before + q) > target) answer((int)(unsigned)entry, kept, logprob_of(v, sum));
+        return;
+      }
+      int padded = 1;
+      while (1 << padded < listed) ++padded;
+      for (int i = listed + tid; i < 1 << padded; i += SAMPLE_THREADS) s.list[i] = ~0ull;
       __syncthreads();
       sort_list(padded);
       // an entry a thread
@@ -240,13 +302,13 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       double w = 0.0;
       if (tid < k) { entry = s.list[tid]; w = weigh.scaled(unordered(~(unsigned)(entry >> 32))); q = Weigher::whole(w); }
       block_scan(q, 0, &bw, &bc, &aw, &ac);
-      const bool keep = tid < k && (!tid || ((!by_p || (double)bw < (double)top_p * (double)aw) && !(w < least)));
+      const bool keep = tid < k && (!tid || ((double)bw < limit * (double)aw && (!(w < least) || (unsigned)~(unsigned)(entry >> 32) == ordered(best))));
       // what is kept is a beginning; in the order of the indices
       const int kept = __syncthreads_count(keep);
-      padded = 2;
-      while (padded < kept) padded *= 2;
+      padded = 1;
+      while (1 << padded < kept) ++padded;
       if (tid < kept) { s.list[tid] = entry << 32 | (unsigned)tid; s.weight[tid] = q; }
-      else if (tid < padded) s.list[tid] = ~0ull;
+      else if (tid < 1 << padded) s.list[tid] = ~0ull;
       const unsigned key = ~(unsigned)(entry >> 32);
       s.count[tid] = key;
       __syncthreads();
@@ -281,7 +343,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
   u64 last_q = 0;
   bool tiny_kept = true;
   if constexpr (std::is_same<T, __bf16>::value) {
-    if (big < INFINITY) {
+    if (!odd && big < INFINITY && (by_p || top_k > 0)) {
       for (int b = tid; b < BINS; b += SAMPLE_THREADS) s.count[b] = 0;
       __syncthreads();
       vectors(mine, tiles, 64 * VEC, [&](int, const u32x4& v) __attribute__((always_inline)) {
@@ -311,7 +373,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
         q[e] = Weigher::whole(w);
         s.weight[4 * tid + e] = q[e];
         w4 += q[e] * c[e]; c4 += c[e];
-        if (c[e] && w < least) cut = min(cut, 4 * tid + e);
+        if (c[e] && w < least && code_of_entry(4 * tid + e) != best) cut = min(cut, 4 * tid + e);
       }
       if (least > 0) atomicMin(&s.cut, cut);
       u64 bw, aw; unsigned bc, ac;
@@ -353,7 +415,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       if (least > 0) {
         // tiny ones lie on both sides of the least weight, or all on one
         int tiny_in = 0, tiny_out = 0;
-        for (int i = tid; i < (int)min(tiny_c, (unsigned)SORTED); i += SAMPLE_THREADS) { if (weigh.scaled(unordered((unsigned)s.list[i])) < least) tiny_out = 1; else tiny_in = 1; }
+        for (int i = tid; i < (int)min(tiny_c, (unsigned)SORTED); i += SAMPLE_THREADS) { const float t = unordered((unsigned)s.list[i]); if (weigh.scaled(t) < least && t != best) tiny_out = 1; else tiny_in = 1; }
         tiny_in = __syncthreads_or(tiny_in); tiny_out = __syncthreads_or(tiny_out);
         const int j = min(s.cut, BINS);                              // the first counted entry that is dropped
         if (tiny_out && tiny_in && last_entry >= 2048) fits = false;
@@ -466,9 +528,9 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
           return base_w + m * q;
         }
         if (!tid) s.listed = 0;
-        int padded = 2;
-        while (padded < (int)size) padded *= 2;
-        for (int i = tid; i < padded; i += SAMPLE_THREADS) s.list[i] = ~0ull;
+        int padded = 1;
+        while (1 << padded < (int)size) ++padded;
+        for (int i = tid; i < 1 << padded; i += SAMPLE_THREADS) s.list[i] = ~0ull;
         __syncthreads();
         all([&](int i, float v) { if (in_group(v)) s.list[atomicAdd(&s.listed, 1)] = (u64)~ordered(v) << 32 | (unsigned)i; });      // larger logits first, equal ones by index
         __syncthreads();
@@ -494,9 +556,10 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       auto histogram = [&]() {
         clear();
         all([&](int, float v) {
-          const double e = weigh.exponent(v);
-          const int k = weigh.steps(e), bin = weigh.bin_of(k);
-          atomicAdd(&s.weight[bin], Weigher::whole(weigh.scaled(e, k)));
+          int k;
+          const u64 q = Weigher::whole(weigh.scaled(weigh.steps(v), &k));
+          const int bin = Weigher::bin_of(k);
+          if (q) atomicAdd(&s.weight[bin], q);
           atomicAdd(&s.count[bin], 1u);
         });
         __syncthreads();
@@ -521,7 +584,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
   }
 
   // ---- the draw -------------------------------------------------------------------------------------------------------------
-  // Weights of what is kept by ranges of positions; f(index, logit, weight) in a lane's own order.  Where codes were counted, tokens of the last code come with ~0 for their weight: the
+  // Weights of what is kept by ranges of positions; f(index, logit, weight, kept) in a lane's own order.  Where codes were counted, tokens of the last code come with ~0 for their weight: the
   // first `ties` of them by index are kept.
   auto weights = [&](int from, int count, int stride, auto&& f) __attribute__((always_inline)) {
     if constexpr (std::is_same<T, __bf16>::value) {
@@ -533,24 +596,32 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
             if ((code & 0x7FFF) > 0x7F80 || code == 0xFF80) continue;
             const int j = entry_of(code);
             const float value16 = __uint_as_float(code << 16);
-            if (j >= 0) f(p + e - skew, value16, j == last_entry ? ~0ull : s.weight[j]);
-            else if (tiny_kept) f(p + e - skew, value16, weigh(value16));
+            if (j >= 0) f(p + e - skew, value16, j == last_entry ? ~0ull : s.weight[j], true);
+            else if (tiny_kept) f(p + e - skew, value16, weigh(value16), true);
           }
         });
         return;
       }
     }
-    each(from, count, stride, [&](int i, float v) __attribute__((always_inline)) {
-      const unsigned key = ordered(v);
-      if (key < last.key || (key == last.key && i > last.at)) return;
-      const double w = weigh.scaled(v);
-      if (!(w < least)) f(i, v, Weigher::whole(w));
+    vectors(from, count, stride, [&](int p, const u32x4& vec) __attribute__((always_inline)) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        const float v = value(vec, e);
+        bool keep = v > -INFINITY;
+        if (last.key) {                                              // the same for all
+          const unsigned key = ordered(v);
+          keep = keep && (key > last.key || (key == last.key && p + e - skew <= last.at));
+        }
+        const double w = weigh.scaled(keep ? v : -INFINITY);
+        if (least > 0) keep = keep && (!(w < least) || v == best);
+        f(p + e - skew, v, keep ? Weigher::whole(w) : 0ull, keep);
+      }
     });
   };
   u64 sum = 0; unsigned count = 0;                                   // count: of what is kept, or of the last code
-  weights(mine, tiles, 64 * VEC, [&](int, float, u64 q) __attribute__((always_inline)) {
+  weights(mine, tiles, 64 * VEC, [&](int, float, u64 q, bool keep) __attribute__((always_inline)) {
     if (counted) { if (q == ~0ull) ++count; else sum += q; }
-    else { sum += q; ++count; }
+    else { sum += q; count += keep; }
   });
   sum = wave_sum(sum); count = wave_sum(count);
   if (!lane) { s.wave_w[wave] = sum; s.wave_c[wave] = count; }
@@ -570,13 +641,13 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
   for (int p0 = range * range_len; p0 < (range + 1) * range_len; p0 += SAMPLE_THREADS * VEC) {
     const bool in = p0 + tid * VEC < (range + 1) * range_len;
     u64 here = 0; unsigned here_n = 0;
-    if (in) weights(p0 + tid * VEC, 1, 0, [&](int, float, u64 q) { if (counted && q == ~0ull) ++here_n; else here += q; });
+    if (in) weights(p0 + tid * VEC, 1, 0, [&](int, float, u64 q, bool) { if (counted && q == ~0ull) ++here_n; else here += q; });
     u64 bw, aw; unsigned bn, an;
     block_scan(here, here_n, &bw, &bn, &aw, &an);
     bw += before; bn += before_n;
     if (in && !((double)weight_of(bw, bn) > target) && (double)weight_of(bw + here, bn + here_n) > target) {
       bool found = false;
-      weights(p0 + tid * VEC, 1, 0, [&](int i, float v, u64 q) {
+      weights(p0 + tid * VEC, 1, 0, [&](int i, float v, u64 q, bool) {
         if (found) return;
         if (counted && q == ~0ull) ++bn; else bw += q;
         if ((double)weight_of(bw, bn) > target) {
