@@ -693,7 +693,7 @@ typedef enum { OCTO_ROWS_PLAIN = 0, OCTO_ROWS_MX8 = 1 } octo_row_format;
  *   s = x (+ d_res),   y = s / sqrt(mean over the row of s^2 + eps) * d_weight       (norm == 0: y = s * d_weight)
  * x, d_res (or NULL) and d_sum (or NULL: s is not kept) are rows of `dtype` (OCTO_F32, _F16, _BF16), d_weight is fp32 [width] or NULL
  * for ones; y goes to d_y in `dtype` (y_format OCTO_ROWS_PLAIN) or to y8 (OCTO_ROWS_MX8; with norm 0 and no weight the call is the
- * conversion to 8 bits).  Arithmetic is in fp32, the norm is that of the unrounded sum, every output is rounded once.  A NaN or an infinity stays in
+ * conversion to 8 bits).  The residual's sum is in fp32, the norm, which is that of the unrounded sum, in fp64, every output is rounded once.  A NaN or an infinity stays in
  * its row.  width: 1 to 32768, for OCTO_ROWS_MX8 a multiple of 32 with d_x, d_res and d_sum 16-byte aligned, their strides multiples of 16
  * bytes (other calls take any address of an element).  d_sum and d_y may each be d_x or d_res with the same stride (not both the same one);
  * apart from that no output may overlap anything else.  d_n: NULL, or the number of rows present, on the device (clamped to n): later rows are left as they were. */
