@@ -9,6 +9,7 @@
 
 #include "mx8.h"
 #include "octo_internal.h"
+#include "product_choice.h"
 
 namespace octo {
 
@@ -439,6 +440,7 @@ __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(Produc
   unrolled<M>([&](auto p) __attribute__((always_inline)) { load_place(1, 1, p); });
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(FIRST) : "memory");
   __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
   load_exps(2);
 
   // Loads and reads beyond the last step are of nothing (zeros go to LDS).  Reads and loads stand between the products, in the order of the code: a product keeps the matrix unit busy for 16 cycles or more, in which the wavefront issues what lies behind it.
@@ -446,6 +448,7 @@ __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(Produc
     place_exps(t + 2);
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
     load_exps(t + 3);
     issue_exps(t + 2);
     cut(t + 2);
@@ -622,7 +625,7 @@ hipError_t launch_product_tile(ProductArgs a, hipStream_t s) {
 // their operands from memory straight into registers, several steps in flight, and add up their sums in LDS at the end, in a fixed order.  A gated block has gates in the first
 // half of its tiles and what they are a gate of in the second.
 template <typename T, int TILES, int TB>
-__global__ __launch_bounds__(512, TILES * TB > 4 ? 1 : 2) void product_few_kernel(ProductArgs a) {
+__global__ __launch_bounds__(512, 2) void product_few_kernel(ProductArgs a) {
   constexpr bool MX = std::is_same<T, f8>::value;
   constexpr int W = 8, U = TILES + TB <= 3 ? 4 : 2;
   __shared__ __attribute__((aligned(16))) floatx4 red[W][TILES][TB][64];
@@ -745,6 +748,130 @@ hipError_t launch_product_few(ProductArgs a, hipStream_t s) {
   return hipGetLastError();
 }
 
+// ---- up to 16 tokens: x stays in registers -----------------------------------------------------------------------------------
+// As above, but a block takes one group of TILES x 16 rows of w after the other, and its wavefronts keep their parts of x, XS steps, for all of them: x is read once a block and not once a
+// group (16 tokens, 4096 -> 131072 bf16: 253 us of reading x with every group).  The weights of the next steps, also of the next group's first, are on their way while products
+// and sums of the present ones are made.  Rows of 8 bits have their exponents in aligned words.
+template <typename T, int TILES, int XS>
+__global__ __launch_bounds__(512, 2) void product_held_kernel(ProductArgs a) {
+  constexpr bool MX = std::is_same<T, f8>::value;
+  constexpr int W = 8, U = XS > 4 && TILES == 1 && !(MX && XS > 8) ? 4 : 2, C = XS / U;  // steps of a part, parts of a group: an even number
+  __shared__ __attribute__((aligned(16))) floatx4 red[2][W][TILES][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
+  const int n = a.n_dyn ? min(max(*a.n_dyn, 0), a.n) : a.n;
+  if (n == 0) return;
+  const int outs = a.gated ? TILES * 8 : TILES * 16, nk = (a.k_bytes + 127) / 128;
+  // chunks g and g + 4 of a step; beyond a row's end, and for steps beyond the last, zeros that no memory is asked for
+  auto beyond = [&](int t, int h) __attribute__((always_inline)) { return t * 128 + h * 64 + g * 16 >= a.k_bytes ? OOB : 0; };
+
+  u32x4 fx[XS][2];
+  unsigned ex[MX ? XS : 1];
+  {
+    const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc((void*)a.x, 0, 0x7FFFFFFF, BUF_FLAGS), rxe = __builtin_amdgcn_make_buffer_rsrc((void*)a.xe, 0, 0x7FFFFFFF, BUF_FLAGS);
+    const int xoff = r16 < n ? r16 * (int)a.x_row + g * 16 : OOB, xeoff = r16 < n ? r16 * (int)a.xe_row : OOB;
+#pragma unroll
+    for (int u = 0; u < XS; ++u) {
+      const int t = wave + u * W;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) fx[u][h] = __builtin_amdgcn_raw_buffer_load_b128(rx, (xoff | beyond(t, h)) + t * 128 + h * 64, 0, 0);
+      if constexpr (MX) ex[u] = __builtin_amdgcn_raw_buffer_load_b32(rxe, (t < nk ? xeoff : OOB) + t * 4, 0, 0);
+    }
+  }
+  u32x4 fw[2][U][TILES][2];
+  unsigned ew[2][U][MX ? TILES : 1];
+  auto load = [&](int buf, int group, int part) __attribute__((always_inline)) {
+    const int n0 = group * outs;
+    const char* const w0 = a.w + n0 * a.w_row;
+    const __amdgpu_buffer_rsrc_t rw[2] = {__builtin_amdgcn_make_buffer_rsrc((void*)w0, 0, 0x7FFFFFFF, BUF_FLAGS),
+                                          __builtin_amdgcn_make_buffer_rsrc((void*)(w0 + (a.gated ? a.cols * a.w_row : 0)), 0, 0x7FFFFFFF, BUF_FLAGS)};
+    const uint8_t* const e0 = a.we + n0 * a.we_row;
+    const __amdgpu_buffer_rsrc_t re[2] = {__builtin_amdgcn_make_buffer_rsrc((void*)e0, 0, 0x7FFFFFFF, BUF_FLAGS),
+                                          __builtin_amdgcn_make_buffer_rsrc((void*)(e0 + (a.gated ? a.cols * a.we_row : 0)), 0, 0x7FFFFFFF, BUF_FLAGS)};
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) {
+      const int col = (a.gated ? i % (TILES > 1 ? TILES / 2 : 1) : i) * 16 + r16;
+      const bool second = a.gated && i >= TILES / 2, there = group < a.tiles_n && n0 + col < a.cols;
+      const int woff = there ? col * (int)a.w_row + g * 16 : OOB, weoff = there ? col * (int)a.we_row : OOB;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int t = wave + (part * U + u) * W;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) fw[buf][u][i][h] = __builtin_amdgcn_raw_buffer_load_b128(rw[second], (woff | beyond(t, h)) + t * 128 + h * 64, 0, 0);
+        if constexpr (MX) ew[buf][u][i] = __builtin_amdgcn_raw_buffer_load_b32(re[second], (t < nk ? weoff : OOB) + t * 4, 0, 0);
+      }
+    }
+  };
+  load(0, blockIdx.x, 0);
+  int turn = 0;
+#pragma nounroll
+  for (int group = blockIdx.x; group < a.tiles_n; group += gridDim.x, turn ^= 1) {
+    floatx4 acc[TILES];
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    if constexpr (MX)
+#pragma unroll
+      for (int u = 0; u < XS; ++u) asm volatile("" : "+v"(ex[u]));     // or every exponent's scale takes a register for the whole loop
+#pragma unroll
+    for (int part = 0; part < C; ++part) {
+      if (part + 1 < C) load((part + 1) & 1, group, part + 1);
+      else load(0, group + gridDim.x, 0);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int s = part * U + u, shift = 8 * (g >> 1) + 16 * h;
+          u32x4 x[2];
+          if constexpr (MX) widen_mx8(fx[s][h], ex[s] >> shift & 255, &x[0], &x[1]);
+#pragma unroll
+          for (int i = 0; i < TILES; ++i) {
+            if constexpr (MX) {
+              u32x4 w[2];
+              widen_mx8(fw[part & 1][u][i][h], ew[part & 1][u][i] >> shift & 255, &w[0], &w[1]);
+              acc[i] = mfma16<__bf16>(w[1], x[1], mfma16<__bf16>(w[0], x[0], acc[i]));
+            } else {
+              acc[i] = mfma_part<T>(fw[part & 1][u][i][h], fx[s][h], acc[i]);
+            }
+          }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) red[turn][wave][i][lane] = acc[i];
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                // and not for the loads
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    const int quads = outs / 4;
+    for (int p = threadIdx.x; p < quads * 16; p += 512) {
+      const int tok = p / quads, q = p % quads, at = (q & 3) * 16 + tok;
+      floatx4 z = red[turn][0][q >> 2][at], up = z;
+      for (int w = 1; w < W; ++w) z += red[turn][w][q >> 2][at];
+      if (a.gated) {
+        const int second = ((q >> 2) + TILES / 2) % TILES;
+        up = red[turn][0][second][at];
+        for (int w = 1; w < W; ++w) up += red[turn][w][second][at];
+      }
+      product_finish4(a, tok < n, tok, group * outs + q * 4, z, up);
+    }
+  }
+}
+
+template <typename T, int TILES, int XS>
+hipError_t launch_product_held(ProductArgs a, hipStream_t s) {
+  constexpr int BLOCKS = 256;                                         // one a CU, whose wavefronts fill its registers
+  const int outs = a.gated ? TILES * 8 : TILES * 16;
+  a.tiles_n = (a.cols + outs - 1) / outs; a.tiles_m = 1;
+  hipLaunchKernelGGL((product_held_kernel<T, TILES, XS>), dim3((unsigned)(a.tiles_n < BLOCKS ? a.tiles_n : BLOCKS)), dim3(512), 0, s, a);
+  return hipGetLastError();
+}
+template <typename T, int TILES>
+hipError_t launch_product_held_steps(const ProductArgs& a, hipStream_t s) {
+  constexpr int MOST = product_held_steps(TILES, std::is_same<T, f8>::value);
+  const int steps = (a.k_bytes + 1023) / 1024;
+  if (steps <= 4) return launch_product_held<T, TILES, 4>(a, s);
+  if constexpr (MOST >= 16) { if (steps > 8) return launch_product_held<T, TILES, 16>(a, s); }
+  if constexpr (MOST >= 8) return launch_product_held<T, TILES, 8>(a, s);
+  return hipErrorInvalidValue;
+}
+
 template <typename T> hipError_t launch_product(int variant, const ProductArgs& a, hipStream_t s);
 
 #ifdef OCTO_PRODUCT_TYPE
@@ -760,6 +887,9 @@ template <> hipError_t launch_product<OCTO_PRODUCT_TYPE>(int variant, const Prod
     case 1: return launch_product_tile<T, false, 4, 4, 2, 2, 1>(a, s);
     case 2: return launch_product_tile<T, false, 2, 2, 2, 2, 2>(a, s);
     case 3: return launch_product_tile<T, false, 2, 1, 2, 2, 2>(a, s);
+    case 10: return launch_product_held_steps<T, 1>(a, s);
+    case 20: return launch_product_held_steps<T, 2>(a, s);
+    case 40: return launch_product_held_steps<T, 4>(a, s);
     case 11: return launch_product_few<T, 1, 1>(a, s);
     case 21: return launch_product_few<T, 2, 1>(a, s);
     case 22: return launch_product_few<T, 2, 2>(a, s);

@@ -1,6 +1,5 @@
 // octo_op_product: arguments, their checks and the choice of a kernel.
 #include "product.h"
-#include "product_choice.h"
 
 using namespace octo;
 
@@ -47,7 +46,7 @@ extern "C" octo_status octo_op_product(const octo_product_op* op, void* hip_stre
   a.vec = !y8 && a.cols % 4 == 0 && a.y_vec && (!a.res || a.res_vec) && (!a.bias || a.bias_vec);
   a.exact8 = x8 && (a.y_kind == PRODUCT_Y_F32 || !a.exp_words);
   if (!op->n) return OCTO_OK;
-  const ProductChoice c = product_choice(op->n, a.cols, a.gated, y8, a.exact8);
+  const ProductChoice c = product_choice(op->n, x8 && !a.exp_words ? 0 : a.k_bytes, a.cols, a.gated, y8, x8, a.exact8);
   if (c.blocks > 0x7FFFFF) return OCTO_EINVAL;                       // HIP counts the threads of a launch, up to 512 a block, in 32 bits
   hipStream_t s = (hipStream_t)hip_stream;
   const hipError_t e = x8 ? launch_product<f8>(c.variant, a, s) : op->dtype == OCTO_F32 ? launch_product<float>(c.variant, a, s)

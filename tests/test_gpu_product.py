@@ -152,6 +152,26 @@ def test_large_products(octo, rows, dtype, n, k, cols, gated):
     _check(y, ref, off, dtype)
 
 
+HELD = [("plain", t, size, n) for t in ("bf16", "f16", "f32") for size, n in ((128, 16), (4096, 1), (4224, 16), (8192, 16), (8320, 5), (16384, 16), (16512, 2))]
+HELD += [("mx8", "bf16", size, n) for size, n in ((128, 16), (4096, 16), (4224, 3), (8192, 16), (8320, 5))]
+
+
+@pytest.mark.parametrize("rows,dtype,bytes_of_k,n", HELD)
+def test_held_tokens_and_more_weights_than_blocks(octo, rows, dtype, bytes_of_k, n):
+    """Several groups of weights to a block, the last of them ragged, at and beyond the longest rows that are held."""
+    import torch
+    k = bytes_of_k // (1 if rows == "mx8" else _t(dtype).itemsize)
+    for cols, gated, to8 in ((4230, False, False), (8300, False, False), (4230, True, False), (8352, False, True), (8352, True, True)):
+        x, w, x64, w64, g = _inputs(octo, rows, dtype, n, k, cols, gated, n + k)
+        y = octo.Mx8.empty(n, cols) if to8 else torch.full((n, cols), float("nan"), dtype=_t(dtype), device="cuda")
+        kernel = octo.op_product(x, w, y, act="silu" if gated else "none", gated=gated)
+        r = 4 if gated and to8 else 2 if gated or to8 or bytes_of_k <= 4096 and cols >= 8192 else 1
+        room = (4 if rows == "mx8" else 8) if r == 4 else 8 if rows == "mx8" else 16
+        assert (kernel == 10 * r) == (bytes_of_k <= 1024 * room), kernel
+        ref, off = _reference(x64, w64, None, "silu" if gated else "none", gated, None, rows == "plain" and dtype == "f32")
+        _check_mx8(y, ref, off) if to8 else _check(y, ref, off, dtype)
+
+
 def test_fp32_results_of_many_rows_in_eight_bits(octo):
     """They are added up in fp32, whichever kernel runs."""
     import torch
