@@ -31,7 +31,10 @@ struct ProductArgs {
   int exact8;                                         // rows of 8 bits go through bf16 also where tokens are many
   int direct;                                         // results of 16 bits, eight of them one aligned vector, or of 8 bits, activations that take few instructions
   int tiles_n, tiles_m;
+  int n_from;                                         // tokens before x's first row, of those that n_dyn counts
 };
+
+__device__ __forceinline__ int product_tokens(const ProductArgs& a) { return a.n_dyn ? min(max(max(*a.n_dyn, 0) - a.n_from, 0), a.n) : a.n; }
 
 typedef __attribute__((address_space(3))) unsigned char LdsBytes;
 
@@ -297,19 +300,32 @@ template <int N, typename F> __device__ __forceinline__ void unrolled(F&& f) { u
 // Rows of 8 bits: the 8-bit matrix instructions add products in groups of eight at the weight of the group's largest and drop what lies 2^13 below it (measured: 1 + 2^-13 comes
 // out, 1 + 2^-14 does not), 2^-14 of a sum's size in the mean.  Results that are rounded to 16 or 8 bits can bear that; for fp32 results, and where exponents are no aligned words (EXACT), the
 // values are widened to bf16, whose products are exact and added in fp32, at half the rate.
-template <typename T, bool EXACT, int TN, int TM, int WN, int WM, int MINB>
+// The size of four stages is given at the launch: a compiler that knows it, and that a CU has room for one block, lets a wavefront have both halves of the registers, and moves sums
+// from one half to the other and back in each step (512 tokens, bf16 4096 -> 4096: 27.6 us, so 21.9).
+template <int D, int BYTES> struct ProductLds {
+  static __device__ __forceinline__ unsigned char* at() { __shared__ __attribute__((aligned(1024))) unsigned char smem[BYTES]; return smem; }
+};
+template <int BYTES> struct ProductLds<4, BYTES> {
+  static __device__ __forceinline__ unsigned char* at() { extern __shared__ __attribute__((aligned(1024))) unsigned char product_stages[]; return product_stages; }
+};
+template <typename T, bool EXACT, int TN, int TM, int WN, int WM, int D> struct ProductTile {
+  static constexpr bool MX = std::is_same<T, f8>::value;
+  static constexpr int NW = WN * WM, BN = WN * TN * 32, BM = WM * TM * 32, ROWS = BN + BM, STAGE = ROWS * 128, LW = BN / 8 / NW, LX = BM / 8 / NW;
+  static constexpr int HT = TM < 2 ? 1 : 2, UNIT = HT * 32 * TN * 32 * 4;      // sums of a wavefront on their way out, of 32 or 64 tokens
+  static constexpr int NE = MX ? (ROWS + NW * 64 - 1) / (NW * 64) : 1, EXPS = NE * NW * 64;   // exponents of a step, whole loads
+  static constexpr int RING = EXACT ? 4 : D, MAIN = D * STAGE + (MX ? RING * EXPS * 4 : 0), LDS = MAIN > NW * UNIT ? MAIN : NW * UNIT;
+};
+template <typename T, bool EXACT, int TN, int TM, int WN, int WM, int MINB, int D>
 __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(ProductArgs a) {
-  constexpr bool MX = std::is_same<T, f8>::value;
-  constexpr int NW = WN * WM, BN = WN * TN * 32, BM = WM * TM * 32, ROWS = BN + BM, STAGE = ROWS * 128, LW = BN / 8 / NW, LX = BM / 8 / NW;
+  using P = ProductTile<T, EXACT, TN, TM, WN, WM, D>;
+  constexpr bool MX = P::MX;
+  constexpr int NW = P::NW, BN = P::BN, BM = P::BM, ROWS = P::ROWS, STAGE = P::STAGE, LW = P::LW, LX = P::LX, HT = P::HT, UNIT = P::UNIT, NE = P::NE, EXPS = P::EXPS, RING = P::RING;
   constexpr int BW = 2 * TN, BX = 2 * TM, M = BW * BX, L = LW + LX;   // blocks of 16 rows of a wavefront, their products, loads of a step
-  constexpr int HT = TM < 2 ? 1 : 2, UNIT = HT * 32 * TN * 32 * 4;    // sums of a wavefront on their way out, of 32 or 64 tokens
-  constexpr int NE = MX ? (ROWS + NW * 64 - 1) / (NW * 64) : 1, EXPS = NE * NW * 64;   // exponents of a step, whole loads
-  constexpr int RING = EXACT ? 4 : 2, MAIN = 2 * STAGE + (MX ? RING * EXPS * 4 : 0), LDS = MAIN > NW * UNIT ? MAIN : NW * UNIT;
   static_assert(BN / 8 % NW == 0 && BM / 8 % NW == 0 && TN % 2 == 0 && NW % 4 == 0, "whole loads a wavefront, pairs of blocks");
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[LDS];
+  using Lds = ProductLds<D, P::LDS>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
   const int wn = wave % WN, wm = wave / WN;
-  const int n = a.n_dyn ? min(max(*a.n_dyn, 0), a.n) : a.n;
+  const int n = product_tokens(a);
 
   // Tiles in groups of eight along the tokens, all outputs of a group one after the other, and an eighth of that list to each die (block b runs on die b % 8): the
   // blocks of a die share rows of w and x in its L2.
@@ -323,7 +339,7 @@ __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(Produc
   const int m0 = tm * BM, n0 = tn * (a.gated ? BN / 2 : BN);         // the tile's first token and output
   if (m0 >= n) return;
 
-  const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(LdsBytes*)smem);
+  const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(LdsBytes*)Lds::at());
   // Load q of a wavefront brings rows 8 (LW wave + q) .. + 7 of the tile (of x: LX wave + ..), 1024 bytes behind load q - 1.  The places in LDS of four loads differ by the instructions' offset
   // alone, which is taken off the addresses again: each write of m0 holds the wavefront up for some twenty cycles (16 a step: 2460 cycles for 2048 of products).
   const int row8 = lane >> 3;
@@ -374,7 +390,7 @@ __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(Produc
 #pragma unroll
         for (int i = 0; i < NE; ++i) {
           const int r = i * NW * 64 + (int)threadIdx.x;
-          if (r < ROWS) *(unsigned*)(smem + 2 * STAGE + ((t & (RING - 1)) * EXPS + r) * 4) = exps[i];
+          if (r < ROWS) *(unsigned*)(Lds::at() + D * STAGE + ((t & (RING - 1)) * EXPS + r) * 4) = exps[i];
         }
       }
     }
@@ -385,7 +401,7 @@ __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(Produc
 #pragma unroll
         for (int i = 0; i < NE; ++i)
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
-                         :: "s"(lds + 2 * STAGE + ((t & (RING - 1)) * EXPS + (i * NW + wave) * 64) * 4), "v"(exp_at[i] + 4 * min(t, nk - 1)) : "memory");
+                         :: "s"(lds + D * STAGE + ((t & (RING - 1)) * EXPS + (i * NW + wave) * 64) * 4), "v"(exp_at[i] + 4 * min(t, nk - 1)) : "memory");
       }
     }
   };
@@ -419,7 +435,7 @@ __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(Produc
   const int wrow = (wn * TN * 32 + r16) * 128, xrow = (BN + wm * TM * 32 + r16) * 128;
   // chunk c of the lane's row of block i of w or x, in one of the two stages
   auto read = [&](bool is_x, int stage, int i, int c) __attribute__((always_inline)) -> u32x4 {
-    return *(const u32x4*)(smem + stage * STAGE + (is_x ? xrow : wrow) + i * 2048 + ((c ^ (r16 >> 1)) << 4));
+    return *(const u32x4*)(Lds::at() + stage * STAGE + (is_x ? xrow : wrow) + i * 2048 + ((c ^ (r16 >> 1)) << 4));
   };
 
   // Loads of step t + 2 have places behind the products, from the barrier of step t on: place s of the 2 M up to the next barrier, the last quarter of which stays free for them to arrive.
@@ -431,14 +447,17 @@ __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(Produc
 
   load_exps(0); place_exps(0);
   load_exps(1); place_exps(1);
-  issue_exps(0);
-  issue_exps(1);
-  cut(0);
 #pragma unroll
-  for (int q = 0; q < L; ++q) issue(0, 0, q);
-  cut(1);
-  unrolled<M>([&](auto p) __attribute__((always_inline)) { load_place(1, 1, p); });
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(FIRST) : "memory");
+  for (int t = 0; t < D; ++t) issue_exps(t);
+#pragma unroll
+  for (int t = 0; t < D - 1; ++t) {
+    cut(t);
+#pragma unroll
+    for (int q = 0; q < L; ++q) issue(t, t, q);
+  }
+  cut(D - 1);
+  unrolled<M>([&](auto p) __attribute__((always_inline)) { load_place(D - 1, D - 1, p); });
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"((D - 2) * L + FIRST) : "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   load_exps(2);
@@ -446,12 +465,12 @@ __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(Produc
   // Loads and reads beyond the last step are of nothing (zeros go to LDS).  Reads and loads stand between the products, in the order of the code: a product keeps the matrix unit busy for 16 cycles or more, in which the wavefront issues what lies behind it.
   auto turn = [&](int t) __attribute__((always_inline)) {             // all are done with step t's place in LDS, and step t + 1 is there
     place_exps(t + 2);
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"((D - 2) * L) : "memory");     // the loads of the D - 2 steps behind it may be under way
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     load_exps(t + 3);
-    issue_exps(t + 2);
-    cut(t + 2);
+    issue_exps(t + D);
+    cut(t + D);
   };
   if constexpr (MX && !EXACT) {
     // A step is one product of k.  Its M products go through four quarters, (w low, x low), (w low, x high), (w high, x high), (w high, x low); each half of an operand is read
@@ -461,7 +480,7 @@ __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(Produc
     auto fetch = [&](bool is_x, int stage, int high, int r) __attribute__((always_inline)) {      // read r of 3 TN or 3 TM of a half
       const int i = high * (is_x ? TM : TN) + r / 3, h = r % 3, at = is_x ? BN + wm * TM * 32 : wn * TN * 32;
       if (h == 2) {
-        (is_x ? ex[is_x ? i : 0] : ew[is_x ? 0 : i]) = *(const uint8_t*)(smem + 2 * STAGE + (stage * EXPS + at + i * 16 + r16) * 4 + g);
+        (is_x ? ex[is_x ? i : 0] : ew[is_x ? 0 : i]) = *(const uint8_t*)(Lds::at() + D * STAGE + (stage * EXPS + at + i * 16 + r16) * 4 + g);
       } else {
         (is_x ? fx[is_x ? i : 0][h & 1] : fw[is_x ? 0 : i][h & 1]) = read(is_x, stage, i, g + 4 * h);
       }
@@ -471,7 +490,8 @@ __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(Produc
 #pragma unroll
     for (int r = 0; r < 3 * TM; ++r) fetch(true, 0, 0, r);
     auto step = [&](int t, auto odd) __attribute__((always_inline)) {
-      constexpr int X = odd() ? 1 : 0;                                // the half of x that comes first, the stage of the step
+      constexpr int X = odd() ? 1 : 0;                                // the half of x that comes first
+      const int here = D == 2 ? X : t & (D - 1), next = D == 2 ? 1 - X : (t + 1) & (D - 1), before = D == 2 ? 1 - X : (t - 1) & (D - 1);      // places of this step, the next and the last
       unrolled<4>([&](auto quarter_) __attribute__((always_inline)) {
         constexpr int quarter = quarter_(), MQ = TN * TM, wh = quarter / 2, xh = (quarter == 1 || quarter == 2) ? 1 - X : X, R = quarter == 0 || quarter == 3 ? 3 * TM : 3 * TN;
         if constexpr (quarter == 2) turn(t);
@@ -481,15 +501,15 @@ __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(Produc
           // quarter 0 reads the other half of x, 1 the other half of w, 2 the first half of w of the next step, 3 the half of x that the next step begins with
           unrolled<last - first>([&](auto d) __attribute__((always_inline)) {
             constexpr int r = first + d();
-            if constexpr (quarter == 0) fetch(true, X, 1 - X, r);
-            else if constexpr (quarter == 1) fetch(false, X, 1, r);
-            else if constexpr (quarter == 2) fetch(false, 1 - X, 0, r);
-            else fetch(true, 1 - X, 1 - X, r);
+            if constexpr (quarter == 0) fetch(true, here, 1 - X, r);
+            else if constexpr (quarter == 1) fetch(false, here, 1, r);
+            else if constexpr (quarter == 2) fetch(false, next, 0, r);
+            else fetch(true, next, 1 - X, r);
           });
           // the barrier lies between quarters 1 and 2
           constexpr int place = (quarter * MQ + m + 2 * MQ) % (4 * MQ) * 2;
-          load_place(quarter >= 2 ? t + 2 : t + 1, quarter >= 2 ? X : 1 - X, std::integral_constant<int, place>{});
-          load_place(quarter >= 2 ? t + 2 : t + 1, quarter >= 2 ? X : 1 - X, std::integral_constant<int, place + 1>{});
+          load_place(quarter >= 2 ? t + D : t + D - 1, quarter >= 2 ? here : before, std::integral_constant<int, place>{});
+          load_place(quarter >= 2 ? t + D : t + D - 1, quarter >= 2 ? here : before, std::integral_constant<int, place + 1>{});
           __builtin_amdgcn_sched_barrier(0);
         });
       });
@@ -503,12 +523,12 @@ __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(Produc
     unsigned ew[2][MX ? BW : 1], ex[2][MX ? BX : 1];
     // read r of an operand set, in the order in which the products want them: the first row of w, all of x, the other rows of w
     auto fetch = [&](int set, int t, int kq, int r) __attribute__((always_inline)) {
-      if (r >= 1 && r <= BX) fx[set][r - 1] = read(true, t & 1, r - 1, 4 * kq + g);
-      else fw[set][r ? r - BX : 0] = read(false, t & 1, r ? r - BX : 0, 4 * kq + g);
+      if (r >= 1 && r <= BX) fx[set][r - 1] = read(true, t & (D - 1), r - 1, 4 * kq + g);
+      else fw[set][r ? r - BX : 0] = read(false, t & (D - 1), r ? r - BX : 0, 4 * kq + g);
     };
     auto scales = [&](int set, int t) __attribute__((always_inline)) {
       if constexpr (MX) {
-        const unsigned char* const p = smem + 2 * STAGE + (t & (RING - 1)) * EXPS * 4;
+        const unsigned char* const p = Lds::at() + D * STAGE + (t & (RING - 1)) * EXPS * 4;
 #pragma unroll
         for (int i = 0; i < BW; ++i) ew[set][i] = *(const unsigned*)(p + (wn * TN * 32 + i * 16 + r16) * 4);
 #pragma unroll
@@ -534,7 +554,7 @@ __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(Produc
           if constexpr (MX) acc[i][j] = mfma16<__bf16>(w8[i][1], x8[j][1], mfma16<__bf16>(w8[i][0], x8[j][0], acc[i][j]));
           else acc[i][j] = mfma_part<T>(fw[kq][i], fx[kq][j], acc[i][j]);
           unrolled<last - first>([&](auto d) __attribute__((always_inline)) { fetch(kq ^ 1, t + kq, kq ^ 1, first + d()); });
-          load_place(kq == 1 ? t + 2 : t + 1, kq == 1 ? t & 1 : ~t & 1, std::integral_constant<int, kq == 1 ? m : M + m>{});
+          load_place(kq == 1 ? t + D : t + D - 1, (kq == 1 ? t : t - 1) & (D - 1), std::integral_constant<int, kq == 1 ? m : M + m>{});
           __builtin_amdgcn_sched_barrier(0);
         });
       });
@@ -560,7 +580,7 @@ __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(Produc
   // Sums leave through LDS, up to 64 tokens of a wavefront at a time, in a place of its own: lanes then hold four neighbouring outputs of a token.  Chunks of four lie at their
   // number xor the token's.
   __syncthreads();
-  float* const out = (float*)(smem + wave * UNIT);
+  float* const out = (float*)(Lds::at() + wave * UNIT);
   const int lpt_log2 = (TN == 4 ? 5 : 4) - a.gated, lpt = 1 << lpt_log2;      // lanes of a token
 #pragma unroll
   for (int h = 0; h < TM; h += HT) {
@@ -611,12 +631,14 @@ __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(Produc
   }
 }
 
-template <typename T, bool EXACT, int TN, int TM, int WN, int WM, int MINB>
+template <typename T, bool EXACT, int TN, int TM, int WN, int WM, int MINB, int D>
 hipError_t launch_product_tile(ProductArgs a, hipStream_t s) {
   constexpr int BN = WN * TN * 32, BM = WM * TM * 32;
   const int outs = a.gated ? BN / 2 : BN;
   a.tiles_n = (a.cols + outs - 1) / outs; a.tiles_m = (a.n + BM - 1) / BM;
-  hipLaunchKernelGGL((product_tile_kernel<T, EXACT, TN, TM, WN, WM, MINB>), dim3((unsigned)(a.tiles_n * a.tiles_m)), dim3(WN * WM * 64), 0, s, a);
+  const int lds = D == 2 ? 0 : ProductTile<T, EXACT, TN, TM, WN, WM, D>::LDS;
+  if (lds) (void)hipFuncSetAttribute((const void*)product_tile_kernel<T, EXACT, TN, TM, WN, WM, MINB, D>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  hipLaunchKernelGGL((product_tile_kernel<T, EXACT, TN, TM, WN, WM, MINB, D>), dim3((unsigned)(a.tiles_n * a.tiles_m)), dim3(WN * WM * 64), lds, s, a);
   return hipGetLastError();
 }
 
@@ -630,7 +652,7 @@ __global__ __launch_bounds__(512, 2) void product_few_kernel(ProductArgs a) {
   constexpr int W = 8, U = TILES + TB <= 3 ? 4 : 2;
   __shared__ __attribute__((aligned(16))) floatx4 red[W][TILES][TB][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
-  const int n = a.n_dyn ? min(max(*a.n_dyn, 0), a.n) : a.n;
+  const int n = product_tokens(a);
   const int outs = a.gated ? TILES * 8 : TILES * 16;
   const int tn = blockIdx.x % a.tiles_n, tm = blockIdx.x / a.tiles_n;
   const int m0 = tm * TB * 16, n0 = tn * outs;
@@ -758,7 +780,7 @@ __global__ __launch_bounds__(512, 2) void product_held_kernel(ProductArgs a) {
   constexpr int W = 8, U = XS > 4 && TILES == 1 && !(MX && XS > 8) ? 4 : 2, C = XS / U;  // steps of a part, parts of a group: an even number
   __shared__ __attribute__((aligned(16))) floatx4 red[2][W][TILES][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
-  const int n = a.n_dyn ? min(max(*a.n_dyn, 0), a.n) : a.n;
+  const int n = product_tokens(a);
   if (n == 0) return;
   const int outs = a.gated ? TILES * 8 : TILES * 16, nk = (a.k_bytes + 127) / 128;
   // chunks g and g + 4 of a step; beyond a row's end, and for steps beyond the last, zeros that no memory is asked for
@@ -879,23 +901,30 @@ template <> hipError_t launch_product<OCTO_PRODUCT_TYPE>(int variant, const Prod
   typedef OCTO_PRODUCT_TYPE T;
   if constexpr (std::is_same<T, f8>::value) {
     if (a.exact8) {
-      if (variant == 1 || variant == 2) return launch_product_tile<T, true, 2, 2, 2, 2, 2>(a, s);
-      if (variant == 3) return launch_product_tile<T, true, 2, 1, 2, 2, 2>(a, s);
+      switch (variant) {
+        case 2: return launch_product_tile<T, true, 2, 2, 2, 2, 2, 2>(a, s);
+        case 3: return launch_product_tile<T, true, 2, 1, 2, 2, 2, 4>(a, s);
+        case 4: return launch_product_tile<T, true, 2, 2, 2, 2, 2, 4>(a, s);
+      }
+    }
+  } else {
+    switch (variant) {
+      case 22: return launch_product_few<T, 2, 2>(a, s);
+      case 24: if constexpr (sizeof(T) == 2) return launch_product_few<T, 2, 4>(a, s); else break;
+      case 42: if constexpr (sizeof(T) == 4) return launch_product_few<T, 4, 2>(a, s); else break;
     }
   }
   switch (variant) {
-    case 1: return launch_product_tile<T, false, 4, 4, 2, 2, 1>(a, s);
-    case 2: return launch_product_tile<T, false, 2, 2, 2, 2, 2>(a, s);
-    case 3: return launch_product_tile<T, false, 2, 1, 2, 2, 2>(a, s);
+    case 1: return launch_product_tile<T, false, 4, 4, 2, 2, 1, 2>(a, s);
+    case 2: return launch_product_tile<T, false, 2, 2, 2, 2, 2, 2>(a, s);
+    case 3: return launch_product_tile<T, false, 2, 1, 2, 2, 2, 4>(a, s);
+    case 4: return launch_product_tile<T, false, 2, 2, 2, 2, 2, 4>(a, s);
     case 10: return launch_product_held_steps<T, 1>(a, s);
     case 20: return launch_product_held_steps<T, 2>(a, s);
     case 40: return launch_product_held_steps<T, 4>(a, s);
     case 11: return launch_product_few<T, 1, 1>(a, s);
     case 21: return launch_product_few<T, 2, 1>(a, s);
-    case 22: return launch_product_few<T, 2, 2>(a, s);
-    case 24: return launch_product_few<T, 2, 4>(a, s);
     case 41: return launch_product_few<T, 4, 1>(a, s);
-    case 42: return launch_product_few<T, 4, 2>(a, s);
   }
   return hipErrorInvalidValue;
 }

@@ -46,12 +46,26 @@ extern "C" octo_status octo_op_product(const octo_product_op* op, void* hip_stre
   a.vec = !y8 && a.cols % 4 == 0 && a.y_vec && (!a.res || a.res_vec) && (!a.bias || a.bias_vec);
   a.exact8 = x8 && (a.y_kind == PRODUCT_Y_F32 || !a.exp_words);
   if (!op->n) return OCTO_OK;
-  const ProductChoice c = product_choice(op->n, x8 && !a.exp_words ? 0 : a.k_bytes, a.cols, a.gated, y8, x8, a.exact8);
-  if (c.blocks > 0x7FFFFF) return OCTO_EINVAL;                       // HIP counts the threads of a launch, up to 512 a block, in 32 bits
   hipStream_t s = (hipStream_t)hip_stream;
-  const hipError_t e = x8 ? launch_product<f8>(c.variant, a, s) : op->dtype == OCTO_F32 ? launch_product<float>(c.variant, a, s)
-                     : op->dtype == OCTO_F16 ? launch_product<_Float16>(c.variant, a, s) : launch_product<__bf16>(c.variant, a, s);
-  if (e != hipSuccess) return OCTO_EHIP;
-  if (kernel_id) *kernel_id = c.variant;
+  const int bits = x8 ? 8 : 8 * es;
+  auto choice = [&](int n) { return product_choice(n, a.k_bytes, a.cols, a.gated, y8, bits, !x8 || a.exp_words, a.exact8); };
+  const ProductChoice first = choice(op->n);
+  if (first.blocks > 0x7FFFFF) return OCTO_EINVAL;                   // HIP counts the threads of a launch, up to 512 a block, in 32 bits
+  for (ProductChoice c = first;;) {
+    a.n = c.tokens;
+    const hipError_t e = x8 ? launch_product<f8>(c.variant, a, s) : op->dtype == OCTO_F32 ? launch_product<float>(c.variant, a, s)
+                       : op->dtype == OCTO_F16 ? launch_product<_Float16>(c.variant, a, s) : launch_product<__bf16>(c.variant, a, s);
+    if (e != hipSuccess) return OCTO_EHIP;
+    const long long m = c.tokens;
+    a.n_from += c.tokens;
+    if (a.n_from >= op->n) break;
+    a.x += m * a.x_row;
+    if (x8) a.xe += m * a.xe_row;
+    if (a.res) a.res = (const char*)a.res + m * a.res_row * ys;
+    if (y8) { a.y8.d_codes += m * a.y8.code_row; a.y8.d_exps += m * a.y8.exp_row; }
+    else a.y = (char*)a.y + m * a.y_row * ys;
+    c = choice(op->n - a.n_from);
+  }
+  if (kernel_id) *kernel_id = first.variant;
   return OCTO_OK;
 }
