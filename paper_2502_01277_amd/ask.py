@@ -4,8 +4,10 @@
                       -> head norms and rotation by (frame, row, column) -> cache of 4 bits a value      RegionReader.look
     text tokens -> queries (1x1 layer) -> head norms and rotation -> attention to one region's tokens each
                 -> output layer                                                                          RegionReader.ask
+    words so far -> layers of: norm, queries, attention as above, output layer; sum and norm to 8 bits, gated layer and the one behind it in 8 bits
+                 -> norm -> a logit for every word of the vocabulary -> one drawn word a question        RegionWriter.write
 
-The layers, norms, rotations, cache and attention run in the library's kernels, indices and copies in torch's, all on the current stream; nothing
+The layers, norms, rotations, cache, attention and draws run in the library's kernels, indices and copies in torch's, all on the current stream; nothing
 waits for the GPU.  The weights are random, as all of this package's: the module shows how the calls go together.
 
     python -m paper_2502_01277_amd.ask        # the tiny cascade's regions, one question each
@@ -103,6 +105,77 @@ class RegionReader:
         return self._linear(self.to_out, out.view(-1, self.q_heads * self.dim))
 
 
+class RegionWriter:
+    """Words about the regions of a reader, one after the other: `layers` blocks that read a region's tokens, and the draw of the next word.  The gated layers (`hidden` wide) and what
+    goes into them are held in 8 bits with an exponent for each 32 values."""
+
+    def __init__(self, reader, vocab=4096, layers=2, hidden=1024, seed=1):
+        import torch
+        rng = np.random.default_rng(seed)
+        self.reader, self.vocab, self.hidden = reader, vocab, hidden
+        attended = reader.q_heads * reader.dim
+
+        def plain(rows, cols):
+            return torch.from_numpy(rng.standard_normal((rows, cols)).astype(np.float32) / math.sqrt(cols)).to(reader.torch_dtype).cuda()
+
+        def eight(rows, cols):
+            return binding.Mx8(*(torch.from_numpy(a).cuda() for a in binding.quantize_mx8(rng.standard_normal((rows, cols)).astype(np.float32) / math.sqrt(cols))))
+
+        self.words = plain(vocab, reader.width)
+        self.layers = [(plain(attended, reader.width), plain(reader.width, attended), eight(2 * hidden, reader.width), eight(reader.width, hidden)) for _ in range(layers)]
+        self.to_logits = plain(vocab, reader.width)
+        self.weight = torch.ones(reader.width, device="cuda")
+
+    def states(self, words, q_start, regions, frame, max_q=None):
+        """[n][width]: what the layers make of words int32 [n], of which rows q_start[b] .. q_start[b + 1] - 1 are about regions[b] (all as in RegionReader.ask)."""
+        import torch
+        r = self.reader
+        x = self.words[words]
+        n = x.shape[0]
+        pos = torch.zeros(n, 3, dtype=torch.int32, device="cuda")
+        pos[:, 0] = frame
+        start = regions % r.capacity * (GRID * GRID)
+        length = torch.full((regions.shape[0],), GRID * GRID, dtype=torch.int32, device="cuda")
+        normed, delta = torch.empty_like(x), torch.empty_like(x)
+        normed8, inner8 = binding.Mx8.empty(n, r.width), binding.Mx8.empty(n, self.hidden)
+        flat = x.new_empty(n, r.q_heads * r.dim)
+        q = flat.view(n, r.q_heads, r.dim)
+        for to_q, to_out, gate, back in self.layers:
+            binding.op_norm(x, normed, self.weight)
+            binding.op_product(normed, to_q, flat)
+            binding.op_rotate([binding.RotatePart(q, q, r.q_weight)], pos, AXES)
+            out = torch.zeros_like(flat)
+            binding.op_attend(q, r.cache, out.view_as(q), q_start, start, length, max_q=max_q, max_kv=GRID * GRID)
+            binding.op_product(out, to_out, delta)
+            binding.op_norm(x, normed8, self.weight, res=delta, total=x)
+            binding.op_product(normed8, gate, inner8, act="silu", gated=True)
+            binding.op_product(inner8, back, x, res=x)
+        return x
+
+    def draw(self, x, u, logprob=None, **choice):
+        """A word int32 [n] for each state of x [n][width] by random numbers u fp32 [n]; choice: temperature, top_k, top_p, min_p as in op_sample."""
+        import torch
+        n = x.shape[0]
+        normed, logits = torch.empty_like(x), torch.empty(n, self.vocab, dtype=torch.float32, device="cuda")
+        word = torch.empty(n, dtype=torch.int32, device="cuda")
+        binding.op_norm(x, normed, self.weight)
+        binding.op_product(normed, self.to_logits, logits)
+        binding.op_sample(logits, u, word, logprob=logprob, **choice)
+        return word
+
+    def write(self, first, regions, frame, u, **choice):
+        """[words][n]: for each of n questions u.shape[0] words, each drawn by a row of u [words][n] after the one before it; first int32 [n], about regions [n] at frames [n]."""
+        import torch
+        n = first.shape[0]
+        q_start = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+        said = torch.empty(u.shape, dtype=torch.int32, device="cuda")
+        word = first
+        for i in range(u.shape[0]):
+            word = self.draw(self.states(word, q_start, regions, frame, max_q=1), u[i], **choice)
+            said[i] = word
+        return said
+
+
 def main() -> int:
     import torch
     from . import synth, zoo
@@ -124,6 +197,9 @@ def main() -> int:
     answer = reader.ask(text, q_start, regions, frame, max_q=words)
     print("%d regions of %d tokens in %.1f KiB, %d questions of %d tokens, answers %s, rms %.3f" % (
         n, GRID * GRID, n * GRID * GRID * reader.kv_heads * reader.dim * 2 * 17 / 32 / 1024, n, words, tuple(answer.shape), float(answer.float().pow(2).mean().sqrt())))
+    writer = RegionWriter(reader)
+    said = writer.write(torch.zeros(n, dtype=torch.int32, device="cuda"), regions, frame[::words], torch.rand(words, n, device="cuda"), temperature=0.7, top_k=50, top_p=0.9)
+    print("%d words of %d about each: the first region's %s" % (words, writer.vocab, said[:, 0].tolist()))
     return 0
 
 
