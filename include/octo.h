@@ -748,10 +748,13 @@ octo_status octo_op_product(const octo_product_op* op, void* hip_stream, int32_t
  *   (and the first).  What all three keep is drawn from in the order of indices: the first token at which the sum of kept weights exceeds u times all of them.
  * temperature <= 0 (or NaN): the first in order.  -infinity and NaN are tokens that may not be drawn; +infinity is the only one drawn where it occurs.  A row without any token: d_token -1, d_kept
  * 0, d_logprob -infinity.  A NaN among top_p and min_p keeps all; u is taken as 0 .. 1 - 2^-24.
- * Weights are computed in 64 bits and added up as integers, multiples of 2^-(62 - log2 vocab) (2^-50 at most) of the largest: same inputs, same token, on any device.
+ * Weights have exponents in 64 bits and a relative error of 2^-35; they are added up as integers, multiples of 2^-(62 - log2 vocab) (2^-50 at most) of the largest: the same inputs give
+ * the same token, with a workspace or without.
  * d_logits: rows of `dtype` (OCTO_F32, _F16, _BF16), `row` elements apart, at any address of an element, vocab up to OCTO_MAX_VOCAB.  d_u: fp32 [n], in [0, 1).  d_temperature,
  * d_top_k, d_top_p, d_min_p: one for each row, on the device, or NULL: the number beside it for all.  d_token: int32 [n]; d_logprob: NULL or fp32 [n], the logarithm of the token's share
- * of the kept weights; d_kept: NULL or int32 [n], how many were kept.  d_n: NULL, or the number of rows present, on the device: later rows are left as they were. */
+ * of the kept weights; d_kept: NULL or int32 [n], how many were kept.  d_n: NULL, or the number of rows present, on the device: later rows are left as they were.
+ * d_workspace: octo_op_sample_workspace_bytes(op) bytes, 16-byte aligned, for this call alone until it is done: few long rows are shared among the compute units.  Or NULL, and each
+ * row is one compute unit's. */
 #define OCTO_MAX_VOCAB (1 << 19)
 typedef struct octo_sample_op {
   int32_t dtype, n, vocab, pad_;
@@ -761,8 +764,11 @@ typedef struct octo_sample_op {
   float temperature; int32_t top_k; float top_p, min_p;
   int32_t* d_token; float* d_logprob; int32_t* d_kept;
   const int32_t* d_n;
+  void* d_workspace; size_t workspace_bytes;
 } octo_sample_op;
 octo_status octo_op_sample(const octo_sample_op* op, void* hip_stream);
+/* Bytes of workspace with which that call shares few long rows among the compute units (0: none, or the arguments are not valid); looks at sizes, types, the presence of d_top_k and top_k only. */
+size_t octo_op_sample_workspace_bytes(const octo_sample_op* op);
 
 #ifdef __cplusplus
 }

@@ -198,7 +198,7 @@ class OctoSampleOp(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("n", C.c_int32), ("vocab", C.c_int32), ("pad_", C.c_int32), ("d_logits", C.c_void_p), ("row", C.c_int64), ("d_u", C.c_void_p),
                 ("d_temperature", C.c_void_p), ("d_top_k", C.c_void_p), ("d_top_p", C.c_void_p), ("d_min_p", C.c_void_p),
                 ("temperature", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float),
-                ("d_token", C.c_void_p), ("d_logprob", C.c_void_p), ("d_kept", C.c_void_p), ("d_n", C.c_void_p)]
+                ("d_token", C.c_void_p), ("d_logprob", C.c_void_p), ("d_kept", C.c_void_p), ("d_n", C.c_void_p), ("d_workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
 
 
 # Every symbol include/octo.h declares.
@@ -216,7 +216,7 @@ EXPORTS = [
     "octo_op_conv", "octo_op_conv_packed_bytes", "octo_op_conv_padded_cout", "octo_op_conv_pack", "octo_quantize_e4m3", "octo_dequantize_e4m3",
     "octo_op_rotate", "octo_op_cache4_store", "octo_op_cache4_load", "octo_quantize_mx4", "octo_dequantize_mx4",
     "octo_op_attend", "octo_op_attend_workspace_bytes",
-    "octo_op_norm", "octo_op_mx8_load", "octo_quantize_mx8", "octo_dequantize_mx8", "octo_op_product", "octo_op_sample",
+    "octo_op_norm", "octo_op_mx8_load", "octo_quantize_mx8", "octo_dequantize_mx8", "octo_op_product", "octo_op_sample", "octo_op_sample_workspace_bytes",
 ]
 
 _lib = None
@@ -319,6 +319,8 @@ def lib() -> C.CDLL:
         L.octo_op_mx8_load.argtypes = [vp, vp]
         L.octo_op_product.argtypes = [vp, vp, vp]
         L.octo_op_sample.argtypes = [vp, vp]
+        L.octo_op_sample_workspace_bytes.argtypes = [vp]
+        L.octo_op_sample_workspace_bytes.restype = C.c_size_t
         L.octo_quantize_mx8.argtypes = [vp, C.c_size_t, vp, vp]
         L.octo_dequantize_mx8.argtypes = [vp, vp, C.c_size_t, vp]
         _lib = L
@@ -859,7 +861,7 @@ _MX8_ROWS = "PPqq"
 _NORM = struct.Struct("@5if4P4q" + _MX8_ROWS + "PP")
 _MX8 = struct.Struct("@4i" + _MX8_ROWS + "PqP")
 _PRODUCT = struct.Struct("@10iPPqq" + 2 * _MX8_ROWS + "PPPqq" + _MX8_ROWS + "P")
-_SAMPLE = struct.Struct("@4iPqP4PfiffPPPP")
+_SAMPLE = struct.Struct("@4iPqP4PfiffPPPPPN")
 _ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 _NO_MX8, _NO_ROWS = (0,) * 4, (0,) * 8
 _NO_PART, _NO_PLANE, _NO_KV, _NO_SECTIONS = {1: (0,) * 9, 2: ()}, (0,) * 6, (0,) * 6, (0,) * MAX_AXES
@@ -1220,10 +1222,8 @@ def op_product(x, w, y, bias=None, act="none", gated=False, res=None, n=None, st
     return kid.value
 
 
-def op_sample(logits, u, token, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, logprob=None, kept=None, n=None, stream=None):
-    """One token of each row of logits [rows][vocab] by random numbers u fp32 [rows] (octo_sample_op in octo.h), into token int32 [rows].  temperature, top_k, top_p,
-    min_p: a number for all rows, or a device tensor with one for each (fp32, top_k int32); logprob fp32 and kept int32 [rows] or None.  n: int32 device tensor with the
-    number of rows present, or None."""
+def _sample_pack(logits, u, token, temperature, top_k, top_p, min_p, logprob, kept, n):
+    """(rows, all fields but the workspace)."""
     t = _torch()
     shape, stride = logits.shape, logits.stride()
     if len(shape) != 2 or not logits.is_cuda or (shape[1] > 1 and stride[1] != 1):
@@ -1235,15 +1235,40 @@ def op_sample(logits, u, token, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, 
         at.append(_optional(x, kind, "%s is a number or %s [rows] on the device" % (what, kind), rows) if each else 0)
         alone.append(none if each or x is None else x)
     if not rows or not shape[1]:
+        return 0, ()
+    return rows, (_CODE[logits.dtype], rows, shape[1], 0, logits.data_ptr(), stride[0], _optional(u, t.float32, "u is fp32 [rows] on the device", rows), *at, *alone,
+                  _optional(token, t.int32, "token is int32 [rows] on the device", rows), 0 if logprob is None else _optional(logprob, t.float32, "logprob is fp32 [rows] on the device", rows),
+                  0 if kept is None else _optional(kept, t.int32, "kept is int32 [rows] on the device", rows), 0 if n is None else _optional(n, t.int32, "n is int32 on the device"))
+
+
+def op_sample(logits, u, token, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, logprob=None, kept=None, n=None, workspace=None, stream=None):
+    """One token of each row of logits [rows][vocab] by random numbers u fp32 [rows] (octo_sample_op in octo.h), into token int32 [rows].  temperature, top_k, top_p,
+    min_p: a number for all rows, or a device tensor with one for each (fp32, top_k int32); logprob fp32 and kept int32 [rows] or None.  n: int32 device tensor with the
+    number of rows present, or None.  workspace: uint8 device tensor of sample_workspace_bytes(...) or None to take one here."""
+    rows, fields = _sample_pack(logits, u, token, temperature, top_k, top_p, min_p, logprob, kept, n)
+    if not rows:
         return
-    op = _SAMPLE.pack(_CODE[logits.dtype], rows, shape[1], 0, logits.data_ptr(), stride[0], _optional(u, t.float32, "u is fp32 [rows] on the device", rows), *at, *alone,
-                      _optional(token, t.int32, "token is int32 [rows] on the device", rows), 0 if logprob is None else _optional(logprob, t.float32, "logprob is fp32 [rows] on the device", rows),
-                      0 if kept is None else _optional(kept, t.int32, "kept is int32 [rows] on the device", rows), 0 if n is None else _optional(n, t.int32, "n is int32 on the device"))
+    if workspace is not None:
+        _optional(workspace, _torch().uint8, "workspace is dense uint8 on the device", 0)
+    L = lib()
+    op = _SAMPLE.pack(*fields, 0, 0)
+    need = L.octo_op_sample_workspace_bytes(op)
+    scratch = ()
+    if need:
+        if workspace is None:
+            workspace = _torch().empty(need, dtype=_torch().uint8, device=logits.device)
+            scratch = (workspace,)
+        op = _SAMPLE.pack(*fields, workspace.data_ptr(), workspace.numel())
     if stream is not None:
-        _order(stream)
-    st = lib().octo_op_sample(op, _stream_ptr(stream))
+        _order(stream, *scratch)
+    st = L.octo_op_sample(op, _stream_ptr(stream))
     if st:
         _st(st)
+
+
+def sample_workspace_bytes(logits, u, token, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, logprob=None, kept=None, n=None) -> int:
+    rows, fields = _sample_pack(logits, u, token, temperature, top_k, top_p, min_p, logprob, kept, n)
+    return lib().octo_op_sample_workspace_bytes(_SAMPLE.pack(*fields, 0, 0)) if rows else 0
 
 
 def quantize_mx8(x: np.ndarray):

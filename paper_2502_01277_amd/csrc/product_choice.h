@@ -15,7 +15,7 @@ constexpr int product_held_steps(int r, bool rows8) { return r == 4 ? (rows8 ? 4
 // go through bf16, which has no tiles of 256 x 256.
 inline ProductChoice product_choice(int n, int k_bytes, int cols, bool gated, bool to8, int bits, bool words, bool exact8) {
   const long long rows = gated ? 2ll * cols : cols;
-  auto blocks = [&](int bn, int bm) { return (rows + bn - 1) / bn * ((n + bm - 1) / bm); };
+  auto blocks = [&](int bn, int bm) { return (rows + bn - 1) / bn * ((n + bm - 1ll) / bm); };
   auto few = [&](int r, int t) { const int outs = gated ? 8 * r : 16 * r; return ProductChoice{10 * r + t, (cols + outs - 1ll) / outs * ((n + 16ll * t - 1) / (16 * t)), n}; };
   if (n <= 16) {
     if (words) {

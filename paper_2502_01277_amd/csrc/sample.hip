@@ -19,7 +19,7 @@
 namespace octo {
 namespace {
 
-constexpr int SAMPLE_THREADS = 1024, SAMPLE_WAVES = 16, BINS = 4096, SORTED = 2048, LISTED = 512;
+constexpr int SAMPLE_THREADS = 1024, SAMPLE_WAVES = 16, BINS = 4096, SORTED = 2048, LISTED = 512, MOST_PARTS = 8;
 typedef unsigned long long u64;
 
 struct SampleArgs {
@@ -29,6 +29,8 @@ struct SampleArgs {
   int* token; float* logprob; int* kept;
   const int* n_dyn;
   int vocab, shift;
+  int parts;                // workgroups of a row where there are few rows, or 0
+  float* part_best; u64* part_weight; unsigned* part_count;           // [n][parts], and histograms [n][parts][BINS]
 };
 
 // Floats as integers of the same order, both zeros alike.
@@ -59,6 +61,8 @@ struct Weigher {
   const double* table;      // 2^(j / STEPS), in LDS
   double best, factor;      // t = (v - best) factor
   int shift;
+  double least;             // min-p as an exponent in steps: weights have no bits where it may lie
+  __device__ __forceinline__ bool dropped(float v) const { return ((double)v - best) * factor < least; }
   static constexpr u64 ZERO = 0x4330000000000000ull;                 // 2^52: integers added to it lie in its low bits
   __device__ __forceinline__ double steps(float v) const {
     return fmax(((double)v - best) * factor, -73728.0);           // 72 octaves down nothing is left; also for what is no number (-infinity, NaN, at an infinite temperature too)
@@ -107,25 +111,15 @@ struct SampleShared {
 // The last token that is kept: all whose ordered logit is above `key`, and of those equal to it the ones up to index `at`.
 struct Last { unsigned key; int at; };
 
-template <typename T>
-__global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
-  constexpr int VEC = 16 / sizeof(T), DEPTH = 4;
-  __shared__ SampleShared s;
-  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  if (a.n_dyn && row >= *a.n_dyn) return;
-  const T* const x = (const T*)a.logits + row * a.row;
-  const float temperature = a.temperature ? a.temperature[row] : a.all_temperature;
-  const int top_k = a.top_k ? a.top_k[row] : a.all_top_k;
-  const float top_p = a.top_p ? a.top_p[row] : a.all_top_p, min_p = a.min_p ? a.min_p[row] : a.all_min_p;
-  const float u = fminf(fmaxf(a.u[row], 0.f), 0.99999994f);
-
-  // Positions are indices plus the distance of the row's start from the last 16-byte border before it, so that vectors are aligned; a wavefront has a range of them, lanes have
-  // neighbouring vectors.
-  const int skew = (int)(((uintptr_t)x & 15) / sizeof(T)), end = a.vocab + skew;
-  const int tiles = (end + SAMPLE_WAVES * 64 * VEC - 1) / (SAMPLE_WAVES * 64 * VEC);                 // vectors of a lane
-  const int range_len = tiles * 64 * VEC;                                                            // positions of a wavefront
-  bool odd = false;
-  auto load = [&](int p) __attribute__((always_inline)) -> u32x4 {
+// Positions are indices plus the distance of the row's start from the last 16-byte border before it, so that vectors are aligned.
+template <typename T> struct SampleRow {
+  static constexpr int VEC = 16 / sizeof(T), DEPTH = 4;
+  const T* x; int skew, end;
+  bool odd;                 // a row with infinite logits is one of zeros and ones: those weigh 1, the others that may be drawn nothing
+  __device__ __forceinline__ SampleRow(const SampleArgs& a, int row) : x((const T*)a.logits + row * a.row), odd(false) {
+    skew = (int)(((uintptr_t)x & 15) / sizeof(T)); end = a.vocab + skew;
+  }
+  __device__ __forceinline__ u32x4 load(int p) const {
     u32x4 v;
     if (p >= skew && p + VEC <= end) {
       v = *(const u32x4*)(x + (p - skew));
@@ -138,9 +132,9 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       for (int e = 0; e < VEC; ++e) { const float f = (float)((T*)&v)[e]; ((T*)&v)[e] = (T)(f == INFINITY ? 0.f : f > -INFINITY ? -1.f : -INFINITY); }
     }
     return v;
-  };
+  }
   // f(position, vector) of the positions from, from + stride ...
-  auto vectors = [&](int from, int count, int stride, auto&& f) __attribute__((always_inline)) {
+  template <typename F> __device__ __forceinline__ void vectors(int from, int count, int stride, F&& f) const {
     for (int i0 = 0; i0 < count; i0 += DEPTH) {
       u32x4 v[DEPTH];
 #pragma unroll
@@ -148,10 +142,10 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
 #pragma unroll
       for (int d = 0; d < DEPTH; ++d) if (i0 + d < count) f(from + (i0 + d) * stride, v[d]);
     }
-  };
-  auto value = [&](const u32x4& v, int e) __attribute__((always_inline)) { return (float)((const T*)&v)[e]; };
+  }
+  static __device__ __forceinline__ float value(const u32x4& v, int e) { return (float)((const T*)&v)[e]; }
   // f(index, logit) of every token there that may be drawn
-  auto each = [&](int from, int count, int stride, auto&& f) __attribute__((always_inline)) {
+  template <typename F> __device__ __forceinline__ void each(int from, int count, int stride, F&& f) const {
     vectors(from, count, stride, [&](int p, const u32x4& v) __attribute__((always_inline)) {
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
@@ -159,7 +153,92 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
         if (f32 > -INFINITY) f(p + e - skew, f32);                   // neither -infinity nor NaN
       }
     });
-  };
+  }
+  // vectors of a lane where `ways` workgroups share the row; a part is whole vectors of all threads of one
+  __device__ __forceinline__ int tiles(int ways) const { return (end + ways * SAMPLE_THREADS * VEC - 1) / (ways * SAMPLE_THREADS * VEC); }
+};
+
+// What a row is drawn by.
+struct SampleChoice {
+  float temperature, top_p, min_p; int top_k;
+  __device__ __forceinline__ SampleChoice(const SampleArgs& a, int row)
+      : temperature(a.temperature ? a.temperature[row] : a.all_temperature), top_p(a.top_p ? a.top_p[row] : a.all_top_p), min_p(a.min_p ? a.min_p[row] : a.all_min_p),
+        top_k(a.top_k ? a.top_k[row] : a.all_top_k) {}
+  __device__ __forceinline__ bool first_alone() const { return !(temperature > 0) || top_k == 1 || top_p <= 0 || min_p > 1; }
+  __device__ __forceinline__ bool short_list() const { return top_k > 0 && top_k <= LISTED; }
+  __device__ __forceinline__ double factor() const { return (double)STEPS * 1.4426950408889634 / (double)temperature; }
+};
+
+// ---- few rows: the largest logit and the histogram of weights by `parts` workgroups a row ----------------------------------
+template <typename T>
+__global__ __launch_bounds__(SAMPLE_THREADS) void sample_best_kernel(SampleArgs a) {
+  __shared__ float wave_max[SAMPLE_WAVES];
+  const int row = blockIdx.x / a.parts, part = blockIdx.x % a.parts, tid = threadIdx.x;
+  if (a.n_dyn && row >= *a.n_dyn) return;
+  const SampleRow<T> x(a, row);
+  const int tiles = x.tiles(a.parts), stride = SAMPLE_THREADS * x.VEC;
+  float best = -INFINITY;
+  x.vectors(part * tiles * stride + tid * x.VEC, tiles, stride, [&](int, const u32x4& v) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < x.VEC; ++e) best = fmaxf(best, x.value(v, e));          // the other one where one is NaN
+  });
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) best = fmaxf(best, __shfl_xor(best, d));
+  if (!(tid & 63)) wave_max[tid >> 6] = best;
+  __syncthreads();
+  if (tid) return;
+  for (int w = 0; w < SAMPLE_WAVES; ++w) best = fmaxf(best, wave_max[w]);
+  a.part_best[blockIdx.x] = best;
+}
+
+template <typename T>
+__global__ __launch_bounds__(SAMPLE_THREADS) void sample_part_kernel(SampleArgs a) {
+  __shared__ double table[STEPS];
+  __shared__ u64 weight[BINS];
+  __shared__ unsigned count[BINS];
+  const int row = blockIdx.x / a.parts, part = blockIdx.x % a.parts, tid = threadIdx.x;
+  if (a.n_dyn && row >= *a.n_dyn) return;
+  const SampleChoice by(a, row);
+  float best = -INFINITY;
+  for (int p = 0; p < a.parts; ++p) best = fmaxf(best, a.part_best[row * a.parts + p]);
+  if (!(best > -INFINITY) || best == INFINITY || by.first_alone() || by.short_list()) return;       // rows that the last kernel does alone
+  const SampleRow<T> x(a, row);
+  const Weigher weigh{table, (double)best, by.factor(), a.shift, -INFINITY};
+  table[tid] = octave.v[tid];
+  for (int b = tid; b < BINS; b += SAMPLE_THREADS) { weight[b] = 0; count[b] = 0; }
+  __syncthreads();
+  const int tiles = x.tiles(a.parts), stride = SAMPLE_THREADS * x.VEC;
+  x.each(part * tiles * stride + tid * x.VEC, tiles, stride, [&](int, float v) __attribute__((always_inline)) {
+    int k;
+    const u64 q = Weigher::whole(weigh.scaled(weigh.steps(v), &k));
+    const int bin = Weigher::bin_of(k);
+    if (q) atomicAdd(&weight[bin], q);
+    atomicAdd(&count[bin], 1u);
+  });
+  __syncthreads();
+  u64* const to_w = a.part_weight + (long long)blockIdx.x * BINS;
+  unsigned* const to_c = a.part_count + (long long)blockIdx.x * BINS;
+  for (int b = tid; b < BINS; b += SAMPLE_THREADS) { to_w[b] = weight[b]; to_c[b] = count[b]; }
+}
+
+template <typename T>
+__global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
+  constexpr int VEC = SampleRow<T>::VEC;
+  __shared__ SampleShared s;
+  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  if (a.n_dyn && row >= *a.n_dyn) return;
+  const SampleChoice by(a, row);
+  const float temperature = by.temperature, top_p = by.top_p, min_p = by.min_p;
+  const int top_k = by.top_k;
+  const float u = fminf(fmaxf(a.u[row], 0.f), 0.99999994f);
+
+  // a wavefront has a range of positions, lanes have neighbouring vectors
+  SampleRow<T> x(a, row);
+  const int skew = x.skew, tiles = x.tiles(1);                       // vectors of a lane
+  const int range_len = tiles * 64 * VEC;                            // positions of a wavefront
+  auto vectors = [&](int from, int count, int stride, auto&& f) __attribute__((always_inline)) { x.vectors(from, count, stride, f); };
+  auto each = [&](int from, int count, int stride, auto&& f) __attribute__((always_inline)) { x.each(from, count, stride, f); };
+  auto value = [&](const u32x4& v, int e) __attribute__((always_inline)) { return x.value(v, e); };
   const int mine = wave * range_len + lane * VEC;
   auto all = [&](auto&& f) __attribute__((always_inline)) { each(mine, tiles, 64 * VEC, f); };
   auto answer = [&](int token, int kept, double logprob) {
@@ -171,7 +250,9 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
   s.table[tid] = octave.v[tid];
   // the largest logit, of this thread and of all, and the largest magnitude
   float own = -INFINITY, big = 0.f;
-  vectors(mine, tiles, 64 * VEC, [&](int, const u32x4& v) __attribute__((always_inline)) {
+  const bool in_parts = !std::is_same<T, __bf16>::value && a.parts && !by.short_list();
+  if (in_parts) { if (tid < a.parts) own = a.part_best[row * a.parts + tid]; }
+  else vectors(mine, tiles, 64 * VEC, [&](int, const u32x4& v) __attribute__((always_inline)) {
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
       const float f = value(v, e);
@@ -190,20 +271,19 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
     if (!tid) answer(-1, 0, -INFINITY);
     return;
   }
-  if (!(temperature > 0) || top_k == 1 || top_p <= 0 || min_p > 1) {
+  if (by.first_alone()) {
     // the first in order alone
     all([&](int i, float v) { if (v == best) atomicMin(&s.at, (unsigned)i); });
     __syncthreads();
     if (!tid) answer((int)s.at, 1, 0.0);
     return;
   }
-  // A row with infinite logits is one of zeros and ones: those weigh 1, the others that may be drawn nothing.
-  odd = best == INFINITY;
+  const bool odd = x.odd = best == INFINITY, split = in_parts && !odd;
   if (odd) { best = 0.f; own = own == INFINITY ? 0.f : own > -INFINITY ? -1.f : -INFINITY; }
-  const double factor = odd ? 1e6 : (double)STEPS * 1.4426950408889634 / (double)temperature;
-  const Weigher weigh{s.table, (double)best, factor, a.shift};
+  const double factor = odd ? 1e6 : by.factor();
+  const Weigher weigh{s.table, (double)best, factor, a.shift, min_p > 0 ? log2((double)min_p) * STEPS : -INFINITY};
   const bool by_p = top_p < 1.0f;
-  const double least = min_p > 0 ? ldexp((double)min_p, a.shift) : -1.0;               // of scaled weights; NaN: none
+  const bool by_min = min_p > 0;                                     // NaN: none
 
   // sums over the threads before this one and over all; ends with all threads past its use of LDS
   auto block_scan = [&](u64 w, unsigned c, u64* before_w, unsigned* before_c, u64* all_w, unsigned* all_c) __attribute__((always_inline)) {
@@ -232,7 +312,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
   auto logprob_of = [&](float v, u64 kept_w) { return weigh.steps(v) * (0.69314718055994530942 / STEPS) - log(ldexp((double)kept_w, -a.shift)); };
 
   // ---- a short list -----------------------------------------------------------------------------------------------------
-  if (top_k > 0 && top_k <= LISTED) {
+  if (by.short_list()) {
     // the largest key of 20 bits that top_k threads reach with their own largest logit, bit by bit (0 where fewer have any)
     unsigned floor_key = 0;
     const unsigned own_key = own > -INFINITY ? ordered(own) : 0;
@@ -276,7 +356,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
         if (!lane) s.wave_w[wave] = sum;
         __syncthreads();
         sum = s.wave_w[0] + s.wave_w[1] + s.wave_w[2] + s.wave_w[3];
-        const bool keep = chosen && (!place || ((double)before < limit * (double)sum && (!(w < least) || v == best)));
+        const bool keep = chosen && (!place || ((double)before < limit * (double)sum && !weigh.dropped(v)));
         if (tid < 256) { s.weight[i] = keep ? q : 0; s.weight[256 + i] = 0; }
         const int kept = __syncthreads_count(keep);
         before = 0;
@@ -302,7 +382,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       double w = 0.0;
       if (tid < k) { entry = s.list[tid]; w = weigh.scaled(unordered(~(unsigned)(entry >> 32))); q = Weigher::whole(w); }
       block_scan(q, 0, &bw, &bc, &aw, &ac);
-      const bool keep = tid < k && (!tid || ((double)bw < limit * (double)aw && (!(w < least) || (unsigned)~(unsigned)(entry >> 32) == ordered(best))));
+      const bool keep = tid < k && (!tid || ((double)bw < limit * (double)aw && !weigh.dropped(unordered(~(unsigned)(entry >> 32)))));
       // what is kept is a beginning; in the order of the indices
       const int kept = __syncthreads_count(keep);
       padded = 1;
@@ -343,7 +423,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
   u64 last_q = 0;
   bool tiny_kept = true;
   if constexpr (std::is_same<T, __bf16>::value) {
-    if (!odd && big < INFINITY && (by_p || top_k > 0)) {
+    if (!odd && !in_parts && big < INFINITY && (by_p || top_k > 0)) {
       for (int b = tid; b < BINS; b += SAMPLE_THREADS) s.count[b] = 0;
       __syncthreads();
       vectors(mine, tiles, 64 * VEC, [&](int, const u32x4& v) __attribute__((always_inline)) {
@@ -373,9 +453,9 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
         q[e] = Weigher::whole(w);
         s.weight[4 * tid + e] = q[e];
         w4 += q[e] * c[e]; c4 += c[e];
-        if (c[e] && w < least && code_of_entry(4 * tid + e) != best) cut = min(cut, 4 * tid + e);
+        if (c[e] && weigh.dropped(code_of_entry(4 * tid + e))) cut = min(cut, 4 * tid + e);
       }
-      if (least > 0) atomicMin(&s.cut, cut);
+      if (by_min) atomicMin(&s.cut, cut);
       u64 bw, aw; unsigned bc, ac;
       block_scan(w4, c4, &bw, &bc, &aw, &ac);
       kept_w = aw; kept = ac;
@@ -412,10 +492,10 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       };
       if (top_k > 0) border(true, (unsigned)top_k, 0.0);
       if (by_p) border(false, 0, (double)top_p * (double)kept_w);
-      if (least > 0) {
+      if (by_min) {
         // tiny ones lie on both sides of the least weight, or all on one
         int tiny_in = 0, tiny_out = 0;
-        for (int i = tid; i < (int)min(tiny_c, (unsigned)SORTED); i += SAMPLE_THREADS) { const float t = unordered((unsigned)s.list[i]); if (weigh.scaled(t) < least && t != best) tiny_out = 1; else tiny_in = 1; }
+        for (int i = tid; i < (int)min(tiny_c, (unsigned)SORTED); i += SAMPLE_THREADS) { const float t = unordered((unsigned)s.list[i]); if (weigh.dropped(t)) tiny_out = 1; else tiny_in = 1; }
         tiny_in = __syncthreads_or(tiny_in); tiny_out = __syncthreads_or(tiny_out);
         const int j = min(s.cut, BINS);                              // the first counted entry that is dropped
         if (tiny_out && tiny_in && last_entry >= 2048) fits = false;
@@ -444,6 +524,12 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       if (!fits) { kept_w = 0; kept = 0; if (!tid) s.listed = 0; __syncthreads(); }
     }
   }
+
+  // the logit that lies `bins` bins below the largest, rounded down or up: what is beyond it needs no exponent to be told from those of a bin two further in
+  auto above = [&](int bins, bool up) __attribute__((always_inline)) {
+    const double v = (double)best - (double)bins * 16.0 / factor;
+    return up ? __double2float_ru(v) : __double2float_rd(v);
+  };
 
   if (!counted) {
     // ---- histograms of weights ------------------------------------------------------------------------------------------------
@@ -478,7 +564,8 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
         u64 base_w = s.before_w;
         __syncthreads();
         if (w_bin < 0) return base_w;
-        auto in_group = [&](float v) __attribute__((always_inline)) { return (ordered(v) & mask) == bits && weigh.bin(v) == w_bin; };
+        const float low = above(w_bin == BINS - 1 ? BINS * 64 : w_bin + 2, false), high = above(w_bin - 2, true);
+        auto in_group = [&](float v) __attribute__((always_inline)) { return v >= low && v <= high && (ordered(v) & mask) == bits && weigh.bin(v) == w_bin; };
         for (int level = 0; size > SORTED && level < 3; ++level) {
           const int down = level == 0 ? 20 : level == 1 ? 8 : 0, digits = level < 2 ? 4096 : 256;
           clear();
@@ -527,25 +614,63 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
           __syncthreads();
           return base_w + m * q;
         }
-        if (!tid) s.listed = 0;
-        int padded = 1;
-        while (1 << padded < (int)size) ++padded;
-        for (int i = tid; i < 1 << padded; i += SAMPLE_THREADS) s.list[i] = ~0ull;
+        if (!tid) { s.listed = 0; s.votes[0] = 0xFFFFFFFFu; s.votes[1] = 0; }
         __syncthreads();
         all([&](int i, float v) { if (in_group(v)) s.list[atomicAdd(&s.listed, 1)] = (u64)~ordered(v) << 32 | (unsigned)i; });      // larger logits first, equal ones by index
         __syncthreads();
-        sort_list(padded);
         // two entries a thread
-        u64 q[2] = {0, 0}; unsigned c = 0;
-        for (int e = 0; e < 2; ++e) if (2 * tid + e < (int)size) { q[e] = weigh(unordered(~(unsigned)(s.list[2 * tid + e] >> 32))); ++c; }
-        u64 bw, aw; unsigned bc, ac;
-        block_scan(q[0] + q[1], c, &bw, &bc, &aw, &ac);
-        bw += base_w; bc += base_c;
-        for (int e = 0; e < (int)c; ++e) {
-          const bool before = by_count ? bc < limit_c : !bc || (double)bw < limit_w;
-          ++bc; bw += q[e];
-          const bool after = by_count ? bc >= limit_c : (double)bw >= limit_w;
-          if (before && after) { s.key = ~(unsigned)(s.list[2 * tid + e] >> 32); s.at = (unsigned)s.list[2 * tid + e]; s.before_w = bw; }
+        u64 entry[2];
+        for (int e = 0; e < 2; ++e) entry[e] = tid + e * SAMPLE_THREADS < (int)size ? s.list[tid + e * SAMPLE_THREADS] : ~0ull;
+        auto key_of = [](u64 x) { return (unsigned)(x >> 32); };
+        auto logit_of = [&](u64 x) { return unordered(~key_of(x)); };
+        if (size > 64) {
+          // one more histogram, of the list's own range of logits
+          unsigned lo = min(key_of(entry[0]), key_of(entry[1])), hi = max(entry[0] == ~0ull ? 0u : key_of(entry[0]), entry[1] == ~0ull ? 0u : key_of(entry[1]));
+#pragma unroll
+          for (int d = 1; d < 64; d *= 2) { lo = min(lo, (unsigned)__shfl_xor((int)lo, d)); hi = max(hi, (unsigned)__shfl_xor((int)hi, d)); }
+          if (!lane) { atomicMin(&s.votes[0], lo); atomicMax(&s.votes[1], hi); }
+          clear();
+          lo = s.votes[0]; hi = s.votes[1];
+          const int down = max(20 - __clz(hi - lo | 1), 0);
+          for (int e = 0; e < 2; ++e)
+            if (entry[e] != ~0ull) { const int d = (int)((key_of(entry[e]) - lo) >> down); atomicAdd(&s.weight[d], weigh(logit_of(entry[e]))); atomicAdd(&s.count[d], 1u); }
+          __syncthreads();
+          find_bin(by_count, limit_c, limit_w, base_c, base_w);
+          const unsigned digit = (unsigned)s.bin;
+          size = s.bin_count; base_c = s.before_c; base_w = s.before_w;
+          for (int e = 0; e < 2; ++e) if (entry[e] != ~0ull && (key_of(entry[e]) - lo) >> down != digit) entry[e] = ~0ull;
+          if (!tid) s.listed = 0;
+          __syncthreads();
+          for (int e = 0; e < 2; ++e) if (entry[e] != ~0ull) s.list[atomicAdd(&s.listed, 1)] = entry[e];
+          __syncthreads();
+        }
+        auto decide = [&](u64 x, bool before, bool after, u64 w) { if (before && after) { s.key = ~key_of(x); s.at = (unsigned)x; s.before_w = w; } };
+        if (size <= 64) {
+          // what lies before an entry is added up by its own thread
+          const u64 x = tid < (int)size ? s.list[tid] : ~0ull, q = tid < (int)size ? weigh(logit_of(x)) : 0;
+          if (tid < 64) s.weight[tid] = q;
+          __syncthreads();
+          unsigned c = base_c; u64 w = base_w;
+          if (tid < (int)size) {
+            for (int j = 0; j < (int)size; ++j) if (s.list[j] < x) { ++c; w += s.weight[j]; }
+            decide(x, by_count ? c < limit_c : !c || (double)w < limit_w, by_count ? c + 1 >= limit_c : (double)(w + q) >= limit_w, w + q);
+          }
+        } else {
+          int padded = 1;
+          while (1 << padded < (int)size) ++padded;
+          for (int i = (int)size + tid; i < 1 << padded; i += SAMPLE_THREADS) s.list[i] = ~0ull;
+          __syncthreads();
+          sort_list(padded);
+          u64 q[2] = {0, 0}; unsigned c = 0;
+          for (int e = 0; e < 2; ++e) if (2 * tid + e < (int)size) { q[e] = weigh(logit_of(s.list[2 * tid + e])); ++c; }
+          u64 bw, aw; unsigned bc, ac;
+          block_scan(q[0] + q[1], c, &bw, &bc, &aw, &ac);
+          bw += base_w; bc += base_c;
+          for (int e = 0; e < (int)c; ++e) {
+            const bool before = by_count ? bc < limit_c : !bc || (double)bw < limit_w;
+            ++bc; bw += q[e];
+            decide(s.list[2 * tid + e], before, by_count ? bc >= limit_c : (double)bw >= limit_w, bw);
+          }
         }
         __syncthreads();
         last = Last{s.key, (int)s.at};
@@ -554,6 +679,16 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
         return sum;
       };
       auto histogram = [&]() {
+        if (split) {
+          const long long at = (long long)row * a.parts * BINS;
+          for (int b = tid; b < BINS; b += SAMPLE_THREADS) {
+            u64 w = 0; unsigned c = 0;
+            for (int p = 0; p < a.parts; ++p) { w += a.part_weight[at + p * BINS + b]; c += a.part_count[at + p * BINS + b]; }
+            s.weight[b] = w; s.count[b] = c;
+          }
+          __syncthreads();
+          return;
+        }
         clear();
         all([&](int, float v) {
           int k;
@@ -613,33 +748,65 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
           keep = keep && (key > last.key || (key == last.key && p + e - skew <= last.at));
         }
         const double w = weigh.scaled(keep ? v : -INFINITY);
-        if (least > 0) keep = keep && (!(w < least) || v == best);
+        keep = keep && !weigh.dropped(v);
         f(p + e - skew, v, keep ? Weigher::whole(w) : 0ull, keep);
       }
     });
   };
-  u64 sum = 0; unsigned count = 0;                                   // count: of what is kept, or of the last code
-  weights(mine, tiles, 64 * VEC, [&](int, float, u64 q, bool keep) __attribute__((always_inline)) {
-    if (counted) { if (q == ~0ull) ++count; else sum += q; }
-    else { sum += q; count += keep; }
-  });
-  sum = wave_sum(sum); count = wave_sum(count);
-  if (!lane) { s.wave_w[wave] = sum; s.wave_c[wave] = count; }
+  const int ranges = split ? a.parts : SAMPLE_WAVES, draw_len = split ? x.tiles(a.parts) * SAMPLE_THREADS * VEC : range_len;
+  if (split) {
+    // Bins before the last one are kept as a whole, their sums are there for each part; tokens of the others are looked at one by one.
+    int whole = last.key ? weigh.bin(unordered(last.key)) : BINS;
+    float low = last.key ? unordered(last.key) : -INFINITY;
+    if (by_min) {
+      const int bins = (int)fmin(-log2((double)min_p) * (STEPS / 16), (double)BINS);
+      whole = min(whole, max(bins - 1, 0));
+      if (bins < BINS) low = fmaxf(low, above(bins + 3, false));
+    }
+    if (tid < SAMPLE_WAVES) { s.wave_w[tid] = 0; s.wave_c[tid] = 0; }
+    __syncthreads();
+    for (int p = 0; p < a.parts; ++p) {
+      const long long at = ((long long)row * a.parts + p) * BINS;
+      u64 w = 0; unsigned c = 0;
+      for (int b = tid; b < whole; b += SAMPLE_THREADS) { w += a.part_weight[at + b]; c += a.part_count[at + b]; }
+      w = wave_sum(w); c = wave_sum(c);
+      if (!lane) { atomicAdd(&s.wave_w[p], w); atomicAdd(&s.wave_c[p], c); }
+    }
+    if (whole < BINS) {
+      const float high = above(whole - 2, true);
+      all([&](int i, float v) {
+        if (v < low || v > high || weigh.bin(v) < whole) return;
+        const unsigned key = ordered(v);
+        if (last.key && !(key > last.key || (key == last.key && i <= last.at))) return;
+        if (weigh.dropped(v)) return;
+        const int p = (i + skew) / draw_len;
+        atomicAdd(&s.wave_w[p], weigh(v)); atomicAdd(&s.wave_c[p], 1u);
+      });
+    }
+  } else {
+    u64 sum = 0; unsigned count = 0;                                 // count: of what is kept, or of the last code
+    weights(mine, tiles, 64 * VEC, [&](int, float, u64 q, bool keep) __attribute__((always_inline)) {
+      if (counted) { if (q == ~0ull) ++count; else sum += q; }
+      else { sum += q; count += keep; }
+    });
+    sum = wave_sum(sum); count = wave_sum(count);
+    if (!lane) { s.wave_w[wave] = sum; s.wave_c[wave] = count; }
+  }
   __syncthreads();
-  if (!counted) for (int w = 0; w < SAMPLE_WAVES; ++w) { kept_w += s.wave_w[w]; kept += s.wave_c[w]; }
+  if (!counted) for (int w = 0; w < ranges; ++w) { kept_w += s.wave_w[w]; kept += s.wave_c[w]; }
   const double target = (double)u * (double)kept_w;
   // weight up to a point: w of other tokens and n of the last code
   auto weight_of = [&](u64 w, unsigned n) { return counted ? w + (u64)min(n, ties) * last_q : w; };
   u64 before = 0; unsigned before_n = 0; int range = 0;
-  for (; range < SAMPLE_WAVES - 1; ++range) {
+  for (; range < ranges - 1; ++range) {
     const u64 w = before + s.wave_w[range]; const unsigned n = before_n + s.wave_c[range];
     if ((double)weight_of(w, n) > target) break;
     before = w; before_n = n;
   }
   __syncthreads();
   // the range that the target is in, in pieces of neighbouring vectors of all threads
-  for (int p0 = range * range_len; p0 < (range + 1) * range_len; p0 += SAMPLE_THREADS * VEC) {
-    const bool in = p0 + tid * VEC < (range + 1) * range_len;
+  for (int p0 = range * draw_len; p0 < (range + 1) * draw_len; p0 += SAMPLE_THREADS * VEC) {
+    const bool in = p0 + tid * VEC < (range + 1) * draw_len;
     u64 here = 0; unsigned here_n = 0;
     if (in) weights(p0 + tid * VEC, 1, 0, [&](int, float, u64 q, bool) { if (counted && q == ~0ull) ++here_n; else here += q; });
     u64 bw, aw; unsigned bn, an;
@@ -668,10 +835,24 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
 
 using namespace octo;
 
+namespace {
+// Workgroups of a row where rows are few and long, or 0.  fp32, top-p: 1 x 131072 113 us alone, so 80; 48 x 131072 115 and 93; 1 x 262144 200 and 115; but 128 x 131072 126 and 133,
+// 1 x 32768 37 and 41.  Counting the codes of bf16 takes as long (1 x 131072 62 and 91), a short list needs no weights of all tokens.
+int sample_parts(const octo_sample_op* op) {
+  const bool short_list = !op->d_top_k && op->top_k > 0 && op->top_k <= LISTED;
+  if (op->dtype == OCTO_BF16 || op->n < 1 || op->n > 64 || op->vocab < 65536 || short_list) return 0;
+  return 256 / op->n < MOST_PARTS ? 256 / op->n : MOST_PARTS;
+}
+constexpr size_t PART_BYTES = (size_t)BINS * (sizeof(u64) + sizeof(unsigned)) + sizeof(float);
+bool sample_sizes(const octo_sample_op* op) { return op && op->dtype >= OCTO_F32 && op->dtype <= OCTO_BF16 && op->n >= 0 && op->n <= 0x3FFFFF && op->vocab >= 1 && op->vocab <= OCTO_MAX_VOCAB; }
+}  // namespace
+
+extern "C" size_t octo_op_sample_workspace_bytes(const octo_sample_op* op) { return sample_sizes(op) ? (size_t)op->n * sample_parts(op) * PART_BYTES : 0; }
+
 extern "C" octo_status octo_op_sample(const octo_sample_op* op, void* hip_stream) {
-  if (!op || (op->dtype != OCTO_F32 && op->dtype != OCTO_F16 && op->dtype != OCTO_BF16)) return OCTO_EINVAL;
+  if (!sample_sizes(op)) return OCTO_EINVAL;
   const int es = op->dtype == OCTO_F32 ? 4 : 2;
-  if (op->n < 0 || op->n > 0x3FFFFF || op->vocab < 1 || op->vocab > OCTO_MAX_VOCAB || !op->d_logits || (uintptr_t)op->d_logits % es || op->row < 0 || !op->d_u || !op->d_token) return OCTO_EINVAL;
+  if (!op->d_logits || (uintptr_t)op->d_logits % es || op->row < 0 || !op->d_u || !op->d_token) return OCTO_EINVAL;
   if (((uintptr_t)op->d_u | (uintptr_t)op->d_token | (uintptr_t)op->d_temperature | (uintptr_t)op->d_top_k | (uintptr_t)op->d_top_p | (uintptr_t)op->d_min_p | (uintptr_t)op->d_logprob |
        (uintptr_t)op->d_kept | (uintptr_t)op->d_n) & 3) return OCTO_EINVAL;
   if (!op->n) return OCTO_OK;
@@ -683,8 +864,20 @@ extern "C" octo_status octo_op_sample(const octo_sample_op* op, void* hip_stream
   int bits = 0;
   while ((1 << bits) < op->vocab) ++bits;
   a.shift = 62 - bits < 50 ? 62 - bits : 50;                         // a sum of `vocab` weights of up to one stays within 63 bits
+  const size_t need = octo_op_sample_workspace_bytes(op);
+  if (op->d_workspace && need) {
+    if (op->workspace_bytes < need || (uintptr_t)op->d_workspace & 15) return OCTO_EINVAL;
+    a.parts = sample_parts(op);
+    const size_t all = (size_t)op->n * a.parts;
+    a.part_weight = (u64*)op->d_workspace; a.part_count = (unsigned*)(a.part_weight + all * BINS); a.part_best = (float*)(a.part_count + all * BINS);
+  }
   hipStream_t s = (hipStream_t)hip_stream;
   const dim3 grid((unsigned)op->n), block(SAMPLE_THREADS);
+  if (a.parts) {
+    const dim3 wide((unsigned)(op->n * a.parts));
+    if (op->dtype == OCTO_F32) { hipLaunchKernelGGL(sample_best_kernel<float>, wide, block, 0, s, a); hipLaunchKernelGGL(sample_part_kernel<float>, wide, block, 0, s, a); }
+    else { hipLaunchKernelGGL(sample_best_kernel<_Float16>, wide, block, 0, s, a); hipLaunchKernelGGL(sample_part_kernel<_Float16>, wide, block, 0, s, a); }
+  }
   if (op->dtype == OCTO_F32) hipLaunchKernelGGL(sample_kernel<float>, grid, block, 0, s, a);
   else if (op->dtype == OCTO_F16) hipLaunchKernelGGL(sample_kernel<_Float16>, grid, block, 0, s, a);
   else hipLaunchKernelGGL(sample_kernel<__bf16>, grid, block, 0, s, a);

@@ -36,7 +36,8 @@ def _expected(x, u, t, k, p, m):
     words = words[np.lexsort((words, -x[words]))]
     if not t > 0:
         return int(words[0]), 1, 0.0
-    w = np.exp((x[words] - x[words[0]]) / t)
+    top = x[words[0]]
+    w = (x[words] == top).astype(np.float64) if np.isinf(top) else np.exp((x[words] - top) / t)
     if k > 0:
         words, w = words[:k], w[:k]
     up_to = np.cumsum(w)
@@ -251,3 +252,78 @@ def test_captured_and_replayed(octo):
         torch.cuda.synchronize()
         assert torch.equal(token, again)
         _check(_run(octo, logits, u, top_p=0.9), logits, u, dict(top_p=0.9))
+
+
+def _hard_rows(dtype, vocab):
+    """Rows on which borders fall among many equal logits, in steep and flat ones, with infinities, NaN and nothing."""
+    import torch
+    g = torch.Generator().manual_seed(vocab)
+    rows = [torch.randn(vocab, generator=g) * s for s in (0.01, 2.0, 30.0)]
+    rows.append(torch.randn(vocab, generator=g).mul(4).round())                        # thousands of equal logits on a step
+    rows.append(torch.zeros(vocab))
+    rows.append(torch.full((vocab,), -float("inf")))
+    rows.append(torch.randn(vocab, generator=g).masked_fill(torch.rand(vocab, generator=g) < 0.9, float("nan")))
+    some = torch.randn(vocab, generator=g)
+    some[vocab // 3::9973] = float("inf")
+    rows.append(some)
+    last = torch.full((vocab,), -200.0)
+    last[-1] = 3.0
+    rows.append(last)
+    rows.append(torch.arange(vocab).float().neg().mul(1e-4))
+    return torch.stack(rows).to(_t(dtype)).cuda()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("vocab", [65536, 70001, 131072])
+@pytest.mark.parametrize("settings", [dict(), dict(top_p=0.9), dict(top_p=0.3, min_p=0.001), dict(min_p=0.2), dict(top_k=700), dict(top_k=20000, top_p=0.99), dict(top_k=40, top_p=0.9),
+                                      dict(temperature=0.3, top_p=0.5), dict(temperature=0.0), dict(temperature=float("inf"), top_p=0.7), dict(min_p=1e-25)])
+def test_rows_shared_among_workgroups(octo, dtype, vocab, settings):
+    """Long rows with a workspace: the same as the definition says, and bit for bit the same as without one."""
+    import torch
+    x = _hard_rows(dtype, vocab)
+    n = x.shape[0]
+    settings = dict(settings)
+    if settings.get("top_k", 0) and settings["top_k"] <= 512:
+        settings["top_k"] = torch.tensor([settings["top_k"], 0] * (n // 2), dtype=torch.int32, device="cuda")      # rows of both kinds in a call
+    u = torch.rand(n, generator=torch.Generator().manual_seed(7)).cuda()
+    u[1], u[2] = 0.0, 0.99999994
+    token = torch.empty(n, dtype=torch.int32, device="cuda")
+    need = octo.sample_workspace_bytes(x, u, token, **settings)
+    assert (need > 0) == (dtype != "bf16")
+    work = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
+    got = _run(octo, x, u, workspace=work, **settings)
+    alone = _run(octo, x, u, workspace=work[:0], **settings)
+    for a, b in zip(got, alone):
+        assert np.array_equal(a, b, equal_nan=True)
+    _check(got, x, u, settings)
+
+
+def test_workspaces(octo):
+    """Sizes, refusals, rows that a count on the device leaves alone, and two captured calls that share one."""
+    import torch
+    g = torch.Generator().manual_seed(0)
+    x, u, token = torch.randn(6, 70000, generator=g).cuda(), torch.rand(6, generator=g).cuda(), torch.full((6,), -7, dtype=torch.int32, device="cuda")
+    need = octo.sample_workspace_bytes(x, u, token)
+    assert need > 0
+    assert octo.sample_workspace_bytes(x, u, token, top_k=50) == 0 == octo.sample_workspace_bytes(x[:, :5000], u, token)
+    assert octo.sample_workspace_bytes(x[:1].expand(300, 70000), u[:1].expand(300).contiguous(), token[:1].expand(300).contiguous()) == 0
+    work = torch.empty(need + 16, dtype=torch.uint8, device="cuda")
+    for bad in (work[:need - 1], work[8:need + 8]):
+        with pytest.raises(Exception):
+            octo.op_sample(x, u, token, workspace=bad)
+    octo.op_sample(x, u, token, top_p=0.9, n=torch.tensor([4], dtype=torch.int32, device="cuda"), workspace=work)
+    assert bool((token[:4] >= 0).all()) and bool((token[4:] == -7).all())
+    y = x.flip(1).contiguous()
+    tokens, graphs = [torch.empty_like(token) for _ in range(2)], [torch.cuda.CUDAGraph() for _ in range(2)]
+    torch.cuda.synchronize()
+    for logits, t, graph in zip((x, y), tokens, graphs):
+        with torch.cuda.graph(graph):
+            octo.op_sample(logits, u, t, top_p=0.9, workspace=work)
+    for turn in range(3):
+        u.copy_(torch.rand(6, generator=g))
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        for logits, t in zip((x, y), tokens):
+            octo.op_sample(logits, u, token, top_p=0.9)
+            assert torch.equal(t, token)
