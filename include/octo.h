@@ -719,18 +719,20 @@ octo_status octo_op_mx8_load(const octo_mx8_op* op, void* hip_stream);
 octo_status octo_quantize_mx8(const float* src, size_t n, uint8_t* codes, uint8_t* exps);
 octo_status octo_dequantize_mx8(const uint8_t* codes, const uint8_t* exps, size_t n, float* dst);
 
-/* Rows of tokens times the weights of a layer (what octo_op_conv's 1x1 layers are to maps):
+/* Rows of tokens times the weights of a layer, in one launch with what follows it (1x1 layers of octo_op_conv have no rows in 8 bits, gates or results in fp32):
  *   z[i][j] = sum over k of x[i][k] * w[j][k] + d_bias[j]
  *   y[i][j] = act(z[i][j]) (+ d_res[i][j]),    gated != 0, w of 2 cols rows:  y[i][j] = act(z[i][j]) * z[i][cols + j] (+ d_res[i][j])
  * act: octo_act, or OCTO_ACT_GELU (x times the normal distribution's integral up to x).  x [n][k] and w [cols or 2 cols][k] are of one format:
  *   OCTO_ROWS_PLAIN: d_x, d_w of `dtype` (OCTO_F32, _F16, _BF16), 16-byte aligned, k and the row strides whole multiples of 16 bytes;
  *   OCTO_ROWS_MX8: x8, w8, k a multiple of 32.
- * Rows of x and w are less than 8 MiB apart.  y goes to d_y in `dtype` (y_format OCTO_ROWS_PLAIN), in fp32 with out_f32 != 0, or to y8 (OCTO_ROWS_MX8: cols a multiple
+ * Rows of x and w are of up to 1 GiB and less than 8 MiB apart (a row of 8 bits by its codes).  y goes to d_y in `dtype` (y_format OCTO_ROWS_PLAIN), in fp32 with out_f32 != 0, or to y8 (OCTO_ROWS_MX8: cols a multiple
  * of 32, no residual).  d_bias: NULL or fp32 [cols or 2 cols]; d_res: NULL or rows of y's type, d_y itself with the same stride allowed.  d_y and d_res may have any address of
  * an element (vectors are used where four values are aligned).  Sums and the epilogue are in fp32, y is rounded once; the same call on the same inputs gives the same bits.
  * d_n: NULL, or the number of tokens present, on the device (clamped to n): later rows are left as they were.
- * Products of rows in 8 bits are added up as the 8-bit matrix instructions do, to about 2^-14 of the sum of their sizes, where y is of 16 or 8 bits and tokens are many; exactly in fp32 otherwise.
- * *kernel_id (may be NULL): 0 nothing to do; 1 to 3: tiles of 256 x 256, 128 x 128 and 128 x 64 (rows of w x tokens) in LDS; 10 R + T: operands straight from memory, R x 16 rows of w and T x 16 tokens a block. */
+ * Products of rows in 8 bits are added up as the 8-bit matrix instructions do, to about 2^-14 of the sum of their sizes, where y is of 16 or 8 bits, tokens are more than 16 and the four exponents of
+ * 128 values of k are one aligned word; exactly, in fp32, otherwise.
+ * *kernel_id (may be NULL): 0 nothing to do; 1 to 4: tiles of 256 x 256, 128 x 128, 128 x 64 and 128 x 128 (rows of w x tokens) in LDS, 3 and 4 with loads four steps deep (with 1, tokens beyond
+ * whole rounds of the compute units are a second launch's); 10 R + T: operands straight from memory, R x 16 rows of w and T x 16 tokens a block; 10 R: the same with up to 16 tokens that stay in registers. */
 #define OCTO_ACT_GELU 3
 typedef struct octo_product_op {
   int32_t dtype, x_format, y_format, out_f32;

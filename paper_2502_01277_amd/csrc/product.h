@@ -637,7 +637,14 @@ hipError_t launch_product_tile(ProductArgs a, hipStream_t s) {
   const int outs = a.gated ? BN / 2 : BN;
   a.tiles_n = (a.cols + outs - 1) / outs; a.tiles_m = (a.n + BM - 1) / BM;
   const int lds = D == 2 ? 0 : ProductTile<T, EXACT, TN, TM, WN, WM, D>::LDS;
-  if (lds) (void)hipFuncSetAttribute((const void*)product_tile_kernel<T, EXACT, TN, TM, WN, WM, MINB, D>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (lds) {
+    static const bool ready = [lds] {     // more than 64 KB of dynamic LDS needs the attribute, once per instance
+      (void)hipFuncSetAttribute((const void*)product_tile_kernel<T, EXACT, TN, TM, WN, WM, MINB, D>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+      (void)hipGetLastError();
+      return true;
+    }();
+    (void)ready;
+  }
   hipLaunchKernelGGL((product_tile_kernel<T, EXACT, TN, TM, WN, WM, MINB, D>), dim3((unsigned)(a.tiles_n * a.tiles_m)), dim3(WN * WM * 64), lds, s, a);
   return hipGetLastError();
 }
@@ -912,10 +919,11 @@ template <> hipError_t launch_product<OCTO_PRODUCT_TYPE>(int variant, const Prod
       case 22: return launch_product_few<T, 2, 2>(a, s);
       case 24: if constexpr (sizeof(T) == 2) return launch_product_few<T, 2, 4>(a, s); else break;
       case 42: if constexpr (sizeof(T) == 4) return launch_product_few<T, 4, 2>(a, s); else break;
+      case 44: if constexpr (sizeof(T) == 4) return launch_product_few<T, 4, 4>(a, s); else break;
     }
   }
   switch (variant) {
-    case 1: return launch_product_tile<T, false, 4, 4, 2, 2, 1, 2>(a, s);
+    case 1: if constexpr (sizeof(T) < 4) return launch_product_tile<T, false, 4, 4, 2, 2, 1, 2>(a, s); else break;
     case 2: return launch_product_tile<T, false, 2, 2, 2, 2, 2, 2>(a, s);
     case 3: return launch_product_tile<T, false, 2, 1, 2, 2, 2, 4>(a, s);
     case 4: return launch_product_tile<T, false, 2, 2, 2, 2, 2, 4>(a, s);

@@ -5,6 +5,7 @@ using namespace octo;
 
 namespace {
 bool rows_near(long long bytes) { return bytes >= 0 && bytes <= 8 << 20; }        // 255 of them stay within 31 bits
+constexpr int MOST_K = 1 << 30;                                                   // bytes of a row: with 63 rows before it, where they are loaded from one address, within 31 bits
 }  // namespace
 
 extern "C" octo_status octo_op_product(const octo_product_op* op, void* hip_stream, int32_t* kernel_id) {
@@ -16,13 +17,13 @@ extern "C" octo_status octo_op_product(const octo_product_op* op, void* hip_stre
   const int es = op->dtype == OCTO_F32 ? 4 : 2;
   ProductArgs a{};
   if (x8) {
-    if (op->k % 32 || !mx8_ok(op->x8) || !mx8_ok(op->w8) || op->x8.exp_row > 8 << 20 || op->w8.exp_row > 8 << 20) return OCTO_EINVAL;
+    if (op->k % 32 || op->k > MOST_K || !mx8_ok(op->x8) || !mx8_ok(op->w8) || op->x8.exp_row > 8 << 20 || op->w8.exp_row > 8 << 20) return OCTO_EINVAL;
     a.x = (const char*)op->x8.d_codes; a.w = (const char*)op->w8.d_codes; a.x_row = op->x8.code_row; a.w_row = op->w8.code_row;
     a.xe = op->x8.d_exps; a.we = op->w8.d_exps; a.xe_row = op->x8.exp_row; a.we_row = op->w8.exp_row;
     a.k_bytes = op->k;
     a.exp_words = op->k % 128 == 0 && !(((uintptr_t)a.xe | (uintptr_t)a.we | (uintptr_t)a.xe_row | (uintptr_t)a.we_row) & 3);
   } else {
-    if (!op->d_x || !op->d_w || (((uintptr_t)op->d_x | (uintptr_t)op->d_w) & 15) || op->k > 0x7FFFFF00 / es || op->k * es % 16) return OCTO_EINVAL;
+    if (!op->d_x || !op->d_w || (((uintptr_t)op->d_x | (uintptr_t)op->d_w) & 15) || op->k > MOST_K / es || op->k * es % 16) return OCTO_EINVAL;
     if (op->x_row < 0 || op->w_row < 0 || op->x_row > 8 << 20 || op->w_row > 8 << 20 || (op->x_row * es & 15) || (op->w_row * es & 15)) return OCTO_EINVAL;
     a.x = (const char*)op->d_x; a.w = (const char*)op->d_w; a.x_row = op->x_row * es; a.w_row = op->w_row * es;
     a.k_bytes = op->k * es;

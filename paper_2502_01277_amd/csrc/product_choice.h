@@ -27,15 +27,17 @@ inline ProductChoice product_choice(int n, int k_bytes, int cols, bool gated, bo
     return few(gated && to8 ? 4 : gated || to8 || rows > 16 * 512 ? 2 : 1, 1);
   }
   if (bits == 32) {
-    // fp32's products are the bound, and small blocks spread them (64 tokens, 4096 -> 4096: 33.7 us, tiles 132)
-    if (blocks(128, 64) < 128) return few(gated && to8 ? 4 : 2, 2);
+    // fp32's products are the bound, and blocks as small as it takes spread them (4096 -> 4096: 64 tokens 34 us, 64 x 64 a block 81, tiles 132; 512 tokens 2048 -> 2048: 60, 43 and 70)
+    const ProductChoice square = few(4, 4);
+    if (square.blocks <= 128) return few(gated && to8 ? 4 : 2, 2);
+    if (square.blocks <= 256) return square;
   } else if (bits == 16 && !(gated && to8)) {
     // A block a CU (64 tokens, 4096 -> 4096: 17.1 us, tiles 18.9; 1024 -> 4096 6.6 and 7.6; with two blocks a CU, 128 tokens, 31.2 and 18.9), larger ones for short rows (308 tokens,
     // 1160 -> 1100: 7.3, tiles 9.3).  In 8 bits widening takes as long as it saves.
     if (few(2, 2).blocks <= 256) return few(2, 2);
     if (k_bytes <= 2560 && few(2, 4).blocks <= 192) return few(2, 4);
   }
-  if (!exact8 && blocks(256, 256) >= 256) {
+  if (!exact8 && bits != 32 && blocks(256, 256) >= 256) {              // fp32, 4096 cubed: 1158 us, tiles of 128 x 128 953
     // Whole rounds of 256 CUs; few tiles that are left over would take a round of their own, in which smaller ones are done in a third of the time.
     const long long across = (rows + 255) / 256, all = blocks(256, 256), m = all / 256 * 256 / across * 256;
     const long long rest = n - m;

@@ -141,10 +141,10 @@ def test_product_refuses():
     assert binding.lib().octo_op_product(None, None, None) == binding.EINVAL
     assert _product_op(n=0) == binding.OK and _product_op(n=0, x_format=1, y_format=1) == binding.OK and _product_op(n=0, gated=1, act=3, d_res=512) == binding.OK
     for bad in (dict(dtype=3), dict(dtype=-1), dict(x_format=2), dict(y_format=-1), dict(n=-1), dict(k=0), dict(cols=0), dict(cols=0x20000001), dict(act=4), dict(act=-1), dict(d_x=None), dict(d_w=None),
-                dict(d_x=4104), dict(d_w=8200), dict(k=60), dict(k=2147483640), dict(x_row=60), dict(w_row=-8), dict(x_row=(8 << 20) // 2 + 8), dict(w_row=1 << 60), dict(d_y=None), dict(d_y=65537), dict(y_row=-1),
+                dict(d_x=4104), dict(d_w=8200), dict(k=60), dict(k=2147483640), dict(k=(1 << 29) + 8), dict(x_row=60), dict(w_row=-8), dict(x_row=(8 << 20) // 2 + 8), dict(w_row=1 << 60), dict(d_y=None), dict(d_y=65537), dict(y_row=-1),
                 dict(d_res=1), dict(d_res=512, res_row=-1), dict(d_bias=2), dict(d_n=2), dict(out_f32=1, d_y=65538)):
         assert _product_op(**bad) == binding.EINVAL, bad
-    for bad in (dict(k=48), dict(x8__d_codes=None), dict(w8__d_exps=None), dict(x8__d_codes=8), dict(w8__code_row=72), dict(x8__code_row=-96), dict(w8__exp_row=-1), dict(x8__code_row=(8 << 20) + 16),
+    for bad in (dict(k=48), dict(k=(1 << 30) + 32), dict(x8__d_codes=None), dict(w8__d_exps=None), dict(x8__d_codes=8), dict(w8__code_row=72), dict(x8__code_row=-96), dict(w8__exp_row=-1), dict(x8__code_row=(8 << 20) + 16),
                 dict(x8__exp_row=1 << 40)):
         assert _product_op(x_format=1, **bad) == binding.EINVAL, bad
     for bad in (dict(cols=100), dict(out_f32=1), dict(d_res=512), dict(y8__d_codes=None), dict(y8__code_row=100), dict(y8__exp_row=-1)):

@@ -172,6 +172,16 @@ def test_held_tokens_and_more_weights_than_blocks(octo, rows, dtype, bytes_of_k,
         _check_mx8(y, ref, off) if to8 else _check(y, ref, off, dtype)
 
 
+@pytest.mark.parametrize("n,k,cols,gated,to8,kernel", [(60, 100, 600, False, False, 22), (500, 260, 1030, False, False, 44), (130, 1028, 1504, True, True, 44), (70, 64, 96, True, True, 42), (1000, 36, 2100, False, False, 4)])
+def test_fp32_in_blocks_of_every_size(octo, n, k, cols, gated, to8, kernel):
+    import torch
+    x, w, x64, w64, g = _inputs(octo, "plain", "f32", n, k, cols, gated, n)
+    y = octo.Mx8.empty(n, cols) if to8 else torch.full((n, cols), float("nan"), device="cuda")
+    assert octo.op_product(x, w, y, act="silu" if gated else "none", gated=gated) == kernel
+    ref, off = _reference(x64, w64, None, "silu" if gated else "none", gated, None, True)
+    _check_mx8(y, ref, off) if to8 else _check(y, ref, off, "f32")
+
+
 def test_fp32_results_of_many_rows_in_eight_bits(octo):
     """They are added up in fp32, whichever kernel runs."""
     import torch
