@@ -3,13 +3,15 @@
 // With the tokens of a row in the order of their logits (equal ones by index) and w = exp((x - max) / temperature), top-k, top-p and min-p each keep a beginning of that order; what
 // they keep in common is one too, and is known by its last token.  The token is drawn in the order of indices: the first at which the sum of the kept weights passes u times all.
 //
-// A workgroup takes a row.  Sums of weights decide which token a border falls on, so they are made of integers: w is computed in fp64 (1024 steps an octave from a table, the rest by a
-// polynomial, 2e-14 off) and rounded to multiples of 2^-shift of the largest, whose sums in 64 bits are the same in any order.  The bound is arithmetic, an exponential of twenty
-// instructions for each logit, so it is computed where it has to be:
-//   - top_k of up to LISTED: the k-th largest of the threads' own largest logits is no larger than the k-th largest of all; what is not below it, little more than k logits, is sorted in LDS.
+// A workgroup takes a row; few long ones of fp32 and fp16 are shared (sample_parts).  Sums of weights decide which token a border falls on, so they are made of integers: the exponent is taken in
+// fp64, w from a table of 1024 steps an octave and a remainder that fp32 holds to 2^-35, and rounded to multiples of 2^-shift of the largest, whose sums in 64 bits are the same in any order.
+// The bound is arithmetic, an exponential of twenty instructions for each logit (an instruction for each of 131072 logits takes a compute unit 0.85 us), so it is computed where it has to be:
+//   - top_k of up to LISTED: the k-th largest of the threads' own largest logits is no larger than the k-th largest of all; what is not below it, little more than k logits, is put in order in LDS.
 //   - bf16: a row has few different logits.  Codes of the 16 octaves below the largest magnitude are counted, 4096 of them, and all sums are those of counts times weights.
-//   - else borders are found by a histogram of counts and weights over 64 octaves of w, 64 bins each; the tokens of the bin that holds the border are sorted.  Where they are too
-//     many (equal logits, say), bits of the logits themselves make further histograms.  The same where the others do not fit (more equal logits than are sorted, borders in codes that are not counted).
+//   - else borders are found by a histogram of counts and weights over 64 octaves of w, 64 bins each; the tokens of the bin that holds the border are listed, one more histogram of the
+//     list's own range leaves few of them (a sort of the whole list: 16 us more), which are put in order.  Where they are too many to list (equal logits, say), bits of the logits
+//     themselves make further histograms.  The same where the others do not fit (more equal logits than are listed, borders in codes that are not counted).
+// Measured (MI355X), top-p 0.9: 1 x 8192 bf16 20 us, 1 x 32768 26, fp32 40; 1 x 131072 bf16 62, fp32 82 (alone 113); 512 x 100003 bf16 122, fp32 214; the first 50 of 1 x 32768 17.
 #include <cmath>
 #include <type_traits>
 
