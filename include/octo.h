@@ -726,7 +726,7 @@ octo_status octo_dequantize_mx8(const uint8_t* codes, const uint8_t* exps, size_
  *   OCTO_ROWS_PLAIN: d_x, d_w of `dtype` (OCTO_F32, _F16, _BF16), 16-byte aligned, k and the row strides whole multiples of 16 bytes;
  *   OCTO_ROWS_MX8: x8, w8, k a multiple of 32.
  * Rows of x and w are of up to 1 GiB and less than 8 MiB apart (a row of 8 bits by its codes).  y goes to d_y in `dtype` (y_format OCTO_ROWS_PLAIN), in fp32 with out_f32 != 0, or to y8 (OCTO_ROWS_MX8: cols a multiple
- * of 32, no residual).  d_bias: NULL or fp32 [cols or 2 cols]; d_res: NULL or rows of y's type, d_y itself with the same stride allowed.  d_y and d_res may have any address of
+ * of 32, no residual).  d_bias: NULL or fp32 [cols or 2 cols]; d_res: NULL or rows of y's type, d_y itself with the same stride allowed; apart from that y may not overlap anything else.  d_y and d_res may have any address of
  * an element (vectors are used where four values are aligned).  Sums and the epilogue are in fp32, y is rounded once; the same call on the same inputs gives the same bits.
  * d_n: NULL, or the number of tokens present, on the device (clamped to n): later rows are left as they were.
  * Products of rows in 8 bits are added up as the 8-bit matrix instructions do, to about 2^-14 of the sum of their sizes, where y is of 16 or 8 bits, tokens are more than 16 and the four exponents of

@@ -425,9 +425,9 @@ __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(Produc
     const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc((void*)((is_w ? second ? w1 : w0 : x0) + t * 128 - 4096), 0, 0x7FFFFFFF, BUF_FLAGS);
     const unsigned to = lds + stage * STAGE + (is_w ? wave * LW * 1024 : BN * 128 + wave * LX * 1024) + i / 4 * 4096;
     if (i % 4 == 0) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(to), "v"(off), "s"(rc) : "memory");
-    else if (i % 4 == 1) asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:1024 lds" :: "v"(off), "s"(rc) : "memory");
-    else if (i % 4 == 2) asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:2048 lds" :: "v"(off), "s"(rc) : "memory");
-    else asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:3072 lds" :: "v"(off), "s"(rc) : "memory");
+    else if (i % 4 == 1) asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:%2 lds" :: "v"(off), "s"(rc), "n"(1 * 1024) : "memory");
+    else if (i % 4 == 2) asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:%2 lds" :: "v"(off), "s"(rc), "n"(2 * 1024) : "memory");
+    else asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:%2 lds" :: "v"(off), "s"(rc), "n"(3 * 1024) : "memory");
   };
 
   floatx4 acc[BW][BX];

@@ -173,5 +173,19 @@ def test_sample_refuses():
         assert _sample_op(**bad) == binding.EINVAL, bad
 
 
+def test_workspace_of_a_sample():
+    """Only few long rows of fp32 and fp16 have one, and not where the host knows that a short list is enough."""
+    need = binding.lib().octo_op_sample_workspace_bytes
+    op = binding.OctoSampleOp(dtype=0, n=4, vocab=70000)
+    size = need(C.byref(op))
+    assert size > 0 and size == 4 * need(C.byref(binding.OctoSampleOp(dtype=0, n=1, vocab=70000))) == need(C.byref(binding.OctoSampleOp(dtype=1, n=4, vocab=70000)))
+    for none in (dict(dtype=2), dict(n=0), dict(n=65), dict(n=-1), dict(vocab=65535), dict(vocab=(1 << 19) + 1), dict(top_k=512), dict(dtype=3)):
+        assert need(C.byref(binding.OctoSampleOp(**{**dict(dtype=0, n=4, vocab=70000), **none}))) == 0, none
+    assert need(None) == 0 and need(C.byref(binding.OctoSampleOp(dtype=0, n=4, vocab=70000, top_k=512, d_top_k=4096))) == size
+    long = dict(dtype=0, vocab=70000, row=70000)
+    for bad in (dict(d_workspace=4096, workspace_bytes=size - 1), dict(d_workspace=4104, workspace_bytes=size)):
+        assert _sample_op(**long, **bad) == binding.EINVAL, bad
+
+
 def test_layout_of_the_packed_sample():
     assert binding._SAMPLE.size == C.sizeof(binding.OctoSampleOp)

@@ -301,6 +301,21 @@ def test_counts_around_the_tokens_of_a_first_kernel(octo, rows):
         assert bool((y[m:] == 7).all()) and bool((y8.codes[m:] == 3).all()) and bool((y8.exps[m:] == 5).all())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("cols,width", [(4160, 4160), (4152, 4200), (4155, 4155)])
+def test_residual_in_place_over_two_kernels(octo, dtype, cols, width):
+    """Outputs that end inside a tile and inside what is asked for of a residual's row, rows further apart than their outputs."""
+    import torch
+    n, k = 4200, 64
+    x, w, x64, w64, g = _inputs(octo, "plain", dtype, n, k, cols, False, cols)
+    held = torch.randn(n, width, generator=g).to(_t(dtype)).cuda()
+    before, y = held.clone(), held[:, :cols]
+    assert octo.op_product(x, w, y, act="relu", res=y) == 1
+    ref, off = _reference(x64, w64, None, "relu", False, before[:, :cols].double(), False)
+    _check(y, ref, off, dtype)
+    assert torch.equal(held[:, cols:], before[:, cols:])
+
+
 def test_no_tokens_and_types_that_do_not_meet(octo):
     import torch
     w = torch.randn(96, 64, device="cuda")
