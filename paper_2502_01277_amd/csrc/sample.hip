@@ -11,7 +11,7 @@
 //   - else borders are found by a histogram of counts and weights over 64 octaves of w, 64 bins each; the tokens of the bin that holds the border are listed, one more histogram of the
 //     list's own range leaves few of them (a sort of the whole list: 16 us more), which are put in order.  Where they are too many to list (equal logits, say), bits of the logits
 //     themselves make further histograms.  The same where the others do not fit (more equal logits than are listed, borders in codes that are not counted).
-// Measured (MI355X), top-p 0.9: 1 x 8192 bf16 20 us, 1 x 32768 26, fp32 40; 1 x 131072 bf16 62, fp32 82 (alone 113); 512 x 100003 bf16 122, fp32 214; the first 50 of 1 x 32768 17.
+// Measured (MI355X), top-p 0.9: 1 x 8192 bf16 20 us, 1 x 32768 26, fp32 40; 1 x 131072 bf16 62, fp32 82 (alone 113); 512 x 100003 bf16 122, fp32 214; the first 50 of 1 x 32768 15 (with votes on 20 bits of a key one after the other 17).
 #include <cmath>
 #include <type_traits>
 
@@ -104,7 +104,7 @@ struct SampleShared {
   u64 wave_w[SAMPLE_WAVES];
   unsigned wave_c[SAMPLE_WAVES];
   float wave_max[SAMPLE_WAVES], wave_big[SAMPLE_WAVES];
-  unsigned votes[3];
+  unsigned key_min, key_max;
   int listed, bin, token, cut;
   unsigned bin_count, key, at, before_c;
   u64 before_w, tiny_w;
@@ -250,6 +250,8 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
   };
 
   s.table[tid] = octave.v[tid];
+  if (by.short_list())
+    for (int b = tid; b < BINS; b += SAMPLE_THREADS) { s.count[b] = 0; ((unsigned*)s.weight)[b] = 0; }
   // the largest logit, of this thread and of all, and the largest magnitude
   float own = -INFINITY, big = 0.f;
   const bool in_parts = !std::is_same<T, __bf16>::value && a.parts && !by.short_list();
@@ -266,7 +268,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) { best = fmaxf(best, __shfl_xor(best, d)); big = fmaxf(big, __shfl_xor(big, d)); }
   if (!lane) { s.wave_max[wave] = best; s.wave_big[wave] = big; }
-  if (tid == 0) { s.listed = 0; s.at = 0x7FFFFFFF; s.token = -1; s.cut = 0x7FFFFFFF; s.tiny_w = 0; s.votes[0] = s.votes[1] = s.votes[2] = 0; }
+  if (tid == 0) { s.listed = 0; s.at = 0x7FFFFFFF; s.token = -1; s.cut = 0x7FFFFFFF; s.tiny_w = 0; }
   __syncthreads();
   for (int w = 0; w < SAMPLE_WAVES; ++w) { best = fmaxf(best, s.wave_max[w]); big = fmaxf(big, s.wave_big[w]); }
   if (!(best > -INFINITY)) {
@@ -315,18 +317,34 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
 
   // ---- a short list -----------------------------------------------------------------------------------------------------
   if (by.short_list()) {
-    // the largest key of 20 bits that top_k threads reach with their own largest logit, bit by bit (0 where fewer have any)
-    unsigned floor_key = 0;
+    // The largest key of 24 bits that top_k threads reach with their own largest logit, by two counts of 12 bits, larger ones first (0 where fewer have any).
     const unsigned own_key = own > -INFINITY ? ordered(own) : 0;
-    for (int bit = 31, slot = 0; bit >= 12; --bit) {
-      const unsigned probe = floor_key | 1u << bit;
-      const unsigned votes = (unsigned)__popcll(__ballot(own_key >= probe));
-      if (!lane && votes) atomicAdd(&s.votes[slot], votes);
-      const int next = slot == 2 ? 0 : slot + 1;
+    unsigned* const low = (unsigned*)s.weight;
+    auto pick = [&](const unsigned* counts, unsigned need) {          // the bin that brings the count to `need`
+      const u32x4 c = *(const u32x4*)(counts + 4 * tid);
+      const unsigned c4 = c[0] + c[1] + c[2] + c[3], sc = wave_scan(c4, lane);
+      if (lane == 63) s.wave_c[wave] = sc;
+      if (!tid) s.bin = -1;
       __syncthreads();
-      if (s.votes[slot] >= (unsigned)top_k) floor_key = probe;
-      if (!tid) s.votes[next == 2 ? 0 : next + 1] = 0;                // two rounds on; all have read it
-      slot = next;
+      unsigned bc = sc - c4;
+      for (int v = 0; v < wave; ++v) bc += s.wave_c[v];
+      if (bc < need && bc + c4 >= need) {
+        int b = 0;
+        while (bc + c[b] < need) bc += c[b++];
+        s.bin = 4 * tid + b; s.before_c = bc;
+      }
+      __syncthreads();
+      return s.bin;
+    };
+    if (own_key) atomicAdd(&s.count[4095 - (own_key >> 20)], 1u);
+    __syncthreads();
+    unsigned floor_key = 0;
+    const int upper = pick(s.count, (unsigned)top_k);
+    if (upper >= 0) {
+      const unsigned digit = 4095 - upper, need = (unsigned)top_k - s.before_c;
+      if (own_key >> 20 == digit) atomicAdd(&low[4095 - (own_key >> 8 & 4095)], 1u);
+      __syncthreads();
+      floor_key = digit << 20 | (unsigned)(4095 - pick(low, need)) << 8;
     }
     if (own_key >= floor_key) {                                       // others have none
       all([&](int i, float v) {
@@ -616,7 +634,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
           __syncthreads();
           return base_w + m * q;
         }
-        if (!tid) { s.listed = 0; s.votes[0] = 0xFFFFFFFFu; s.votes[1] = 0; }
+        if (!tid) { s.listed = 0; s.key_min = 0xFFFFFFFFu; s.key_max = 0; }
         __syncthreads();
         all([&](int i, float v) { if (in_group(v)) s.list[atomicAdd(&s.listed, 1)] = (u64)~ordered(v) << 32 | (unsigned)i; });      // larger logits first, equal ones by index
         __syncthreads();
@@ -630,9 +648,9 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
           unsigned lo = min(key_of(entry[0]), key_of(entry[1])), hi = max(entry[0] == ~0ull ? 0u : key_of(entry[0]), entry[1] == ~0ull ? 0u : key_of(entry[1]));
 #pragma unroll
           for (int d = 1; d < 64; d *= 2) { lo = min(lo, (unsigned)__shfl_xor((int)lo, d)); hi = max(hi, (unsigned)__shfl_xor((int)hi, d)); }
-          if (!lane) { atomicMin(&s.votes[0], lo); atomicMax(&s.votes[1], hi); }
+          if (!lane) { atomicMin(&s.key_min, lo); atomicMax(&s.key_max, hi); }
           clear();
-          lo = s.votes[0]; hi = s.votes[1];
+          lo = s.key_min; hi = s.key_max;
           const int down = max(20 - __clz(hi - lo | 1), 0);
           for (int e = 0; e < 2; ++e)
             if (entry[e] != ~0ull) { const int d = (int)((key_of(entry[e]) - lo) >> down); atomicAdd(&s.weight[d], weigh(logit_of(entry[e]))); atomicAdd(&s.count[d], 1u); }
