@@ -33,9 +33,15 @@ inline ProductChoice product_choice(int n, int k_bytes, int cols, bool gated, bo
     if (square.blocks <= 256) return square;
   } else if (bits == 16 && !(gated && to8)) {
     // A block a CU (64 tokens, 4096 -> 4096: 17.1 us, tiles 18.9; 1024 -> 4096 6.6 and 7.6; with two blocks a CU, 128 tokens, 31.2 and 18.9), larger ones for short rows (308 tokens,
-    // 1160 -> 1100: 7.3, tiles 9.3).  In 8 bits widening takes as long as it saves.
+    // 1160 -> 1100: 7.3, tiles 9.3)
     if (few(2, 2).blocks <= 256) return few(2, 2);
     if (k_bytes <= 2560 && few(2, 4).blocks <= 192) return few(2, 4);
+  } else if (bits == 8) {
+    // The same (64 tokens, 4096 -> 1024: 9.5 us, two sets of rows a block 13.0, tiles 15.7; 32 tokens, 4096 -> 4096: 13.1, tiles 15.5).  Tiles that take exponents byte by byte are slow beyond a
+    // block a CU too (64 tokens, 4000 -> 4096: 13.7, tiles 37; 300 tokens, 4000 -> 2000: 34, tiles 42; 1000 tokens, 4000 -> 1000: 46, tiles 43).
+    if (!gated && !to8 && few(1, 1).blocks <= 256) return few(1, 1);
+    if (!(gated && to8) && few(2, 1).blocks <= 256) return few(2, 1);
+    if (!words && few(4, 1).blocks <= 768) return few(4, 1);
   }
   if (!exact8 && bits != 32 && blocks(256, 256) >= 256) {              // fp32, 4096 cubed: 1158 us, tiles of 128 x 128 953
     // Whole rounds of 256 CUs; few tiles that are left over would take a round of their own, in which smaller ones are done in a third of the time.

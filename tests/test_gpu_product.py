@@ -6,7 +6,7 @@ Activations have slopes of at most 1.13.  SiLU: its exponent is rounded (2^-24 o
 GELU: erf within 2^-21, a product and a sum: |v| 2^-20 absolutely.  A gate multiplies errors by the other half's size; the residual's sum is one rounding; then one rounding to the type.  All
 of these are small beside the type's rounding for 16 bits.
 
-Rows of 8 bits whose results are of 16 or 8 bits are multiplied by the 8-bit instructions where tokens are more than 16 (kernels 1 to 4).  Those add products in groups of eight aligned to the
+Rows of 8 bits whose results are of 16 or 8 bits are multiplied by the 8-bit instructions where tokens are many (kernels 1 to 4).  Those add products in groups of eight aligned to the
 largest, 2^E <= its size, and drop what lies below 2^(E - 13) (1 + 2^-13 comes out as it is, 1 + 2^-14 as 1; the largest has six bits of fraction and loses none): up to seven
 products of a group lose less than 2^-13 of its largest, so a sum loses less than 7 * 2^-13 sum |x w|."""
 import math
@@ -180,6 +180,17 @@ def test_fp32_in_blocks_of_every_size(octo, n, k, cols, gated, to8, kernel):
     assert octo.op_product(x, w, y, act="silu" if gated else "none", gated=gated) == kernel
     ref, off = _reference(x64, w64, None, "silu" if gated else "none", gated, None, True)
     _check_mx8(y, ref, off) if to8 else _check(y, ref, off, "f32")
+
+
+@pytest.mark.parametrize("n,k,cols,gated,to8,kernel", [(60, 1120, 500, False, False, 11), (40, 2048, 2000, False, False, 21), (90, 1184, 600, True, False, 21), (20, 160, 640, False, True, 21),
+                                                       (300, 288, 2000, False, False, 41), (70, 96, 320, True, True, 41), (90, 1024, 2016, True, True, 3), (1200, 96, 2060, False, False, 4)])
+def test_rows_of_eight_bits_in_every_kernel(octo, n, k, cols, gated, to8, kernel):
+    import torch
+    x, w, x64, w64, g = _inputs(octo, "mx8", "bf16", n, k, cols, gated, n)
+    y = octo.Mx8.empty(n, cols) if to8 else torch.full((n, cols), float("nan"), dtype=torch.bfloat16, device="cuda")
+    assert octo.op_product(x, w, y, act="silu" if gated else "none", gated=gated) == kernel
+    ref, off = _reference(x64, w64, None, "silu" if gated else "none", gated, None, False, GRAIN if kernel < 10 else 0.0)
+    _check_mx8(y, ref, off) if to8 else _check(y, ref, off, "bf16")
 
 
 def test_fp32_results_of_many_rows_in_eight_bits(octo):
