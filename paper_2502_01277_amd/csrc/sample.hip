@@ -11,7 +11,7 @@
 //   - else borders are found by a histogram of counts and weights over 64 octaves of w, 64 bins each; the tokens of the bin that holds the border are listed, one more histogram of the
 //     list's own range leaves few of them (a sort of the whole list: 16 us more), which are put in order.  Where they are too many to list (equal logits, say), bits of the logits
 //     themselves make further histograms.  The same where the others do not fit (more equal logits than are listed, borders in codes that are not counted).
-// Measured (MI355X), top-p 0.9: 1 x 8192 bf16 20 us, 1 x 32768 26, fp32 40; 1 x 131072 bf16 62, fp32 82 (alone 113); 512 x 100003 bf16 122, fp32 214; the first 50 of 1 x 32768 15 (with votes on 20 bits of a key one after the other 17).
+// Measured (MI355X), top-p 0.9: 1 x 8192 bf16 21 us, 1 x 32768 27, fp32 40; 1 x 131072 bf16 49, fp32 82 (alone 113); 512 x 100003 bf16 100, fp32 214; the first 50 of 1 x 32768 15 (with votes on 20 bits of a key one after the other 17).
 #include <cmath>
 #include <type_traits>
 
@@ -96,7 +96,10 @@ template <typename V> __device__ __forceinline__ V wave_scan(V v, int lane) {   
   return v;
 }
 
-struct SampleShared {
+// RANGE_WORDS: counts of codes, two of 16 bits a word, for each of CODE_RANGES parts of the row (bf16 alone)
+constexpr int CODE_RANGES = 8;
+template <int RANGE_WORDS> struct SampleShared {
+  unsigned codes[CODE_RANGES][RANGE_WORDS];
   double table[STEPS];
   u64 weight[BINS];
   unsigned count[BINS];
@@ -226,7 +229,8 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_part_kernel(SampleArgs 
 template <typename T>
 __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
   constexpr int VEC = SampleRow<T>::VEC;
-  __shared__ SampleShared s;
+  constexpr bool CODES = std::is_same<T, __bf16>::value;
+  __shared__ SampleShared<CODES ? BINS / 2 : 1> s;
   const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   if (a.n_dyn && row >= *a.n_dyn) return;
   const SampleChoice by(a, row);
@@ -442,9 +446,12 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
   int last_entry = BINS;
   u64 last_q = 0;
   bool tiny_kept = true;
-  if constexpr (std::is_same<T, __bf16>::value) {
-    if (!odd && !in_parts && big < INFINITY && (by_p || top_k > 0)) {
-      for (int b = tid; b < BINS; b += SAMPLE_THREADS) s.count[b] = 0;
+  // Parts of long rows are counted apart, and the draw needs no look at all tokens for their sums (512 x 100003 top-p 122 -> 101 us; 1 x 8192 20 -> 23).
+  const bool apart = tiles >= 4;
+  const int code_ranges = apart ? CODE_RANGES : 1, code_range = apart ? wave / (SAMPLE_WAVES / CODE_RANGES) : 0, code_len = range_len * (SAMPLE_WAVES / CODE_RANGES);
+  if constexpr (CODES) {
+    if (!odd && big < INFINITY && (by_p || top_k > 0) && code_len < 65536) {
+      for (int b = tid; b < code_ranges * BINS / 2; b += SAMPLE_THREADS) s.codes[0][b] = 0;
       __syncthreads();
       vectors(mine, tiles, 64 * VEC, [&](int, const u32x4& v) __attribute__((always_inline)) {
 #pragma unroll
@@ -452,11 +459,11 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
           const unsigned code = (e & 1 ? v[e / 2] >> 16 : v[e / 2] & 0xFFFF);
           if ((code & 0x7FFF) > 0x7F80 || code == 0xFF80) continue;             // NaN, -infinity
           const int j = entry_of(code);
-          if (j >= 0) { atomicAdd(&s.count[j], 1u); continue; }
+          if (j >= 0) { atomicAdd(&s.codes[code_range][j >> 1], (j & 1) ? 0x10000u : 1u); continue; }
           const float t = __uint_as_float(code << 16);
           const int at = atomicAdd(&s.listed, 1);
           atomicAdd(&s.tiny_w, weigh(t));
-          if (at < SORTED) s.list[at] = ordered(t);
+          if (at < SORTED) s.list[at] = (u64)code_range << 32 | ordered(t);
         }
       });
       __syncthreads();
@@ -467,8 +474,14 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       u64 q[4], w4 = tid == 512 ? tiny_w : 0; unsigned c[4], c4 = tid == 512 ? tiny_c : 0;
       int cut = 0x7FFFFFFF;                                          // the first entry that min-p drops
 #pragma unroll
+      for (int e = 0; e < 4; ++e) c[e] = 0;
+      for (int d = 0; d < code_ranges; ++d) {
+        const unsigned lo = s.codes[d][2 * tid], hi = s.codes[d][2 * tid + 1];
+        c[0] += lo & 0xFFFF; c[1] += lo >> 16; c[2] += hi & 0xFFFF; c[3] += hi >> 16;
+      }
+#pragma unroll
       for (int e = 0; e < 4; ++e) {
-        c[e] = s.count[4 * tid + e];
+        s.count[4 * tid + e] = c[e];
         const double w = c[e] ? weigh.scaled(code_of_entry(4 * tid + e)) : 0.0;
         q[e] = Weigher::whole(w);
         s.weight[4 * tid + e] = q[e];
@@ -773,8 +786,26 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       }
     });
   };
-  const int ranges = split ? a.parts : SAMPLE_WAVES, draw_len = split ? x.tiles(a.parts) * SAMPLE_THREADS * VEC : range_len;
-  if (split) {
+  const bool by_counts = CODES && counted && apart;
+  const int ranges = split ? a.parts : by_counts ? CODE_RANGES : SAMPLE_WAVES;
+  const int draw_len = split ? x.tiles(a.parts) * SAMPLE_THREADS * VEC : by_counts ? code_len : range_len;
+  if (by_counts) {
+    // sums of counts times weights; `count`: of the last code
+    if constexpr (CODES) {
+      if (tid < CODE_RANGES) { s.wave_w[tid] = 0; s.wave_c[tid] = last_entry < BINS ? s.codes[tid][last_entry >> 1] >> (last_entry & 1) * 16 & 0xFFFF : 0; }
+      __syncthreads();
+      u64 q[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) q[e] = s.weight[4 * tid + e];
+#pragma unroll
+      for (int d = 0; d < CODE_RANGES; ++d) {
+        const unsigned lo = s.codes[d][2 * tid], hi = s.codes[d][2 * tid + 1];
+        const u64 w = wave_sum(q[0] * (lo & 0xFFFF) + q[1] * (lo >> 16) + q[2] * (hi & 0xFFFF) + q[3] * (hi >> 16));
+        if (!lane && w) atomicAdd(&s.wave_w[d], w);
+      }
+      if (tiny_kept) for (int i = tid; i < s.listed; i += SAMPLE_THREADS) atomicAdd(&s.wave_w[s.list[i] >> 32], weigh(unordered((unsigned)s.list[i])));
+    }
+  } else if (split) {
     // Bins before the last one are kept as a whole, their sums are there for each part; tokens of the others are looked at one by one.
     int whole = last.key ? weigh.bin(unordered(last.key)) : BINS;
     float low = last.key ? unordered(last.key) : -INFINITY;
@@ -857,7 +888,7 @@ using namespace octo;
 
 namespace {
 // Workgroups of a row where rows are few and long, or 0.  fp32, top-p: 1 x 131072 113 us alone, so 80; 48 x 131072 115 and 93; 1 x 262144 200 and 115; but 128 x 131072 126 and 133,
-// 1 x 32768 37 and 41.  Counting the codes of bf16 takes as long (1 x 131072 62 and 91), a short list needs no weights of all tokens.
+// 1 x 32768 37 and 41.  Counting the codes of bf16 takes less (1 x 131072 49, shared by weights 91), a short list needs no weights of all tokens.
 int sample_parts(const octo_sample_op* op) {
   const bool short_list = !op->d_top_k && op->top_k > 0 && op->top_k <= LISTED;
   if (op->dtype == OCTO_BF16 || op->n < 1 || op->n > 64 || op->vocab < 65536 || short_list) return 0;

@@ -274,7 +274,7 @@ def _hard_rows(dtype, vocab):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
-@pytest.mark.parametrize("vocab", [65536, 70001, 131072])
+@pytest.mark.parametrize("vocab", [65536, 70001, 131072, 524288])
 @pytest.mark.parametrize("settings", [dict(), dict(top_p=0.9), dict(top_p=0.3, min_p=0.001), dict(min_p=0.2), dict(top_k=700), dict(top_k=20000, top_p=0.99), dict(top_k=40, top_p=0.9),
                                       dict(temperature=0.3, top_p=0.5), dict(temperature=0.0), dict(temperature=float("inf"), top_p=0.7), dict(min_p=1e-25)])
 def test_rows_shared_among_workgroups(octo, dtype, vocab, settings):
