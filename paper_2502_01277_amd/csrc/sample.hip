@@ -11,7 +11,7 @@
 //   - else borders are found by a histogram of counts and weights over 64 octaves of w, 64 bins each; the tokens of the bin that holds the border are listed, one more histogram of the
 //     list's own range leaves few of them (a sort of the whole list: 16 us more), which are put in order.  Where they are too many to list (equal logits, say), bits of the logits
 //     themselves make further histograms.  The same where the others do not fit (more equal logits than are listed, borders in codes that are not counted).
-// Measured (MI355X), top-p 0.9: 1 x 8192 bf16 21 us, 1 x 32768 27, fp32 40; 1 x 131072 bf16 49, fp32 82 (alone 113); 512 x 100003 bf16 100, fp32 214; the first 50 of 1 x 32768 15 (with votes on 20 bits of a key one after the other 17).
+// Measured (MI355X), top-p 0.9: 1 x 8192 bf16 21 us, 1 x 32768 27, fp32 40; 1 x 131072 bf16 49, fp32 76 (alone 113: of the 76, two looks at a row by one workgroup take 15 each, at the 35 GB/s that a compute unit draws from beyond its L2); 512 x 100003 bf16 100, fp32 214; the first 50 of 1 x 32768 15 (with votes on 20 bits of a key one after the other 17).
 #include <cmath>
 #include <type_traits>
 
@@ -563,6 +563,29 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
     const double v = (double)best - (double)bins * 16.0 / factor;
     return up ? __double2float_ru(v) : __double2float_rd(v);
   };
+  // bin b of all parts, on its way from memory at once (0 of parts that are not there)
+  auto of_parts = [&](int b, u64 (&w)[MOST_PARTS], unsigned (&c)[MOST_PARTS]) __attribute__((always_inline)) {
+    const long long at = (long long)row * a.parts * BINS + b;
+#pragma unroll
+    for (int p = 0; p < MOST_PARTS; ++p) {
+      w[p] = 0; c[p] = 0;
+      if (p < a.parts) { w[p] = a.part_weight[at + p * BINS]; c[p] = a.part_count[at + p * BINS]; }
+    }
+  };
+  // f(index, logit) of the tokens between two logits, which are few: one branch a vector
+  auto between = [&](float low, float high, auto&& f) __attribute__((always_inline)) {
+    vectors(mine, tiles, 64 * VEC, [&](int p, const u32x4& vec) __attribute__((always_inline)) {
+      bool any = false;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) any |= (value(vec, e) >= low) & (value(vec, e) <= high);
+      if (!any) return;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        const float v = value(vec, e);
+        if (v >= low && v <= high && v > -INFINITY) f(p + e - skew, v);
+      }
+    });
+  };
 
   if (!counted) {
     // ---- histograms of weights ------------------------------------------------------------------------------------------------
@@ -598,11 +621,11 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
         __syncthreads();
         if (w_bin < 0) return base_w;
         const float low = above(w_bin == BINS - 1 ? BINS * 64 : w_bin + 2, false), high = above(w_bin - 2, true);
-        auto in_group = [&](float v) __attribute__((always_inline)) { return v >= low && v <= high && (ordered(v) & mask) == bits && weigh.bin(v) == w_bin; };
+        auto in_group = [&](float v) __attribute__((always_inline)) { return (ordered(v) & mask) == bits && weigh.bin(v) == w_bin; };
         for (int level = 0; size > SORTED && level < 3; ++level) {
           const int down = level == 0 ? 20 : level == 1 ? 8 : 0, digits = level < 2 ? 4096 : 256;
           clear();
-          all([&](int, float v) {
+          between(low, high, [&](int, float v) {
             if (in_group(v)) { const int d = digits - 1 - (int)(ordered(v) >> down & (digits - 1)); atomicAdd(&s.weight[d], weigh(v)); atomicAdd(&s.count[d], 1u); }
           });
           __syncthreads();
@@ -649,7 +672,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
         }
         if (!tid) { s.listed = 0; s.key_min = 0xFFFFFFFFu; s.key_max = 0; }
         __syncthreads();
-        all([&](int i, float v) { if (in_group(v)) s.list[atomicAdd(&s.listed, 1)] = (u64)~ordered(v) << 32 | (unsigned)i; });      // larger logits first, equal ones by index
+        between(low, high, [&](int i, float v) { if (in_group(v)) s.list[atomicAdd(&s.listed, 1)] = (u64)~ordered(v) << 32 | (unsigned)i; });      // larger logits first, equal ones by index
         __syncthreads();
         // two entries a thread
         u64 entry[2];
@@ -713,10 +736,11 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       };
       auto histogram = [&]() {
         if (split) {
-          const long long at = (long long)row * a.parts * BINS;
           for (int b = tid; b < BINS; b += SAMPLE_THREADS) {
-            u64 w = 0; unsigned c = 0;
-            for (int p = 0; p < a.parts; ++p) { w += a.part_weight[at + p * BINS + b]; c += a.part_count[at + p * BINS + b]; }
+            u64 w = 0, w8[MOST_PARTS]; unsigned c = 0, c8[MOST_PARTS];
+            of_parts(b, w8, c8);
+#pragma unroll
+            for (int p = 0; p < MOST_PARTS; ++p) { w += w8[p]; c += c8[p]; }
             s.weight[b] = w; s.count[b] = c;
           }
           __syncthreads();
@@ -816,17 +840,22 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
     }
     if (tid < SAMPLE_WAVES) { s.wave_w[tid] = 0; s.wave_c[tid] = 0; }
     __syncthreads();
-    for (int p = 0; p < a.parts; ++p) {
-      const long long at = ((long long)row * a.parts + p) * BINS;
-      u64 w = 0; unsigned c = 0;
-      for (int b = tid; b < whole; b += SAMPLE_THREADS) { w += a.part_weight[at + b]; c += a.part_count[at + b]; }
-      w = wave_sum(w); c = wave_sum(c);
-      if (!lane) { atomicAdd(&s.wave_w[p], w); atomicAdd(&s.wave_c[p], c); }
+    u64 sums[MOST_PARTS] = {}; unsigned counts[MOST_PARTS] = {};
+    for (int b = tid; b < whole; b += SAMPLE_THREADS) {
+      u64 w[MOST_PARTS]; unsigned c[MOST_PARTS];
+      of_parts(b, w, c);
+#pragma unroll
+      for (int p = 0; p < MOST_PARTS; ++p) { sums[p] += w[p]; counts[p] += c[p]; }
+    }
+#pragma unroll
+    for (int p = 0; p < MOST_PARTS; ++p) {
+      const u64 w = wave_sum(sums[p]); const unsigned c = wave_sum(counts[p]);
+      if (!lane && c) { atomicAdd(&s.wave_w[p], w); atomicAdd(&s.wave_c[p], c); }
     }
     if (whole < BINS) {
       const float high = above(whole - 2, true);
-      all([&](int i, float v) {
-        if (v < low || v > high || weigh.bin(v) < whole) return;
+      between(low, high, [&](int i, float v) {
+        if (weigh.bin(v) < whole) return;
         const unsigned key = ordered(v);
         if (last.key && !(key > last.key || (key == last.key && i <= last.at))) return;
         if (weigh.dropped(v)) return;
@@ -887,7 +916,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
 using namespace octo;
 
 namespace {
-// Workgroups of a row where rows are few and long, or 0.  fp32, top-p: 1 x 131072 113 us alone, so 80; 48 x 131072 115 and 93; 1 x 262144 200 and 115; but 128 x 131072 126 and 133,
+// Workgroups of a row where rows are few and long, or 0.  fp32, top-p: 1 x 131072 113 us alone, so 76; 48 x 131072 115 and 94; 1 x 262144 200 and 115; but 128 x 131072 126 and 133,
 // 1 x 32768 37 and 41.  Counting the codes of bf16 takes less (1 x 131072 49, shared by weights 91), a short list needs no weights of all tokens.
 int sample_parts(const octo_sample_op* op) {
   const bool short_list = !op->d_top_k && op->top_k > 0 && op->top_k <= LISTED;
