@@ -729,14 +729,14 @@ octo_status octo_dequantize_mx8(const uint8_t* codes, const uint8_t* exps, size_
  * of 32, no residual).  d_bias: NULL or fp32 [cols or 2 cols]; d_res: NULL or rows of y's type, d_y itself with the same stride allowed; apart from that y may not overlap anything else.  d_y and d_res may have any address of
  * an element (vectors are used where four values are aligned).  Sums and the epilogue are in fp32, y is rounded once; the same call on the same inputs gives the same bits.
  * d_n: NULL, or the number of tokens present, on the device (clamped to n): later rows are left as they were.
- * Products of rows in 8 bits are added up as the 8-bit matrix instructions do, to about 2^-14 of the sum of their sizes, where y is of 16 or 8 bits, the four exponents of 128 values of k are
- * one aligned word, and the kernel is one of 1 to 4; exactly, in fp32, otherwise.
+ * Products of rows in 8 bits are exact and their sums in fp32, like all others.  fast8 != 0 permits the sums of the 8-bit matrix instructions, which are twice as fast and good to some 2^-14 of the sum
+ * of the products' sizes: they are taken where y is of 16 or 8 bits, the four exponents of 128 values of k are one aligned word, and the kernel is one of 1 to 4.
  * *kernel_id (may be NULL): 0 nothing to do; 1 to 4: tiles of 256 x 256, 128 x 128, 128 x 64 and 128 x 128 (rows of w x tokens) in LDS, 3 and 4 with loads four steps deep (with 1, tokens beyond
  * whole rounds of the compute units are a second launch's); 10 R + T: operands straight from memory, R x 16 rows of w and T x 16 tokens a block; 10 R: the same with up to 16 tokens that stay in registers. */
 #define OCTO_ACT_GELU 3
 typedef struct octo_product_op {
   int32_t dtype, x_format, y_format, out_f32;
-  int32_t n, k, cols, act, gated, pad_;
+  int32_t n, k, cols, act, gated, fast8;
   const void* d_x; const void* d_w; int64_t x_row, w_row;
   octo_mx8_rows x8, w8;
   const float* d_bias; const void* d_res; void* d_y; int64_t res_row, y_row;

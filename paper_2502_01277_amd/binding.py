@@ -189,7 +189,7 @@ class OctoMx8Op(C.Structure):
 
 class OctoProductOp(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("x_format", C.c_int32), ("y_format", C.c_int32), ("out_f32", C.c_int32), ("n", C.c_int32), ("k", C.c_int32), ("cols", C.c_int32),
-                ("act", C.c_int32), ("gated", C.c_int32), ("pad_", C.c_int32), ("d_x", C.c_void_p), ("d_w", C.c_void_p), ("x_row", C.c_int64), ("w_row", C.c_int64),
+                ("act", C.c_int32), ("gated", C.c_int32), ("fast8", C.c_int32), ("d_x", C.c_void_p), ("d_w", C.c_void_p), ("x_row", C.c_int64), ("w_row", C.c_int64),
                 ("x8", OctoMx8Rows), ("w8", OctoMx8Rows), ("d_bias", C.c_void_p), ("d_res", C.c_void_p), ("d_y", C.c_void_p), ("res_row", C.c_int64), ("y_row", C.c_int64),
                 ("y8", OctoMx8Rows), ("d_n", C.c_void_p)]
 
@@ -1170,10 +1170,11 @@ def op_mx8_load(x: Mx8, y, n=None, stream=None):
         _st(st)
 
 
-def op_product(x, w, y, bias=None, act="none", gated=False, res=None, n=None, stream=None) -> int:
+def op_product(x, w, y, bias=None, act="none", gated=False, res=None, n=None, stream=None, fast8=False) -> int:
     """y = act(x w^T + bias) (+ res), gated: the first half of w's rows, activated, times the second (octo_product_op in octo.h).  x [tokens][k] and w [rows][k]: tensors of
     one type, or Mx8 both; y [tokens][cols]: a tensor of x's type or fp32 (of any type where x is Mx8), or an Mx8; bias fp32 [rows of w]; res like y;
-    act: "none", "relu", "silu" or "gelu".  n: int32 device tensor with the number of tokens present, or None.  Returns the id of the kernel that ran."""
+    act: "none", "relu", "silu" or "gelu".  n: int32 device tensor with the number of tokens present, or None.  fast8: sums of Mx8 rows may be those of the 8-bit matrix
+    instructions, to some 2^-14 of the products' sizes and twice as fast.  Returns the id of the kernel that ran."""
     t = _torch()
     if isinstance(x, Mx8):
         if not isinstance(w, Mx8):
@@ -1210,7 +1211,7 @@ def op_product(x, w, y, bias=None, act="none", gated=False, res=None, n=None, st
             d_res, res_row = _rows(res, y.dtype, (tokens, cols), "res is like y")
     if not tokens or not cols:
         return 0
-    op = _PRODUCT.pack(code, x_fmt, y_fmt, out_f32, tokens, k, cols, _ACTS[act], 1 if gated else 0, 0, *x_fields,
+    op = _PRODUCT.pack(code, x_fmt, y_fmt, out_f32, tokens, k, cols, _ACTS[act], 1 if gated else 0, 1 if fast8 else 0, *x_fields,
                        0 if bias is None else _optional(bias, t.float32, "bias is fp32 [rows of w] on the device", rows), d_res, d_y, res_row, y_row, *y8,
                        0 if n is None else _optional(n, t.int32, "n is int32 on the device"))
     if stream is not None:

@@ -5,7 +5,7 @@
 // Rows of w and of x are alike: both are read along k, 16 bytes a lane, and go into the matrix instructions as they lie in memory.  w is the first operand, so a lane gets
 // results of neighbouring outputs of one token.
 //
-// Measured (MI355X): 8192 cubed bf16 1447 TFLOP/s (a large library product 1580), 8 bits 2508, fp32 144; 12800 tokens 4096 -> 4096 bf16 318 us; 512 tokens of it 22; 16 tokens 4096 -> 131072
+// Measured (MI355X): 8192 cubed bf16 1447 TFLOP/s (a large library product 1580), 8 bits 1451 (with fast8 2540), fp32 144; 12800 tokens 4096 -> 4096 bf16 318 us; 512 tokens of it 22; 16 tokens 4096 -> 131072
 // bf16 184 us, 5.8 TB/s; 16 tokens 4096 -> 2 x 12288 in 8 bits, gated, 24 us and to 8 bits 28, 4.2 and 3.6 TB/s.
 #pragma once
 #include <utility>
@@ -31,7 +31,7 @@ struct ProductArgs {
   int y_vec, res_vec, bias_vec;                       // four values at a multiple of four outputs are one aligned vector
   int vec;                                            // all of them are (or are not there), and outputs are whole vectors, not in 8 bits
   int exp_words;                                      // the exponents of 128 values of k are one aligned word
-  int exact8;                                         // rows of 8 bits go through bf16 also where tokens are many
+  int exact8;                                         // rows of 8 bits go through bf16 also where tokens are many: sums in fp32
   int direct;                                         // results of 16 bits, eight of them one aligned vector, or of 8 bits, activations that take few instructions
   int tiles_n, tiles_m;
   int n_from;                                         // tokens before x's first row, of those that n_dyn counts
@@ -177,18 +177,14 @@ __device__ __forceinline__ floatx4 mfma_mx8(const u32x4* a, const u32x4* b, floa
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(__builtin_bit_cast(i32x8, x), __builtin_bit_cast(i32x8, y), c, 0, 0, 0, ea, 0, eb);
 }
 
-// Sixteen values of 8 bits in bf16, which holds them and their power of two exactly; `e`: their exponent byte.
-__device__ __forceinline__ void widen_mx8(u32x4 v, unsigned e, u32x4* lo, u32x4* hi) {
+// Eight and sixteen values of 8 bits in bf16, which holds them and their power of two exactly (codes of the bytes 1 and 2 to the next multiple of 2^-133); `e`: their exponent byte.
+__device__ __forceinline__ u32x4 widen_mx8(unsigned v0, unsigned v1, unsigned e) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
   const float scale = __uint_as_float(e << 23);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const unsigned a = __builtin_bit_cast(unsigned, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)v[i], scale, false));
-    const unsigned b = __builtin_bit_cast(unsigned, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)v[i], scale, true));
-    if (i < 2) { (*lo)[2 * i] = a; (*lo)[2 * i + 1] = b; }
-    else { (*hi)[2 * i - 4] = a; (*hi)[2 * i - 3] = b; }
-  }
+  return u32x4{__builtin_bit_cast(unsigned, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)v0, scale, false)), __builtin_bit_cast(unsigned, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)v0, scale, true)),
+               __builtin_bit_cast(unsigned, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)v1, scale, false)), __builtin_bit_cast(unsigned, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)v1, scale, true))};
 }
+__device__ __forceinline__ void widen_mx8(u32x4 v, unsigned e, u32x4* lo, u32x4* hi) { *lo = widen_mx8(v[0], v[1], e); *hi = widen_mx8(v[2], v[3], e); }
 
 // A wavefront's sums, 2 TN x 2 TM blocks of 16 rows of w times 16 tokens (of a gated layer: two of gates, two of what they are gates of, ...), straight from its registers.  An
 // exchange between rows of 16 lanes makes 16 bytes of neighbouring outputs a lane, 64 bytes a token of every store: the lane's chunk of eight outputs is then {0, 2, 1, 3}[g].  For
@@ -300,9 +296,10 @@ template <int N, typename F> __device__ __forceinline__ void unrolled(F&& f) { u
 // products.  The 16-byte chunks of a row lie at their number xor half
 // the row's, which spreads the rows that sixteen lanes read together over all banks.
 //
-// Rows of 8 bits: the 8-bit matrix instructions add products in groups of eight at the weight of the group's largest and drop what lies 2^13 below it (measured: 1 + 2^-13 comes
-// out, 1 + 2^-14 does not), 2^-14 of a sum's size in the mean.  Results that are rounded to 16 or 8 bits can bear that; for fp32 results, and where exponents are no aligned words (EXACT), the
-// values are widened to bf16, whose products are exact and added in fp32, at half the rate.
+// Rows of 8 bits (EXACT): values are widened to bf16, whose products are exact and added in fp32.  The 8-bit matrix instructions are twice as fast, but add products in groups of eight at the weight
+// of the group's largest and drop what lies 2^13 below it (measured: 1 + 2^-13 comes out, 1 + 2^-14 does not), 2^-14 of a sum's size in the mean, and all of it where the large ones cancel: they
+// run where the caller permits it, and results are rounded to 16 or 8 bits.  (12800 tokens 4096 -> 2 x 12288, gated: 1867 us, with fast8 1070; 8192 cubed 758 and 433; 128 tokens 4096 -> 4096
+// 25.6 and 16.3.)
 // The size of four stages is given at the launch: a compiler that knows it, and that a CU has room for one block, lets a wavefront have both halves of the registers, and moves sums
 // from one half to the other and back in each step (512 tokens, bf16 4096 -> 4096: 27.6 us, so 21.9).
 template <int D, int BYTES> struct ProductLds {
@@ -519,54 +516,74 @@ __global__ __launch_bounds__(WN * WM * 64, MINB) void product_tile_kernel(Produc
     };
 #pragma nounroll
     for (int t = 0; t < nk; t += 2) { step(t, std::false_type{}); step(t + 1, std::true_type{}); }
+  } else if constexpr (MX) {
+    // A step is two halves of k.  An operand is widened shortly before its first product: a row of w during the row of products before its own, x along the first row.  What it was widened
+    // from is read again at once, for the next half, so one set of registers does for what lies in LDS (256 x 256: 64 of it, 80 widened, 16 of exponents beside the sums' 256).
+    u32x4 fw[BW], fx[BX], w16[2][2], x16[BX][2];
+    unsigned ew[BW], ex[BX];
+    auto fetch = [&](bool is_x, int t, int kq, int i) __attribute__((always_inline)) { (is_x ? fx[is_x ? i : 0] : fw[is_x ? 0 : i]) = read(is_x, t & (D - 1), i, 4 * kq + g); };
+    auto scale = [&](bool is_x, int t, int i) __attribute__((always_inline)) {
+      (is_x ? ex[is_x ? i : 0] : ew[is_x ? 0 : i]) =
+          *(const unsigned*)(Lds::at() + D * STAGE + ((t & (RING - 1)) * EXPS + (is_x ? BN + wm * TM * 32 : wn * TN * 32) + i * 16 + r16) * 4);
+    };
+#pragma unroll
+    for (int i = 0; i < BW; ++i) { fetch(false, 0, 0, i); scale(false, 0, i); }
+#pragma unroll
+    for (int j = 0; j < BX; ++j) { fetch(true, 0, 0, j); scale(true, 0, j); }
+    auto step = [&](int t) __attribute__((always_inline)) {
+      unrolled<2>([&](auto kq_) __attribute__((always_inline)) {
+        constexpr int kq = kq_();
+        if constexpr (kq == 1) turn(t);
+        const int shift = 16 * kq + 8 * (g >> 1);
+        // a quarter of 16 values of block i at a time, then the next half's in their place
+        auto widen = [&](bool is_x, int i, int part) __attribute__((always_inline)) {
+          const u32x4 v = is_x ? fx[is_x ? i : 0] : fw[is_x ? 0 : i];
+          u32x4& to = is_x ? x16[is_x ? i : 0][part] : w16[i & 1][part];
+          to = widen_mx8(v[2 * part], v[2 * part + 1], (is_x ? ex[is_x ? i : 0] : ew[is_x ? 0 : i]) >> shift & 255);
+          if (part == 1) {
+            fetch(is_x, t + kq, kq ^ 1, i);
+            if (kq == 1) scale(is_x, t + 1, i);
+          }
+        };
+        widen(false, 0, 0); widen(true, 0, 0); widen(false, 0, 1); widen(true, 0, 1);
+        unrolled<M>([&](auto m_) __attribute__((always_inline)) {
+          constexpr int m = m_(), i = m / BX, j = m % BX;
+          unrolled<2>([&](auto part_) __attribute__((always_inline)) {
+            constexpr int part = part_();
+            acc[i][j] = mfma16<__bf16>(w16[i & 1][part], x16[j][part], acc[i][j]);
+            if constexpr (i == 0 && j + 1 < BX) widen(true, j + 1, part);
+            if constexpr (i + 1 < BW && j == BX - 2 + part) widen(false, i + 1, part);
+            if constexpr (part == 1) load_place(kq == 1 ? t + D : t + D - 1, (kq == 1 ? t : t - 1) & (D - 1), std::integral_constant<int, kq == 1 ? m : M + m>{});
+            __builtin_amdgcn_sched_barrier(0);
+          });
+        });
+      });
+    };
+#pragma nounroll
+    for (int t = 0; t < nk; ++t) step(t);
   } else {
     // A step is two products of k; two sets of operands.
     constexpr int R = BW + BX;
     u32x4 fw[2][BW], fx[2][BX];
-    unsigned ew[2][MX ? BW : 1], ex[2][MX ? BX : 1];
     // read r of an operand set, in the order in which the products want them: the first row of w, all of x, the other rows of w
     auto fetch = [&](int set, int t, int kq, int r) __attribute__((always_inline)) {
       if (r >= 1 && r <= BX) fx[set][r - 1] = read(true, t & (D - 1), r - 1, 4 * kq + g);
       else fw[set][r ? r - BX : 0] = read(false, t & (D - 1), r ? r - BX : 0, 4 * kq + g);
     };
-    auto scales = [&](int set, int t) __attribute__((always_inline)) {
-      if constexpr (MX) {
-        const unsigned char* const p = Lds::at() + D * STAGE + (t & (RING - 1)) * EXPS * 4;
-#pragma unroll
-        for (int i = 0; i < BW; ++i) ew[set][i] = *(const unsigned*)(p + (wn * TN * 32 + i * 16 + r16) * 4);
-#pragma unroll
-        for (int j = 0; j < BX; ++j) ex[set][j] = *(const unsigned*)(p + (BN + wm * TM * 32 + j * 16 + r16) * 4);
-      }
-    };
 #pragma unroll
     for (int r = 0; r < R; ++r) fetch(0, 0, 0, r);
-    scales(0, 0);
     auto step = [&](int t) __attribute__((always_inline)) {
       unrolled<2>([&](auto kq_) __attribute__((always_inline)) {
         constexpr int kq = kq_();
-        if constexpr (kq == 1) { turn(t); scales(1, t + 1); }
-        u32x4 w8[MX ? BW : 1][2], x8[MX ? BX : 1][2];
-        if constexpr (MX) {
-#pragma unroll
-          for (int i = 0; i < BW; ++i) widen_mx8(fw[kq][i], ew[0][i] >> (16 * kq + 8 * (g >> 1)) & 255, &w8[i][0], &w8[i][1]);
-#pragma unroll
-          for (int j = 0; j < BX; ++j) widen_mx8(fx[kq][j], ex[0][j] >> (16 * kq + 8 * (g >> 1)) & 255, &x8[j][0], &x8[j][1]);
-        }
+        if constexpr (kq == 1) turn(t);
         unrolled<M>([&](auto m_) __attribute__((always_inline)) {
           constexpr int m = m_(), i = m / BX, j = m % BX, first = (m * R + M - 1) / M, last = ((m + 1) * R + M - 1) / M;
-          if constexpr (MX) acc[i][j] = mfma16<__bf16>(w8[i][1], x8[j][1], mfma16<__bf16>(w8[i][0], x8[j][0], acc[i][j]));
-          else acc[i][j] = mfma_part<T>(fw[kq][i], fx[kq][j], acc[i][j]);
+          acc[i][j] = mfma_part<T>(fw[kq][i], fx[kq][j], acc[i][j]);
           unrolled<last - first>([&](auto d) __attribute__((always_inline)) { fetch(kq ^ 1, t + kq, kq ^ 1, first + d()); });
           load_place(kq == 1 ? t + D : t + D - 1, (kq == 1 ? t : t - 1) & (D - 1), std::integral_constant<int, kq == 1 ? m : M + m>{});
           __builtin_amdgcn_sched_barrier(0);
         });
       });
-      if constexpr (MX) {
-#pragma unroll
-        for (int i = 0; i < BW; ++i) ew[0][i] = ew[1][i];
-#pragma unroll
-        for (int j = 0; j < BX; ++j) ex[0][j] = ex[1][j];
-      }
     };
 #pragma nounroll
     for (int t = 0; t < nk; ++t) step(t);
@@ -912,6 +929,7 @@ template <> hipError_t launch_product<OCTO_PRODUCT_TYPE>(int variant, const Prod
   if constexpr (std::is_same<T, f8>::value) {
     if (a.exact8) {
       switch (variant) {
+        case 1: return launch_product_tile<T, true, 4, 4, 2, 2, 1, 2>(a, s);
         case 2: return launch_product_tile<T, true, 2, 2, 2, 2, 2, 2>(a, s);
         case 3: return launch_product_tile<T, true, 2, 1, 2, 2, 2, 4>(a, s);
         case 4: return launch_product_tile<T, true, 2, 2, 2, 2, 2, 4>(a, s);

@@ -45,11 +45,11 @@ extern "C" octo_status octo_op_product(const octo_product_op* op, void* hip_stre
   const uintptr_t at = (uintptr_t)op->d_y | (uintptr_t)op->d_res;
   a.direct = op->act != OCTO_ACT_GELU && (!a.bias || a.bias_vec) && (y8 || (ys == 2 && !(at & 15) && op->cols % 8 == 0 && op->y_row % 8 == 0 && (!a.res || op->res_row % 8 == 0)));
   a.vec = !y8 && a.cols % 4 == 0 && a.y_vec && (!a.res || a.res_vec) && (!a.bias || a.bias_vec);
-  a.exact8 = x8 && (a.y_kind == PRODUCT_Y_F32 || !a.exp_words);
+  a.exact8 = x8 && (!op->fast8 || a.y_kind == PRODUCT_Y_F32 || !a.exp_words);
   if (!op->n) return OCTO_OK;
   hipStream_t s = (hipStream_t)hip_stream;
   const int bits = x8 ? 8 : 8 * es;
-  auto choice = [&](int n) { return product_choice(n, a.k_bytes, a.cols, a.gated, y8, bits, !x8 || a.exp_words, a.exact8); };
+  auto choice = [&](int n) { return product_choice(n, a.k_bytes, a.cols, a.gated, y8, bits, !x8 || a.exp_words, x8 && !a.exp_words); };
   const ProductChoice first = choice(op->n);
   if (first.blocks > 0x7FFFFF) return OCTO_EINVAL;                   // HIP counts the threads of a launch, up to 512 a block, in 32 bits
   for (ProductChoice c = first;;) {

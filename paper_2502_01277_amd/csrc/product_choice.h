@@ -11,9 +11,9 @@ constexpr int product_held_steps(int r, bool rows8) { return r == 4 ? (rows8 ? 4
 
 // variant: 1, 2: tiles in LDS of 256 x 256 and 128 x 128 (rows of w x tokens) with two stages; 3, 4: of 128 x 64 and 128 x 128 with four; 10 R + T: operands straight from memory,
 // R x 16 rows of w and T x 16 tokens a block; 10 R: the same with up to 16 tokens, held.
-// bits: of a value of x and w.  words: exponents of 8 bits come in aligned words.  to8: results in 8 bits, whose groups of 32 outputs one block holds.  exact8: rows of 8 bits that
-// go through bf16, which has no tiles of 256 x 256.
-inline ProductChoice product_choice(int n, int k_bytes, int cols, bool gated, bool to8, int bits, bool words, bool exact8) {
+// bits: of a value of x and w.  words: exponents of 8 bits come in aligned words.  to8: results in 8 bits, whose groups of 32 outputs one block holds.  bytes8: rows of 8 bits whose exponents
+// come byte by byte, for which there are no tiles of 256 x 256.
+inline ProductChoice product_choice(int n, int k_bytes, int cols, bool gated, bool to8, int bits, bool words, bool bytes8) {
   const long long rows = gated ? 2ll * cols : cols;
   auto blocks = [&](int bn, int bm) { return (rows + bn - 1) / bn * ((n + bm - 1ll) / bm); };
   auto few = [&](int r, int t) { const int outs = gated ? 8 * r : 16 * r; return ProductChoice{10 * r + t, (cols + outs - 1ll) / outs * ((n + 16ll * t - 1) / (16 * t)), n}; };
@@ -37,13 +37,13 @@ inline ProductChoice product_choice(int n, int k_bytes, int cols, bool gated, bo
     if (few(2, 2).blocks <= 256) return few(2, 2);
     if (k_bytes <= 2560 && few(2, 4).blocks <= 192) return few(2, 4);
   } else if (bits == 8) {
-    // The same (64 tokens, 4096 -> 1024: 9.5 us, two sets of rows a block 13.0, tiles 15.7; 32 tokens, 4096 -> 4096: 13.1, tiles 15.5).  Tiles that take exponents byte by byte are slow beyond a
+    // The same (64 tokens, 4096 -> 1024: 9.5 us, two sets of rows a block 13.0, tiles 15.7; 32 tokens, 4096 -> 4096: 13.0, tiles 25.7).  Tiles that take exponents byte by byte are slow beyond a
     // block a CU too (64 tokens, 4000 -> 4096: 13.7, tiles 37; 300 tokens, 4000 -> 2000: 34, tiles 42; 1000 tokens, 4000 -> 1000: 46, tiles 43).
     if (!gated && !to8 && few(1, 1).blocks <= 256) return few(1, 1);
     if (!(gated && to8) && few(2, 1).blocks <= 256) return few(2, 1);
     if (!words && few(4, 1).blocks <= 768) return few(4, 1);
   }
-  if (!exact8 && bits != 32 && blocks(256, 256) >= 256) {              // fp32, 4096 cubed: 1158 us, tiles of 128 x 128 953
+  if (!bytes8 && bits != 32 && blocks(256, 256) >= 256) {              // fp32, 4096 cubed: 1158 us, tiles of 128 x 128 953
     // Whole rounds of 256 CUs; few tiles that are left over would take a round of their own, in which smaller ones are done in a third of the time.
     const long long across = (rows + 255) / 256, all = blocks(256, 256), m = all / 256 * 256 / across * 256;
     const long long rest = n - m;
