@@ -591,7 +591,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
     // ---- histograms of weights ------------------------------------------------------------------------------------------------
     if (top_k > 0 || by_p) {
       // One border: the first token in order at which the count reaches `limit_c` (by_count), or the weight `limit_w`.  Its bin is looked for among the bins of w, then among bits of the
-      // logits, until few enough share it; those are sorted.  Returns the weight up to and with the token; all of it where the limit is not reached.
+      // logits, until few enough share it; those are sorted.  Returns the weight up to and with the token; all of it, and `last` as it was, where the limit is not reached.
       auto clear = [&]() { for (int b = tid; b < BINS; b += SAMPLE_THREADS) { s.weight[b] = 0; s.count[b] = 0; } __syncthreads(); };
       auto find_bin = [&](bool by_count, unsigned limit_c, double limit_w, unsigned base_c, u64 base_w) {
         // four bins a thread
@@ -620,7 +620,9 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
         u64 base_w = s.before_w;
         __syncthreads();
         if (w_bin < 0) return base_w;
-        const float low = above(w_bin == BINS - 1 ? BINS * 64 : w_bin + 2, false), high = above(w_bin - 2, true);
+        // the last bin holds whatever lies 64 octaves down or more: words ruled out by large numbers, most words at a low temperature
+        const float low = w_bin == BINS - 1 ? -INFINITY : above(w_bin + 2, false), high = above(w_bin - 2, true);
+        auto none_reached = [&]() { const u64 w = base_w + s.before_w; __syncthreads(); return w; };
         auto in_group = [&](float v) __attribute__((always_inline)) { return (ordered(v) & mask) == bits && weigh.bin(v) == w_bin; };
         for (int level = 0; size > SORTED && level < 3; ++level) {
           const int down = level == 0 ? 20 : level == 1 ? 8 : 0, digits = level < 2 ? 4096 : 256;
@@ -630,6 +632,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
           });
           __syncthreads();
           find_bin(by_count, limit_c, limit_w, base_c, base_w);
+          if (s.bin < 0) return none_reached();
           bits |= (unsigned)(digits - 1 - s.bin) << down; mask |= (unsigned)(digits - 1) << down;
           size = s.bin_count; base_c = s.before_c; base_w = s.before_w;
           __syncthreads();
@@ -670,10 +673,15 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
           __syncthreads();
           return base_w + m * q;
         }
-        if (!tid) { s.listed = 0; s.key_min = 0xFFFFFFFFu; s.key_max = 0; }
+        if (!tid) { s.listed = 0; s.key_min = 0xFFFFFFFFu; s.key_max = 0; s.key = 0; s.at = 0x7FFFFFFF; s.before_w = base_w; }
         __syncthreads();
-        between(low, high, [&](int i, float v) { if (in_group(v)) s.list[atomicAdd(&s.listed, 1)] = (u64)~ordered(v) << 32 | (unsigned)i; });      // larger logits first, equal ones by index
+        between(low, high, [&](int i, float v) {
+          if (!in_group(v)) return;
+          const int at = atomicAdd(&s.listed, 1);
+          if (at < SORTED) s.list[at] = (u64)~ordered(v) << 32 | (unsigned)i;      // larger logits first, equal ones by index
+        });
         __syncthreads();
+        size = min((unsigned)s.listed, (unsigned)SORTED);
         // two entries a thread
         u64 entry[2];
         for (int e = 0; e < 2; ++e) entry[e] = tid + e * SAMPLE_THREADS < (int)size ? s.list[tid + e * SAMPLE_THREADS] : ~0ull;
@@ -692,6 +700,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
             if (entry[e] != ~0ull) { const int d = (int)((key_of(entry[e]) - lo) >> down); atomicAdd(&s.weight[d], weigh(logit_of(entry[e]))); atomicAdd(&s.count[d], 1u); }
           __syncthreads();
           find_bin(by_count, limit_c, limit_w, base_c, base_w);
+          if (s.bin < 0) return none_reached();
           const unsigned digit = (unsigned)s.bin;
           size = s.bin_count; base_c = s.before_c; base_w = s.before_w;
           for (int e = 0; e < 2; ++e) if (entry[e] != ~0ull && (key_of(entry[e]) - lo) >> down != digit) entry[e] = ~0ull;
