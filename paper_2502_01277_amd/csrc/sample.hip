@@ -213,13 +213,17 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_part_kernel(SampleArgs 
   for (int b = tid; b < BINS; b += SAMPLE_THREADS) { weight[b] = 0; count[b] = 0; }
   __syncthreads();
   const int tiles = x.tiles(a.parts), stride = SAMPLE_THREADS * x.VEC;
+  unsigned below = 0;                                                // of the last bin, which words that are ruled out by a number share: they weigh nothing
   x.each(part * tiles * stride + tid * x.VEC, tiles, stride, [&](int, float v) __attribute__((always_inline)) {
     int k;
     const u64 q = Weigher::whole(weigh.scaled(weigh.steps(v), &k));
     const int bin = Weigher::bin_of(k);
+    if (bin == BINS - 1) { ++below; return; }
     if (q) atomicAdd(&weight[bin], q);
     atomicAdd(&count[bin], 1u);
   });
+  below = wave_sum(below);
+  if (!(tid & 63) && below) atomicAdd(&count[BINS - 1], below);
   __syncthreads();
   u64* const to_w = a.part_weight + (long long)blockIdx.x * BINS;
   unsigned* const to_c = a.part_count + (long long)blockIdx.x * BINS;
@@ -353,6 +357,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
     if (own_key >= floor_key) {                                       // others have none
       all([&](int i, float v) {
         if (ordered(v) < floor_key) return;
+        if (*(volatile int*)&s.listed > SORTED) return;              // too many already
         const int at = atomicAdd(&s.listed, 1);
         if (at < SORTED) s.list[at] = (u64)~ordered(v) << 32 | (unsigned)i;      // ascending: larger logits first, equal ones by index
       });
@@ -460,6 +465,8 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
           if ((code & 0x7FFF) > 0x7F80 || code == 0xFF80) continue;             // NaN, -infinity
           const int j = entry_of(code);
           if (j >= 0) { atomicAdd(&s.codes[code_range][j >> 1], (j & 1) ? 0x10000u : 1u); continue; }
+          // more than are listed do not fit and are not counted on (words ruled out by -1e9 make all others tiny: 1 x 131072, one in a hundred ruled out, top-p, 612 us with all of them added up, so 159)
+          if (*(volatile int*)&s.listed > SORTED) continue;
           const float t = __uint_as_float(code << 16);
           const int at = atomicAdd(&s.listed, 1);
           atomicAdd(&s.tiny_w, weigh(t));
@@ -628,7 +635,16 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
           const int down = level == 0 ? 20 : level == 1 ? 8 : 0, digits = level < 2 ? 4096 : 256;
           clear();
           between(low, high, [&](int, float v) {
-            if (in_group(v)) { const int d = digits - 1 - (int)(ordered(v) >> down & (digits - 1)); atomicAdd(&s.weight[d], weigh(v)); atomicAdd(&s.count[d], 1u); }
+            if (!in_group(v)) return;
+            const int d = digits - 1 - (int)(ordered(v) >> down & (digits - 1));
+            const u64 q = weigh(v);
+            if (q) atomicAdd(&s.weight[d], q);
+            // lanes with the digit of the first of them, equal logits most often, are counted together (1 x 131072 fp32, 99 % ruled out by -1e9, top_k 3500 and top-p: 754 us one by one,
+            // with the last bin's one by one as well, so 238)
+            const int first = __builtin_amdgcn_readfirstlane(d);
+            const u64 alike = __ballot(d == first);
+            if (d != first) atomicAdd(&s.count[d], 1u);
+            else if (lane == __ffsll(alike) - 1) atomicAdd(&s.count[d], (unsigned)__popcll(alike));
           });
           __syncthreads();
           find_bin(by_count, limit_c, limit_w, base_c, base_w);
@@ -756,13 +772,17 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
           return;
         }
         clear();
+        unsigned below = 0;                                          // of the last bin, as in sample_part_kernel
         all([&](int, float v) {
           int k;
           const u64 q = Weigher::whole(weigh.scaled(weigh.steps(v), &k));
           const int bin = Weigher::bin_of(k);
+          if (bin == BINS - 1) { ++below; return; }
           if (q) atomicAdd(&s.weight[bin], q);
           atomicAdd(&s.count[bin], 1u);
         });
+        below = wave_sum(below);
+        if (!lane && below) atomicAdd(&s.count[BINS - 1], below);
         __syncthreads();
       };
       histogram();
