@@ -41,8 +41,9 @@ __device__ __forceinline__ int product_tokens(const ProductArgs& a) { return a.n
 
 typedef __attribute__((address_space(3))) unsigned char LdsBytes;
 
+__device__ __forceinline__ float relu(float v) { return v < 0.f ? 0.f : v; }      // NaN stays (fmaxf would take the other one)
 __device__ __forceinline__ float product_act(int act, float v) {
-  if (act == PRODUCT_ACT_RELU) return fmaxf(v, 0.f);
+  if (act == PRODUCT_ACT_RELU) return relu(v);
   if (act == PRODUCT_ACT_SILU) return silu(v);
   if (act == PRODUCT_ACT_GELU) return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f));
   return v;
@@ -138,7 +139,7 @@ __device__ __forceinline__ void product_finish_vec(const ProductArgs& a, const b
       for (int e = 0; e < 4; ++e) z[b][e] = f(z[b][e]);
   };
   if (a.act == PRODUCT_ACT_SILU) act([](float v) { return silu(v); });
-  else if (a.act == PRODUCT_ACT_RELU) act([](float v) { return fmaxf(v, 0.f); });
+  else if (a.act == PRODUCT_ACT_RELU) act([](float v) { return relu(v); });
   else if (a.act == PRODUCT_ACT_GELU) act([](float v) { return product_act(PRODUCT_ACT_GELU, v); });
   if (a.gated) {
 #pragma unroll
@@ -241,7 +242,7 @@ __device__ __forceinline__ void finish_direct_as(const ProductArgs& a, floatx4 (
           for (int e = 0; e < 4; ++e) v[h][e] = f(v[h][e]);
       };
       if (a.act == PRODUCT_ACT_SILU) each([](float z) { return silu(z); });
-      else if (a.act == PRODUCT_ACT_RELU) each([](float z) { return fmaxf(z, 0.f); });
+      else if (a.act == PRODUCT_ACT_RELU) each([](float z) { return relu(z); });
       if constexpr (GATED) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) v[h] *= acc[i + 2 + h][j] + b1[h];
