@@ -45,7 +45,7 @@ __device__ __forceinline__ float relu(float v) { return v < 0.f ? 0.f : v; }    
 __device__ __forceinline__ float product_act(int act, float v) {
   if (act == PRODUCT_ACT_RELU) return relu(v);
   if (act == PRODUCT_ACT_SILU) return silu(v);
-  if (act == PRODUCT_ACT_GELU) return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f));
+  if (act == PRODUCT_ACT_GELU) return 0.5f * v * erfcf(v * -0.70710678118654752f);      // 1 + erf cancels: at v = -4.5 a twentieth is wrong, below -5.5 all of it
   return v;
 }
 

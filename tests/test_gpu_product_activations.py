@@ -3,7 +3,7 @@ import math
 
 import pytest
 
-from test_gpu_product import _t
+from test_gpu_product import STEP, _t
 
 pytestmark = pytest.mark.gpu
 
@@ -62,3 +62,25 @@ def test_numbers_that_are_none_pass_every_activation(octo, rows, dtype, n, cols,
         y = torch.empty(n, cols, dtype=_t(dtype), device="cuda")
         octo.op_product(x, w, y, bias=b, act=act, gated=gated, fast8=True)
         assert torch.equal(torch.isnan(y), nan)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("n,cols", [(14, 96), (60, 96), (300, 4128), (4200, 4160)])
+@pytest.mark.parametrize("gated", [False, True])
+def test_gelu_of_negative_values(octo, dtype, n, cols, gated):
+    """Its error is relative, also where the result is a millionth of the argument.  y = v/2 erfc(t), t = -v / sqrt 2, with v exact: t is off by 2^-23 of itself (the constant and the product), which erfc,
+    whose logarithm has slopes up to 2 t + 1.13, makes (v^2 + 0.8 |v|) 2^-23; erfc itself is within 4 of its last bits, at most 2^-21; two products are 2^-24 each, and a gate is one more: (v^2 + |v| + 6) 2^-23 in
+    all, then the type's rounding."""
+    import torch
+    v = torch.linspace(-12.0, 4.0, n).to(_t(dtype)).cuda()
+    x = torch.zeros(n, 32, dtype=_t(dtype), device="cuda")
+    x[:, 5] = v
+    w = torch.ones(cols * (2 if gated else 1), 32, dtype=_t(dtype), device="cuda")
+    v = v.double()
+    ref = (_activate("gelu", v) * (v if gated else 1.0))[:, None].expand(n, cols)
+    off = ref.abs() * (v * v + v.abs() + 6)[:, None] * 2.0 ** -23
+    for kind in {dtype, "f32"}:
+        y = torch.full((n, cols), float("nan"), dtype=_t(kind), device="cuda")
+        octo.op_product(x, w, y, act="gelu", gated=gated)
+        rel, absolute = STEP[kind]
+        assert bool(((y.double() - ref).abs() <= off + rel * (ref.abs() + off) + absolute).all())
