@@ -49,7 +49,7 @@ extern "C" octo_status octo_op_product(const octo_product_op* op, void* hip_stre
   if (!op->n) return OCTO_OK;
   hipStream_t s = (hipStream_t)hip_stream;
   const int bits = x8 ? 8 : 8 * es;
-  auto choice = [&](int n) { return product_choice(n, a.k_bytes, a.cols, a.gated, y8, bits, !x8 || a.exp_words, x8 && !a.exp_words); };
+  auto choice = [&](int n) { return product_choice(n, a.k_bytes, a.cols, a.gated, y8, bits, !x8 || a.exp_words, x8 && !a.exp_words, a.direct); };
   const ProductChoice first = choice(op->n);
   if (first.blocks > 0x7FFFFF) return OCTO_EINVAL;                   // HIP counts the threads of a launch, up to 512 a block, in 32 bits
   for (ProductChoice c = first;;) {

@@ -12,8 +12,8 @@ constexpr int product_held_steps(int r, bool rows8) { return r == 4 ? (rows8 ? 4
 // variant: 1, 2: tiles in LDS of 256 x 256 and 128 x 128 (rows of w x tokens) with two stages; 3, 4: of 128 x 64 and 128 x 128 with four; 10 R + T: operands straight from memory,
 // R x 16 rows of w and T x 16 tokens a block; 10 R: the same with up to 16 tokens, held.
 // bits: of a value of x and w.  words: exponents of 8 bits come in aligned words.  to8: results in 8 bits, whose groups of 32 outputs one block holds.  bytes8: rows of 8 bits whose exponents
-// come byte by byte, for which there are no tiles of 256 x 256.
-inline ProductChoice product_choice(int n, int k_bytes, int cols, bool gated, bool to8, int bits, bool words, bool bytes8) {
+// come byte by byte, for which there are no tiles of 256 x 256.  direct: results leave tiles straight from registers (ProductArgs).
+inline ProductChoice product_choice(int n, int k_bytes, int cols, bool gated, bool to8, int bits, bool words, bool bytes8, bool direct = true) {
   const long long rows = gated ? 2ll * cols : cols;
   auto blocks = [&](int bn, int bm) { return (rows + bn - 1) / bn * ((n + bm - 1ll) / bm); };
   auto few = [&](int r, int t) { const int outs = gated ? 8 * r : 16 * r; return ProductChoice{10 * r + t, (cols + outs - 1ll) / outs * ((n + 16ll * t - 1) / (16 * t)), n}; };
@@ -32,10 +32,11 @@ inline ProductChoice product_choice(int n, int k_bytes, int cols, bool gated, bo
     if (square.blocks <= 128) return few(gated && to8 ? 4 : 2, 2);
     if (square.blocks <= 256) return square;
   } else if (bits == 16 && !(gated && to8)) {
-    // A block a CU (64 tokens, 4096 -> 4096: 17.1 us, tiles 18.9; 1024 -> 4096 6.6 and 7.6; with two blocks a CU, 128 tokens, 31.2 and 18.9), larger ones for short rows (308 tokens,
-    // 1160 -> 1100: 7.3, tiles 9.3)
+    // A block a CU (64 tokens, 4096 -> 4096: 17.1 us, tiles 18.9; 1024 -> 4096 6.6 and 7.6; with two blocks a CU, 128 tokens, 31.2 and 18.9).  Larger ones for short rows whose results leave tiles
+    // through LDS, which takes as long as some ten steps: bf16 without activation, in 17 sizes of up to 256 blocks and 2560 bytes 0.65 to 1.09 of the tiles' time (308 tokens, 1160 -> 1100: 7.3 and
+    // 9.3; 1000 tokens, 904 -> 470: 7.1 and 11.0), GELU 0.44 to 0.81; rows of 2816 to 4096 bytes 1.12 to 1.16, beyond 256 blocks 1.17 to 1.56.  Straight from registers tiles are as fast (0.86 to 1.14).
     if (few(2, 2).blocks <= 256) return few(2, 2);
-    if (k_bytes <= 2560 && few(2, 4).blocks <= 192) return few(2, 4);
+    if (!direct && k_bytes <= 2560 && few(2, 4).blocks <= 256) return few(2, 4);
   } else if (bits == 8) {
     // The same (64 tokens, 4096 -> 1024: 9.5 us, two sets of rows a block 13.0, tiles 15.7; 32 tokens, 4096 -> 4096: 13.0, tiles 25.7).  Tiles that take exponents byte by byte are slow beyond a
     // block a CU too (64 tokens, 4000 -> 4096: 13.7, tiles 37; 300 tokens, 4000 -> 2000: 34, tiles 42; 1000 tokens, 4000 -> 1000: 46, tiles 43).

@@ -76,3 +76,16 @@ def test_the_same_bits_from_every_call(octo, n):
         y = _result(octo, "bf16", n, 2080)
         octo.op_product(x, w, y)
         assert torch.equal(y, first)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("n,k,cols,gated", [(308, 1160, 1100, False), (1000, 904, 470, False), (120, 72, 2300, False), (700, 1160, 700, False), (90, 800, 1495, True), (65, 1272, 4001, False)])
+def test_short_rows_in_larger_blocks(octo, dtype, n, k, cols, gated):
+    """Operands from memory, 64 tokens a block, where results would leave tiles through LDS."""
+    x, w, x64, w64, g = _inputs(octo, "plain", dtype, n, k, cols, gated, n + k)
+    import torch
+    b, res = torch.randn(w64.shape[0], generator=g).cuda(), torch.randn(n, cols, generator=g).to(_t(dtype)).cuda()
+    y = _result(octo, dtype, n, cols)
+    assert octo.op_product(x, w, y, bias=b, act="gelu", gated=gated, res=res) == 24
+    ref, off = _reference(x64, w64, b.double(), "gelu", gated, res.double(), False)
+    _check(y, ref, off, dtype)
