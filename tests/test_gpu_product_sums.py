@@ -89,3 +89,19 @@ def test_short_rows_in_larger_blocks(octo, dtype, n, k, cols, gated):
     assert octo.op_product(x, w, y, bias=b, act="gelu", gated=gated, res=res) == 24
     ref, off = _reference(x64, w64, b.double(), "gelu", gated, res.double(), False)
     _check(y, ref, off, dtype)
+
+
+@pytest.mark.parametrize("rows,dtype", [("plain", "bf16"), ("plain", "f16"), ("plain", "f32"), ("mx8", "bf16")])
+@pytest.mark.parametrize("n,k,cols", [(5, 1184, 96), (40, 1184, 96), (308, 1184, 1120), (300, 2048, 1120), (1200, 256, 2080), (2100, 384, 2080), (4200, 128, 4160)])
+@pytest.mark.parametrize("gated,bias", [(False, True), (True, False), (True, True)])
+def test_gelu_to_eight_bits(octo, rows, dtype, n, k, cols, gated, bias):
+    """Groups of 32 outputs that leave tiles through LDS, and those of every other kernel."""
+    import torch
+    x, w, x64, w64, g = _inputs(octo, rows, dtype, n, k, cols, gated, n + k)
+    b = torch.randn(w64.shape[0], generator=g).cuda() if bias else None
+    y = octo.Mx8.empty(n, cols)
+    y.codes.fill_(0x55)
+    y.exps.fill_(0x55)
+    octo.op_product(x, w, y, bias=b, act="gelu", gated=gated)
+    ref, off = _reference(x64, w64, None if b is None else b.double(), "gelu", gated, None, rows == "plain" and dtype == "f32")
+    _check_mx8(y, ref, off)

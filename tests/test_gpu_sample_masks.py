@@ -31,7 +31,7 @@ MORE = (dict(), dict(top_p=0.9), dict(min_p=0.01))
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("others", [1500, 30000])
-@pytest.mark.parametrize("top_k", [50, 400, 700, 1000, 3500])
+@pytest.mark.parametrize("top_k", [0, 50, 400, 700, 1000, 3500])
 def test_words_ruled_out_by_finite_numbers(octo, dtype, others, top_k):
     logits, u = _masked(dtype, others, others + top_k)
     for temperature, more in itertools.product((1.0, 0.005, 1e-3), MORE):
@@ -40,7 +40,7 @@ def test_words_ruled_out_by_finite_numbers(octo, dtype, others, top_k):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
-@pytest.mark.parametrize("top_k,temperature", [(50, 1.0), (700, 1.0), (1000, 0.005), (3500, 1e-3), (60000, 1.0)])
+@pytest.mark.parametrize("top_k,temperature", [(0, 1.0), (50, 1.0), (700, 1.0), (1000, 0.005), (3500, 1e-3), (60000, 1.0)])
 def test_the_same_in_long_rows(octo, dtype, top_k, temperature):
     """With a workspace, without one, and with the numbers of each row on the device."""
     import torch
