@@ -39,7 +39,7 @@ inline ProductChoice product_choice(int n, int k_bytes, int cols, bool gated, bo
     if (!direct && k_bytes <= 2560 && few(2, 4).blocks <= 256) return few(2, 4);
   } else if (bits == 8) {
     // The same (64 tokens, 4096 -> 1024: 9.5 us, two sets of rows a block 13.0, tiles 15.7; 32 tokens, 4096 -> 4096: 13.0, tiles 25.7).  Tiles that take exponents byte by byte are slow beyond a
-    // block a CU too (64 tokens, 4000 -> 4096: 13.7, tiles 37; 300 tokens, 4000 -> 2000: 34, tiles 42; 1000 tokens, 4000 -> 1000: 46, tiles 43).
+    // block a CU too (64 tokens, 4000 -> 4096: 14.3, tiles 34.8; 300 tokens, 4000 -> 2000: 34.8, tiles 39.4; 1000 tokens, 4000 -> 1000: 45.8, tiles 40.7).
     if (!gated && !to8 && few(1, 1).blocks <= 256) return few(1, 1);
     if (!(gated && to8) && few(2, 1).blocks <= 256) return few(2, 1);
     if (!words && few(4, 1).blocks <= 768) return few(4, 1);
