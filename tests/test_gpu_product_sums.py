@@ -9,7 +9,7 @@ from test_gpu_product import GRAIN, _check, _check_mx8, _inputs, _reference, _t
 pytestmark = pytest.mark.gpu
 
 # tokens, k, outputs and the tile kernel that they take: the widest k of a step and several of them, ragged on both sides
-TILES = [(4200, 128, 4160, 1), (4100, 896, 4128, 1), (2100, 384, 2080, 2), (129, 1024, 4096, 3), (70, 4096, 8224, 3), (1200, 256, 2080, 4)]
+TILES = [(4200, 128, 4160, 1), (4100, 896, 4128, 1), (2100, 384, 2080, 2), (129, 1024, 4096, 3), (70, 1152, 8224, 3), (1200, 256, 2080, 4)]
 
 
 def _result(octo, out, n, cols):
